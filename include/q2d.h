@@ -369,6 +369,64 @@ q2d_status q2d_grouped_gemm(const q2d_tensor *A, int transA, const q2d_tensor *B
                             int32_t nseg, const int64_t *seg_offsets, int64_t total_rows, void *C,
                             q2d_dtype c_dt, int64_t ldc, int accumulate, hipStream_t stream);
 
+/*
+ * Attention between the query/key/value projections and the output projection of a
+ * block.  For query i at position p = i + len_k - len_q and key j of one sequence and head:
+ *   x = scale q_i.k_j;  s = softcap tanh(x / softcap) where softcap > 0, else x;
+ *   s = s - slopes[head] |p - j| where slopes is set;
+ *   i sees j where (documents unset, or documents[j] == documents[p] >= 0) and
+ *     (j < prefix, or (causal == 0 or j <= p) and (window == 0 or |p - j| < window));
+ *   out_i = sum_j P_ij v_j with P the softmax of s over the keys that i sees, and
+ *   lse_i = log sum_j exp s_ij.
+ * A query that sees no key has out = 0, lse = -infinity and adds nothing to any gradient.
+ * Keys and values that a query does not see have no influence on its results, whatever
+ * they hold (infinities and NaN included), and likewise in the gradients.
+ *
+ * heads_q is a multiple of heads_kv; query head h reads key head h / (heads_q / heads_kv).
+ * dim is a multiple of 8 up to 128 (Q2D_EUNSUPPORTED otherwise).  Lengths are 1 to 2^30.
+ *
+ * Sums, softmax statistics and the gradients' accumulators are float32.  bfloat16 operands
+ * run on bf16 MFMA with the probabilities (and dS) rounded to bfloat16 for the second
+ * products; float32 operands on float32 MFMA.
+ */
+
+/* A [batch][length][heads][dim] tensor: strides in elements, unit stride along dim; rows
+ * start on 16-byte boundaries (the pointer, and every stride whose extent exceeds 1).
+ * A length stride is below 2^24 elements. */
+typedef struct {
+    void *data;
+    int64_t stride_batch, stride_length, stride_head;
+} q2d_heads;
+
+typedef struct {
+    int32_t dtype;           /* q2d_dtype of q, k, v, out and the gradients */
+    int32_t causal;          /* 0 or 1 */
+    int32_t batch, heads_q, heads_kv, dim;
+    int64_t len_q, len_k;
+    int64_t window;          /* 0: no window */
+    float scale;             /* > 0 */
+    float softcap;           /* 0: no cap; > 0 otherwise */
+    const float *slopes;     /* device [heads_q], or NULL: no distance bias */
+    const int32_t *documents;/* device [batch][len_k], or NULL; a negative number is padding */
+    const int32_t *prefix;   /* device [batch], or NULL; clamped to [0, len_k] */
+    q2d_heads q, k, v, out;
+    float *lse;              /* device [batch][heads_q][len_q]; NULL in a forward call that needs none */
+} q2d_attention;
+
+/* Bytes of device workspace that q2d_attention_fwd (backward == 0) or q2d_attention_bwd
+ * (1) needs for these sizes and masks, possibly 0; -1 for invalid arguments.  Host only. */
+int64_t q2d_attention_workspace(const q2d_attention *a, int backward);
+
+/* Forward: writes out and, where set, lse.  workspace: at least q2d_attention_workspace
+ * bytes, 256-byte aligned (may be NULL for 0 bytes); free for reuse in stream order. */
+q2d_status q2d_attention_fwd(const q2d_attention *a, void *workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/* Backward: from dout and the forward call's inputs, out and lse, writes dq, dk and dv
+ * (the shared key and value heads' gradients summed over their query heads).  slopes get no
+ * gradient.  Results do not depend on the order in which workgroups run. */
+q2d_status q2d_attention_bwd(const q2d_attention *a, const q2d_heads *dout, const q2d_heads *dq, const q2d_heads *dk,
+                             const q2d_heads *dv, void *workspace, int64_t workspace_bytes, hipStream_t stream);
+
 /* Static description of a status code (never NULL). */
 const char *q2d_status_string(q2d_status s);
 

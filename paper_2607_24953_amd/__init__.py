@@ -19,6 +19,7 @@ __all__ = [
     "q2d_tensor_init", "q2d_quantize", "q2d_quantize_1d", "mxfp8_quantize", "q2d_gemm",
     "q2d_linear_fwd", "q2d_linear_bwd", "q2d_grouped_tensor_init", "q2d_grouped_quantize",
     "q2d_grouped_gemm", "q2d_dequantize", "q2d_gemm_quantized", "q2d_status_string",
+    "q2d_attention_fwd", "q2d_attention_bwd",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -427,3 +428,7 @@ def q2d_grouped_gemm(A: QTensor, transA: int, B: QTensor, transB: int, seg_offse
                                  out.stride(0), int(bool(accumulate)), _stream(A.device)),
            "q2d_grouped_gemm")
     return out
+
+
+# (at the end: these modules use the names above)
+from .attention import q2d_attention_bwd, q2d_attention_fwd  # noqa: E402

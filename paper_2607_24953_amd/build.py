@@ -3,8 +3,11 @@ from __future__ import annotations
 
 import glob
 import os
+import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -12,7 +15,7 @@ LIB = os.path.join(HERE, "libq2d.so")
 ROOT = os.path.dirname(HERE)
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-ffp-contract=off",
     # no packed-fp32 instructions anywhere in the library
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -30,10 +33,27 @@ def hipcc() -> str:
 def build(verbose: bool = False) -> str:
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
     tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [hipcc()] + HIPCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-o", tmp] + srcs
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
+    inc = ["-I", os.path.join(ROOT, "include")]
+    work = tempfile.mkdtemp(prefix="q2d_build")
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.check_call(cmd)
+
+    def compile_one(src):
+        obj = os.path.join(work, os.path.basename(src) + ".o")
+        run([hipcc()] + HIPCC_FLAGS + inc + ["-c", src, "-o", obj])
+        return obj
+
+    try:
+        # the largest sources first: they take the longest
+        with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            jobs = {s: pool.submit(compile_one, s) for s in sorted(srcs, key=os.path.getsize, reverse=True)}
+            objs = [jobs[s].result() for s in srcs]
+        run([hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs)
+    finally:
+        shutil.rmtree(work, ignore_errors=True)
     os.replace(tmp, LIB)
     return LIB
 

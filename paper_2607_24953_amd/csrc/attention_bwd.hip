@@ -1,0 +1,417 @@
+// Attention backward.  With P = exp(S - lse), dP = dO V^T and delta = rowsum(dO * O):
+//   dS = P (dP - delta) (1 - tanh^2 where scores are capped)
+//   dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K.
+// One kernel owns keys and sums dK and dV over the queries (of all query heads that share
+// the key head), one owns queries and sums dQ over the keys.  Both form S and dP again:
+// seven products in place of five, but every sum has one owner, so there are no atomics and
+// the results do not depend on the order of workgroups.
+//
+// As in the forward kernel, the first products leave the tile in the registers that the
+// second ones take as operand: S, dP as [query][key] where keys are owned (columns), as
+// [key][query] where queries are.
+#include "attention_common.hpp"
+
+namespace q2d {
+
+namespace {
+
+// delta of 4 rows a wave: 16 lanes a row
+template <typename T>
+__global__ __launch_bounds__(256) void attention_delta_kernel(const AttentionArgs a)
+{
+    const int64_t rows = (int64_t)a.batch * a.heads_q * a.len_q;
+    const int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (r >= rows) return;
+    const int l = threadIdx.x & 15;
+    // neighbouring rows are neighbouring heads of a token
+    const int hq = (int)(r % a.heads_q);
+    const int64_t bl = r / a.heads_q;
+    const int i = (int)(bl % a.len_q), b = (int)(bl / a.len_q);
+    const T *o = (const T *)a.out.p + b * a.out.sb + (int64_t)i * a.out.sl + hq * a.out.sh;
+    const T *g = (const T *)a.dout.p + b * a.dout.sb + (int64_t)i * a.dout.sl + hq * a.dout.sh;
+    float s = 0.f;
+    if (8 * l < a.dim) {
+        const Frag<T> x = global_frag<T>(o, true, l >> 1, l & 1, a.dim);
+        const Frag<T> y = global_frag<T>(g, true, l >> 1, l & 1, a.dim);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += (float)x[j] * (float)y[j];
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) s += __shfl_xor(s, d);
+    if (l == 0) a.delta[((int64_t)b * a.heads_q + hq) * a.len_q + i] = s;
+}
+
+// Ranges of document numbers of 64 positions
+__global__ __launch_bounds__(64) void document_ranges_kernel(const int32_t *docs, int len, int2 *ranges)
+{
+    const int n = (len + 63) / 64, b = blockIdx.x / n, t = blockIdx.x % n, j = t * 64 + threadIdx.x;
+    int lo = INT32_MAX, hi = INT32_MIN;
+    if (j < len) lo = hi = docs[(int64_t)b * len + j];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        lo = min(lo, __shfl_xor(lo, d));
+        hi = max(hi, __shfl_xor(hi, d));
+    }
+    if (threadIdx.x == 0) ranges[blockIdx.x] = make_int2(lo, hi);
+}
+
+// ---------------------------------------------------------------- dQ
+
+template <typename T, int DT, int MODS>
+__global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArgs a)
+{
+    constexpr int BN = sizeof(T) == 2 ? 64 : 32, NW = 4, BM = 32 * NW, KS = DT / 16, DS = DT / 32;
+    constexpr bool CAP = MODS & 1, BIAS = MODS & 2, F32 = sizeof(T) == 4;
+    typedef Tile<T, DT> Lds;
+    __shared__ __align__(16) uint8_t smem[2][2][BN * Lds::kRowBytes];
+
+    const AttentionMask &m = a.mask;
+    const uint32_t tiles = (a.len_q + BM - 1) / BM;
+    uint32_t head, qt;
+    head_tile(blockIdx.x, gridDim.x, tiles, head, qt);
+    qt = tiles - 1 - qt;
+    const int b = head / a.heads_q, hq = head % a.heads_q, hk = hq / (a.heads_q / a.heads_kv);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = lane >> 5, col = lane & 31;
+    const int shift = a.len_k - a.len_q, D = a.dim;
+    const int i0 = qt * BM, iw = i0 + wave * 32, i = iw + col;
+    const int p = i + shift;
+    const bool row = i < a.len_q;
+
+    const T *q = (const T *)a.q.p + b * a.q.sb + (int64_t)i * a.q.sl + hq * a.q.sh;
+    const T *g = (const T *)a.dout.p + b * a.dout.sb + (int64_t)i * a.dout.sl + hq * a.dout.sh;
+    const T *k = (const T *)a.k.p + b * a.k.sb + hk * a.k.sh;
+    const T *v = (const T *)a.v.p + b * a.v.sb + hk * a.v.sh;
+    Frag<T> qf[KS], gf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        qf[ks] = global_frag<T>(q, row, ks, h, D);
+        gf[ks] = global_frag<T>(g, row, ks, h, D);
+    }
+    const int64_t at = ((int64_t)b * a.heads_q + hq) * a.len_q + i;
+    // (rows outside: probabilities of 0)
+    const float lse2 = row ? a.lse[at] * kLog2e : INFINITY, delta = row ? a.delta[at] : 0.f;
+
+    const int prefix = m.prefix ? min(max(m.prefix[b], 0), a.len_k) : 0;
+    const int32_t *docs = m.documents ? m.documents + (int64_t)b * a.len_k : nullptr;
+    const int2 *ranges = a.ranges + (int64_t)b * ((a.len_k + 63) / 64);
+    const int p0 = i0 + shift, p1 = min(i0 + BM, a.len_q) - 1 + shift;
+    const int pw0 = iw + shift, pw1 = min(iw + 32, a.len_q) - 1 + shift;
+    int2 dg = make_int2(0, 0), dw = dg;
+    int my_doc = 0;
+    if (docs) {
+        dg = range_of(ranges, p0, p1);
+        if (pw1 >= pw0) dw = range_of(ranges, pw0, pw1);
+        my_doc = row && p >= 0 ? docs[p] : -1;
+    }
+    const ScoreMap sm = score_map(m, hq);
+    const float pos = (float)p;
+    int lo, hi;
+    seen_by_query(m, p, lo, hi);
+    hi = min(hi, a.len_k);
+
+    int end = (a.len_k + BN - 1) / BN;
+    if (m.causal && !m.prefix) end = p1 < 0 ? 0 : min(end, p1 / BN + 1);
+    auto see = [&](int t, Seen &s, Seen &w) {
+        const int j0 = t * BN, j1 = min(j0 + BN, a.len_k) - 1;
+        const int2 dk = docs ? ranges[j0 >> 6] : make_int2(0, 0);
+        s = classify(m, prefix, p0, p1, j0, j1, dg.x, dg.y, dk.x, dk.y);
+        if (pw1 >= pw0) {
+            w = classify(m, prefix, pw0, pw1, j0, j1, dw.x, dw.y, dk.x, dk.y);
+            w.all = w.all && j0 + BN <= a.len_k;
+        }
+    };
+    if (D < DT) {
+        Lds::template clear<NW * 64>(smem[0][0], sizeof(smem));
+        __syncthreads();
+    }
+    v16f dq[DS] = {};
+    Schedule sched;
+    int cur = sched.next(end, see), stage = 0;
+    bool wave_any = sched.wave_any, wave_all = sched.wave_all;
+    if (cur >= 0) {
+        Lds::template load<BN, NW * 64>(smem[0][0], k, a.k.sl, cur * BN, a.len_k, D);
+        Lds::template load<BN, NW * 64>(smem[0][1], v, a.v.sl, cur * BN, a.len_k, D);
+    }
+    while (cur >= 0) {
+        wait_vmcnt<0>();
+        block_barrier();
+        const int next = sched.next(end, see);
+        if (next >= 0) {
+            Lds::template load<BN, NW * 64>(smem[stage ^ 1][0], k, a.k.sl, next * BN, a.len_k, D);
+            Lds::template load<BN, NW * 64>(smem[stage ^ 1][1], v, a.v.sl, next * BN, a.len_k, D);
+        }
+        if (wave_any) {
+            const uint8_t *kt = smem[stage][0], *vt = smem[stage][1];
+            const int j0 = cur * BN;
+            const bool apart = !wave_all && Lds::template non_finite<BN>(kt);
+#pragma unroll 1
+            for (int t = 0; t < BN / 32; ++t) {
+                v16f z = {}, e = {};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(kt, 32 * t + col, ks, h), qf[ks], z);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(vt, 32 * t + col, ks, h), gf[ks], e);
+                const int jt = j0 + 32 * t;
+                const float d0 = pos - (float)jt - (float)(4 * h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    float x = z[r], u = 1.f;
+                    if constexpr (CAP) {
+                        x = tanh_of(x * sm.k1, F32);
+                        u = 1.f - x * x;
+                    }
+                    if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 - (float)tile_row(r, 0)), x);
+                    const float pr = __builtin_amdgcn_exp2f(fmaf(x, sm.c, -lse2));
+                    e[r] = pr * (e[r] - delta) * u;
+                }
+                uint32_t seen = 0;
+                if (!wave_all) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = jt + tile_row(r, h);
+                        bool ok = (j >= lo && j < hi) || j < prefix;
+                        if (docs) {
+                            const int dk = j < a.len_k ? docs[j] : -1;
+                            ok = ok && dk == my_doc && dk >= 0;
+                        }
+                        e[r] = ok ? e[r] : 0.f;
+                        seen |= (uint32_t)ok << tile_row(r, h);
+                    }
+                }
+                if (apart) {
+                    add_rows<T, DT>(dq, e, seen | __shfl_xor(seen, 32), kt, 32 * t);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const Frag<T> ef = to_frag<T>(e, s);
+#pragma unroll
+                        for (int dt = 0; dt < DS; ++dt)
+                            dq[dt] = mma(Lds::column_frag(kt, 32 * t + 16 * s, dt, lane), ef, dq[dt]);
+                    }
+                }
+            }
+        }
+        wait_lgkm();
+        cur = next;
+        wave_any = sched.wave_any;
+        wave_all = sched.wave_all;
+        stage ^= 1;
+    }
+    if (!row) return;
+    T *out = (T *)a.dq.p + b * a.dq.sb + (int64_t)i * a.dq.sl + hq * a.dq.sh;
+    store_columns<T, DS>(out, dq, m.scale, h, D);
+}
+
+// ---------------------------------------------------------------- dK, dV
+
+template <typename T, int DT, int MODS>
+__global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionArgs a)
+{
+    constexpr int BQ = sizeof(T) == 2 ? 64 : 32, NW = 4, BN = 32 * NW, KS = DT / 16, DS = DT / 32;
+    constexpr bool CAP = MODS & 1, BIAS = MODS & 2, F32 = sizeof(T) == 4;
+    typedef Tile<T, DT> Lds;
+    __shared__ __align__(16) uint8_t smem[2][2][BQ * Lds::kRowBytes];
+    __shared__ __align__(16) float rows[2][2][BQ];             // lse, delta
+
+    const AttentionMask &m = a.mask;
+    const uint32_t tiles = (a.len_k + BN - 1) / BN;
+    uint32_t head, kt;
+    head_tile(blockIdx.x, gridDim.x, tiles, head, kt);
+    const int b = head / a.heads_kv, hk = head % a.heads_kv, group = a.heads_q / a.heads_kv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = lane >> 5, col = lane & 31;
+    const int shift = a.len_k - a.len_q, D = a.dim;
+    const int j0 = kt * BN, jw = j0 + wave * 32, j = jw + col;
+    const bool key = j < a.len_k;
+
+    const T *k = (const T *)a.k.p + b * a.k.sb + (int64_t)j * a.k.sl + hk * a.k.sh;
+    const T *v = (const T *)a.v.p + b * a.v.sb + (int64_t)j * a.v.sl + hk * a.v.sh;
+    Frag<T> kf[KS], vf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        kf[ks] = global_frag<T>(k, key, ks, h, D);
+        vf[ks] = global_frag<T>(v, key, ks, h, D);
+    }
+    const int prefix = m.prefix ? min(max(m.prefix[b], 0), a.len_k) : 0;
+    const int32_t *docs = m.documents ? m.documents + (int64_t)b * a.len_k : nullptr;
+    const int2 *ranges = a.ranges + (int64_t)b * ((a.len_k + 63) / 64);
+    const int j1 = min(j0 + BN, a.len_k) - 1, jw1 = min(jw + 32, a.len_k) - 1;
+    int2 dg = make_int2(0, 0), dw = dg;
+    int my_doc = 0;
+    if (docs) {
+        dg = range_of(ranges, j0, j1);
+        if (jw1 >= jw) dw = range_of(ranges, jw, jw1);
+        my_doc = key ? docs[j] : -1;
+    }
+    int lo, hi;
+    seen_by_key(m, prefix, j, lo, hi);
+    hi = min(hi, a.len_k);                                     // (queries end at position len_k)
+
+    // tiles of query rows [t BQ, ..); all rows of a tile are queries only where it is whole
+    const int end = (a.len_q + BQ - 1) / BQ;
+    auto see = [&](int t, Seen &s, Seen &w) {
+        const int p0 = t * BQ + shift, p1 = min(t * BQ + BQ, a.len_q) - 1 + shift;
+        const int2 dq = docs ? range_of(ranges, p0, p1) : make_int2(0, 0);
+        s = classify(m, prefix, p0, p1, j0, j1, dq.x, dq.y, dg.x, dg.y);
+        if (jw1 >= jw) {
+            w = classify(m, prefix, p0, p1, jw, jw1, dq.x, dq.y, dw.x, dw.y);
+            w.all = w.all && t * BQ + BQ <= a.len_q;
+        }
+    };
+    if (D < DT) {
+        Lds::template clear<NW * 64>(smem[0][0], sizeof(smem));
+        __syncthreads();
+    }
+    v16f dk[DS] = {}, dv[DS] = {};
+    for (int gh = 0; gh < group; ++gh) {
+        const int hq = hk * group + gh;
+        const T *q = (const T *)a.q.p + b * a.q.sb + hq * a.q.sh;
+        const T *g = (const T *)a.dout.p + b * a.dout.sb + hq * a.dout.sh;
+        const float *lse = a.lse + ((int64_t)b * a.heads_q + hq) * a.len_q;
+        const float *delta = a.delta + ((int64_t)b * a.heads_q + hq) * a.len_q;
+        const ScoreMap sm = score_map(m, hq);
+        auto fetch = [&](int st, int t) {
+            Lds::template load<BQ, NW * 64>(smem[st][0], q, a.q.sl, t * BQ, a.len_q, D);
+            Lds::template load<BQ, NW * 64>(smem[st][1], g, a.dout.sl, t * BQ, a.len_q, D);
+            // (repeats the last row's past the end: those rows are masked)
+            if (wave < 2 && lane < BQ) {
+                const int i = min(t * BQ + lane, a.len_q - 1);
+                lds_dma4(reinterpret_cast<const uint8_t *>((wave ? delta : lse) + i),
+                         __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(
+                             __attribute__((address_space(3))) const float *)rows[st][wave]));
+            }
+        };
+        Schedule sched;
+        int cur = sched.next(end, see), stage = 0;
+        bool wave_any = sched.wave_any, wave_all = sched.wave_all;
+        if (cur >= 0) fetch(0, cur);
+        while (cur >= 0) {
+            wait_vmcnt<0>();
+            block_barrier();
+            const int next = sched.next(end, see);
+            if (next >= 0) fetch(stage ^ 1, next);
+            if (wave_any) {
+                const uint8_t *qt = smem[stage][0], *gt = smem[stage][1];
+                const int i0 = cur * BQ;
+                const bool apart = !wave_all && (Lds::template non_finite<BQ>(qt) || Lds::template non_finite<BQ>(gt));
+#pragma unroll 1
+                for (int t = 0; t < BQ / 32; ++t) {
+                    v16f z = {}, e = {};
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(qt, 32 * t + col, ks, h), kf[ks], z);
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(gt, 32 * t + col, ks, h), vf[ks], e);
+                    const int p0 = i0 + 32 * t + shift;
+                    const float d0 = (float)(p0 + 4 * h) - (float)j;
+#pragma unroll
+                    for (int x4 = 0; x4 < 4; ++x4) {
+                        const v4f l4 = *reinterpret_cast<const v4f *>(&rows[stage][0][32 * t + tile_row(4 * x4, h)]);
+                        const v4f e4 = *reinterpret_cast<const v4f *>(&rows[stage][1][32 * t + tile_row(4 * x4, h)]);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const int r = 4 * x4 + y;
+                            float x = z[r], u = 1.f;
+                            if constexpr (CAP) {
+                                x = tanh_of(x * sm.k1, F32);
+                                u = 1.f - x * x;
+                            }
+                            if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 + (float)tile_row(r, 0)), x);
+                            z[r] = __builtin_amdgcn_exp2f(fmaf(x, sm.c, -l4[y] * kLog2e));
+                            e[r] = z[r] * (e[r] - e4[y]) * u;
+                        }
+                    }
+                    uint32_t seen = 0;
+                    if (!wave_all) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int pr = p0 + tile_row(r, h);
+                            bool ok = pr >= lo && pr < hi;
+                            if (docs) {
+                                const int dq = pr >= 0 && pr < a.len_k ? docs[pr] : -1;
+                                ok = ok && dq == my_doc && dq >= 0;
+                            }
+                            z[r] = ok ? z[r] : 0.f;
+                            e[r] = ok ? e[r] : 0.f;
+                            seen |= (uint32_t)ok << tile_row(r, h);
+                        }
+                    }
+                    if (apart) {
+                        const uint32_t both = seen | __shfl_xor(seen, 32);
+                        add_rows<T, DT>(dv, z, both, gt, 32 * t);
+                        add_rows<T, DT>(dk, e, both, qt, 32 * t);
+                    } else {
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) {
+                            const Frag<T> pf = to_frag<T>(z, s), ef = to_frag<T>(e, s);
+#pragma unroll
+                            for (int dt = 0; dt < DS; ++dt) {
+                                dv[dt] = mma(Lds::column_frag(gt, 32 * t + 16 * s, dt, lane), pf, dv[dt]);
+                                dk[dt] = mma(Lds::column_frag(qt, 32 * t + 16 * s, dt, lane), ef, dk[dt]);
+                            }
+                        }
+                    }
+                }
+            }
+            wait_lgkm();
+            cur = next;
+            wave_any = sched.wave_any;
+            wave_all = sched.wave_all;
+            stage ^= 1;
+        }
+        block_barrier();           // the next head's first tile takes stage 0
+    }
+    if (!key) return;
+    store_columns<T, DS>((T *)a.dk.p + b * a.dk.sb + (int64_t)j * a.dk.sl + hk * a.dk.sh, dk, m.scale, h, D);
+    store_columns<T, DS>((T *)a.dv.p + b * a.dv.sb + (int64_t)j * a.dv.sl + hk * a.dv.sh, dv, 1.f, h, D);
+}
+
+template <typename T, int DT, int MODS>
+hipError_t launch(const AttentionArgs &a, hipStream_t stream)
+{
+    const int64_t nq = (int64_t)((a.len_q + 127) / 128) * a.heads_q * a.batch;
+    const int64_t nk = (int64_t)((a.len_k + 127) / 128) * a.heads_kv * a.batch;
+    if (nq > INT32_MAX || nk > INT32_MAX) return hipErrorInvalidConfiguration;
+    attention_dkv_kernel<T, DT, MODS><<<(uint32_t)nk, 256, 0, stream>>>(a);
+    attention_dq_kernel<T, DT, MODS><<<(uint32_t)nq, 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, int DT>
+hipError_t launch_mods(const AttentionArgs &a, hipStream_t stream)
+{
+    switch ((a.mask.cap > 0.f ? 1 : 0) | (a.mask.slopes ? 2 : 0)) {
+    case 0: return launch<T, DT, 0>(a, stream);
+    case 1: return launch<T, DT, 1>(a, stream);
+    case 2: return launch<T, DT, 2>(a, stream);
+    default: return launch<T, DT, 3>(a, stream);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_document_ranges(const AttentionArgs &a, hipStream_t stream)
+{
+    const int64_t n = (int64_t)a.batch * ((a.len_k + 63) / 64);
+    if (n > INT32_MAX) return hipErrorInvalidConfiguration;
+    document_ranges_kernel<<<(uint32_t)n, 64, 0, stream>>>(a.mask.documents, a.len_k, a.ranges);
+    return hipGetLastError();
+}
+
+hipError_t launch_attention_bwd(const AttentionArgs &a, bool f32, hipStream_t stream)
+{
+    if (a.mask.documents) {
+        const hipError_t e = launch_document_ranges(a, stream);
+        if (e != hipSuccess) return e;
+    }
+    const int64_t rows = ((int64_t)a.batch * a.heads_q * a.len_q + 15) / 16;
+    if (rows > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (f32) attention_delta_kernel<float><<<(uint32_t)rows, 256, 0, stream>>>(a);
+    else attention_delta_kernel<__bf16><<<(uint32_t)rows, 256, 0, stream>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (f32) return a.dim <= 64 ? launch_mods<float, 64>(a, stream) : launch_mods<float, 128>(a, stream);
+    return a.dim <= 64 ? launch_mods<__bf16, 64>(a, stream) : launch_mods<__bf16, 128>(a, stream);
+}
+
+}  // namespace q2d
