@@ -427,6 +427,92 @@ q2d_status q2d_attention_fwd(const q2d_attention *a, void *workspace, int64_t wo
 q2d_status q2d_attention_bwd(const q2d_attention *a, const q2d_heads *dout, const q2d_heads *dq, const q2d_heads *dk,
                              const q2d_heads *dv, void *workspace, int64_t workspace_bytes, hipStream_t stream);
 
+/*
+ * Paged key/value cache in 8 bits: E4M3 codes with one power-of-two scale (E8M0 byte) for
+ * each block of 32 tokens and head, keys and values apart.  A page holds page_size tokens of
+ * every head, page_size a multiple of 32; token t of a sequence lies in its page t /
+ * page_size.  Codes of a block are x / 2^(byte - 127) rounded to nearest even, the byte
+ * being the smallest with 448 * 2^(byte - 127) >= the block's largest magnitude (the MXFP8
+ * rule, over 32 tokens x dim); a block that has been given an infinity or a NaN has byte
+ * 0xFF and zero codes, and its values are NaN.
+ *   k_codes   [pages][heads][page_size][dim]
+ *   v_codes_t [pages][heads][page_size / 32][dim][32]   values transposed in their block
+ *   k_scales, v_scales [pages][heads][page_size / 32]
+ * Buffers are device memory on 16-byte boundaries.  dim is a multiple of 16 up to 128.
+ */
+typedef struct {
+    int32_t pages, heads, dim, page_size;
+    uint8_t *k_codes, *v_codes_t, *k_scales, *v_scales;
+} q2d_kv_cache;
+
+/* Fill `c` (pointers NULL) and, if `bytes` is not NULL, the sizes of its four buffers.  Host
+ * only.  Q2D_EINVAL for sizes <= 0 or a page_size that is no multiple of 32;
+ * Q2D_EUNSUPPORTED for a dim that is no multiple of 16 or above 128, a page_size above 65536
+ * or more than 2^31 - 1 blocks. */
+q2d_status q2d_kv_cache_init(q2d_kv_cache *c, int32_t pages, int32_t heads, int32_t dim, int32_t page_size,
+                             int64_t bytes[4]);
+
+/*
+ * The sequences of a call on the cache.  Sequence b has lens[b] tokens, the call's own among
+ * them; these are its last n_b, at rows offsets[b] .. offsets[b + 1] of the token tensors
+ * (offsets NULL: tokens / batch rows each, in order).  Its token t is in page
+ * table[b * table_stride + t / page_size].
+ *
+ * All three arrays are read on the device, where they cannot be checked before a launch:
+ * offsets are clamped to [0, tokens] and each to the one before it, lens to [0, table_pages *
+ * page_size], and a table entry outside [0, pages) names no page: its tokens are not
+ * written, read back as nothing and not seen.
+ */
+typedef struct {
+    int32_t batch, table_pages;  /* table_pages: entries of a table row */
+    int64_t tokens, table_stride;
+    const int64_t *offsets;      /* device [batch + 1], ascending, or NULL */
+    const int32_t *lens;         /* device [batch] */
+    const int32_t *table;        /* device [batch][table_stride] */
+} q2d_sequences;
+
+/*
+ * Append: quantizes k and v [tokens][heads][dim] (dtype dt; strides of tokens and heads in
+ * elements, unit stride along dim, 16-byte rows) into the cache at positions [lens[b] - n_b,
+ * lens[b]).  A block that holds earlier tokens keeps its scale or, where a new token needs a
+ * larger one, takes that: the earlier codes are then rounded to it.  What a block held
+ * behind the new tokens is void.  No block may belong to two sequences of the call.
+ */
+q2d_status q2d_kv_write(const q2d_kv_cache *c, const q2d_sequences *s, q2d_dtype dt, const void *k, int64_t k_stride_token,
+                        int64_t k_stride_head, const void *v, int64_t v_stride_token, int64_t v_stride_head,
+                        hipStream_t stream);
+
+/* Read back: the values of the tokens at positions [lens[b] - n_b, lens[b]) into k and v
+ * (layouts as in q2d_kv_write; exact in Q2D_F32 and, within its range, in Q2D_BF16). */
+q2d_status q2d_kv_read(const q2d_kv_cache *c, const q2d_sequences *s, q2d_dtype dt, void *k, int64_t k_stride_token,
+                       int64_t k_stride_head, void *v, int64_t v_stride_token, int64_t v_stride_head,
+                       hipStream_t stream);
+
+/*
+ * Attention of the call's tokens, q [tokens][heads_q][dim], over the cache: query i of
+ * sequence b is at position p = lens[b] - n_b + i and sees key j < lens[b] where j < prefix
+ * or (j <= p and (window == 0 or p - j < window)).  Scores, softcap, slopes, window and
+ * prefix as in q2d_attention, with the values that the codes stand for.  The call's own
+ * keys and values have to be in the cache (q2d_kv_write).  q and out are bfloat16
+ * (Q2D_EUNSUPPORTED otherwise); sums and statistics are float32, probabilities are rounded
+ * to bfloat16 for the second product.
+ */
+typedef struct {
+    int32_t dtype, heads_q;
+    float scale, softcap;
+    int64_t window;
+    const float *slopes;         /* device [heads_q], or NULL */
+    const int32_t *prefix;       /* device [batch], or NULL */
+    const void *q;   int64_t q_stride_token, q_stride_head;
+    void *out;       int64_t out_stride_token, out_stride_head;
+} q2d_cached_attention;
+
+/* Bytes of device workspace for a call of these sizes, possibly 0; -1 for invalid sizes. */
+int64_t q2d_attention_cached_workspace(const q2d_kv_cache *c, const q2d_sequences *s, int32_t heads_q);
+
+q2d_status q2d_attention_cached(const q2d_kv_cache *c, const q2d_sequences *s, const q2d_cached_attention *a,
+                                void *workspace, int64_t workspace_bytes, hipStream_t stream);
+
 /* Static description of a status code (never NULL). */
 const char *q2d_status_string(q2d_status s);
 

@@ -19,7 +19,7 @@ __all__ = [
     "q2d_tensor_init", "q2d_quantize", "q2d_quantize_1d", "mxfp8_quantize", "q2d_gemm",
     "q2d_linear_fwd", "q2d_linear_bwd", "q2d_grouped_tensor_init", "q2d_grouped_quantize",
     "q2d_grouped_gemm", "q2d_dequantize", "q2d_gemm_quantized", "q2d_status_string",
-    "q2d_attention_fwd", "q2d_attention_bwd",
+    "q2d_attention_fwd", "q2d_attention_bwd", "KVCache", "q2d_kv_write", "q2d_kv_read", "q2d_attention_cached",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -431,4 +431,5 @@ def q2d_grouped_gemm(A: QTensor, transA: int, B: QTensor, transB: int, seg_offse
 
 
 # (at the end: these modules use the names above)
-from .attention import q2d_attention_bwd, q2d_attention_fwd  # noqa: E402
+from .attention import (KVCache, q2d_attention_bwd, q2d_attention_cached, q2d_attention_fwd,  # noqa: E402
+                        q2d_kv_read, q2d_kv_write)

@@ -1,5 +1,6 @@
 """Attention operators of the binding (argument marshalling only): whole sequences forward
-and backward.  The definitions stand in ``include/q2d.h``."""
+and backward, and new tokens over a paged 8-bit key/value cache.  The definitions stand in
+``include/q2d.h``."""
 from __future__ import annotations
 
 import ctypes
@@ -25,11 +26,41 @@ class _Attention(ctypes.Structure):
                 ("q", _Heads), ("k", _Heads), ("v", _Heads), ("out", _Heads), ("lse", ctypes.c_void_p)]
 
 
+class _Cache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("k_codes", ctypes.c_void_p), ("v_codes_t", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class _Sequences(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("table_pages", ctypes.c_int32), ("tokens", ctypes.c_int64),
+                ("table_stride", ctypes.c_int64), ("offsets", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("table", ctypes.c_void_p)]
+
+
+class _CachedAttention(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("heads_q", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("softcap", ctypes.c_float), ("window", ctypes.c_int64), ("slopes", ctypes.c_void_p),
+                ("prefix", ctypes.c_void_p),
+                ("q", ctypes.c_void_p), ("q_stride_token", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("out_stride_token", ctypes.c_int64), ("out_stride_head", ctypes.c_int64)]
+
+
 _P, _I64, _I32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
 _AP, _HP = ctypes.POINTER(_Attention), ctypes.POINTER(_Heads)
 _lib.q2d_attention_workspace.argtypes, _lib.q2d_attention_workspace.restype = [_AP, _I32], _I64
 _lib.q2d_attention_fwd.argtypes, _lib.q2d_attention_fwd.restype = [_AP, _P, _I64, _P], _I32
 _lib.q2d_attention_bwd.argtypes, _lib.q2d_attention_bwd.restype = [_AP, _HP, _HP, _HP, _HP, _P, _I64, _P], _I32
+
+_CP, _SP = ctypes.POINTER(_Cache), ctypes.POINTER(_Sequences)
+_lib.q2d_kv_cache_init.argtypes = [_CP, _I32, _I32, _I32, _I32, ctypes.POINTER(_I64)]
+_lib.q2d_kv_cache_init.restype = _I32
+for _name in ("q2d_kv_write", "q2d_kv_read"):
+    getattr(_lib, _name).argtypes = [_CP, _SP, _I32, _P, _I64, _I64, _P, _I64, _I64, _P]
+    getattr(_lib, _name).restype = _I32
+_lib.q2d_attention_cached_workspace.argtypes, _lib.q2d_attention_cached_workspace.restype = [_CP, _SP, _I32], _I64
+_lib.q2d_attention_cached.argtypes = [_CP, _SP, ctypes.POINTER(_CachedAttention), _P, _I64, _P]
+_lib.q2d_attention_cached.restype = _I32
 
 
 def _vector(t, n, dtype, device, what):
@@ -138,3 +169,116 @@ def q2d_attention_bwd(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
     _check(_lib.q2d_attention_bwd(ctypes.byref(a), *[ctypes.byref(x) for x in g], ws, max(sizes[1], 0),
                                   _stream(q.device)), "q2d_attention_bwd")
     return dq, dk, dv
+
+
+class KVCache:
+    """A paged key/value cache in 8 bits: E4M3 codes with one power-of-two scale for each
+    block of 32 tokens and head.  ``pages`` pages of ``page_size`` tokens (a multiple of 32)
+    are shared by all sequences; which page holds which tokens is the caller's page table.
+
+    ``k_codes`` [pages, heads, page_size, dim], ``v_codes_t`` [pages, heads, page_size / 32,
+    dim, 32] (values transposed in their block), ``k_scales`` and ``v_scales`` [pages, heads,
+    page_size / 32], all uint8 and zeroed here."""
+
+    def __init__(self, pages: int, heads: int, dim: int, page_size: int = 64, device="cuda"):
+        self.desc = _Cache()
+        _check(_lib.q2d_kv_cache_init(ctypes.byref(self.desc), int(pages), int(heads), int(dim), int(page_size), None),
+               "q2d_kv_cache_init")
+        self._ref = ctypes.byref(self.desc)
+        self.pages, self.heads, self.dim, self.page_size = int(pages), int(heads), int(dim), int(page_size)
+        self.device = torch.device(device)
+        blocks = self.page_size // 32
+        shapes = {"k_codes": (pages, heads, page_size, dim), "v_codes_t": (pages, heads, blocks, dim, 32),
+                  "k_scales": (pages, heads, blocks), "v_scales": (pages, heads, blocks)}
+        for name, shape in shapes.items():
+            t = torch.zeros(shape, dtype=torch.uint8, device=self.device)
+            setattr(self, name, t)
+            setattr(self.desc, name, t.data_ptr())
+
+
+def _sequences(cache, table, lens, tokens, offsets):
+    if not isinstance(cache, KVCache):
+        raise Q2DError("expected a KVCache")
+    if table.dim() != 2 or table.dtype != torch.int32 or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise Q2DError("block_table: an int32 tensor [sequences, pages] with unit column stride is expected")
+    _same_device(cache.device, table)
+    batch = table.shape[0]
+    s = _Sequences(batch=batch, table_pages=table.shape[1], tokens=tokens,
+                   table_stride=table.stride(0) if batch > 1 else max(table.stride(0), table.shape[1]))
+    s.table = table.data_ptr()
+    s.lens = _vector(lens, batch, torch.int32, cache.device, "lens")
+    s.offsets = _vector(offsets, batch + 1, torch.int64, cache.device, "offsets")
+    return s
+
+
+def _token_rows(t, heads, dim, device, what):
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.stride(2) != 1:
+        raise Q2DError("%s: a [tokens, %d, %d] tensor with unit stride along the last dimension is expected"
+                       % (what, heads, dim))
+    _same_device(device, t)
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def q2d_kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor,
+                 offsets: torch.Tensor | None = None) -> KVCache:
+    """Append the tokens of k and v [tokens, heads, dim] to the cache.
+
+    lens (int32 [sequences]) counts each sequence's tokens with the new ones; the new ones are
+    rows offsets[b] .. offsets[b + 1] (int64 [sequences + 1]; None: equally many each, in
+    order).  block_table (int32 [sequences, pages]) names the pages."""
+    if k.dim() != 3 or k.shape != v.shape or k.dtype != v.dtype:
+        raise Q2DError("expected k and v as [tokens, heads, dim] of one dtype")
+    s = _sequences(cache, block_table, lens, k.shape[0], offsets)
+    _check(_lib.q2d_kv_write(cache._ref, ctypes.byref(s), _dtype_code(k.dtype),
+                             *_token_rows(k, cache.heads, cache.dim, cache.device, "k"),
+                             *_token_rows(v, cache.heads, cache.dim, cache.device, "v"), _stream(cache.device)),
+           "q2d_kv_write")
+    return cache
+
+
+def q2d_kv_read(cache: KVCache, block_table: torch.Tensor, lens: torch.Tensor, tokens: int,
+                offsets: torch.Tensor | None = None, out_dtype=torch.float32,
+                k: torch.Tensor | None = None, v: torch.Tensor | None = None):
+    """Values (k, v) [tokens, heads, dim] of each sequence's last tokens (offsets as in
+    q2d_kv_write, ``tokens`` in all)."""
+    shape = (int(tokens), cache.heads, cache.dim)
+    k = torch.empty(shape, dtype=out_dtype, device=cache.device) if k is None else k
+    v = torch.empty(shape, dtype=k.dtype, device=cache.device) if v is None else v
+    if k.shape != v.shape or k.dtype != v.dtype or k.dim() != 3 or k.shape[0] != int(tokens):
+        raise Q2DError("expected k and v as [tokens, heads, dim] of one dtype")
+    s = _sequences(cache, block_table, lens, int(tokens), offsets)
+    _check(_lib.q2d_kv_read(cache._ref, ctypes.byref(s), _dtype_code(k.dtype),
+                            *_token_rows(k, cache.heads, cache.dim, cache.device, "k"),
+                            *_token_rows(v, cache.heads, cache.dim, cache.device, "v"), _stream(cache.device)),
+           "q2d_kv_read")
+    return k, v
+
+
+def q2d_attention_cached(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, lens: torch.Tensor,
+                         offsets: torch.Tensor | None = None, scale: float | None = None, window: int = 0,
+                         softcap: float = 0.0, slopes: torch.Tensor | None = None,
+                         prefix: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Causal attention of each sequence's last tokens, q [tokens, heads_q, dim] in bfloat16,
+    over its keys and values in the cache, these tokens' own among them.  offsets, lens and
+    block_table as in q2d_kv_write; scale, window, softcap, slopes and prefix as in
+    q2d_attention_fwd."""
+    if q.dim() != 3:
+        raise Q2DError("expected q as [tokens, heads, dim]")
+    s = _sequences(cache, block_table, lens, q.shape[0], offsets)
+    heads = q.shape[1]
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if out.dtype != q.dtype or out.shape != q.shape:
+        raise Q2DError("out: the shape and dtype of q are expected")
+    a = _CachedAttention(dtype=_dtype_code(q.dtype), heads_q=heads,
+                         scale=cache.dim ** -0.5 if scale is None else float(scale), softcap=float(softcap),
+                         window=int(window))
+    a.slopes = _vector(slopes, heads, torch.float32, cache.device, "slopes")
+    a.prefix = _vector(prefix, s.batch, torch.int32, cache.device, "prefix")
+    a.q, a.q_stride_token, a.q_stride_head = _token_rows(q, heads, cache.dim, cache.device, "q")
+    a.out, a.out_stride_token, a.out_stride_head = _token_rows(out, heads, cache.dim, cache.device, "out")
+    size = _lib.q2d_attention_cached_workspace(cache._ref, ctypes.byref(s), heads)
+    keep, ws = _workspace(size, cache.device)
+    _check(_lib.q2d_attention_cached(cache._ref, ctypes.byref(s), ctypes.byref(a), ws, max(size, 0),
+                                     _stream(cache.device)), "q2d_attention_cached")
+    return out

@@ -37,4 +37,48 @@ hipError_t launch_document_ranges(const AttentionArgs &a, hipStream_t stream);
 hipError_t launch_attention_fwd(const AttentionArgs &a, bool f32, hipStream_t stream);
 hipError_t launch_attention_bwd(const AttentionArgs &a, bool f32, hipStream_t stream);
 
+// A paged cache of E4M3 keys and values: one scale byte for each block of 32 tokens and
+// head; keys [page][head][token][dim], values transposed in their block
+// [page][head][block][dim][32].
+struct CacheView {
+    uint8_t *k, *v, *ks, *vs;
+    int32_t pages, heads, dim, page_blocks;      // blocks of 32 tokens a page
+};
+
+// Sequences whose last n[b] = offsets[b + 1] - offsets[b] tokens a call works on (offsets
+// null: tokens / batch each); lens[b]: tokens of the sequence, table[b][i]: its pages
+struct SequencesView {
+    const int64_t *offsets;
+    const int32_t *lens, *table;
+    int64_t table_stride;
+    int32_t table_pages, batch;
+    int64_t tokens;
+};
+
+struct CacheCopyArgs {
+    CacheView cache;
+    SequencesView seq;
+    void *k, *v;
+    int64_t k_st, k_sh, v_st, v_sh;              // strides of tokens and heads, elements
+};
+
+struct CachedArgs {
+    CacheView cache;
+    SequencesView seq;
+    const void *q;
+    void *out;
+    int64_t q_st, q_sh, out_st, out_sh;
+    AttentionMask mask;
+    int32_t heads_q;
+    int32_t splits;                              // parts of a sequence's tokens
+    int32_t wide;                                // 64 query rows a workgroup, not 16
+    int64_t tiles;                               // bound of the query tiles of all sequences
+    float *part;                                 // workspace: [tile][head][split][rows][dim] sums,
+    float *stat;                                 // [tile][head][split][rows] maximum and sum
+};
+
+hipError_t launch_kv_write(const CacheCopyArgs &a, bool f32, hipStream_t stream);
+hipError_t launch_kv_read(const CacheCopyArgs &a, bool f32, hipStream_t stream);
+hipError_t launch_attention_cached(const CachedArgs &a, hipStream_t stream);
+
 }  // namespace q2d

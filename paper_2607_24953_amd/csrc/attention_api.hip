@@ -110,6 +110,94 @@ q2d_status check_workspace(int64_t need, const void *workspace, int64_t bytes)
     return Q2D_OK;
 }
 
+inline bool on4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+
+q2d_status check_cache_sizes(const q2d_kv_cache &c)
+{
+    if (c.pages <= 0 || c.heads <= 0 || c.dim <= 0 || c.page_size <= 0 || c.page_size % 32 != 0) return Q2D_EINVAL;
+    if (c.dim % 16 != 0 || c.dim > 128 || c.page_size > 65536 || c.heads > 16384) return Q2D_EUNSUPPORTED;
+    int64_t blocks;
+    if (__builtin_mul_overflow((int64_t)c.pages * c.heads, (int64_t)(c.page_size / 32), &blocks) || blocks > INT32_MAX)
+        return Q2D_EUNSUPPORTED;
+    return Q2D_OK;
+}
+
+q2d_status check_cache(const q2d_kv_cache *c)
+{
+    if (!c) return Q2D_EINVAL;
+    const q2d_status s = check_cache_sizes(*c);
+    if (s != Q2D_OK) return s;
+    if (!c->k_codes || !c->v_codes_t || !c->k_scales || !c->v_scales || !on16(c->k_codes) || !on16(c->v_codes_t))
+        return Q2D_EINVAL;
+    return Q2D_OK;
+}
+
+q2d_status check_sequence_sizes(const q2d_sequences *s)
+{
+    if (!s || s->batch <= 0 || s->tokens < 0 || s->table_pages <= 0 || s->table_stride < s->table_pages) return Q2D_EINVAL;
+    if (!s->offsets && s->tokens % s->batch != 0) return Q2D_EINVAL;
+    if (s->tokens > kMaxLen || s->batch > (1 << 20) || s->table_stride > kMaxLen) return Q2D_EUNSUPPORTED;
+    return Q2D_OK;
+}
+
+q2d_status check_sequences(const q2d_sequences *s)
+{
+    const q2d_status r = check_sequence_sizes(s);
+    if (r != Q2D_OK) return r;
+    if (!s->lens || !s->table || !on4(s->lens) || !on4(s->table) || (reinterpret_cast<uintptr_t>(s->offsets) & 7) != 0)
+        return Q2D_EINVAL;
+    return Q2D_OK;
+}
+
+// [tokens][heads][dim] rows of whole 16 bytes
+q2d_status check_rows(const void *p, int64_t tokens, int64_t st, int64_t heads, int64_t sh, int64_t dim, int per, bool output)
+{
+    const q2d_heads u = {const_cast<void *>(p), st, 0, sh};
+    return output ? check_output(u, tokens, 1, heads, dim, per) : check_heads(u, tokens, 1, heads, dim, per);
+}
+
+CacheView cache_view(const q2d_kv_cache *c)
+{
+    return {c->k_codes, c->v_codes_t, c->k_scales, c->v_scales, c->pages, c->heads, c->dim, c->page_size / 32};
+}
+
+SequencesView sequences_view(const q2d_sequences *s)
+{
+    return {s->offsets, s->lens, s->table, s->table_stride, s->table_pages, s->batch, s->tokens};
+}
+
+struct CachedSplit {
+    int32_t splits, wide;
+    int64_t tiles, stat_at, bytes;
+};
+
+// Query tiles of 16 rows where the sequences have no more on average (decoding), of 64
+// otherwise; and enough parts of the sequences' tokens to give each compute unit a few
+// workgroups, none below four super-blocks of 64 tokens, one a wave.
+CachedSplit split_cached(const q2d_kv_cache *c, const q2d_sequences *s, int32_t heads_q)
+{
+    CachedSplit p;
+    const int64_t group = heads_q / c->heads;
+    p.wide = s->tokens * group > 16 * (int64_t)s->batch;
+    const int64_t rows = p.wide ? 64 : 16;
+    if (s->offsets) {
+        const int64_t some = s->tokens < s->batch ? s->tokens : s->batch, each = s->tokens * ((group + rows - 1) / rows);
+        p.tiles = s->tokens * group / rows + some;
+        if (each < p.tiles) p.tiles = each;
+    } else {
+        p.tiles = s->batch * ((s->tokens / s->batch * group + rows - 1) / rows);
+    }
+    const int64_t units = p.tiles * c->heads, longest = (int64_t)s->table_pages * c->page_size;
+    int64_t n = units > 0 ? (1024 + units - 1) / units : 1;
+    if (n > (longest + 255) / 256) n = (longest + 255) / 256;
+    if (n > 64) n = 64;
+    p.splits = (int32_t)(n < 1 ? 1 : n);
+    const int64_t parts = p.splits > 1 ? units * p.splits * rows : 0;
+    p.stat_at = up256(parts * c->dim * 4);
+    p.bytes = p.stat_at + up256(parts * 8);
+    return p;
+}
+
 }  // namespace
 
 extern "C" {
@@ -145,6 +233,101 @@ q2d_status q2d_attention_bwd(const q2d_attention *a, const q2d_heads *dout, cons
     AttentionArgs r = make_args(a, workspace);
     r.dout = view(*dout); r.dq = view(*dq); r.dk = view(*dk); r.dv = view(*dv);
     if (launch_attention_bwd(r, a->dtype == Q2D_F32, stream) != hipSuccess) return Q2D_ELAUNCH;
+    return Q2D_OK;
+}
+
+q2d_status q2d_kv_cache_init(q2d_kv_cache *c, int32_t pages, int32_t heads, int32_t dim, int32_t page_size,
+                             int64_t bytes[4])
+{
+    if (!c) return Q2D_EINVAL;
+    q2d_kv_cache t = {};
+    t.pages = pages; t.heads = heads; t.dim = dim; t.page_size = page_size;
+    const q2d_status s = check_cache_sizes(t);
+    if (s != Q2D_OK) return s;
+    *c = t;
+    if (bytes) {
+        const int64_t blocks = (int64_t)pages * heads * (page_size / 32);
+        bytes[0] = bytes[1] = blocks * 32 * dim;
+        bytes[2] = bytes[3] = blocks;
+    }
+    return Q2D_OK;
+}
+
+static q2d_status kv_copy(const q2d_kv_cache *c, const q2d_sequences *s, q2d_dtype dt, const void *k, int64_t kst,
+                          int64_t ksh, const void *v, int64_t vst, int64_t vsh, bool write, hipStream_t stream)
+{
+    q2d_status r = check_cache(c);
+    if (r == Q2D_OK) r = check_sequences(s);
+    if (r != Q2D_OK) return r;
+    if (dt != Q2D_F32 && dt != Q2D_BF16) return Q2D_EINVAL;
+    const int per = dt == Q2D_F32 ? 4 : 8;
+    if (s->tokens == 0) return Q2D_OK;
+    r = check_rows(k, s->tokens, kst, c->heads, ksh, c->dim, per, !write);
+    if (r == Q2D_OK) r = check_rows(v, s->tokens, vst, c->heads, vsh, c->dim, per, !write);
+    if (r != Q2D_OK) return r;
+    CacheCopyArgs a = {};
+    a.cache = cache_view(c);
+    a.seq = sequences_view(s);
+    a.k = const_cast<void *>(k); a.k_st = kst; a.k_sh = ksh;
+    a.v = const_cast<void *>(v); a.v_st = vst; a.v_sh = vsh;
+    const hipError_t e = write ? launch_kv_write(a, dt == Q2D_F32, stream) : launch_kv_read(a, dt == Q2D_F32, stream);
+    return e == hipSuccess ? Q2D_OK : Q2D_ELAUNCH;
+}
+
+q2d_status q2d_kv_write(const q2d_kv_cache *c, const q2d_sequences *s, q2d_dtype dt, const void *k, int64_t k_stride_token,
+                        int64_t k_stride_head, const void *v, int64_t v_stride_token, int64_t v_stride_head,
+                        hipStream_t stream)
+{
+    return kv_copy(c, s, dt, k, k_stride_token, k_stride_head, v, v_stride_token, v_stride_head, true, stream);
+}
+
+q2d_status q2d_kv_read(const q2d_kv_cache *c, const q2d_sequences *s, q2d_dtype dt, void *k, int64_t k_stride_token,
+                       int64_t k_stride_head, void *v, int64_t v_stride_token, int64_t v_stride_head,
+                       hipStream_t stream)
+{
+    return kv_copy(c, s, dt, k, k_stride_token, k_stride_head, v, v_stride_token, v_stride_head, false, stream);
+}
+
+int64_t q2d_attention_cached_workspace(const q2d_kv_cache *c, const q2d_sequences *s, int32_t heads_q)
+{
+    if (!c || !s || check_cache_sizes(*c) != Q2D_OK || check_sequence_sizes(s) != Q2D_OK) return -1;
+    if (heads_q <= 0 || heads_q % c->heads != 0) return -1;
+    return split_cached(c, s, heads_q).bytes;
+}
+
+q2d_status q2d_attention_cached(const q2d_kv_cache *c, const q2d_sequences *s, const q2d_cached_attention *a,
+                                void *workspace, int64_t workspace_bytes, hipStream_t stream)
+{
+    q2d_status r = check_cache(c);
+    if (r == Q2D_OK) r = check_sequences(s);
+    if (r != Q2D_OK) return r;
+    if (!a) return Q2D_EINVAL;
+    if (a->dtype != Q2D_F32 && a->dtype != Q2D_BF16) return Q2D_EINVAL;
+    if (a->dtype != Q2D_BF16) return Q2D_EUNSUPPORTED;
+    if (a->heads_q <= 0 || a->heads_q % c->heads != 0 || a->window < 0) return Q2D_EINVAL;
+    if (!(a->scale > 0.f) || !isfinite(a->scale) || !(a->softcap >= 0.f) || !isfinite(a->softcap)) return Q2D_EINVAL;
+    if (!on4(a->slopes) || !on4(a->prefix)) return Q2D_EINVAL;
+    if (s->tokens == 0) return Q2D_OK;
+    r = check_rows(a->q, s->tokens, a->q_stride_token, a->heads_q, a->q_stride_head, c->dim, 8, false);
+    if (r == Q2D_OK) r = check_rows(a->out, s->tokens, a->out_stride_token, a->heads_q, a->out_stride_head, c->dim, 8, true);
+    if (r != Q2D_OK) return r;
+    const CachedSplit p = split_cached(c, s, a->heads_q);
+    r = check_workspace(p.bytes, workspace, workspace_bytes);
+    if (r != Q2D_OK) return r;
+    CachedArgs g = {};
+    g.cache = cache_view(c);
+    g.seq = sequences_view(s);
+    g.q = a->q; g.q_st = a->q_stride_token; g.q_sh = a->q_stride_head;
+    g.out = a->out; g.out_st = a->out_stride_token; g.out_sh = a->out_stride_head;
+    g.mask.causal = 1;
+    g.mask.window = (int32_t)(a->window > kMaxLen ? kMaxLen : a->window);
+    g.mask.scale = a->scale; g.mask.cap = a->softcap;
+    g.mask.slopes = a->slopes; g.mask.prefix = a->prefix;
+    g.heads_q = a->heads_q;
+    g.splits = p.splits; g.wide = p.wide; g.tiles = p.tiles;
+    g.part = reinterpret_cast<float *>(workspace);
+    g.stat = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + p.stat_at);
+    if (launch_attention_cached(g, stream) != hipSuccess) return Q2D_ELAUNCH;
     return Q2D_OK;
 }
 
