@@ -63,7 +63,9 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArg
     constexpr int BN = sizeof(T) == 2 ? 64 : 32, NW = 4, BM = 32 * NW, KS = DT / 16, DS = DT / 32;
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2, F32 = sizeof(T) == 4;
     typedef Tile<T, DT> Lds;
-    __shared__ __align__(16) uint8_t smem[2][2][BN * Lds::kRowBytes];
+    __shared__ __align__(1024) uint8_t smem[2][2][BN * Lds::kRowBytes];
+    __shared__ __align__(16) int32_t doc_of[2][64];            // documents of a tile's keys
+    __shared__ uint32_t found[NW][BN / 32];                    // rows with infinities and NaN
 
     const AttentionMask &m = a.mask;
     const uint32_t tiles = (a.len_q + BM - 1) / BM;
@@ -106,9 +108,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArg
     }
     const ScoreMap sm = score_map(m, hq);
     const float pos = (float)p;
-    int lo, hi;
-    seen_by_query(m, p, lo, hi);
-    hi = min(hi, a.len_k);
+    const Sight sight = query_sight(m, p, a.len_k, prefix, my_doc);
 
     int end = (a.len_k + BN - 1) / BN;
     if (m.causal && !m.prefix) end = p1 < 0 ? 0 : min(end, p1 / BN + 1);
@@ -126,81 +126,83 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArg
         __syncthreads();
     }
     v16f dq[DS] = {};
+
+    bool spoilt = false;                // this query sees an infinity or a NaN among the keys
+
+    // one tile of keys; all: no pair of this wave is masked
+    auto tile = [&](bool all, int stage, int j0) __attribute__((always_inline)) {
+        const uint8_t *kt = smem[stage][0], *vt = smem[stage][1];
+        const uint32_t kr = Lds::row_base(kt, lane), vr = Lds::row_base(vt, lane), kc = Lds::column_base(kt, lane);
+#pragma unroll
+        for (int t = 0; t < BN / 32; ++t) {
+            v16f z = {}, e = {};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(kr, t, ks), qf[ks], z);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(vr, t, ks), gf[ks], e);
+            const float d0 = pos - (float)(j0 + 32 * t) - (float)(4 * h);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                float x = z[r], u = 1.f;
+                if constexpr (CAP) {
+                    x = tanh_of(x * sm.k1, F32);
+                    u = 1.f - x * x;
+                }
+                if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 - (float)tile_row(r, 0)), x);
+                const float pr = __builtin_amdgcn_exp2f(fmaf(x, sm.c, -lse2));
+                e[r] = pr * (e[r] - delta) * u;
+            }
+            if (!all) {
+                const uint32_t w = sight.word(j0 + 32 * t, docs ? &doc_of[stage][32 * t] : nullptr) >> (4 * h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) e[r] = word_bit(w, r) ? e[r] : 0.f;
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const Frag<T> ef = to_frag<T>(e, s);
+#pragma unroll
+                for (int dt = 0; dt < DS; ++dt)
+                    dq[dt] = mma(Lds::column_frag(kc, 32 * t + 16 * s, dt), ef, dq[dt]);
+            }
+        }
+    };
+    auto check = [&](int stage, int j0, bool any, bool all) __attribute__((always_inline)) {
+        uint32_t bad[BN / 32], some = 0;
+        non_finite<Lds, BN, NW>(smem[stage][0], &found[0][0], bad);
+#pragma unroll
+        for (int t = 0; t < BN / 32; ++t) some |= bad[t];
+        if (!some) return;
+#pragma unroll
+        for (int t = 0; t < BN / 32; ++t) {
+            const uint32_t w = all ? ~0u : sight.word(j0 + 32 * t, docs ? &doc_of[stage][32 * t] : nullptr);
+            spoilt = spoilt || (any && (w & bad[t]));
+        }
+        Lds::template clean<BN, NW * 64>(smem[stage][0]);
+    };
+    auto fetch = [&](int stage, int t) __attribute__((always_inline)) {
+        Lds::template load<BN, NW * 64>(smem[stage][0], k, a.k.sl, t * BN, a.len_k, D);
+        Lds::template load<BN, NW * 64>(smem[stage][1], v, a.v.sl, t * BN, a.len_k, D);
+        if (docs && wave == 0) load_words64(doc_of[stage], docs, t * BN, a.len_k);
+    };
+
     Schedule sched;
     int cur = sched.next(end, see), stage = 0;
-    bool wave_any = sched.wave_any, wave_all = sched.wave_all;
-    if (cur >= 0) {
-        Lds::template load<BN, NW * 64>(smem[0][0], k, a.k.sl, cur * BN, a.len_k, D);
-        Lds::template load<BN, NW * 64>(smem[0][1], v, a.v.sl, cur * BN, a.len_k, D);
-    }
+    if (cur >= 0) fetch(0, cur);
     while (cur >= 0) {
+        const bool part = sched.part, any = sched.wave_any, all = sched.wave_all;
         wait_vmcnt<0>();
         block_barrier();
         const int next = sched.next(end, see);
-        if (next >= 0) {
-            Lds::template load<BN, NW * 64>(smem[stage ^ 1][0], k, a.k.sl, next * BN, a.len_k, D);
-            Lds::template load<BN, NW * 64>(smem[stage ^ 1][1], v, a.v.sl, next * BN, a.len_k, D);
-        }
-        if (wave_any) {
-            const uint8_t *kt = smem[stage][0], *vt = smem[stage][1];
-            const int j0 = cur * BN;
-            const bool apart = !wave_all && Lds::template non_finite<BN>(kt);
-#pragma unroll 1
-            for (int t = 0; t < BN / 32; ++t) {
-                v16f z = {}, e = {};
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(kt, 32 * t + col, ks, h), qf[ks], z);
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(vt, 32 * t + col, ks, h), gf[ks], e);
-                const int jt = j0 + 32 * t;
-                const float d0 = pos - (float)jt - (float)(4 * h);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float x = z[r], u = 1.f;
-                    if constexpr (CAP) {
-                        x = tanh_of(x * sm.k1, F32);
-                        u = 1.f - x * x;
-                    }
-                    if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 - (float)tile_row(r, 0)), x);
-                    const float pr = __builtin_amdgcn_exp2f(fmaf(x, sm.c, -lse2));
-                    e[r] = pr * (e[r] - delta) * u;
-                }
-                uint32_t seen = 0;
-                if (!wave_all) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = jt + tile_row(r, h);
-                        bool ok = (j >= lo && j < hi) || j < prefix;
-                        if (docs) {
-                            const int dk = j < a.len_k ? docs[j] : -1;
-                            ok = ok && dk == my_doc && dk >= 0;
-                        }
-                        e[r] = ok ? e[r] : 0.f;
-                        seen |= (uint32_t)ok << tile_row(r, h);
-                    }
-                }
-                if (apart) {
-                    add_rows<T, DT>(dq, e, seen | __shfl_xor(seen, 32), kt, 32 * t);
-                } else {
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const Frag<T> ef = to_frag<T>(e, s);
-#pragma unroll
-                        for (int dt = 0; dt < DS; ++dt)
-                            dq[dt] = mma(Lds::column_frag(kt, 32 * t + 16 * s, dt, lane), ef, dq[dt]);
-                    }
-                }
-            }
-        }
+        if (next >= 0) fetch(stage ^ 1, next);
+        if (part) check(stage, cur * BN, any, all);
+        if (any) tile(all, stage, cur * BN);
         wait_lgkm();
         cur = next;
-        wave_any = sched.wave_any;
-        wave_all = sched.wave_all;
         stage ^= 1;
     }
     if (!row) return;
     T *out = (T *)a.dq.p + b * a.dq.sb + (int64_t)i * a.dq.sl + hq * a.dq.sh;
-    store_columns<T, DS>(out, dq, m.scale, h, D);
+    store_columns<T, DS>(out, dq, spoilt ? __builtin_nanf("") : m.scale, h, D);
 }
 
 // ---------------------------------------------------------------- dK, dV
@@ -211,8 +213,10 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionAr
     constexpr int BQ = sizeof(T) == 2 ? 64 : 32, NW = 4, BN = 32 * NW, KS = DT / 16, DS = DT / 32;
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2, F32 = sizeof(T) == 4;
     typedef Tile<T, DT> Lds;
-    __shared__ __align__(16) uint8_t smem[2][2][BQ * Lds::kRowBytes];
-    __shared__ __align__(16) float rows[2][2][BQ];             // lse, delta
+    __shared__ __align__(1024) uint8_t smem[2][2][BQ * Lds::kRowBytes];
+    __shared__ __align__(16) float rows[2][2][64];             // lse, delta of a tile's queries
+    __shared__ __align__(16) int32_t doc_of[2][64];            // and their documents
+    __shared__ uint32_t found[2][NW][BQ / 32];                 // rows with infinities and NaN
 
     const AttentionMask &m = a.mask;
     const uint32_t tiles = (a.len_k + BN - 1) / BN;
@@ -244,9 +248,8 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionAr
         if (jw1 >= jw) dw = range_of(ranges, jw, jw1);
         my_doc = key ? docs[j] : -1;
     }
-    int lo, hi;
-    seen_by_key(m, prefix, j, lo, hi);
-    hi = min(hi, a.len_k);                                     // (queries end at position len_k)
+    Sight sight = key_sight(m, j, a.len_k, prefix, my_doc);    // (queries end at position len_k)
+    if (docs) sight.lo = max(sight.lo, 0);                     // (and have no document below 0)
 
     // tiles of query rows [t BQ, ..); all rows of a tile are queries only where it is whole
     const int end = (a.len_q + BQ - 1) / BQ;
@@ -264,6 +267,7 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionAr
         __syncthreads();
     }
     v16f dk[DS] = {}, dv[DS] = {};
+    bool spoilt = false;                // an infinity or a NaN among the queries that see this key
     for (int gh = 0; gh < group; ++gh) {
         const int hq = hk * group + gh;
         const T *q = (const T *)a.q.p + b * a.q.sb + hq * a.q.sh;
@@ -271,99 +275,100 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionAr
         const float *lse = a.lse + ((int64_t)b * a.heads_q + hq) * a.len_q;
         const float *delta = a.delta + ((int64_t)b * a.heads_q + hq) * a.len_q;
         const ScoreMap sm = score_map(m, hq);
-        auto fetch = [&](int st, int t) {
+        // one tile of queries; all: no pair of this wave is masked
+        auto tile = [&](bool all, int stage, int i0) __attribute__((always_inline)) {
+            const uint8_t *qt = smem[stage][0], *gt = smem[stage][1];
+            const uint32_t qr = Lds::row_base(qt, lane), gr = Lds::row_base(gt, lane);
+            const uint32_t qc = Lds::column_base(qt, lane), gc = Lds::column_base(gt, lane);
+#pragma unroll
+            for (int t = 0; t < BQ / 32; ++t) {
+                v16f z = {}, e = {};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(qr, t, ks), kf[ks], z);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(gr, t, ks), vf[ks], e);
+                const int p0 = i0 + 32 * t + shift;
+                const float d0 = (float)(p0 + 4 * h) - (float)j;
+#pragma unroll
+                for (int x4 = 0; x4 < 4; ++x4) {
+                    const v4f l4 = *reinterpret_cast<const v4f *>(&rows[stage][0][32 * t + tile_row(4 * x4, h)]);
+                    const v4f e4 = *reinterpret_cast<const v4f *>(&rows[stage][1][32 * t + tile_row(4 * x4, h)]);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const int r = 4 * x4 + y;
+                        float x = z[r], u = 1.f;
+                        if constexpr (CAP) {
+                            x = tanh_of(x * sm.k1, F32);
+                            u = 1.f - x * x;
+                        }
+                        if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 + (float)tile_row(r, 0)), x);
+                        z[r] = __builtin_amdgcn_exp2f(fmaf(x, sm.c, -l4[y] * kLog2e));
+                        e[r] = z[r] * (e[r] - e4[y]) * u;
+                    }
+                }
+                if (!all) {
+                    const uint32_t w = sight.word(p0, docs ? &doc_of[stage][32 * t] : nullptr) >> (4 * h);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        z[r] = word_bit(w, r) ? z[r] : 0.f;
+                        e[r] = word_bit(w, r) ? e[r] : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const Frag<T> pf = to_frag<T>(z, s), ef = to_frag<T>(e, s);
+#pragma unroll
+                    for (int dt = 0; dt < DS; ++dt) {
+                        dv[dt] = mma(Lds::column_frag(gc, 32 * t + 16 * s, dt), pf, dv[dt]);
+                        dk[dt] = mma(Lds::column_frag(qc, 32 * t + 16 * s, dt), ef, dk[dt]);
+                    }
+                }
+            }
+        };
+        auto check = [&](int stage, int i0, bool any, bool all) __attribute__((always_inline)) {
+            uint32_t bq[BQ / 32], bg[BQ / 32], some = 0;
+            non_finite<Lds, BQ, NW>(smem[stage][0], &found[0][0][0], bq);
+            non_finite<Lds, BQ, NW>(smem[stage][1], &found[1][0][0], bg);
+#pragma unroll
+            for (int t = 0; t < BQ / 32; ++t) some |= bq[t] | bg[t];
+            if (!some) return;
+#pragma unroll
+            for (int t = 0; t < BQ / 32; ++t) {
+                const uint32_t w = all ? ~0u : sight.word(i0 + 32 * t + shift, docs ? &doc_of[stage][32 * t] : nullptr);
+                spoilt = spoilt || (any && (w & (bq[t] | bg[t])));
+            }
+            Lds::template clean<BQ, NW * 64>(smem[stage][0]);
+            Lds::template clean<BQ, NW * 64>(smem[stage][1]);
+        };
+        // (numbers past the ends repeat the last: those rows are masked, and a position
+        // below zero has no document)
+        auto fetch = [&](int st, int t) __attribute__((always_inline)) {
             Lds::template load<BQ, NW * 64>(smem[st][0], q, a.q.sl, t * BQ, a.len_q, D);
             Lds::template load<BQ, NW * 64>(smem[st][1], g, a.dout.sl, t * BQ, a.len_q, D);
-            // (repeats the last row's past the end: those rows are masked)
-            if (wave < 2 && lane < BQ) {
-                const int i = min(t * BQ + lane, a.len_q - 1);
-                lds_dma4(reinterpret_cast<const uint8_t *>((wave ? delta : lse) + i),
-                         __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(
-                             __attribute__((address_space(3))) const float *)rows[st][wave]));
-            }
+            if (wave < 2) load_words64(rows[st][wave], wave ? delta : lse, t * BQ, a.len_q);
+            if (docs && wave == 2) load_words64(doc_of[st], docs, t * BQ + shift, a.len_k);
         };
         Schedule sched;
         int cur = sched.next(end, see), stage = 0;
-        bool wave_any = sched.wave_any, wave_all = sched.wave_all;
         if (cur >= 0) fetch(0, cur);
         while (cur >= 0) {
+            const bool part = sched.part, any = sched.wave_any, all = sched.wave_all;
             wait_vmcnt<0>();
             block_barrier();
             const int next = sched.next(end, see);
             if (next >= 0) fetch(stage ^ 1, next);
-            if (wave_any) {
-                const uint8_t *qt = smem[stage][0], *gt = smem[stage][1];
-                const int i0 = cur * BQ;
-                const bool apart = !wave_all && (Lds::template non_finite<BQ>(qt) || Lds::template non_finite<BQ>(gt));
-#pragma unroll 1
-                for (int t = 0; t < BQ / 32; ++t) {
-                    v16f z = {}, e = {};
-#pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(qt, 32 * t + col, ks, h), kf[ks], z);
-#pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(gt, 32 * t + col, ks, h), vf[ks], e);
-                    const int p0 = i0 + 32 * t + shift;
-                    const float d0 = (float)(p0 + 4 * h) - (float)j;
-#pragma unroll
-                    for (int x4 = 0; x4 < 4; ++x4) {
-                        const v4f l4 = *reinterpret_cast<const v4f *>(&rows[stage][0][32 * t + tile_row(4 * x4, h)]);
-                        const v4f e4 = *reinterpret_cast<const v4f *>(&rows[stage][1][32 * t + tile_row(4 * x4, h)]);
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const int r = 4 * x4 + y;
-                            float x = z[r], u = 1.f;
-                            if constexpr (CAP) {
-                                x = tanh_of(x * sm.k1, F32);
-                                u = 1.f - x * x;
-                            }
-                            if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 + (float)tile_row(r, 0)), x);
-                            z[r] = __builtin_amdgcn_exp2f(fmaf(x, sm.c, -l4[y] * kLog2e));
-                            e[r] = z[r] * (e[r] - e4[y]) * u;
-                        }
-                    }
-                    uint32_t seen = 0;
-                    if (!wave_all) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int pr = p0 + tile_row(r, h);
-                            bool ok = pr >= lo && pr < hi;
-                            if (docs) {
-                                const int dq = pr >= 0 && pr < a.len_k ? docs[pr] : -1;
-                                ok = ok && dq == my_doc && dq >= 0;
-                            }
-                            z[r] = ok ? z[r] : 0.f;
-                            e[r] = ok ? e[r] : 0.f;
-                            seen |= (uint32_t)ok << tile_row(r, h);
-                        }
-                    }
-                    if (apart) {
-                        const uint32_t both = seen | __shfl_xor(seen, 32);
-                        add_rows<T, DT>(dv, z, both, gt, 32 * t);
-                        add_rows<T, DT>(dk, e, both, qt, 32 * t);
-                    } else {
-#pragma unroll
-                        for (int s = 0; s < 2; ++s) {
-                            const Frag<T> pf = to_frag<T>(z, s), ef = to_frag<T>(e, s);
-#pragma unroll
-                            for (int dt = 0; dt < DS; ++dt) {
-                                dv[dt] = mma(Lds::column_frag(gt, 32 * t + 16 * s, dt, lane), pf, dv[dt]);
-                                dk[dt] = mma(Lds::column_frag(qt, 32 * t + 16 * s, dt, lane), ef, dk[dt]);
-                            }
-                        }
-                    }
-                }
-            }
+            if (part) check(stage, cur * BQ, any, all);
+            if (any) tile(all, stage, cur * BQ);
             wait_lgkm();
             cur = next;
-            wave_any = sched.wave_any;
-            wave_all = sched.wave_all;
             stage ^= 1;
         }
         block_barrier();           // the next head's first tile takes stage 0
     }
     if (!key) return;
-    store_columns<T, DS>((T *)a.dk.p + b * a.dk.sb + (int64_t)j * a.dk.sl + hk * a.dk.sh, dk, m.scale, h, D);
-    store_columns<T, DS>((T *)a.dv.p + b * a.dv.sb + (int64_t)j * a.dv.sl + hk * a.dv.sh, dv, 1.f, h, D);
+    const float nan = __builtin_nanf("");
+    store_columns<T, DS>((T *)a.dk.p + b * a.dk.sb + (int64_t)j * a.dk.sl + hk * a.dk.sh, dk, spoilt ? nan : m.scale, h, D);
+    store_columns<T, DS>((T *)a.dv.p + b * a.dv.sb + (int64_t)j * a.dv.sl + hk * a.dv.sh, dv, spoilt ? nan : 1.f, h, D);
 }
 
 template <typename T, int DT, int MODS>

@@ -193,17 +193,13 @@ __global__ __launch_bounds__(256, 1) void attention_cached_kernel(const CachedAr
                     z[u][i] = x;
                 }
             if (!all) {
-                int lo, hi;
-                AttentionMask cm = m;
-                cm.causal = 1;
-                seen_by_query(cm, pos[nt], lo, hi);
-                hi = min(hi, s.len);
+                const Sight sight = query_sight(m, pos[nt], s.len, prefix, 0);
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int j = jl + 4 * u + i;
-                        const bool ok = ((j >= lo && j < hi) || j < prefix) && c.vs != kNoBlock;
+                        const bool ok = ((j >= sight.lo && j < sight.hi) || j < prefix) && c.vs != kNoBlock;
                         z[u][i] = ok ? z[u][i] : -INFINITY;
                     }
             }

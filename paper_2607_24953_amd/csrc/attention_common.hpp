@@ -83,50 +83,79 @@ struct Tile {
     }
     static __device__ __forceinline__ int offset(int r, int chunk) { return r * kRowBytes + ((chunk ^ swizzle(r)) << 4); }
 
-    // 8 elements 16 ks + 8 h .. of row r (h = lane / 32)
-    static __device__ __forceinline__ Frag<T> row_frag(const uint8_t *t, int r, int ks, int h)
+    // LDS address of a tile for the reads below, per lane.  The kernels form it anew for each
+    // tile (fresh): the addresses of the reads are then sums and XORs with constants at the
+    // read, in place of dozens of registers kept over the loop.
+    static __device__ __forceinline__ uint32_t address(const uint8_t *t)
     {
-        if constexpr (sizeof(T) == 2) {
-            return *reinterpret_cast<const bf16x8 *>(t + offset(r, 2 * ks + h));
-        } else {
-            const v4f a = *reinterpret_cast<const v4f *>(t + offset(r, 4 * ks + 2 * h));
-            const v4f b = *reinterpret_cast<const v4f *>(t + offset(r, 4 * ks + 2 * h + 1));
-            return v8f{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        }
+        return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t *)t;
     }
-
-    // column 32 dt + lane % 32, rows r0 + 4 h + 0..3 and r0 + 8 + 4 h + 0..3
-    static __device__ __forceinline__ Frag<T> column_frag(const uint8_t *t, int r0, int dt, int lane)
+    // of row lane % 32, for row_frag
+    static __device__ __forceinline__ uint32_t row_base(const uint8_t *t, int lane)
+    {
+        const int r = lane & 31, h = lane >> 5;
+        return fresh(address(t) + offset(r, sizeof(T) == 2 ? h : 2 * h));
+    }
+    // for column_frag
+    static __device__ __forceinline__ uint32_t column_base(const uint8_t *t, int lane)
     {
         const int h = lane >> 5;
         if constexpr (sizeof(T) == 2) {
             // ds_read_b64_tr_b16 hands lane i of each 16 the i-th column of a 4 x 16 block
             // whose rows the lanes 4 r .. 4 r + 3 point at
-            const int i = lane & 15, r = r0 + 4 * h + (i >> 2);
-            const int chunk = 4 * dt + 2 * ((lane >> 4) & 1) + ((i >> 1) & 1), half = (i & 1) << 3;
-            typedef __attribute__((address_space(3))) v4s *lp;
-            const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t *)t;
-            const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(uintptr_t)(base + offset(r, chunk) + half));
-            const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(uintptr_t)(base + offset(r + 8, chunk) + half));
-            const bf16x4 x = __builtin_bit_cast(bf16x4, a), y = __builtin_bit_cast(bf16x4, b);
-            return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+            const int i = lane & 15, r = 4 * h + (i >> 2);
+            const int chunk = 2 * ((lane >> 4) & 1) + ((i >> 1) & 1), half = (i & 1) << 3;
+            return fresh(address(t) + offset(r, chunk) + half);
         } else {
-            const int d = 32 * dt + (lane & 31);
+            const int d = lane & 31;
+            return fresh(address(t) + offset(4 * h, d >> 2) + ((d & 3) << 2));
+        }
+    }
+    static __device__ __forceinline__ uint32_t fresh(uint32_t a)
+    {
+        asm("" : "+v"(a));
+        return a;
+    }
+
+    // 8 elements 16 ks + 8 h .. (h = lane / 32) of row 32 t + lane % 32; tiles are aligned to
+    // kRowBytes, and swizzle(r + 32) == swizzle(r), so that a chunk number's bits are XORed in
+    static __device__ __forceinline__ Frag<T> row_frag(uint32_t base, int t, int ks)
+    {
+        if constexpr (sizeof(T) == 2) {
+            return *lds_ptr<bf16x8>((base ^ (uint32_t)(ks << 5)) + 32 * t * kRowBytes);
+        } else {
+            const v4f a = *lds_ptr<v4f>((base ^ (uint32_t)(ks << 6)) + 32 * t * kRowBytes);
+            const v4f b = *lds_ptr<v4f>((base ^ (uint32_t)((ks << 6) | 16)) + 32 * t * kRowBytes);
+            return v8f{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        }
+    }
+
+    // column 32 dt + lane % 32, rows r0 + 4 h + 0..3 and r0 + 8 + 4 h + 0..3, r0 a multiple of 16
+    static __device__ __forceinline__ Frag<T> column_frag(uint32_t base, int r0, int dt)
+    {
+        if constexpr (sizeof(T) == 2) {
+            typedef __attribute__((address_space(3))) v4s *lp;
+            // (swizzle(r + 8) differs from swizzle(r) in bit 1)
+            const uint32_t x = base ^ (uint32_t)(dt << 6);
+            const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(uintptr_t)(x + r0 * kRowBytes));
+            const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(uintptr_t)((x ^ 32u) + (r0 + 8) * kRowBytes));
+            const bf16x4 u = __builtin_bit_cast(bf16x4, a), v = __builtin_bit_cast(bf16x4, b);
+            return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
             v8f f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int r = r0 + 4 * h + (j & 3) + 2 * (j & 4);
-                f[j] = *reinterpret_cast<const float *>(t + offset(r, d >> 2) + ((d & 3) << 2));
+                const int r = r0 + (j & 3) + 2 * (j & 4);              // + 4 h in the base: swizzle's bits 0, 1 and 3
+                const uint32_t x = base ^ (uint32_t)((swizzle(r) << 4) ^ (dt << 7));
+                f[j] = *lds_ptr<float>(x + r * kRowBytes);
             }
             return f;
         }
     }
-
-    static __device__ __forceinline__ float element(const uint8_t *t, int r, int d)
+    template <typename V>
+    static __device__ __forceinline__ const __attribute__((address_space(3))) V *lds_ptr(uint32_t a)
     {
-        const uint8_t *p = t + offset(r, d / kPer) + (d % kPer) * sizeof(T);
-        if constexpr (sizeof(T) == 4) return *reinterpret_cast<const float *>(p);
-        else return bf16_to_f(*reinterpret_cast<const uint16_t *>(p));
+        return (const __attribute__((address_space(3))) V *)(uintptr_t)a;
     }
 
     // Fills ROWS rows from row r0 of a matrix of n rows (base; stride in elements, below
@@ -163,23 +192,49 @@ struct Tile {
         for (int i = threadIdx.x * 16; i < bytes; i += NT * 16) *reinterpret_cast<u4v *>(t + i) = u4v{0, 0, 0, 0};
     }
 
-    // whether rows 0 .. ROWS - 1 hold an infinity or a NaN (one wave, the same answer in all lanes)
-    template <int ROWS>
-    static __device__ __forceinline__ bool non_finite(const uint8_t *t)
+    static __device__ __forceinline__ bool chunk_non_finite(u4v v)
     {
         bool bad = false;
-#pragma unroll 4
-        for (int i = threadIdx.x & 63; i < ROWS * kChunks; i += 64) {
-            const u4v v = *reinterpret_cast<const u4v *>(t + i * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (sizeof(T) == 4) bad |= (v[j] & 0x7f800000u) == 0x7f800000u;
+            else bad |= (v[j] & 0x7f80u) == 0x7f80u || (v[j] & 0x7f800000u) == 0x7f800000u;
+        }
+        return bad;
+    }
+
+    // zeros in place of infinities and NaN, by all threads; barriers before and after
+    template <int ROWS, int NT>
+    static __device__ __forceinline__ void clean(uint8_t *t)
+    {
+        wait_lgkm();
+        block_barrier();
+#pragma unroll 1
+        for (int i = threadIdx.x; i < ROWS * kChunks; i += NT) {
+            u4v v = *reinterpret_cast<const u4v *>(t + i * 16);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if constexpr (sizeof(T) == 4) bad |= (v[j] & 0x7f800000u) == 0x7f800000u;
-                else bad |= (v[j] & 0x7f80u) == 0x7f80u || (v[j] & 0x7f800000u) == 0x7f800000u;
+                if constexpr (sizeof(T) == 4) {
+                    v[j] = (v[j] & 0x7f800000u) == 0x7f800000u ? 0u : v[j];
+                } else {
+                    v[j] = (v[j] & 0x7f80u) == 0x7f80u ? v[j] & 0xffff0000u : v[j];
+                    v[j] = (v[j] & 0x7f800000u) == 0x7f800000u ? v[j] & 0xffffu : v[j];
+                }
             }
+            *reinterpret_cast<u4v *>(t + i * 16) = v;
         }
-        return __ballot(bad) != 0;
+        wait_lgkm();
+        block_barrier();
     }
 };
+
+// 64 neighbouring 32-bit numbers from base[i0] to LDS, by one wave; indices clamped to [0, n)
+__device__ __forceinline__ void load_words64(void *lds, const void *base, int i0, int n)
+{
+    const int i = min(max(i0 + (int)(threadIdx.x & 63), 0), n - 1);
+    lds_dma4(reinterpret_cast<const uint8_t *>(base) + (int64_t)i * 4,
+             __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds));
+}
 
 // row of an output tile that register i of lane half h holds
 __device__ __forceinline__ int tile_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
@@ -202,31 +257,77 @@ __device__ __forceinline__ Frag<T> global_frag(const T *row, bool valid, int ks,
     return f;
 }
 
-// acc (rows d, column n) += sum over the 32 rows r of x's tile that column n sees of
-// w[r] X[r0 + r][d], one value at a time: what a matrix product of zeroed weights would
-// spoil where a row that is not seen holds an infinity or a NaN.  seen: bit r of a
-// column's rows (the same in both lanes of the column).
-template <typename T, int DT>
-__device__ __forceinline__ void add_rows(v16f *acc, const v16f &w, uint32_t seen, const uint8_t *t, int r0)
+// ---------------------------------------------------------------- non-finite operands
+//
+// Weights of pairs that are not seen are 0, and 0 times an infinity or a NaN is NaN in a
+// matrix product.  So where a workgroup has masked pairs in a tile, its waves first look
+// through the tile that meets those weights (non_finite), and in the rare case take what is
+// not finite out of it (Tile::clean) and put it back for the pairs that are seen.
+
+// Row bits of the tile's rows with an infinity or a NaN, the same in all waves of the
+// workgroup.  words: LDS, [NW][ROWS / 32]; one barrier.
+template <typename L, int ROWS, int NW>
+__device__ __forceinline__ void non_finite(const uint8_t *t, uint32_t *words, uint32_t *bad)
 {
-    const int lane = threadIdx.x & 63, h = lane >> 5;
-#pragma unroll 1
-    for (int r = 0; r < 32; ++r) {
-        // register and half that hold row r
-        const int i = 4 * (r >> 3) + (r & 3), from = ((r >> 2) & 1) * 32 + (lane & 31);
-        float mine = 0.f;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int N = ROWS * L::kChunks / (64 * NW);
+    uint32_t mine[ROWS / 32] = {};
 #pragma unroll
-        for (int j = 0; j < 16; ++j) mine = i == j ? w[j] : mine;
-        const float wr = __shfl(mine, from);
-        if (!((seen >> r) & 1)) continue;
+    for (int i = 0; i < N; ++i) {
+        const int slot = (wave * N + i) * 64 + lane, r = slot / L::kChunks;
+        const uint32_t b = L::chunk_non_finite(*reinterpret_cast<const u4v *>(t + slot * 16)) ? 1u << (r & 31) : 0u;
 #pragma unroll
-        for (int dt = 0; dt < DT / 32; ++dt)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                acc[dt][j] += wr * Tile<T, DT>::element(t, r0 + r, 32 * dt + tile_row(j, h));
-                asm volatile("" ::: "memory");          // one read at a time: registers, not speed
-            }
+        for (int x = 0; x < ROWS / 32; ++x) mine[x] |= (r >> 5) == x ? b : 0u;
     }
+#pragma unroll
+    for (int x = 0; x < ROWS / 32; ++x) {
+        if (__any(mine[x] != 0)) {
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) mine[x] |= __shfl_xor(mine[x], d);
+        }
+        if (lane == 0) words[wave * (ROWS / 32) + x] = mine[x];
+    }
+    wait_lgkm();
+    block_barrier();
+#pragma unroll
+    for (int x = 0; x < ROWS / 32; ++x) {
+        bad[x] = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) bad[x] |= words[w * (ROWS / 32) + x];
+        bad[x] = __builtin_amdgcn_readfirstlane(bad[x]);
+    }
+}
+
+// acc (rows d, column n) += the infinities and NaN of X's 32 rows from r0 that column n sees
+// (bits of `seen`), times weights above zero: a count of them by matrix products
+template <typename T, int DT>
+__device__ __forceinline__ void add_non_finite(v16f *acc, uint32_t seen, uint32_t column_base, int r0, int h)
+{
+    const uint32_t bits = seen >> (4 * h);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        Frag<T> ones;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ones[j] = ((bits >> tile_row(8 * s + j, 0)) & 1) ? 1.f : 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT / 32; ++dt) {
+            __builtin_amdgcn_sched_barrier(0);           // one tile at a time: registers, not speed
+            const Frag<T> x = Tile<T, DT>::column_frag(column_base, r0 + 16 * s, dt);
+            Frag<T> up, down;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = (float)x[j];
+                const bool fin = fabsf(v) < INFINITY;
+                up[j] = !fin && !(v == -INFINITY) ? 1.f : 0.f;
+                down[j] = !fin && !(v == INFINITY) ? 1.f : 0.f;
+            }
+            const v16f zero = {};
+            const v16f a = mma(up, ones, zero), b = mma(down, ones, zero);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[dt][i] += (a[i] > 0.f ? INFINITY : 0.f) + (b[i] > 0.f ? -INFINITY : 0.f);
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // ---------------------------------------------------------------- masks
@@ -261,11 +362,13 @@ __device__ __forceinline__ Seen classify(const AttentionMask &m, int prefix, int
 }
 
 // Tiles of one loop axis that a workgroup visits, 64 at a time: lane t classifies tile
-// base + t, and three ballots hold what the workgroup and this wave see of them.
+// base + t, and ballots hold what the workgroup and this wave see of them.
 struct Schedule {
-    uint64_t visit = 0, any = 0, all = 0;
-    int base = -64, cur = -1;
-    bool wave_any = false, wave_all = false;
+    uint64_t visit = 0, whole = 0, any = 0, all = 0;
+    int base = -64;
+    // of the tile that next() gave: whether some pair of the workgroup is masked, whether this
+    // wave sees some and all pairs
+    bool part = false, wave_any = false, wave_all = false;
 
     // next visited tile below `end`, or -1 (the same in all waves); f(tile) -> {of the
     // workgroup, of this wave}
@@ -279,29 +382,74 @@ struct Schedule {
             Seen g = {false, false}, w = {false, false};
             if (t < end) f(t, g, w);
             visit = __ballot(g.any);
+            whole = __ballot(g.all);
             any = __ballot(w.any);
             all = __ballot(w.all);
         }
         const int b = __builtin_ctzll(visit);
         visit &= visit - 1;
+        part = !((whole >> b) & 1);
         wave_any = (any >> b) & 1;
         wave_all = (all >> b) & 1;
         return base + b;
     }
 };
 
-// Interval of the other side's positions that one side's position sees, apart from the prefix
-__device__ __forceinline__ void seen_by_query(const AttentionMask &m, int p, int &lo, int &hi)
+// Which of 32 neighbouring positions of the other side one position sees: bit r for position
+// base + r.  Positions in [lo, hi) are seen, and on the queries' side those below the prefix.
+struct Sight {
+    int lo, hi, prefix, doc;
+
+    static __device__ __forceinline__ uint32_t below(int n)
+    {
+        n = min(max(n, 0), 32);
+        return n == 32 ? ~0u : (1u << n) - 1;
+    }
+    // docs: LDS, the document numbers of the 32 positions (null: no documents)
+    __device__ __forceinline__ uint32_t word(int base, const int32_t *docs) const
+    {
+        uint32_t w = (below(hi - base) & ~below(lo - base)) | below(prefix - base);
+        if (docs) {
+            uint32_t same = 0;
+#pragma unroll
+            for (int r = 0; r < 32; r += 4) {
+                const v4i d = *reinterpret_cast<const v4i *>(docs + r);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) same |= d[x] == doc ? 1u << (r + x) : 0u;
+            }
+            w = doc >= 0 ? w & same : 0u;
+        }
+        return w;
+    }
+};
+
+// what query position p sees of len_k keys
+__device__ __forceinline__ Sight query_sight(const AttentionMask &m, int p, int len_k, int prefix, int doc)
 {
-    lo = m.window ? p - m.window + 1 : INT32_MIN;
-    hi = m.causal ? p + 1 : (m.window ? p + m.window : INT32_MAX);
+    Sight s;
+    s.lo = m.window ? p - m.window + 1 : INT32_MIN / 2;
+    s.hi = min(m.causal ? p + 1 : (m.window ? p + m.window : len_k), len_k);
+    s.prefix = prefix;
+    s.doc = doc;
+    return s;
 }
-__device__ __forceinline__ void seen_by_key(const AttentionMask &m, int prefix, int j, int &lo, int &hi)
+// the query positions that see key j
+__device__ __forceinline__ Sight key_sight(const AttentionMask &m, int j, int len_k, int prefix, int doc)
 {
-    lo = m.causal ? j : (m.window ? j - m.window + 1 : INT32_MIN);
-    hi = m.window ? j + m.window : INT32_MAX;
-    if (j < prefix) { lo = INT32_MIN; hi = INT32_MAX; }
+    Sight s;
+    s.lo = m.causal ? j : (m.window ? j - m.window + 1 : INT32_MIN / 2);
+    s.hi = min(m.window ? j + m.window : len_k, len_k);
+    if (j < prefix) {
+        s.lo = INT32_MIN / 2;
+        s.hi = len_k;
+    }
+    s.prefix = INT32_MIN / 2;
+    s.doc = doc;
+    return s;
 }
+
+// Whether bit tile_row(r, h) of a word is set, the word shifted right by 4 h beforehand
+__device__ __forceinline__ bool word_bit(uint32_t w, int r) { return (w >> tile_row(r, 0)) & 1; }
 
 // Document range of the positions [p0, p1] from the ranges of 64 positions; positions
 // below zero have no document

@@ -18,7 +18,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
     constexpr int BN = sizeof(T) == 2 ? 64 : 32, BM = 32 * NW, KS = DT / 16, DS = DT / 32;
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2, F32 = sizeof(T) == 4;
     typedef Tile<T, DT> Lds;
-    __shared__ __align__(16) uint8_t smem[2][2][BN * Lds::kRowBytes];
+    __shared__ __align__(1024) uint8_t smem[2][2][BN * Lds::kRowBytes];
+    __shared__ __align__(16) int32_t doc_of[2][64];            // documents of a tile's keys
+    __shared__ uint32_t found[NW][BN / 32];                    // rows with infinities and NaN
 
     const AttentionMask &m = a.mask;
     const uint32_t tiles = (a.len_q + BM - 1) / BM;
@@ -54,9 +56,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
     }
     const ScoreMap sm = score_map(m, hq);
     const float thr = 8.f / sm.c, pos = (float)p;
-    int lo, hi;
-    seen_by_query(m, p, lo, hi);
-    hi = min(hi, a.len_k);
+    const Sight sight = query_sight(m, p, a.len_k, prefix, my_doc);
 
     int end = (a.len_k + BN - 1) / BN;
     if (m.causal && !m.prefix) end = p1 < 0 ? 0 : min(end, p1 / BN + 1);
@@ -76,105 +76,107 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
     }
     v16f o[DS] = {};
     float mx = -INFINITY, sum = 0.f;
-    Schedule sched;
-    int cur = sched.next(end, see), stage = 0;
-    bool wave_any = sched.wave_any, wave_all = sched.wave_all;
-    if (cur >= 0) {
-        Lds::template load<BN, NW * 64>(smem[0][0], k, a.k.sl, cur * BN, a.len_k, D);
-        Lds::template load<BN, NW * 64>(smem[0][1], v, a.v.sl, cur * BN, a.len_k, D);
-    }
-    while (cur >= 0) {
-        wait_vmcnt<0>();
-        block_barrier();
-        const int next = sched.next(end, see);
-        if (next >= 0) {
-            Lds::template load<BN, NW * 64>(smem[stage ^ 1][0], k, a.k.sl, next * BN, a.len_k, D);
-            Lds::template load<BN, NW * 64>(smem[stage ^ 1][1], v, a.v.sl, next * BN, a.len_k, D);
-        }
-        if (wave_any) {
-            const uint8_t *kt = smem[stage][0], *vt = smem[stage][1];
-            v16f z[BN / 32] = {};
+
+    // one tile of keys; all: no pair of this wave is masked
+    auto tile = [&](bool all, int stage, int j0) __attribute__((always_inline)) {
+        const uint8_t *kt = smem[stage][0], *vt = smem[stage][1];
+        const uint32_t kr = Lds::row_base(kt, lane), vc = Lds::column_base(vt, lane);
+        v16f z[BN / 32] = {};
 #pragma unroll
-            for (int t = 0; t < BN / 32; ++t)
+        for (int t = 0; t < BN / 32; ++t)
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) z[t] = mma(Lds::row_frag(kt, 32 * t + col, ks, h), qf[ks], z[t]);
-            const int j0 = cur * BN;
-            if constexpr (CAP || BIAS) {
-                const float d0 = pos - (float)j0;
-#pragma unroll
-                for (int t = 0; t < BN / 32; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        float x = z[t][r];
-                        if constexpr (CAP) x = tanh_of(x * sm.k1, F32);
-                        if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 - (float)(32 * t + tile_row(r, 0)) - (float)(4 * h)), x);
-                        z[t][r] = x;
-                    }
-            }
-            uint32_t seen[BN / 32];
-            if (!wave_all) {
-#pragma unroll
-                for (int t = 0; t < BN / 32; ++t) {
-                    seen[t] = 0;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = j0 + 32 * t + tile_row(r, h);
-                        bool ok = (j >= lo && j < hi) || j < prefix;
-                        if (docs) {
-                            const int dk = j < a.len_k ? docs[j] : -1;
-                            ok = ok && dk == my_doc && dk >= 0;
-                        }
-                        z[t][r] = ok ? z[t][r] : -INFINITY;
-                        seen[t] |= (uint32_t)ok << tile_row(r, h);
-                    }
-                }
-            }
-            float top = z[0][0];
-#pragma unroll
-            for (int t = 0; t < BN / 32; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, z[t][r]);
-            top = fmaxf(top, __shfl_xor(top, 32));
-            // The running maximum moves only where it has been passed by 2^8: exponents up to
-            // 8 above it are as good, and most tiles leave the sums as they are.
-            if (__any(top > mx + thr)) {
-                const float now = fmaxf(mx, top);
-                const float f = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx - now) * sm.c);
-#pragma unroll
-                for (int dt = 0; dt < DS; ++dt) o[dt] *= f;
-                sum *= f;
-                mx = now;
-            }
-            const float base = mx == -INFINITY ? 0.f : mx;
-            const float off = -base * sm.c;
+            for (int ks = 0; ks < KS; ++ks) z[t] = mma(Lds::row_frag(kr, t, ks), qf[ks], z[t]);
+        if constexpr (CAP || BIAS) {
+            const float d0 = pos - (float)j0 - (float)(4 * h);
 #pragma unroll
             for (int t = 0; t < BN / 32; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const float e = F32 ? (z[t][r] - base) * sm.c : fmaf(z[t][r], sm.c, off);
-                    z[t][r] = __builtin_amdgcn_exp2f(e);
-                    sum += z[t][r];
+                    float x = z[t][r];
+                    if constexpr (CAP) x = tanh_of(x * sm.k1, F32);
+                    if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 - (float)(32 * t + tile_row(r, 0))), x);
+                    z[t][r] = x;
                 }
-            if (!wave_all && Lds::template non_finite<BN>(vt)) {
+        }
+        if (!all) {
 #pragma unroll
-                for (int t = 0; t < BN / 32; ++t)
-                    add_rows<T, DT>(o, z[t], seen[t] | __shfl_xor(seen[t], 32), vt, 32 * t);
-            } else {
+            for (int t = 0; t < BN / 32; ++t) {
+                const uint32_t w = sight.word(j0 + 32 * t, docs ? &doc_of[stage][32 * t] : nullptr) >> (4 * h);
 #pragma unroll
-                for (int t = 0; t < BN / 32; ++t)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const Frag<T> pf = to_frag<T>(z[t], s);
-#pragma unroll
-                        for (int dt = 0; dt < DS; ++dt)
-                            o[dt] = mma(Lds::column_frag(vt, 32 * t + 16 * s, dt, lane), pf, o[dt]);
-                    }
+                for (int r = 0; r < 16; ++r) z[t][r] = word_bit(w, r) ? z[t][r] : -INFINITY;
             }
         }
+        float top = z[0][0];
+#pragma unroll
+        for (int t = 0; t < BN / 32; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, z[t][r]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        // The running maximum moves only where it has been passed by 2^8: exponents up to
+        // 8 above it are as good, and most tiles leave the sums as they are.
+        if (__any(top > mx + thr)) {
+            const float now = fmaxf(mx, top);
+            const float f = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx - now) * sm.c);
+#pragma unroll
+            for (int dt = 0; dt < DS; ++dt) o[dt] *= f;
+            sum *= f;
+            mx = now;
+        }
+        const float base = mx == -INFINITY ? 0.f : mx;
+        const float off = -base * sm.c;
+#pragma unroll
+        for (int t = 0; t < BN / 32; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float e = F32 ? (z[t][r] - base) * sm.c : fmaf(z[t][r], sm.c, off);
+                z[t][r] = __builtin_amdgcn_exp2f(e);
+                sum += z[t][r];
+            }
+#pragma unroll
+        for (int t = 0; t < BN / 32; ++t)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const Frag<T> pf = to_frag<T>(z[t], s);
+#pragma unroll
+                for (int dt = 0; dt < DS; ++dt)
+                    o[dt] = mma(Lds::column_frag(vc, 32 * t + 16 * s, dt), pf, o[dt]);
+            }
+    };
+    auto check = [&](int stage, int j0, bool any, bool all) __attribute__((always_inline)) {
+        uint32_t bad[BN / 32];
+        non_finite<Lds, BN, NW>(smem[stage][1], &found[0][0], bad);
+        uint32_t some = 0;
+#pragma unroll
+        for (int t = 0; t < BN / 32; ++t) some |= bad[t];
+        if (!some) return;
+        if (any) {
+            const uint32_t vc = Lds::column_base(smem[stage][1], lane);
+#pragma unroll 1
+            for (int t = 0; t < BN / 32; ++t)
+                add_non_finite<T, DT>(o, all ? ~0u : sight.word(j0 + 32 * t, docs ? &doc_of[stage][32 * t] : nullptr), vc,
+                                      32 * t, h);
+        }
+        Lds::template clean<BN, NW * 64>(smem[stage][1]);
+    };
+    auto fetch = [&](int stage, int t) __attribute__((always_inline)) {
+        Lds::template load<BN, NW * 64>(smem[stage][0], k, a.k.sl, t * BN, a.len_k, D);
+        Lds::template load<BN, NW * 64>(smem[stage][1], v, a.v.sl, t * BN, a.len_k, D);
+        if (docs && wave == 0) load_words64(doc_of[stage], docs, t * BN, a.len_k);
+    };
+
+    Schedule sched;
+    int cur = sched.next(end, see), stage = 0;
+    if (cur >= 0) fetch(0, cur);
+    while (cur >= 0) {
+        const bool part = sched.part, any = sched.wave_any, all = sched.wave_all;
+        wait_vmcnt<0>();
+        block_barrier();
+        const int next = sched.next(end, see);
+        if (next >= 0) fetch(stage ^ 1, next);
+        if (part) check(stage, cur * BN, any, all);
+        if (any) tile(all, stage, cur * BN);
         wait_lgkm();
         cur = next;
-        wave_any = sched.wave_any;
-        wave_all = sched.wave_all;
         stage ^= 1;
     }
 
