@@ -26,7 +26,7 @@ struct AttentionArgs {
     HeadsView q, k, v, out;
     HeadsView dout, dq, dk, dv;      // backward
     float *lse;                      // [batch][heads_q][len_q], natural logarithm
-    float *delta;                    // [batch][heads_q][len_q], backward workspace
+    float *delta, *lse2;             // [batch][heads_q][len_q], backward workspace: delta, lse log2 e
     int2 *ranges;                    // [batch][ceil(len_k / 64)] document ranges (workspace)
     AttentionMask mask;
     int32_t batch, len_q, len_k, heads_q, heads_kv, dim;

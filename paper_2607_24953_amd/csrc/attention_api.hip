@@ -81,9 +81,11 @@ int64_t ranges_bytes(const q2d_attention *a)
     return a->documents ? up256((int64_t)a->batch * ((a->len_k + 63) / 64) * 8) : 0;
 }
 
+int64_t rows_bytes(const q2d_attention *a) { return up256((int64_t)a->batch * a->heads_q * a->len_q * 4); }
+
 int64_t workspace_of(const q2d_attention *a, bool backward)
 {
-    return ranges_bytes(a) + (backward ? up256((int64_t)a->batch * a->heads_q * a->len_q * 4) : 0);
+    return ranges_bytes(a) + (backward ? 2 * rows_bytes(a) : 0);
 }
 
 AttentionArgs make_args(const q2d_attention *a, void *workspace)
@@ -93,6 +95,7 @@ AttentionArgs make_args(const q2d_attention *a, void *workspace)
     r.lse = a->lse;
     r.ranges = reinterpret_cast<int2 *>(workspace);
     r.delta = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + ranges_bytes(a));
+    r.lse2 = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(r.delta) + rows_bytes(a));
     r.mask.causal = a->causal;
     // (no distance reaches 2^30)
     r.mask.window = (int32_t)(a->window > kMaxLen ? kMaxLen : a->window);

@@ -38,21 +38,30 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(const AttentionArg
     }
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) s += __shfl_xor(s, d);
-    if (l == 0) a.delta[((int64_t)b * a.heads_q + hq) * a.len_q + i] = s;
+    if (l != 0) return;
+    const int64_t at = ((int64_t)b * a.heads_q + hq) * a.len_q + i;
+    a.delta[at] = s;
+    a.lse2[at] = a.lse[at] * kLog2e;
 }
 
-// Ranges of document numbers of 64 positions
+// Documents of 64 positions at a time (struct Documents)
 __global__ __launch_bounds__(64) void document_ranges_kernel(const int32_t *docs, int len, int2 *ranges)
 {
     const int n = (len + 63) / 64, b = blockIdx.x / n, t = blockIdx.x % n, j = t * 64 + threadIdx.x;
-    int lo = INT32_MAX, hi = INT32_MIN;
-    if (j < len) lo = hi = docs[(int64_t)b * len + j];
+    int lo = INT32_MAX, hi = -1;
+    bool padding = false;
+    if (j < len) {
+        const int d = docs[(int64_t)b * len + j];
+        padding = d < 0;
+        if (!padding) lo = hi = d;
+    }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         lo = min(lo, __shfl_xor(lo, d));
         hi = max(hi, __shfl_xor(hi, d));
     }
-    if (threadIdx.x == 0) ranges[blockIdx.x] = make_int2(lo, hi);
+    padding = __any(padding);
+    if (threadIdx.x == 0) ranges[blockIdx.x] = make_int2(padding ? ~lo : lo, hi);
 }
 
 // ---------------------------------------------------------------- dQ
@@ -92,14 +101,14 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArg
     }
     const int64_t at = ((int64_t)b * a.heads_q + hq) * a.len_q + i;
     // (rows outside: probabilities of 0)
-    const float lse2 = row ? a.lse[at] * kLog2e : INFINITY, delta = row ? a.delta[at] : 0.f;
+    const float lse2 = row ? a.lse2[at] : INFINITY, delta = row ? a.delta[at] : 0.f;
 
     const int prefix = m.prefix ? min(max(m.prefix[b], 0), a.len_k) : 0;
     const int32_t *docs = m.documents ? m.documents + (int64_t)b * a.len_k : nullptr;
     const int2 *ranges = a.ranges + (int64_t)b * ((a.len_k + 63) / 64);
     const int p0 = i0 + shift, p1 = min(i0 + BM, a.len_q) - 1 + shift;
     const int pw0 = iw + shift, pw1 = min(iw + 32, a.len_q) - 1 + shift;
-    int2 dg = make_int2(0, 0), dw = dg;
+    Documents dg = {}, dw = {};
     int my_doc = 0;
     if (docs) {
         dg = range_of(ranges, p0, p1);
@@ -114,10 +123,10 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArg
     if (m.causal && !m.prefix) end = p1 < 0 ? 0 : min(end, p1 / BN + 1);
     auto see = [&](int t, Seen &s, Seen &w) {
         const int j0 = t * BN, j1 = min(j0 + BN, a.len_k) - 1;
-        const int2 dk = docs ? ranges[j0 >> 6] : make_int2(0, 0);
-        s = classify(m, prefix, p0, p1, j0, j1, dg.x, dg.y, dk.x, dk.y);
+        const Documents dk = docs ? range_of(ranges, j0, j0) : Documents{};
+        s = classify(m, prefix, p0, p1, j0, j1, dg, dk);
         if (pw1 >= pw0) {
-            w = classify(m, prefix, pw0, pw1, j0, j1, dw.x, dw.y, dk.x, dk.y);
+            w = classify(m, prefix, pw0, pw1, j0, j1, dw, dk);
             w.all = w.all && j0 + BN <= a.len_k;
         }
     };
@@ -214,7 +223,7 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionAr
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2, F32 = sizeof(T) == 4;
     typedef Tile<T, DT> Lds;
     __shared__ __align__(1024) uint8_t smem[2][2][BQ * Lds::kRowBytes];
-    __shared__ __align__(16) float rows[2][2][64];             // lse, delta of a tile's queries
+    __shared__ __align__(16) float rows[2][2][64];             // lse2, delta of a tile's queries
     __shared__ __align__(16) int32_t doc_of[2][64];            // and their documents
     __shared__ uint32_t found[2][NW][BQ / 32];                 // rows with infinities and NaN
 
@@ -241,7 +250,7 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionAr
     const int32_t *docs = m.documents ? m.documents + (int64_t)b * a.len_k : nullptr;
     const int2 *ranges = a.ranges + (int64_t)b * ((a.len_k + 63) / 64);
     const int j1 = min(j0 + BN, a.len_k) - 1, jw1 = min(jw + 32, a.len_k) - 1;
-    int2 dg = make_int2(0, 0), dw = dg;
+    Documents dg = {}, dw = {};
     int my_doc = 0;
     if (docs) {
         dg = range_of(ranges, j0, j1);
@@ -255,10 +264,10 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionAr
     const int end = (a.len_q + BQ - 1) / BQ;
     auto see = [&](int t, Seen &s, Seen &w) {
         const int p0 = t * BQ + shift, p1 = min(t * BQ + BQ, a.len_q) - 1 + shift;
-        const int2 dq = docs ? range_of(ranges, p0, p1) : make_int2(0, 0);
-        s = classify(m, prefix, p0, p1, j0, j1, dq.x, dq.y, dg.x, dg.y);
+        const Documents dq = docs ? range_of(ranges, p0, p1) : Documents{};
+        s = classify(m, prefix, p0, p1, j0, j1, dq, dg);
         if (jw1 >= jw) {
-            w = classify(m, prefix, p0, p1, jw, jw1, dq.x, dq.y, dw.x, dw.y);
+            w = classify(m, prefix, p0, p1, jw, jw1, dq, dw);
             w.all = w.all && t * BQ + BQ <= a.len_q;
         }
     };
@@ -272,7 +281,7 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionAr
         const int hq = hk * group + gh;
         const T *q = (const T *)a.q.p + b * a.q.sb + hq * a.q.sh;
         const T *g = (const T *)a.dout.p + b * a.dout.sb + hq * a.dout.sh;
-        const float *lse = a.lse + ((int64_t)b * a.heads_q + hq) * a.len_q;
+        const float *lse = a.lse2 + ((int64_t)b * a.heads_q + hq) * a.len_q;
         const float *delta = a.delta + ((int64_t)b * a.heads_q + hq) * a.len_q;
         const ScoreMap sm = score_map(m, hq);
         // one tile of queries; all: no pair of this wave is masked
@@ -302,7 +311,7 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionAr
                             u = 1.f - x * x;
                         }
                         if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 + (float)tile_row(r, 0)), x);
-                        z[r] = __builtin_amdgcn_exp2f(fmaf(x, sm.c, -l4[y] * kLog2e));
+                        z[r] = __builtin_amdgcn_exp2f(fmaf(x, sm.c, -l4[y]));
                         e[r] = z[r] * (e[r] - e4[y]) * u;
                     }
                 }
@@ -371,13 +380,274 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionAr
     store_columns<T, DS>((T *)a.dv.p + b * a.dv.sb + (int64_t)j * a.dv.sl + hk * a.dv.sh, dv, spoilt ? nan : 1.f, h, D);
 }
 
+// The same for bfloat16 as a software pipeline.  The accumulators of 32 keys and their K and V
+// fragments take 192 registers of a wave at 128 dims, so only one wave fits a SIMD and nothing
+// but its own instructions can fill the time of a matrix product.  Over steps n of 32 query
+// rows, block n therefore forms S and dP of step n + 1 and the products of step n - 1 while
+// its vector instructions turn step n's S and dP into P and dS: after each MFMA stands its
+// share of them and of the LDS reads for the MFMAs to come (sched_barrier keeps the order).
+// Tiles of 64 rows pass through three LDS stages: the last, this and the next one.
+template <int DT, int MODS>
+__global__ __launch_bounds__(256, 1) void attention_dkv_pipe_kernel(const AttentionArgs a)
+{
+    typedef __bf16 T;
+    constexpr int BQ = 64, NW = 4, BN = 32 * NW, KS = DT / 16, DS = DT / 32;
+    constexpr bool CAP = MODS & 1, BIAS = MODS & 2;
+    typedef Tile<T, DT> Lds;
+    __shared__ __align__(1024) uint8_t smem[3][2][BQ * Lds::kRowBytes];
+    __shared__ __align__(16) float rows[3][2][64];             // lse2, delta of a tile's queries
+    __shared__ __align__(16) int32_t doc_of[3][64];            // and their documents
+    __shared__ uint32_t found[2][NW][BQ / 32];                 // rows with infinities and NaN
+
+    const AttentionMask &m = a.mask;
+    const uint32_t tiles = (a.len_k + BN - 1) / BN;
+    uint32_t head, kt;
+    head_tile(blockIdx.x, gridDim.x, tiles, head, kt);
+    const int b = head / a.heads_kv, hk = head % a.heads_kv, group = a.heads_q / a.heads_kv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = lane >> 5, col = lane & 31;
+    const int shift = a.len_k - a.len_q, D = a.dim;
+    const int j0 = kt * BN, jw = j0 + wave * 32, j = jw + col;
+    const bool key = j < a.len_k;
+
+    const T *k = (const T *)a.k.p + b * a.k.sb + (int64_t)j * a.k.sl + hk * a.k.sh;
+    const T *v = (const T *)a.v.p + b * a.v.sb + (int64_t)j * a.v.sl + hk * a.v.sh;
+    Frag<T> kf[KS], vf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        kf[ks] = global_frag<T>(k, key, ks, h, D);
+        vf[ks] = global_frag<T>(v, key, ks, h, D);
+    }
+    const int prefix = m.prefix ? min(max(m.prefix[b], 0), a.len_k) : 0;
+    const int32_t *docs = m.documents ? m.documents + (int64_t)b * a.len_k : nullptr;
+    const int2 *ranges = a.ranges + (int64_t)b * ((a.len_k + 63) / 64);
+    const int j1 = min(j0 + BN, a.len_k) - 1, jw1 = min(jw + 32, a.len_k) - 1;
+    Documents dg = {}, dw = {};
+    int my_doc = 0;
+    if (docs) {
+        dg = range_of(ranges, j0, j1);
+        if (jw1 >= jw) dw = range_of(ranges, jw, jw1);
+        my_doc = key ? docs[j] : -1;
+    }
+    Sight sight = key_sight(m, j, a.len_k, prefix, my_doc);    // (queries end at position len_k)
+    if (docs) sight.lo = max(sight.lo, 0);                     // (and have no document below 0)
+
+    const int end = (a.len_q + BQ - 1) / BQ;
+    auto see = [&](int t, Seen &s, Seen &w) {
+        const int p0 = t * BQ + shift, p1 = min(t * BQ + BQ, a.len_q) - 1 + shift;
+        const Documents dq = docs ? range_of(ranges, p0, p1) : Documents{};
+        s = classify(m, prefix, p0, p1, j0, j1, dq, dg);
+        if (jw1 >= jw) {
+            w = classify(m, prefix, p0, p1, jw, jw1, dq, dw);
+            w.all = w.all && t * BQ + BQ <= a.len_q;
+        }
+    };
+    if (D < DT) {
+        Lds::template clear<NW * 64>(smem[0][0], sizeof(smem));
+        __syncthreads();
+    }
+
+    // the visited tiles of all query heads, in order
+    struct At { int tile, head; bool part, all; };
+    Schedule sched;
+    int gh = 0;
+    auto advance = [&]() __attribute__((always_inline)) {
+        int t = sched.next(end, see);
+        while (t < 0 && ++gh < group) {
+            sched = Schedule();
+            t = sched.next(end, see);
+        }
+        return At{t, gh, sched.part, sched.wave_all};
+    };
+    auto fetch = [&](int st, const At &at) __attribute__((always_inline)) {
+        const int hq = hk * group + at.head, i0 = at.tile * BQ;
+        Lds::template load<BQ, NW * 64>(smem[st][0], (const T *)a.q.p + b * a.q.sb + hq * a.q.sh, a.q.sl, i0, a.len_q, D);
+        Lds::template load<BQ, NW * 64>(smem[st][1], (const T *)a.dout.p + b * a.dout.sb + hq * a.dout.sh, a.dout.sl, i0,
+                                        a.len_q, D);
+        // (numbers past the ends repeat the last: those rows are masked)
+        if (wave < 2)
+            load_words64(rows[st][wave], (wave ? a.delta : a.lse2) + ((int64_t)b * a.heads_q + hq) * a.len_q, i0, a.len_q);
+        if (docs && wave == 2) load_words64(doc_of[st], docs, i0 + shift, a.len_k);
+    };
+    bool spoilt = false;                // an infinity or a NaN among the queries that see this key
+    auto check = [&](int stage, const At &at) __attribute__((always_inline)) {
+        uint32_t bq[BQ / 32], bg[BQ / 32], some = 0;
+        non_finite<Lds, BQ, NW>(smem[stage][0], &found[0][0][0], bq);
+        non_finite<Lds, BQ, NW>(smem[stage][1], &found[1][0][0], bg);
+#pragma unroll
+        for (int t = 0; t < BQ / 32; ++t) some |= bq[t] | bg[t];
+        if (!some) return;
+#pragma unroll
+        for (int t = 0; t < BQ / 32; ++t) {
+            const uint32_t w =
+                at.all ? ~0u : sight.word(at.tile * BQ + 32 * t + shift, docs ? &doc_of[stage][32 * t] : nullptr);
+            spoilt = spoilt || (w & (bq[t] | bg[t]));
+        }
+        Lds::template clean<BQ, NW * 64>(smem[stage][0]);
+        Lds::template clean<BQ, NW * 64>(smem[stage][1]);
+    };
+
+    v16f dk[DS] = {}, dv[DS] = {};
+    v16f z = {}, e = {};                                 // S and dP of the step at hand
+    uint32_t pw[8] = {}, ew[8] = {};                     // P and dS of the step before, bf16 pairs
+
+    // Block of step n: rows 32 t of stage `now`; its S and dP are in z and e.  (next, tn): the
+    // following step's rows, (last, tl): the preceding one's.
+    auto block = [&](int now, int t, const At &at, int next, int tn, int last, int tl) __attribute__((always_inline)) {
+        constexpr int N = 8 * DS;                        // MFMAs: 2 DS each of dV, dK, S and dP
+        constexpr int AHEAD = 4;
+        const uint32_t qr = Lds::row_base(smem[next][0], lane) + tn * 32 * Lds::kRowBytes;
+        const uint32_t gr = Lds::row_base(smem[next][1], lane) + tn * 32 * Lds::kRowBytes;
+        const uint32_t qc = Lds::column_base(smem[last][0], lane) + tl * 32 * Lds::kRowBytes;
+        const uint32_t gc = Lds::column_base(smem[last][1], lane) + tl * 32 * Lds::kRowBytes;
+        const int p0 = at.tile * BQ + 32 * t + shift;
+        const ScoreMap sm = score_map(m, hk * group + at.head);
+        const float d0 = BIAS ? (float)(p0 + 4 * h) - (float)j : 0.f;
+        const uint32_t w = (at.all ? ~0u : sight.word(p0, docs ? &doc_of[now][32 * t] : nullptr)) >> (4 * h);
+        const float *l2 = &rows[now][0][32 * t + 4 * h], *dl = &rows[now][1][32 * t + 4 * h];
+        uint32_t pn[8], en[8];
+        v16f zn = {}, en_ = {};
+        Frag<T> f[AHEAD + 1];
+        v4f l4, e4;
+        bf16x8 pf[2], ef[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            pf[s] = __builtin_bit_cast(bf16x8, u4v{pw[4 * s], pw[4 * s + 1], pw[4 * s + 2], pw[4 * s + 3]});
+            ef[s] = __builtin_bit_cast(bf16x8, u4v{ew[4 * s], ew[4 * s + 1], ew[4 * s + 2], ew[4 * s + 3]});
+        }
+        // operand of MFMA i: i % 4 = 0: dV, 1: S, 2: dK, 3: dP; number x = i / 4 of its kind
+        auto read = [&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value, x = i / 4;
+            if constexpr (i >= N) return;
+            else if constexpr (i % 4 == 0) f[i % (AHEAD + 1)] = Lds::column_frag(gc, 16 * (x / DS), x % DS);
+            else if constexpr (i % 4 == 1) f[i % (AHEAD + 1)] = Lds::row_frag(qr, 0, x);
+            else if constexpr (i % 4 == 2) f[i % (AHEAD + 1)] = Lds::column_frag(qc, 16 * (x / DS), x % DS);
+            else f[i % (AHEAD + 1)] = Lds::row_frag(gr, 0, x);
+        };
+        float pr = 0.f, ds = 0.f, u = 1.f, p_even = 0.f, e_even = 0.f;
+        // half the work on element r: its probability, its dS
+        auto first = [&](auto rc) __attribute__((always_inline)) {
+            constexpr int r = decltype(rc)::value;
+            if constexpr (r % 4 == 0) {
+                l4 = *reinterpret_cast<const v4f *>(l2 + tile_row(r, 0));
+                e4 = *reinterpret_cast<const v4f *>(dl + tile_row(r, 0));
+            }
+            float x = z[r];
+            if constexpr (CAP) {
+                x = tanh_of(x * sm.k1, false);
+                u = 1.f - x * x;
+            }
+            if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 + (float)tile_row(r, 0)), x);
+            const int keep = (int)(w << (31 - tile_row(r, 0))) >> 31;
+            pr = bits_f(f_bits(__builtin_amdgcn_exp2f(fmaf(x, sm.c, -l4[r % 4]))) & keep);
+        };
+        auto second = [&](auto rc) __attribute__((always_inline)) {
+            constexpr int r = decltype(rc)::value;
+            const int keep = (int)(w << (31 - tile_row(r, 0))) >> 31;
+            ds = pr * (e[r] - e4[r % 4]);
+            if constexpr (CAP) ds *= u;
+            ds = bits_f(f_bits(ds) & keep);
+            if constexpr (r % 2 == 0) {
+                p_even = pr;
+                e_even = ds;
+            } else {
+                pn[r / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{p_even, pr}, bf16x2v));
+                en[r / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{e_even, ds}, bf16x2v));
+            }
+        };
+        unroll<AHEAD>(read);
+        unroll<N>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value, x = i / 4;
+            read(std::integral_constant<int, i + AHEAD>{});
+            const Frag<T> &g = f[i % (AHEAD + 1)];
+            if constexpr (i % 4 == 0) dv[x % DS] = mma(g, pf[x / DS], dv[x % DS]);
+            else if constexpr (i % 4 == 1) zn = mma(g, kf[x], zn);
+            else if constexpr (i % 4 == 2) dk[x % DS] = mma(g, ef[x / DS], dk[x % DS]);
+            else en_ = mma(g, vf[x], en_);
+            // 32 halves of elements over N MFMAs
+            unroll<32 / N>([&](auto yc) __attribute__((always_inline)) {
+                constexpr int half = (32 / N) * i + decltype(yc)::value;
+                if constexpr (half % 2 == 0) first(std::integral_constant<int, half / 2>{});
+                else second(std::integral_constant<int, half / 2>{});
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        z = zn;
+        e = en_;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            pw[x] = pn[x];
+            ew[x] = en[x];
+        }
+    };
+
+    At cur = advance();
+    if (cur.tile >= 0) {
+        At nxt = advance();
+        fetch(0, cur);
+        wait_vmcnt<0>();
+        block_barrier();
+        if (nxt.tile >= 0) fetch(1, nxt);
+        if (cur.part) check(0, cur);
+        {
+            const uint32_t qr = Lds::row_base(smem[0][0], lane), gr = Lds::row_base(smem[0][1], lane);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(qr, 0, ks), kf[ks], z);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(gr, 0, ks), vf[ks], e);
+        }
+        int now = 0, last = 0;
+        bool begun = false;
+        while (true) {
+            const int next = now == 2 ? 0 : now + 1;
+            // (the first block's products take weights of 0 on rows that may hold anything)
+            block(now, 0, cur, now, 1, last, 1);
+            if (!begun) {
+#pragma unroll
+                for (int dt = 0; dt < DS; ++dt) dv[dt] = dk[dt] = v16f{};
+                begun = true;
+            }
+            // the next tile is here, and all waves are done with the last one
+            wait_lgkm();
+            wait_vmcnt<0>();
+            block_barrier();
+            const At after = nxt.tile >= 0 ? advance() : nxt;
+            if (after.tile >= 0) fetch(next == 2 ? 0 : next + 1, after);
+            if (nxt.tile >= 0 && nxt.part) check(next, nxt);
+            // (behind the last tile: S and dP of what the stage holds, not used)
+            block(now, 1, cur, nxt.tile >= 0 ? next : now, 0, now, 0);
+            last = now;
+            if (nxt.tile < 0) break;
+            now = next;
+            cur = nxt;
+            nxt = after;
+        }
+        const uint32_t qc = Lds::column_base(smem[last][0], lane), gc = Lds::column_base(smem[last][1], lane);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const bf16x8 pf = __builtin_bit_cast(bf16x8, u4v{pw[4 * s], pw[4 * s + 1], pw[4 * s + 2], pw[4 * s + 3]});
+            const bf16x8 ef = __builtin_bit_cast(bf16x8, u4v{ew[4 * s], ew[4 * s + 1], ew[4 * s + 2], ew[4 * s + 3]});
+#pragma unroll
+            for (int dt = 0; dt < DS; ++dt) {
+                dv[dt] = mma(Lds::column_frag(gc, 32 + 16 * s, dt), pf, dv[dt]);
+                dk[dt] = mma(Lds::column_frag(qc, 32 + 16 * s, dt), ef, dk[dt]);
+            }
+        }
+    }
+    if (!key) return;
+    const float nan = __builtin_nanf("");
+    store_columns<T, DS>((T *)a.dk.p + b * a.dk.sb + (int64_t)j * a.dk.sl + hk * a.dk.sh, dk, spoilt ? nan : m.scale, h, D);
+    store_columns<T, DS>((T *)a.dv.p + b * a.dv.sb + (int64_t)j * a.dv.sl + hk * a.dv.sh, dv, spoilt ? nan : 1.f, h, D);
+}
+
 template <typename T, int DT, int MODS>
 hipError_t launch(const AttentionArgs &a, hipStream_t stream)
 {
     const int64_t nq = (int64_t)((a.len_q + 127) / 128) * a.heads_q * a.batch;
     const int64_t nk = (int64_t)((a.len_k + 127) / 128) * a.heads_kv * a.batch;
     if (nq > INT32_MAX || nk > INT32_MAX) return hipErrorInvalidConfiguration;
-    attention_dkv_kernel<T, DT, MODS><<<(uint32_t)nk, 256, 0, stream>>>(a);
+    if constexpr (sizeof(T) == 2) attention_dkv_pipe_kernel<DT, MODS><<<(uint32_t)nk, 256, 0, stream>>>(a);
+    else attention_dkv_kernel<T, DT, MODS><<<(uint32_t)nk, 256, 0, stream>>>(a);
     attention_dq_kernel<T, DT, MODS><<<(uint32_t)nq, 256, 0, stream>>>(a);
     return hipGetLastError();
 }

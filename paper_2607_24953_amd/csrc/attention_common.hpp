@@ -333,11 +333,18 @@ __device__ __forceinline__ void add_non_finite(v16f *acc, uint32_t seen, uint32_
 // ---------------------------------------------------------------- masks
 
 // What the masks leave between query positions [p0, p1] and keys [j0, j1]: nothing, some
-// or all pairs.  (qmin, qmax), (kmin, kmax): ranges of their document numbers.
+// or all pairs.
 struct Seen { bool any, all; };
 
+// Range of the document numbers of some positions, and whether there is padding among them
+// (negative numbers, which the range leaves out).  In memory: {lo, or ~lo with padding; hi}.
+struct Documents {
+    int lo, hi;
+    bool padding;
+};
+
 __device__ __forceinline__ Seen classify(const AttentionMask &m, int prefix, int p0, int p1, int j0, int j1,
-                                         int qmin, int qmax, int kmin, int kmax)
+                                         const Documents &q, const Documents &k)
 {
     bool any = true, all = true;
     if (m.causal) {
@@ -355,8 +362,8 @@ __device__ __forceinline__ Seen classify(const AttentionMask &m, int prefix, int
     any = any || j0 < prefix;
     all = all || j1 < prefix;
     if (m.documents) {
-        any = any && qmin <= kmax && kmin <= qmax && kmax >= 0 && qmax >= 0;
-        all = all && qmin == qmax && kmin == kmax && qmin == kmin && qmin >= 0;
+        any = any && q.lo <= k.hi && k.lo <= q.hi;
+        all = all && q.lo == q.hi && k.lo == k.hi && q.lo == k.lo && !q.padding && !k.padding;
     }
     return {any, all && any};
 }
@@ -451,18 +458,17 @@ __device__ __forceinline__ Sight key_sight(const AttentionMask &m, int j, int le
 // Whether bit tile_row(r, h) of a word is set, the word shifted right by 4 h beforehand
 __device__ __forceinline__ bool word_bit(uint32_t w, int r) { return (w >> tile_row(r, 0)) & 1; }
 
-// Document range of the positions [p0, p1] from the ranges of 64 positions; positions
-// below zero have no document
-__device__ __forceinline__ int2 range_of(const int2 *ranges, int p0, int p1)
+// Documents of the positions [p0, p1] from the ranges of 64 positions; positions below zero
+// have none
+__device__ __forceinline__ Documents range_of(const int2 *ranges, int p0, int p1)
 {
-    if (p1 < 0) return make_int2(-1, -1);
-    int2 r = ranges[(p0 < 0 ? 0 : p0) >> 6];
-    for (int i = ((p0 < 0 ? 0 : p0) >> 6) + 1; i <= p1 >> 6; ++i) {
+    Documents r = {INT32_MAX, -1, p0 < 0};
+    for (int i = max(p0, 0) >> 6; i <= p1 >> 6; ++i) {
         const int2 s = ranges[i];
-        r.x = min(r.x, s.x);
-        r.y = max(r.y, s.y);
+        r.lo = min(r.lo, s.x < 0 ? ~s.x : s.x);
+        r.hi = max(r.hi, s.y);
+        r.padding = r.padding || s.x < 0;
     }
-    if (p0 < 0) r.x = min(r.x, -1);
     return r;
 }
 

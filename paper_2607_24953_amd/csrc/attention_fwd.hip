@@ -47,7 +47,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
     const int2 *ranges = a.ranges + (int64_t)b * ((a.len_k + 63) / 64);
     const int p0 = i0 + shift, p1 = min(i0 + BM, a.len_q) - 1 + shift;
     const int pw0 = iw + shift, pw1 = min(iw + 32, a.len_q) - 1 + shift;
-    int2 dg = make_int2(0, 0), dw = dg;
+    Documents dg = {}, dw = {};
     int my_doc = 0;
     if (docs) {
         dg = range_of(ranges, p0, p1);
@@ -62,10 +62,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
     if (m.causal && !m.prefix) end = p1 < 0 ? 0 : min(end, p1 / BN + 1);
     auto see = [&](int t, Seen &g, Seen &w) {
         const int j0 = t * BN, j1 = min(j0 + BN, a.len_k) - 1;
-        const int2 dk = docs ? ranges[j0 >> 6] : make_int2(0, 0);
-        g = classify(m, prefix, p0, p1, j0, j1, dg.x, dg.y, dk.x, dk.y);
+        const Documents dk = docs ? range_of(ranges, j0, j0) : Documents{};
+        g = classify(m, prefix, p0, p1, j0, j1, dg, dk);
         if (pw1 >= pw0) {
-            w = classify(m, prefix, pw0, pw1, j0, j1, dw.x, dw.y, dk.x, dk.y);
+            w = classify(m, prefix, pw0, pw1, j0, j1, dw, dk);
             w.all = w.all && j0 + BN <= a.len_k;
         }
     };
