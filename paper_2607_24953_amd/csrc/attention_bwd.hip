@@ -217,7 +217,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArg
 // ---------------------------------------------------------------- dK, dV
 
 template <typename T, int DT, int MODS>
-__global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionArgs a)
+__global__ __launch_bounds__(256, DT == 64 && sizeof(T) == 2 ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a)
 {
     constexpr int BQ = sizeof(T) == 2 ? 64 : 32, NW = 4, BN = 32 * NW, KS = DT / 16, DS = DT / 32;
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2, F32 = sizeof(T) == 4;
@@ -380,21 +380,21 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttentionAr
     store_columns<T, DS>((T *)a.dv.p + b * a.dv.sb + (int64_t)j * a.dv.sl + hk * a.dv.sh, dv, spoilt ? nan : 1.f, h, D);
 }
 
-// The same for bfloat16 as a software pipeline.  The accumulators of 32 keys and their K and V
-// fragments take 192 registers of a wave at 128 dims, so only one wave fits a SIMD and nothing
-// but its own instructions can fill the time of a matrix product.  Over steps n of 32 query
-// rows, block n therefore forms S and dP of step n + 1 and the products of step n - 1 while
-// its vector instructions turn step n's S and dP into P and dS: after each MFMA stands its
-// share of them and of the LDS reads for the MFMAs to come (sched_barrier keeps the order).
-// Tiles of 64 rows pass through three LDS stages: the last, this and the next one.
+// The same for bfloat16 with more than 64 dims, where the two accumulators of 32 keys and
+// their K and V fragments take 192 registers: one wave a SIMD could hold them, and would then
+// be bound by issuing one instruction after the other.  So two waves share 32 keys: the first
+// keeps K and dV, forms S and P, and leaves P in LDS; the second keeps V and dK, forms dP and,
+// one tile later, dS.  P passes in the registers' own order (operand fragments), rounded to
+// bfloat16 as the product with dO takes it, and with the cap's derivative multiplied in.
 template <int DT, int MODS>
-__global__ __launch_bounds__(256, 1) void attention_dkv_pipe_kernel(const AttentionArgs a)
+__global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const AttentionArgs a)
 {
     typedef __bf16 T;
-    constexpr int BQ = 64, NW = 4, BN = 32 * NW, KS = DT / 16, DS = DT / 32;
+    constexpr int BQ = 64, NW = 8, BN = 128, KS = DT / 16, DS = DT / 32;
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2;
     typedef Tile<T, DT> Lds;
     __shared__ __align__(1024) uint8_t smem[3][2][BQ * Lds::kRowBytes];
+    __shared__ u4v shared_p[2][4][BQ / 32][2][64];             // [tile parity][keys][rows][half][lane]
     __shared__ __align__(16) float rows[3][2][64];             // lse2, delta of a tile's queries
     __shared__ __align__(16) int32_t doc_of[3][64];            // and their documents
     __shared__ uint32_t found[2][NW][BQ / 32];                 // rows with infinities and NaN
@@ -405,19 +405,19 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_pipe_kernel(const Attent
     head_tile(blockIdx.x, gridDim.x, tiles, head, kt);
     const int b = head / a.heads_kv, hk = head % a.heads_kv, group = a.heads_q / a.heads_kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool second = wave >= 4;
+    const int keys = wave & 3;
     const int h = lane >> 5, col = lane & 31;
     const int shift = a.len_k - a.len_q, D = a.dim;
-    const int j0 = kt * BN, jw = j0 + wave * 32, j = jw + col;
+    const int j0 = kt * BN, jw = j0 + keys * 32, j = jw + col;
     const bool key = j < a.len_k;
 
-    const T *k = (const T *)a.k.p + b * a.k.sb + (int64_t)j * a.k.sl + hk * a.k.sh;
-    const T *v = (const T *)a.v.p + b * a.v.sb + (int64_t)j * a.v.sl + hk * a.v.sh;
-    Frag<T> kf[KS], vf[KS];
+    // K rows for the first wave, V rows for the second
+    const HeadsView &mine = second ? a.v : a.k;
+    const T *kv = (const T *)mine.p + b * mine.sb + (int64_t)j * mine.sl + hk * mine.sh;
+    Frag<T> f[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-        kf[ks] = global_frag<T>(k, key, ks, h, D);
-        vf[ks] = global_frag<T>(v, key, ks, h, D);
-    }
+    for (int ks = 0; ks < KS; ++ks) f[ks] = global_frag<T>(kv, key, ks, h, D);
     const int prefix = m.prefix ? min(max(m.prefix[b], 0), a.len_k) : 0;
     const int32_t *docs = m.documents ? m.documents + (int64_t)b * a.len_k : nullptr;
     const int2 *ranges = a.ranges + (int64_t)b * ((a.len_k + 63) / 64);
@@ -448,7 +448,7 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_pipe_kernel(const Attent
     }
 
     // the visited tiles of all query heads, in order
-    struct At { int tile, head; bool part, all; };
+    struct At { int tile, head; bool part, any, all; };
     Schedule sched;
     int gh = 0;
     auto advance = [&]() __attribute__((always_inline)) {
@@ -457,7 +457,7 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_pipe_kernel(const Attent
             sched = Schedule();
             t = sched.next(end, see);
         }
-        return At{t, gh, sched.part, sched.wave_all};
+        return At{t, gh, sched.part, sched.wave_any, sched.wave_all};
     };
     auto fetch = [&](int st, const At &at) __attribute__((always_inline)) {
         const int hq = hk * group + at.head, i0 = at.tile * BQ;
@@ -481,163 +481,127 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_pipe_kernel(const Attent
         for (int t = 0; t < BQ / 32; ++t) {
             const uint32_t w =
                 at.all ? ~0u : sight.word(at.tile * BQ + 32 * t + shift, docs ? &doc_of[stage][32 * t] : nullptr);
-            spoilt = spoilt || (w & (bq[t] | bg[t]));
+            spoilt = spoilt || (at.any && (w & (bq[t] | bg[t])));
         }
         Lds::template clean<BQ, NW * 64>(smem[stage][0]);
         Lds::template clean<BQ, NW * 64>(smem[stage][1]);
     };
 
-    v16f dk[DS] = {}, dv[DS] = {};
-    v16f z = {}, e = {};                                 // S and dP of the step at hand
-    uint32_t pw[8] = {}, ew[8] = {};                     // P and dS of the step before, bf16 pairs
-
-    // Block of step n: rows 32 t of stage `now`; its S and dP are in z and e.  (next, tn): the
-    // following step's rows, (last, tl): the preceding one's.
-    auto block = [&](int now, int t, const At &at, int next, int tn, int last, int tl) __attribute__((always_inline)) {
-        constexpr int N = 8 * DS;                        // MFMAs: 2 DS each of dV, dK, S and dP
-        constexpr int AHEAD = 4;
-        const uint32_t qr = Lds::row_base(smem[next][0], lane) + tn * 32 * Lds::kRowBytes;
-        const uint32_t gr = Lds::row_base(smem[next][1], lane) + tn * 32 * Lds::kRowBytes;
-        const uint32_t qc = Lds::column_base(smem[last][0], lane) + tl * 32 * Lds::kRowBytes;
-        const uint32_t gc = Lds::column_base(smem[last][1], lane) + tl * 32 * Lds::kRowBytes;
-        const int p0 = at.tile * BQ + 32 * t + shift;
+    // The first wave on a tile: P, and its product with dO
+    auto probabilities = [&](v16f *acc, int stage, int parity, const At &at) __attribute__((always_inline)) {
+        const uint32_t qr = Lds::row_base(smem[stage][0], lane), gc = Lds::column_base(smem[stage][1], lane);
         const ScoreMap sm = score_map(m, hk * group + at.head);
-        const float d0 = BIAS ? (float)(p0 + 4 * h) - (float)j : 0.f;
-        const uint32_t w = (at.all ? ~0u : sight.word(p0, docs ? &doc_of[now][32 * t] : nullptr)) >> (4 * h);
-        const float *l2 = &rows[now][0][32 * t + 4 * h], *dl = &rows[now][1][32 * t + 4 * h];
-        uint32_t pn[8], en[8];
-        v16f zn = {}, en_ = {};
-        Frag<T> f[AHEAD + 1];
-        v4f l4, e4;
-        bf16x8 pf[2], ef[2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            pf[s] = __builtin_bit_cast(bf16x8, u4v{pw[4 * s], pw[4 * s + 1], pw[4 * s + 2], pw[4 * s + 3]});
-            ef[s] = __builtin_bit_cast(bf16x8, u4v{ew[4 * s], ew[4 * s + 1], ew[4 * s + 2], ew[4 * s + 3]});
+        for (int t = 0; t < BQ / 32; ++t) {
+            v16f z = {};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(qr, t, ks), f[ks], z);
+            const int p0 = at.tile * BQ + 32 * t + shift;
+            const float d0 = BIAS ? (float)(p0 + 4 * h) - (float)j : 0.f;
+            v16f pu;
+#pragma unroll
+            for (int x4 = 0; x4 < 4; ++x4) {
+                const v4f l4 = *reinterpret_cast<const v4f *>(&rows[stage][0][32 * t + tile_row(4 * x4, h)]);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int r = 4 * x4 + y;
+                    float x = z[r], u = 1.f;
+                    if constexpr (CAP) {
+                        x = tanh_of(x * sm.k1, false);
+                        u = 1.f - x * x;
+                    }
+                    if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 + (float)tile_row(r, 0)), x);
+                    z[r] = __builtin_amdgcn_exp2f(fmaf(x, sm.c, -l4[y]));
+                    if constexpr (CAP) pu[r] = z[r] * u;
+                }
+            }
+            if (!at.all) {
+                const uint32_t w = sight.word(p0, docs ? &doc_of[stage][32 * t] : nullptr) >> (4 * h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    z[r] = word_bit(w, r) ? z[r] : 0.f;
+                    if constexpr (CAP) pu[r] = word_bit(w, r) ? pu[r] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const Frag<T> pf = to_frag<T>(z, s);
+                shared_p[parity][keys][t][s][lane] = __builtin_bit_cast(u4v, CAP ? to_frag<T>(pu, s) : pf);
+#pragma unroll
+                for (int dt = 0; dt < DS; ++dt) acc[dt] = mma(Lds::column_frag(gc, 32 * t + 16 * s, dt), pf, acc[dt]);
+            }
         }
-        // operand of MFMA i: i % 4 = 0: dV, 1: S, 2: dK, 3: dP; number x = i / 4 of its kind
-        auto read = [&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value, x = i / 4;
-            if constexpr (i >= N) return;
-            else if constexpr (i % 4 == 0) f[i % (AHEAD + 1)] = Lds::column_frag(gc, 16 * (x / DS), x % DS);
-            else if constexpr (i % 4 == 1) f[i % (AHEAD + 1)] = Lds::row_frag(qr, 0, x);
-            else if constexpr (i % 4 == 2) f[i % (AHEAD + 1)] = Lds::column_frag(qc, 16 * (x / DS), x % DS);
-            else f[i % (AHEAD + 1)] = Lds::row_frag(gr, 0, x);
-        };
-        float pr = 0.f, ds = 0.f, u = 1.f, p_even = 0.f, e_even = 0.f;
-        // half the work on element r: its probability, its dS
-        auto first = [&](auto rc) __attribute__((always_inline)) {
-            constexpr int r = decltype(rc)::value;
-            if constexpr (r % 4 == 0) {
-                l4 = *reinterpret_cast<const v4f *>(l2 + tile_row(r, 0));
-                e4 = *reinterpret_cast<const v4f *>(dl + tile_row(r, 0));
-            }
-            float x = z[r];
-            if constexpr (CAP) {
-                x = tanh_of(x * sm.k1, false);
-                u = 1.f - x * x;
-            }
-            if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 + (float)tile_row(r, 0)), x);
-            const int keep = (int)(w << (31 - tile_row(r, 0))) >> 31;
-            pr = bits_f(f_bits(__builtin_amdgcn_exp2f(fmaf(x, sm.c, -l4[r % 4]))) & keep);
-        };
-        auto second = [&](auto rc) __attribute__((always_inline)) {
-            constexpr int r = decltype(rc)::value;
-            const int keep = (int)(w << (31 - tile_row(r, 0))) >> 31;
-            ds = pr * (e[r] - e4[r % 4]);
-            if constexpr (CAP) ds *= u;
-            ds = bits_f(f_bits(ds) & keep);
-            if constexpr (r % 2 == 0) {
-                p_even = pr;
-                e_even = ds;
-            } else {
-                pn[r / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{p_even, pr}, bf16x2v));
-                en[r / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{e_even, ds}, bf16x2v));
-            }
-        };
-        unroll<AHEAD>(read);
-        unroll<N>([&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value, x = i / 4;
-            read(std::integral_constant<int, i + AHEAD>{});
-            const Frag<T> &g = f[i % (AHEAD + 1)];
-            if constexpr (i % 4 == 0) dv[x % DS] = mma(g, pf[x / DS], dv[x % DS]);
-            else if constexpr (i % 4 == 1) zn = mma(g, kf[x], zn);
-            else if constexpr (i % 4 == 2) dk[x % DS] = mma(g, ef[x / DS], dk[x % DS]);
-            else en_ = mma(g, vf[x], en_);
-            // 32 halves of elements over N MFMAs
-            unroll<32 / N>([&](auto yc) __attribute__((always_inline)) {
-                constexpr int half = (32 / N) * i + decltype(yc)::value;
-                if constexpr (half % 2 == 0) first(std::integral_constant<int, half / 2>{});
-                else second(std::integral_constant<int, half / 2>{});
-            });
-            __builtin_amdgcn_sched_barrier(0);
-        });
-        z = zn;
-        e = en_;
+    };
+    // The second wave on the tile before: dS, and its product with Q
+    auto gradients = [&](v16f *acc, int stage, int parity, const At &at) __attribute__((always_inline)) {
+        const uint32_t gr = Lds::row_base(smem[stage][1], lane), qc = Lds::column_base(smem[stage][0], lane);
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            pw[x] = pn[x];
-            ew[x] = en[x];
+        for (int t = 0; t < BQ / 32; ++t) {
+            v16f e = {};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(gr, t, ks), f[ks], e);
+            u4v pw[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) pw[s] = shared_p[parity][keys][t][s][lane];
+            auto p_of = [&](int r) __attribute__((always_inline)) {
+                const uint32_t w = pw[r / 8][r % 8 / 2];
+                return bits_f(r % 2 ? w & 0xffff0000u : w << 16);
+            };
+#pragma unroll
+            for (int x4 = 0; x4 < 4; ++x4) {
+                const v4f e4 = *reinterpret_cast<const v4f *>(&rows[stage][1][32 * t + tile_row(4 * x4, h)]);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) e[4 * x4 + y] = p_of(4 * x4 + y) * (e[4 * x4 + y] - e4[y]);
+            }
+            if (!at.all) {
+                // (what is not seen may have brought a NaN into dP)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) e[r] = p_of(r) != 0.f ? e[r] : 0.f;
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const Frag<T> ef = to_frag<T>(e, s);
+#pragma unroll
+                for (int dt = 0; dt < DS; ++dt) acc[dt] = mma(Lds::column_frag(qc, 32 * t + 16 * s, dt), ef, acc[dt]);
+            }
         }
     };
 
-    At cur = advance();
-    if (cur.tile >= 0) {
-        At nxt = advance();
-        fetch(0, cur);
-        wait_vmcnt<0>();
-        block_barrier();
-        if (nxt.tile >= 0) fetch(1, nxt);
-        if (cur.part) check(0, cur);
-        {
-            const uint32_t qr = Lds::row_base(smem[0][0], lane), gr = Lds::row_base(smem[0][1], lane);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(qr, 0, ks), kf[ks], z);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(gr, 0, ks), vf[ks], e);
-        }
-        int now = 0, last = 0;
-        bool begun = false;
-        while (true) {
-            const int next = now == 2 ? 0 : now + 1;
-            // (the first block's products take weights of 0 on rows that may hold anything)
-            block(now, 0, cur, now, 1, last, 1);
-            if (!begun) {
-#pragma unroll
-                for (int dt = 0; dt < DS; ++dt) dv[dt] = dk[dt] = v16f{};
-                begun = true;
-            }
-            // the next tile is here, and all waves are done with the last one
-            wait_lgkm();
+    // (a loop for each of the two: they share nothing but the barriers)
+    auto run = [&](auto second) __attribute__((always_inline)) {
+        constexpr bool SECOND = decltype(second)::value;
+        v16f acc[DS] = {};                               // dV, or dK
+        At cur = advance(), before = {-1, 0, false, false, false};
+        int stage = 0, parity = 0;
+        if (cur.tile >= 0) fetch(0, cur);
+        while (cur.tile >= 0 || before.tile >= 0) {
+            // this tile is here, the last one's P too, and all waves are done with the one before
             wait_vmcnt<0>();
+            wait_lgkm();
             block_barrier();
-            const At after = nxt.tile >= 0 ? advance() : nxt;
-            if (after.tile >= 0) fetch(next == 2 ? 0 : next + 1, after);
-            if (nxt.tile >= 0 && nxt.part) check(next, nxt);
-            // (behind the last tile: S and dP of what the stage holds, not used)
-            block(now, 1, cur, nxt.tile >= 0 ? next : now, 0, now, 0);
-            last = now;
-            if (nxt.tile < 0) break;
-            now = next;
-            cur = nxt;
-            nxt = after;
-        }
-        const uint32_t qc = Lds::column_base(smem[last][0], lane), gc = Lds::column_base(smem[last][1], lane);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const bf16x8 pf = __builtin_bit_cast(bf16x8, u4v{pw[4 * s], pw[4 * s + 1], pw[4 * s + 2], pw[4 * s + 3]});
-            const bf16x8 ef = __builtin_bit_cast(bf16x8, u4v{ew[4 * s], ew[4 * s + 1], ew[4 * s + 2], ew[4 * s + 3]});
-#pragma unroll
-            for (int dt = 0; dt < DS; ++dt) {
-                dv[dt] = mma(Lds::column_frag(gc, 32 + 16 * s, dt), pf, dv[dt]);
-                dk[dt] = mma(Lds::column_frag(qc, 32 + 16 * s, dt), ef, dk[dt]);
+            At next = cur;
+            if (cur.tile >= 0) {
+                next = advance();
+                if (next.tile >= 0) fetch(stage == 2 ? 0 : stage + 1, next);
+                if (cur.part) check(stage, cur);
             }
+            if constexpr (SECOND) {
+                if (before.tile >= 0 && before.any) gradients(acc, stage == 0 ? 2 : stage - 1, parity ^ 1, before);
+            } else {
+                if (cur.tile >= 0 && cur.any) probabilities(acc, stage, parity, cur);
+            }
+            before = cur;
+            cur = next;
+            stage = stage == 2 ? 0 : stage + 1;
+            parity ^= 1;
         }
-    }
-    if (!key) return;
-    const float nan = __builtin_nanf("");
-    store_columns<T, DS>((T *)a.dk.p + b * a.dk.sb + (int64_t)j * a.dk.sl + hk * a.dk.sh, dk, spoilt ? nan : m.scale, h, D);
-    store_columns<T, DS>((T *)a.dv.p + b * a.dv.sb + (int64_t)j * a.dv.sl + hk * a.dv.sh, dv, spoilt ? nan : 1.f, h, D);
+        if (!key) return;
+        const HeadsView &to = SECOND ? a.dk : a.dv;
+        store_columns<T, DS>((T *)to.p + b * to.sb + (int64_t)j * to.sl + hk * to.sh, acc,
+                             spoilt ? __builtin_nanf("") : SECOND ? m.scale : 1.f, h, D);
+    };
+    if (second) run(std::true_type{});
+    else run(std::false_type{});
 }
 
 template <typename T, int DT, int MODS>
@@ -646,7 +610,7 @@ hipError_t launch(const AttentionArgs &a, hipStream_t stream)
     const int64_t nq = (int64_t)((a.len_q + 127) / 128) * a.heads_q * a.batch;
     const int64_t nk = (int64_t)((a.len_k + 127) / 128) * a.heads_kv * a.batch;
     if (nq > INT32_MAX || nk > INT32_MAX) return hipErrorInvalidConfiguration;
-    if constexpr (sizeof(T) == 2) attention_dkv_pipe_kernel<DT, MODS><<<(uint32_t)nk, 256, 0, stream>>>(a);
+    if constexpr (sizeof(T) == 2 && DT == 128) attention_dkv_pair_kernel<DT, MODS><<<(uint32_t)nk, 512, 0, stream>>>(a);
     else attention_dkv_kernel<T, DT, MODS><<<(uint32_t)nk, 256, 0, stream>>>(a);
     attention_dq_kernel<T, DT, MODS><<<(uint32_t)nq, 256, 0, stream>>>(a);
     return hipGetLastError();
