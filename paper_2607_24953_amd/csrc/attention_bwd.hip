@@ -66,14 +66,18 @@ __global__ __launch_bounds__(64) void document_ranges_kernel(const int32_t *docs
 
 // ---------------------------------------------------------------- dQ
 
-template <typename T, int DT, int MODS>
-__global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArgs a)
+// (NARROW as in the forward kernel)
+template <typename T, int DC, int MODS, bool NARROW>
+__global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const AttentionArgs a)
 {
-    constexpr int BN = sizeof(T) == 2 ? 64 : 32, NW = 4, BM = 32 * NW, KS = DT / 16, DS = DT / 32;
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2, F32 = sizeof(T) == 4;
+    // DC dims are computed (a multiple of 32, dim rounded up), DT lie in an LDS row
+    constexpr int DT = DC <= 64 ? 64 : 128, KS = DC / 16, DS = DC / 32;
+    constexpr int NW = 4, BM = NARROW ? 32 : 32 * NW, BN = NARROW ? 32 * NW : F32 ? 32 : 64, WN = NARROW ? 32 : BN;
     typedef Tile<T, DT> Lds;
-    __shared__ __align__(1024) uint8_t smem[2][2][BN * Lds::kRowBytes];
-    __shared__ __align__(16) int32_t doc_of[2][64];            // documents of a tile's keys
+    constexpr int kBytes = BN * Lds::kRowBytes, NS = stages_of(2 * kBytes);
+    __shared__ __align__(1024) uint8_t smem[NS][2][kBytes];
+    __shared__ __align__(16) int32_t doc_of[NS][BN < 64 ? 64 : BN];   // documents of a tile's keys
     __shared__ uint32_t found[NW][BN / 32];                    // rows with infinities and NaN
 
     const AttentionMask &m = a.mask;
@@ -85,7 +89,8 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArg
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, col = lane & 31;
     const int shift = a.len_k - a.len_q, D = a.dim;
-    const int i0 = qt * BM, iw = i0 + wave * 32, i = iw + col;
+    const int i0 = qt * BM, iw = NARROW ? i0 : i0 + wave * 32, i = iw + col;
+    const int jw = NARROW ? 32 * wave : 0;                     // the wave's first key of a tile
     const int p = i + shift;
     const bool row = i < a.len_q;
 
@@ -121,13 +126,12 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArg
 
     int end = (a.len_k + BN - 1) / BN;
     if (m.causal && !m.prefix) end = p1 < 0 ? 0 : min(end, p1 / BN + 1);
-    auto see = [&](int t, Seen &s, Seen &w) {
-        const int j0 = t * BN, j1 = min(j0 + BN, a.len_k) - 1;
-        const Documents dk = docs ? range_of(ranges, j0, j0) : Documents{};
-        s = classify(m, prefix, p0, p1, j0, j1, dg, dk);
-        if (pw1 >= pw0) {
-            w = classify(m, prefix, pw0, pw1, j0, j1, dw, dk);
-            w.all = w.all && j0 + BN <= a.len_k;
+    auto see = [&](int t, Seen &g, Seen &w) __attribute__((always_inline)) {
+        const int j0 = t * BN, j1 = min(j0 + BN, a.len_k) - 1, k0 = j0 + jw, k1 = min(k0 + WN, a.len_k) - 1;
+        g = classify(m, prefix, p0, p1, j0, j1, dg, docs ? range_of(ranges, j0, j1) : Documents{});
+        if (pw1 >= pw0 && k1 >= k0) {
+            w = classify(m, prefix, pw0, pw1, k0, k1, dw, docs ? range_of(ranges, k0, k1) : Documents{});
+            w.all = w.all && k0 + WN <= a.len_k;
         }
     };
     if (D < DT) {
@@ -138,12 +142,12 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArg
 
     bool spoilt = false;                // this query sees an infinity or a NaN among the keys
 
-    // one tile of keys; all: no pair of this wave is masked
-    auto tile = [&](bool all, int stage, int j0) __attribute__((always_inline)) {
-        const uint8_t *kt = smem[stage][0], *vt = smem[stage][1];
+    auto tile = [&](const Visit &at, int stage) __attribute__((always_inline)) {
+        const int j0 = at.tile * BN + jw;
+        const uint8_t *kt = smem[stage][0] + jw * Lds::kRowBytes, *vt = smem[stage][1] + jw * Lds::kRowBytes;
         const uint32_t kr = Lds::row_base(kt, lane), vr = Lds::row_base(vt, lane), kc = Lds::column_base(kt, lane);
 #pragma unroll
-        for (int t = 0; t < BN / 32; ++t) {
+        for (int t = 0; t < WN / 32; ++t) {
             v16f z = {}, e = {};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(kr, t, ks), qf[ks], z);
@@ -161,8 +165,8 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArg
                 const float pr = __builtin_amdgcn_exp2f(fmaf(x, sm.c, -lse2));
                 e[r] = pr * (e[r] - delta) * u;
             }
-            if (!all) {
-                const uint32_t w = sight.word(j0 + 32 * t, docs ? &doc_of[stage][32 * t] : nullptr) >> (4 * h);
+            if (!at.all) {
+                const uint32_t w = sight.word(j0 + 32 * t, docs ? &doc_of[stage][jw + 32 * t] : nullptr) >> (4 * h);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) e[r] = word_bit(w, r) ? e[r] : 0.f;
             }
@@ -175,56 +179,55 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttentionArg
             }
         }
     };
-    auto check = [&](int stage, int j0, bool any, bool all) __attribute__((always_inline)) {
+    auto check = [&](const Visit &at, int stage) __attribute__((always_inline)) {
         uint32_t bad[BN / 32], some = 0;
         non_finite<Lds, BN, NW>(smem[stage][0], &found[0][0], bad);
 #pragma unroll
         for (int t = 0; t < BN / 32; ++t) some |= bad[t];
         if (!some) return;
 #pragma unroll
-        for (int t = 0; t < BN / 32; ++t) {
-            const uint32_t w = all ? ~0u : sight.word(j0 + 32 * t, docs ? &doc_of[stage][32 * t] : nullptr);
-            spoilt = spoilt || (any && (w & bad[t]));
+        for (int t = 0; t < WN / 32; ++t) {
+            const uint32_t w = sight.word(at.tile * BN + jw + 32 * t, docs ? &doc_of[stage][jw + 32 * t] : nullptr);
+            spoilt = spoilt || (at.any && ((at.all ? ~0u : w) & pick<BN / 32>(bad, NARROW ? wave : t)));
         }
         Lds::template clean<BN, NW * 64>(smem[stage][0]);
     };
     auto fetch = [&](int stage, int t) __attribute__((always_inline)) {
         Lds::template load<BN, NW * 64>(smem[stage][0], k, a.k.sl, t * BN, a.len_k, D);
         Lds::template load<BN, NW * 64>(smem[stage][1], v, a.v.sl, t * BN, a.len_k, D);
-        if (docs && wave == 0) load_words64(doc_of[stage], docs, t * BN, a.len_k);
+        if (docs && wave < (BN + 63) / 64) load_words64(&doc_of[stage][64 * wave], docs, t * BN + 64 * wave, a.len_k);
     };
-
-    Schedule sched;
-    int cur = sched.next(end, see), stage = 0;
-    if (cur >= 0) fetch(0, cur);
-    while (cur >= 0) {
-        const bool part = sched.part, any = sched.wave_any, all = sched.wave_all;
-        wait_vmcnt<0>();
-        block_barrier();
-        const int next = sched.next(end, see);
-        if (next >= 0) fetch(stage ^ 1, next);
-        if (part) check(stage, cur * BN, any, all);
-        if (any) tile(all, stage, cur * BN);
-        wait_lgkm();
-        cur = next;
-        stage ^= 1;
+    tile_loop<NS, 2 * kBytes / (NW * 1024)>(end, see, fetch, check, tile);
+    if (spoilt) {
+#pragma unroll
+        for (int dt = 0; dt < DS; ++dt) dq[dt] += __builtin_nanf("");
+    }
+    if constexpr (NARROW) {
+        __syncthreads();                       // no wave reads a tile any more
+        join_waves<DS>(dq, smem[0][0]);
+        if (wave != 0) return;
     }
     if (!row) return;
     T *out = (T *)a.dq.p + b * a.dq.sb + (int64_t)i * a.dq.sl + hq * a.dq.sh;
-    store_columns<T, DS>(out, dq, spoilt ? __builtin_nanf("") : m.scale, h, D);
+    store_columns<T, DS>(out, dq, m.scale, h, D);
 }
 
 // ---------------------------------------------------------------- dK, dV
 
-template <typename T, int DT, int MODS>
-__global__ __launch_bounds__(256, DT == 64 && sizeof(T) == 2 ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a)
+// A workgroup of four waves owns 128 keys and its waves share tiles of 64 (float32: 32)
+// queries; or (NARROW) 32 keys, and each wave takes its quarter of tiles of 128 queries.
+template <typename T, int DC, int MODS, bool NARROW>
+__global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a)
 {
-    constexpr int BQ = sizeof(T) == 2 ? 64 : 32, NW = 4, BN = 32 * NW, KS = DT / 16, DS = DT / 32;
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2, F32 = sizeof(T) == 4;
+    // DC dims are computed (a multiple of 32, dim rounded up), DT lie in an LDS row
+    constexpr int DT = DC <= 64 ? 64 : 128, KS = DC / 16, DS = DC / 32;
+    constexpr int NW = 4, BN = NARROW ? 32 : 32 * NW, BQ = NARROW ? 32 * NW : F32 ? 32 : 64, WQ = NARROW ? 32 : BQ;
     typedef Tile<T, DT> Lds;
-    __shared__ __align__(1024) uint8_t smem[2][2][BQ * Lds::kRowBytes];
-    __shared__ __align__(16) float rows[2][2][64];             // lse2, delta of a tile's queries
-    __shared__ __align__(16) int32_t doc_of[2][64];            // and their documents
+    constexpr int kBytes = BQ * Lds::kRowBytes, NS = stages_of(2 * kBytes), kWords = BQ < 64 ? 64 : BQ;
+    __shared__ __align__(1024) uint8_t smem[NS][2][kBytes];
+    __shared__ __align__(16) float rows[NS][2][kWords];         // lse2, delta of a tile's queries
+    __shared__ __align__(16) int32_t doc_of[NS][kWords];        // and their documents
     __shared__ uint32_t found[2][NW][BQ / 32];                 // rows with infinities and NaN
 
     const AttentionMask &m = a.mask;
@@ -235,7 +238,8 @@ __global__ __launch_bounds__(256, DT == 64 && sizeof(T) == 2 ? 2 : 1) void atten
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, col = lane & 31;
     const int shift = a.len_k - a.len_q, D = a.dim;
-    const int j0 = kt * BN, jw = j0 + wave * 32, j = jw + col;
+    const int j0 = kt * BN, jw = NARROW ? j0 : j0 + wave * 32, j = jw + col;
+    const int iw = NARROW ? 32 * wave : 0;                     // the wave's first query of a tile
     const bool key = j < a.len_k;
 
     const T *k = (const T *)a.k.p + b * a.k.sb + (int64_t)j * a.k.sl + hk * a.k.sh;
@@ -260,15 +264,16 @@ __global__ __launch_bounds__(256, DT == 64 && sizeof(T) == 2 ? 2 : 1) void atten
     Sight sight = key_sight(m, j, a.len_k, prefix, my_doc);    // (queries end at position len_k)
     if (docs) sight.lo = max(sight.lo, 0);                     // (and have no document below 0)
 
-    // tiles of query rows [t BQ, ..); all rows of a tile are queries only where it is whole
+    // tiles of query rows [t BQ, ..)
     const int end = (a.len_q + BQ - 1) / BQ;
-    auto see = [&](int t, Seen &s, Seen &w) {
-        const int p0 = t * BQ + shift, p1 = min(t * BQ + BQ, a.len_q) - 1 + shift;
-        const Documents dq = docs ? range_of(ranges, p0, p1) : Documents{};
-        s = classify(m, prefix, p0, p1, j0, j1, dq, dg);
-        if (jw1 >= jw) {
-            w = classify(m, prefix, p0, p1, jw, jw1, dq, dw);
-            w.all = w.all && t * BQ + BQ <= a.len_q;
+    auto see = [&](int t, Seen &g, Seen &w) __attribute__((always_inline)) {
+        const int i0 = t * BQ, i1 = min(i0 + BQ, a.len_q) - 1, k0 = i0 + iw, k1 = min(k0 + WQ, a.len_q) - 1;
+        g = classify(m, prefix, i0 + shift, i1 + shift, j0, j1,
+                     docs ? range_of(ranges, i0 + shift, i1 + shift) : Documents{}, dg);
+        if (jw1 >= jw && k1 >= k0) {
+            w = classify(m, prefix, k0 + shift, k1 + shift, jw, jw1,
+                         docs ? range_of(ranges, k0 + shift, k1 + shift) : Documents{}, dw);
+            w.all = w.all && k0 + WQ <= a.len_q;
         }
     };
     if (D < DT) {
@@ -284,13 +289,13 @@ __global__ __launch_bounds__(256, DT == 64 && sizeof(T) == 2 ? 2 : 1) void atten
         const float *lse = a.lse2 + ((int64_t)b * a.heads_q + hq) * a.len_q;
         const float *delta = a.delta + ((int64_t)b * a.heads_q + hq) * a.len_q;
         const ScoreMap sm = score_map(m, hq);
-        // one tile of queries; all: no pair of this wave is masked
-        auto tile = [&](bool all, int stage, int i0) __attribute__((always_inline)) {
-            const uint8_t *qt = smem[stage][0], *gt = smem[stage][1];
+        auto tile = [&](const Visit &at, int stage) __attribute__((always_inline)) {
+            const int i0 = at.tile * BQ + iw;
+            const uint8_t *qt = smem[stage][0] + iw * Lds::kRowBytes, *gt = smem[stage][1] + iw * Lds::kRowBytes;
             const uint32_t qr = Lds::row_base(qt, lane), gr = Lds::row_base(gt, lane);
             const uint32_t qc = Lds::column_base(qt, lane), gc = Lds::column_base(gt, lane);
 #pragma unroll
-            for (int t = 0; t < BQ / 32; ++t) {
+            for (int t = 0; t < WQ / 32; ++t) {
                 v16f z = {}, e = {};
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(qr, t, ks), kf[ks], z);
@@ -300,8 +305,8 @@ __global__ __launch_bounds__(256, DT == 64 && sizeof(T) == 2 ? 2 : 1) void atten
                 const float d0 = (float)(p0 + 4 * h) - (float)j;
 #pragma unroll
                 for (int x4 = 0; x4 < 4; ++x4) {
-                    const v4f l4 = *reinterpret_cast<const v4f *>(&rows[stage][0][32 * t + tile_row(4 * x4, h)]);
-                    const v4f e4 = *reinterpret_cast<const v4f *>(&rows[stage][1][32 * t + tile_row(4 * x4, h)]);
+                    const v4f l4 = *reinterpret_cast<const v4f *>(&rows[stage][0][iw + 32 * t + tile_row(4 * x4, h)]);
+                    const v4f e4 = *reinterpret_cast<const v4f *>(&rows[stage][1][iw + 32 * t + tile_row(4 * x4, h)]);
 #pragma unroll
                     for (int y = 0; y < 4; ++y) {
                         const int r = 4 * x4 + y;
@@ -315,8 +320,8 @@ __global__ __launch_bounds__(256, DT == 64 && sizeof(T) == 2 ? 2 : 1) void atten
                         e[r] = z[r] * (e[r] - e4[y]) * u;
                     }
                 }
-                if (!all) {
-                    const uint32_t w = sight.word(p0, docs ? &doc_of[stage][32 * t] : nullptr) >> (4 * h);
+                if (!at.all) {
+                    const uint32_t w = sight.word(p0, docs ? &doc_of[stage][iw + 32 * t] : nullptr) >> (4 * h);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         z[r] = word_bit(w, r) ? z[r] : 0.f;
@@ -334,17 +339,21 @@ __global__ __launch_bounds__(256, DT == 64 && sizeof(T) == 2 ? 2 : 1) void atten
                 }
             }
         };
-        auto check = [&](int stage, int i0, bool any, bool all) __attribute__((always_inline)) {
+        auto check = [&](const Visit &at, int stage) __attribute__((always_inline)) {
             uint32_t bq[BQ / 32], bg[BQ / 32], some = 0;
             non_finite<Lds, BQ, NW>(smem[stage][0], &found[0][0][0], bq);
             non_finite<Lds, BQ, NW>(smem[stage][1], &found[1][0][0], bg);
 #pragma unroll
-            for (int t = 0; t < BQ / 32; ++t) some |= bq[t] | bg[t];
+            for (int t = 0; t < BQ / 32; ++t) {
+                bq[t] |= bg[t];
+                some |= bq[t];
+            }
             if (!some) return;
 #pragma unroll
-            for (int t = 0; t < BQ / 32; ++t) {
-                const uint32_t w = all ? ~0u : sight.word(i0 + 32 * t + shift, docs ? &doc_of[stage][32 * t] : nullptr);
-                spoilt = spoilt || (any && (w & (bq[t] | bg[t])));
+            for (int t = 0; t < WQ / 32; ++t) {
+                const uint32_t w =
+                    sight.word(at.tile * BQ + iw + 32 * t + shift, docs ? &doc_of[stage][iw + 32 * t] : nullptr);
+                spoilt = spoilt || (at.any && ((at.all ? ~0u : w) & pick<BQ / 32>(bq, NARROW ? wave : t)));
             }
             Lds::template clean<BQ, NW * 64>(smem[stage][0]);
             Lds::template clean<BQ, NW * 64>(smem[stage][1]);
@@ -354,30 +363,32 @@ __global__ __launch_bounds__(256, DT == 64 && sizeof(T) == 2 ? 2 : 1) void atten
         auto fetch = [&](int st, int t) __attribute__((always_inline)) {
             Lds::template load<BQ, NW * 64>(smem[st][0], q, a.q.sl, t * BQ, a.len_q, D);
             Lds::template load<BQ, NW * 64>(smem[st][1], g, a.dout.sl, t * BQ, a.len_q, D);
-            if (wave < 2) load_words64(rows[st][wave], wave ? delta : lse, t * BQ, a.len_q);
-            if (docs && wave == 2) load_words64(doc_of[st], docs, t * BQ + shift, a.len_k);
+            // 64 numbers a wave: lse2 by the first waves, delta by the last
+            constexpr int kW = kWords / 64;
+            if (wave < kW) load_words64(&rows[st][0][64 * wave], lse, t * BQ + 64 * wave, a.len_q);
+            const int w = NW - 1 - wave;
+            if (w < kW) load_words64(&rows[st][1][64 * w], delta, t * BQ + 64 * w, a.len_q);
+            if (docs && wave < kW) load_words64(&doc_of[st][64 * wave], docs, t * BQ + 64 * wave + shift, a.len_k);
         };
-        Schedule sched;
-        int cur = sched.next(end, see), stage = 0;
-        if (cur >= 0) fetch(0, cur);
-        while (cur >= 0) {
-            const bool part = sched.part, any = sched.wave_any, all = sched.wave_all;
-            wait_vmcnt<0>();
-            block_barrier();
-            const int next = sched.next(end, see);
-            if (next >= 0) fetch(stage ^ 1, next);
-            if (part) check(stage, cur * BQ, any, all);
-            if (any) tile(all, stage, cur * BQ);
-            wait_lgkm();
-            cur = next;
-            stage ^= 1;
-        }
+        tile_loop<NS, 2 * kBytes / (NW * 1024)>(end, see, fetch, check, tile);
         block_barrier();           // the next head's first tile takes stage 0
     }
+    if (spoilt) {
+#pragma unroll
+        for (int dt = 0; dt < DS; ++dt) {
+            dk[dt] += __builtin_nanf("");
+            dv[dt] += __builtin_nanf("");
+        }
+    }
+    if constexpr (NARROW) {
+        join_waves<DS>(dk, smem[0][0]);
+        __syncthreads();
+        join_waves<DS>(dv, smem[0][0]);
+        if (wave != 0) return;
+    }
     if (!key) return;
-    const float nan = __builtin_nanf("");
-    store_columns<T, DS>((T *)a.dk.p + b * a.dk.sb + (int64_t)j * a.dk.sl + hk * a.dk.sh, dk, spoilt ? nan : m.scale, h, D);
-    store_columns<T, DS>((T *)a.dv.p + b * a.dv.sb + (int64_t)j * a.dv.sl + hk * a.dv.sh, dv, spoilt ? nan : 1.f, h, D);
+    store_columns<T, DS>((T *)a.dk.p + b * a.dk.sb + (int64_t)j * a.dk.sl + hk * a.dk.sh, dk, m.scale, h, D);
+    store_columns<T, DS>((T *)a.dv.p + b * a.dv.sb + (int64_t)j * a.dv.sl + hk * a.dv.sh, dv, 1.f, h, D);
 }
 
 // The same for bfloat16 with more than 64 dims, where the two accumulators of 32 keys and
@@ -386,12 +397,12 @@ __global__ __launch_bounds__(256, DT == 64 && sizeof(T) == 2 ? 2 : 1) void atten
 // keeps K and dV, forms S and P, and leaves P in LDS; the second keeps V and dK, forms dP and,
 // one tile later, dS.  P passes in the registers' own order (operand fragments), rounded to
 // bfloat16 as the product with dO takes it, and with the cap's derivative multiplied in.
-template <int DT, int MODS>
+template <int DC, int MODS>
 __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const AttentionArgs a)
 {
     typedef __bf16 T;
-    constexpr int BQ = 64, NW = 8, BN = 128, KS = DT / 16, DS = DT / 32;
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2;
+    constexpr int DT = 128, KS = DC / 16, DS = DC / 32, BQ = 64, NW = 8, BN = 128;
     typedef Tile<T, DT> Lds;
     __shared__ __align__(1024) uint8_t smem[3][2][BQ * Lds::kRowBytes];
     __shared__ u4v shared_p[2][4][BQ / 32][2][64];             // [tile parity][keys][rows][half][lane]
@@ -604,27 +615,40 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
     else run(std::false_type{});
 }
 
-template <typename T, int DT, int MODS>
+template <typename T, int DC, int MODS>
 hipError_t launch(const AttentionArgs &a, hipStream_t stream)
 {
-    const int64_t nq = (int64_t)((a.len_q + 127) / 128) * a.heads_q * a.batch;
-    const int64_t nk = (int64_t)((a.len_k + 127) / 128) * a.heads_kv * a.batch;
+    const int64_t hq = (int64_t)a.heads_q * a.batch, hk = (int64_t)a.heads_kv * a.batch;
+    int64_t nq = hq * ((a.len_q + 127) / 128), nk = hk * ((a.len_k + 127) / 128);
+    // 32 rows a workgroup where 128 would leave compute units without one
+    const bool narrow_q = nq < cu_count(), narrow_k = nk < cu_count();
+    if (narrow_q) nq = hq * ((a.len_q + 31) / 32);
+    if (narrow_k) nk = hk * ((a.len_k + 31) / 32);
     if (nq > INT32_MAX || nk > INT32_MAX) return hipErrorInvalidConfiguration;
-    if constexpr (sizeof(T) == 2 && DT == 128) attention_dkv_pair_kernel<DT, MODS><<<(uint32_t)nk, 512, 0, stream>>>(a);
-    else attention_dkv_kernel<T, DT, MODS><<<(uint32_t)nk, 256, 0, stream>>>(a);
-    attention_dq_kernel<T, DT, MODS><<<(uint32_t)nq, 256, 0, stream>>>(a);
+    if (narrow_k) attention_dkv_kernel<T, DC, MODS, true><<<(uint32_t)nk, 256, 0, stream>>>(a);
+    else if constexpr (sizeof(T) == 2 && DC > 64) attention_dkv_pair_kernel<DC, MODS><<<(uint32_t)nk, 512, 0, stream>>>(a);
+    else attention_dkv_kernel<T, DC, MODS, false><<<(uint32_t)nk, 256, 0, stream>>>(a);
+    if (narrow_q) attention_dq_kernel<T, DC, MODS, true><<<(uint32_t)nq, 256, 0, stream>>>(a);
+    else attention_dq_kernel<T, DC, MODS, false><<<(uint32_t)nq, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, int DT>
+template <typename T, int DC>
 hipError_t launch_mods(const AttentionArgs &a, hipStream_t stream)
 {
     switch ((a.mask.cap > 0.f ? 1 : 0) | (a.mask.slopes ? 2 : 0)) {
-    case 0: return launch<T, DT, 0>(a, stream);
-    case 1: return launch<T, DT, 1>(a, stream);
-    case 2: return launch<T, DT, 2>(a, stream);
-    default: return launch<T, DT, 3>(a, stream);
+    case 0: return launch<T, DC, 0>(a, stream);
+    case 1: return launch<T, DC, 1>(a, stream);
+    case 2: return launch<T, DC, 2>(a, stream);
+    default: return launch<T, DC, 3>(a, stream);
     }
+}
+
+template <typename T>
+hipError_t launch_dims(const AttentionArgs &a, hipStream_t stream)
+{
+    if (a.dim <= 64) return launch_mods<T, 64>(a, stream);
+    return a.dim <= 96 ? launch_mods<T, 96>(a, stream) : launch_mods<T, 128>(a, stream);
 }
 
 }  // namespace
@@ -649,8 +673,7 @@ hipError_t launch_attention_bwd(const AttentionArgs &a, bool f32, hipStream_t st
     else attention_delta_kernel<__bf16><<<(uint32_t)rows, 256, 0, stream>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (f32) return a.dim <= 64 ? launch_mods<float, 64>(a, stream) : launch_mods<float, 128>(a, stream);
-    return a.dim <= 64 ? launch_mods<__bf16, 64>(a, stream) : launch_mods<__bf16, 128>(a, stream);
+    return f32 ? launch_dims<float>(a, stream) : launch_dims<__bf16>(a, stream);
 }
 
 }  // namespace q2d

@@ -298,9 +298,19 @@ __device__ __forceinline__ void non_finite(const uint8_t *t, uint32_t *words, ui
     }
 }
 
+// word t of `bad` where t is the same in all lanes but not a constant
+template <int N>
+__device__ __forceinline__ uint32_t pick(const uint32_t *bad, int t)
+{
+    uint32_t w = bad[0];
+#pragma unroll
+    for (int x = 1; x < N; ++x) w = t == x ? bad[x] : w;
+    return w;
+}
+
 // acc (rows d, column n) += the infinities and NaN of X's 32 rows from r0 that column n sees
 // (bits of `seen`), times weights above zero: a count of them by matrix products
-template <typename T, int DT>
+template <typename T, int DC, int DT>
 __device__ __forceinline__ void add_non_finite(v16f *acc, uint32_t seen, uint32_t column_base, int r0, int h)
 {
     const uint32_t bits = seen >> (4 * h);
@@ -310,7 +320,7 @@ __device__ __forceinline__ void add_non_finite(v16f *acc, uint32_t seen, uint32_
 #pragma unroll
         for (int j = 0; j < 8; ++j) ones[j] = ((bits >> tile_row(8 * s + j, 0)) & 1) ? 1.f : 0.f;
 #pragma unroll
-        for (int dt = 0; dt < DT / 32; ++dt) {
+        for (int dt = 0; dt < DC / 32; ++dt) {
             __builtin_amdgcn_sched_barrier(0);           // one tile at a time: registers, not speed
             const Frag<T> x = Tile<T, DT>::column_frag(column_base, r0 + 16 * s, dt);
             Frag<T> up, down;
@@ -368,6 +378,13 @@ __device__ __forceinline__ Seen classify(const AttentionMask &m, int prefix, int
     return {any, all && any};
 }
 
+// A visited tile (-1: none): whether some pair of the workgroup is masked, whether this wave
+// sees some and all pairs
+struct Visit {
+    int tile;
+    bool part, any, all;
+};
+
 // Tiles of one loop axis that a workgroup visits, 64 at a time: lane t classifies tile
 // base + t, and ballots hold what the workgroup and this wave see of them.
 struct Schedule {
@@ -376,6 +393,7 @@ struct Schedule {
     // of the tile that next() gave: whether some pair of the workgroup is masked, whether this
     // wave sees some and all pairs
     bool part = false, wave_any = false, wave_all = false;
+
 
     // next visited tile below `end`, or -1 (the same in all waves); f(tile) -> {of the
     // workgroup, of this wave}
@@ -400,7 +418,91 @@ struct Schedule {
         wave_all = (all >> b) & 1;
         return base + b;
     }
+    template <typename F>
+    __device__ __forceinline__ Visit take(int end, F &&f)
+    {
+        const int t = next(end, f);
+        return {t, part, wave_any, wave_all};
+    }
 };
+
+// LDS stages of a tile loop for tiles of so many bytes (both operands): three where they leave
+// room for two workgroups a compute unit, two, or one
+constexpr int stages_of(int bytes) { return 3 * bytes <= 49152 ? 3 : 2 * bytes <= 131072 ? 2 : 1; }
+
+// The loop over a workgroup's tiles: body(visit, stage) on each visited one, with fetch(stage,
+// tile) two tiles ahead where there are three stages, one ahead with two, and after use with
+// one; check(visit, stage) where some pair is masked.  LOADS: a thread's loads of a tile, at
+// least.  Ends with no load under way, but without a barrier.
+template <int NS, int LOADS, typename See, typename Fetch, typename Check, typename Body>
+__device__ __forceinline__ void tile_loop(int end, See &&see, Fetch &&fetch, Check &&check, Body &&body)
+{
+    Schedule sched;
+    Visit cur = sched.take(end, see), next = {};
+    int stage = 0;
+    if (cur.tile >= 0) {
+        fetch(0, cur.tile);
+        if constexpr (NS == 3) {
+            next = sched.take(end, see);
+            if (next.tile >= 0) fetch(1, next.tile);
+        }
+    }
+    while (cur.tile >= 0) {
+        if (NS == 3 && next.tile >= 0) wait_vmcnt<LOADS>();
+        else wait_vmcnt<0>();
+        block_barrier();
+        const Visit ahead = NS == 3 && next.tile < 0 ? next : sched.take(end, see);
+        if (NS > 1 && ahead.tile >= 0) fetch(NS == 3 ? (stage == 0 ? 2 : stage - 1) : stage ^ 1, ahead.tile);
+        if (cur.part) check(cur, stage);
+        if (cur.any) body(cur, stage);
+        wait_lgkm();
+        if constexpr (NS == 3) {
+            cur = next;
+            next = ahead;
+            stage = stage == 2 ? 0 : stage + 1;
+        } else {
+            if (NS == 1 && ahead.tile >= 0) {
+                block_barrier();
+                fetch(0, ahead.tile);
+            }
+            cur = ahead;
+            stage = NS == 1 ? 0 : stage ^ 1;
+        }
+    }
+}
+
+// Sum over the four waves of a workgroup of accumulators x (N tiles), left in wave 0; buf: LDS
+// of 2 x N x 4096 bytes, which no wave still reads
+template <int N>
+__device__ __forceinline__ void join_waves(v16f *x, uint8_t *buf)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    v4f *at = reinterpret_cast<v4f *>(buf) + lane;
+    auto put = [&](int k) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                at[((k * N + n) * 4 + g) * 64] = v4f{x[n][4 * g], x[n][4 * g + 1], x[n][4 * g + 2], x[n][4 * g + 3]};
+    };
+    auto add = [&](int k) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const v4f v = at[((k * N + n) * 4 + g) * 64];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[n][4 * g + i] += v[i];
+            }
+    };
+    if (wave >= 2) put(wave - 2);
+    __syncthreads();
+    if (wave < 2) add(wave);
+    __syncthreads();
+    if (wave == 1) put(0);
+    __syncthreads();
+    if (wave == 0) add(0);
+}
 
 // Which of 32 neighbouring positions of the other side one position sees: bit r for position
 // base + r.  Positions in [lo, hi) are seen, and on the queries' side those below the prefix.

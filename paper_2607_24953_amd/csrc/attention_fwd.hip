@@ -11,16 +11,23 @@ namespace q2d {
 
 namespace {
 
-// MODS bit 0: capped scores, bit 1: distance bias
-template <typename T, int DT, int MODS, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const AttentionArgs a)
+// MODS bit 0: capped scores, bit 1: distance bias.  A workgroup of four waves owns 128
+// queries and its waves share tiles of 64 (float32: 32) keys; or (NARROW) 32 queries, and
+// each wave takes its quarter of tiles of 128 keys.
+template <typename T, int DC, int MODS, bool NARROW>
+__global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 3 : NARROW ? 1 : 2)
+void attention_fwd_kernel(const AttentionArgs a)
 {
-    constexpr int BN = sizeof(T) == 2 ? 64 : 32, BM = 32 * NW, KS = DT / 16, DS = DT / 32;
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2, F32 = sizeof(T) == 4;
+    // DC dims are computed (a multiple of 32, dim rounded up), DT lie in an LDS row
+    constexpr int DT = DC <= 64 ? 64 : 128, KS = DC / 16, DS = DC / 32;
+    constexpr int NW = 4, BM = NARROW ? 32 : 32 * NW, BN = NARROW ? 32 * NW : F32 ? 32 : 64, WN = NARROW ? 32 : BN;
     typedef Tile<T, DT> Lds;
-    __shared__ __align__(1024) uint8_t smem[2][2][BN * Lds::kRowBytes];
-    __shared__ __align__(16) int32_t doc_of[2][64];            // documents of a tile's keys
+    constexpr int kBytes = BN * Lds::kRowBytes, NS = stages_of(2 * kBytes);
+    __shared__ __align__(1024) uint8_t smem[NS][2][kBytes];
+    __shared__ __align__(16) int32_t doc_of[NS][BN < 64 ? 64 : BN];   // documents of a tile's keys
     __shared__ uint32_t found[NW][BN / 32];                    // rows with infinities and NaN
+    __shared__ float stat[2][NW][32];                          // maxima and sums of the waves
 
     const AttentionMask &m = a.mask;
     const uint32_t tiles = (a.len_q + BM - 1) / BM;
@@ -31,7 +38,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, col = lane & 31;
     const int shift = a.len_k - a.len_q, D = a.dim;
-    const int i0 = qt * BM, iw = i0 + wave * 32, i = iw + col;
+    const int i0 = qt * BM, iw = NARROW ? i0 : i0 + wave * 32, i = iw + col;
+    const int jw = NARROW ? 32 * wave : 0;                     // the wave's first key of a tile
     const int p = i + shift;
     const bool row = i < a.len_q;
 
@@ -60,16 +68,14 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
 
     int end = (a.len_k + BN - 1) / BN;
     if (m.causal && !m.prefix) end = p1 < 0 ? 0 : min(end, p1 / BN + 1);
-    auto see = [&](int t, Seen &g, Seen &w) {
-        const int j0 = t * BN, j1 = min(j0 + BN, a.len_k) - 1;
-        const Documents dk = docs ? range_of(ranges, j0, j0) : Documents{};
-        g = classify(m, prefix, p0, p1, j0, j1, dg, dk);
-        if (pw1 >= pw0) {
-            w = classify(m, prefix, pw0, pw1, j0, j1, dw, dk);
-            w.all = w.all && j0 + BN <= a.len_k;
+    auto see = [&](int t, Seen &g, Seen &w) __attribute__((always_inline)) {
+        const int j0 = t * BN, j1 = min(j0 + BN, a.len_k) - 1, k0 = j0 + jw, k1 = min(k0 + WN, a.len_k) - 1;
+        g = classify(m, prefix, p0, p1, j0, j1, dg, docs ? range_of(ranges, j0, j1) : Documents{});
+        if (pw1 >= pw0 && k1 >= k0) {
+            w = classify(m, prefix, pw0, pw1, k0, k1, dw, docs ? range_of(ranges, k0, k1) : Documents{});
+            w.all = w.all && k0 + WN <= a.len_k;
         }
     };
-
     if (D < DT) {
         Lds::template clear<NW * 64>(smem[0][0], sizeof(smem));
         __syncthreads();
@@ -77,19 +83,19 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
     v16f o[DS] = {};
     float mx = -INFINITY, sum = 0.f;
 
-    // one tile of keys; all: no pair of this wave is masked
-    auto tile = [&](bool all, int stage, int j0) __attribute__((always_inline)) {
-        const uint8_t *kt = smem[stage][0], *vt = smem[stage][1];
-        const uint32_t kr = Lds::row_base(kt, lane), vc = Lds::column_base(vt, lane);
-        v16f z[BN / 32] = {};
+    auto tile = [&](const Visit &at, int stage) __attribute__((always_inline)) {
+        const int j0 = at.tile * BN + jw;
+        const uint32_t kr = Lds::row_base(smem[stage][0] + jw * Lds::kRowBytes, lane);
+        const uint32_t vc = Lds::column_base(smem[stage][1] + jw * Lds::kRowBytes, lane);
+        v16f z[WN / 32] = {};
 #pragma unroll
-        for (int t = 0; t < BN / 32; ++t)
+        for (int t = 0; t < WN / 32; ++t)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) z[t] = mma(Lds::row_frag(kr, t, ks), qf[ks], z[t]);
         if constexpr (CAP || BIAS) {
             const float d0 = pos - (float)j0 - (float)(4 * h);
 #pragma unroll
-            for (int t = 0; t < BN / 32; ++t)
+            for (int t = 0; t < WN / 32; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     float x = z[t][r];
@@ -98,17 +104,17 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
                     z[t][r] = x;
                 }
         }
-        if (!all) {
+        if (!at.all) {
 #pragma unroll
-            for (int t = 0; t < BN / 32; ++t) {
-                const uint32_t w = sight.word(j0 + 32 * t, docs ? &doc_of[stage][32 * t] : nullptr) >> (4 * h);
+            for (int t = 0; t < WN / 32; ++t) {
+                const uint32_t w = sight.word(j0 + 32 * t, docs ? &doc_of[stage][jw + 32 * t] : nullptr) >> (4 * h);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) z[t][r] = word_bit(w, r) ? z[t][r] : -INFINITY;
             }
         }
         float top = z[0][0];
 #pragma unroll
-        for (int t = 0; t < BN / 32; ++t)
+        for (int t = 0; t < WN / 32; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, z[t][r]);
         top = fmaxf(top, __shfl_xor(top, 32));
@@ -116,7 +122,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
         // 8 above it are as good, and most tiles leave the sums as they are.
         if (__any(top > mx + thr)) {
             const float now = fmaxf(mx, top);
-            const float f = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx - now) * sm.c);
+            const float f = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mx - now) * sm.c);
 #pragma unroll
             for (int dt = 0; dt < DS; ++dt) o[dt] *= f;
             sum *= f;
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
         const float base = mx == -INFINITY ? 0.f : mx;
         const float off = -base * sm.c;
 #pragma unroll
-        for (int t = 0; t < BN / 32; ++t)
+        for (int t = 0; t < WN / 32; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const float e = F32 ? (z[t][r] - base) * sm.c : fmaf(z[t][r], sm.c, off);
@@ -133,7 +139,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
                 sum += z[t][r];
             }
 #pragma unroll
-        for (int t = 0; t < BN / 32; ++t)
+        for (int t = 0; t < WN / 32; ++t)
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const Frag<T> pf = to_frag<T>(z[t], s);
@@ -142,45 +148,54 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
                     o[dt] = mma(Lds::column_frag(vc, 32 * t + 16 * s, dt), pf, o[dt]);
             }
     };
-    auto check = [&](int stage, int j0, bool any, bool all) __attribute__((always_inline)) {
-        uint32_t bad[BN / 32];
+    auto check = [&](const Visit &at, int stage) __attribute__((always_inline)) {
+        uint32_t bad[BN / 32], some = 0;
         non_finite<Lds, BN, NW>(smem[stage][1], &found[0][0], bad);
-        uint32_t some = 0;
 #pragma unroll
         for (int t = 0; t < BN / 32; ++t) some |= bad[t];
         if (!some) return;
-        if (any) {
-            const uint32_t vc = Lds::column_base(smem[stage][1], lane);
+        if (at.any) {
+            const uint32_t vc = Lds::column_base(smem[stage][1] + jw * Lds::kRowBytes, lane);
 #pragma unroll 1
-            for (int t = 0; t < BN / 32; ++t)
-                add_non_finite<T, DT>(o, all ? ~0u : sight.word(j0 + 32 * t, docs ? &doc_of[stage][32 * t] : nullptr), vc,
-                                      32 * t, h);
+            for (int t = 0; t < WN / 32; ++t) {
+                const uint32_t w = sight.word(at.tile * BN + jw + 32 * t, docs ? &doc_of[stage][jw + 32 * t] : nullptr);
+                add_non_finite<T, DC, DT>(o, at.all ? ~0u : w, vc, 32 * t, h);
+            }
         }
         Lds::template clean<BN, NW * 64>(smem[stage][1]);
     };
     auto fetch = [&](int stage, int t) __attribute__((always_inline)) {
         Lds::template load<BN, NW * 64>(smem[stage][0], k, a.k.sl, t * BN, a.len_k, D);
         Lds::template load<BN, NW * 64>(smem[stage][1], v, a.v.sl, t * BN, a.len_k, D);
-        if (docs && wave == 0) load_words64(doc_of[stage], docs, t * BN, a.len_k);
+        if (docs && wave < (BN + 63) / 64) load_words64(&doc_of[stage][64 * wave], docs, t * BN + 64 * wave, a.len_k);
     };
-
-    Schedule sched;
-    int cur = sched.next(end, see), stage = 0;
-    if (cur >= 0) fetch(0, cur);
-    while (cur >= 0) {
-        const bool part = sched.part, any = sched.wave_any, all = sched.wave_all;
-        wait_vmcnt<0>();
-        block_barrier();
-        const int next = sched.next(end, see);
-        if (next >= 0) fetch(stage ^ 1, next);
-        if (part) check(stage, cur * BN, any, all);
-        if (any) tile(all, stage, cur * BN);
-        wait_lgkm();
-        cur = next;
-        stage ^= 1;
-    }
+    tile_loop<NS, 2 * kBytes / (NW * 1024)>(end, see, fetch, check, tile);
 
     sum += __shfl_xor(sum, 32);
+    if constexpr (NARROW) {
+        // the four waves' rows on a common maximum
+        if (h == 0) {
+            stat[0][wave][col] = mx;
+            stat[1][wave][col] = sum;
+        }
+        __syncthreads();                       // (and no wave reads a tile any more)
+        float most = -INFINITY, total = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) most = fmaxf(most, stat[0][w][col]);
+        auto weight = [&](float x, float l) {
+            // (a sum of nothing counts 0, one that is NaN stays)
+            return l == 0.f ? 0.f : x == most ? 1.f : __builtin_amdgcn_exp2f((x - most) * sm.c);
+        };
+#pragma unroll
+        for (int w = 0; w < NW; ++w) total += weight(stat[0][w][col], stat[1][w][col]) * stat[1][w][col];
+        const float f = weight(mx, sum);
+#pragma unroll
+        for (int dt = 0; dt < DS; ++dt) o[dt] *= f;
+        join_waves<DS>(o, smem[0][0]);
+        if (wave != 0) return;
+        mx = most;
+        sum = total;
+    }
     if (!row) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T *out = (T *)a.out.p + b * a.out.sb + (int64_t)i * a.out.sl + hq * a.out.sh;
@@ -190,24 +205,35 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_fwd_kernel(const Attenti
             sum == 0.f ? -INFINITY : (mx * sm.c + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-template <typename T, int DT, int MODS, int NW>
+template <typename T, int DC, int MODS>
 hipError_t launch(const AttentionArgs &a, hipStream_t stream)
 {
-    const int64_t n = (int64_t)((a.len_q + 32 * NW - 1) / (32 * NW)) * a.heads_q * a.batch;
-    if (n > INT32_MAX) return hipErrorInvalidConfiguration;
-    attention_fwd_kernel<T, DT, MODS, NW><<<(uint32_t)n, NW * 64, 0, stream>>>(a);
+    const int64_t heads = (int64_t)a.heads_q * a.batch, n = heads * ((a.len_q + 127) / 128);
+    // 32 rows a workgroup where 128 would leave compute units without one
+    const bool narrow = n < cu_count();
+    const int64_t grid = narrow ? heads * ((a.len_q + 31) / 32) : n;
+    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (narrow) attention_fwd_kernel<T, DC, MODS, true><<<(uint32_t)grid, 256, 0, stream>>>(a);
+    else attention_fwd_kernel<T, DC, MODS, false><<<(uint32_t)grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, int DT>
+template <typename T, int DC>
 hipError_t launch_mods(const AttentionArgs &a, hipStream_t stream)
 {
     switch ((a.mask.cap > 0.f ? 1 : 0) | (a.mask.slopes ? 2 : 0)) {
-    case 0: return launch<T, DT, 0, 4>(a, stream);
-    case 1: return launch<T, DT, 1, 4>(a, stream);
-    case 2: return launch<T, DT, 2, 4>(a, stream);
-    default: return launch<T, DT, 3, 4>(a, stream);
+    case 0: return launch<T, DC, 0>(a, stream);
+    case 1: return launch<T, DC, 1>(a, stream);
+    case 2: return launch<T, DC, 2>(a, stream);
+    default: return launch<T, DC, 3>(a, stream);
     }
+}
+
+template <typename T>
+hipError_t launch_dims(const AttentionArgs &a, hipStream_t stream)
+{
+    if (a.dim <= 64) return launch_mods<T, 64>(a, stream);
+    return a.dim <= 96 ? launch_mods<T, 96>(a, stream) : launch_mods<T, 128>(a, stream);
 }
 
 }  // namespace
@@ -218,8 +244,7 @@ hipError_t launch_attention_fwd(const AttentionArgs &a, bool f32, hipStream_t st
         const hipError_t e = launch_document_ranges(a, stream);
         if (e != hipSuccess) return e;
     }
-    if (f32) return a.dim <= 64 ? launch_mods<float, 64>(a, stream) : launch_mods<float, 128>(a, stream);
-    return a.dim <= 64 ? launch_mods<__bf16, 64>(a, stream) : launch_mods<__bf16, 128>(a, stream);
+    return f32 ? launch_dims<float>(a, stream) : launch_dims<__bf16>(a, stream);
 }
 
 }  // namespace q2d

@@ -143,6 +143,23 @@ def test_masks(q2d, name, D, dtype):
     check(q2d, *make(2, 250, 250, 4, 2, D, dtype, seed=3), **MASKS[name])
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("name", ["cap", "slopes", "window_full", "prefix_wide", "documents", "documents_prefix", "all"])
+def test_masks_of_many_heads(q2d, name, D, dtype):
+    """The kernels whose workgroups own 128 rows: as many heads as give each compute unit one."""
+    mask = dict(MASKS[name])
+    if "slopes" in mask:
+        mask["slopes"] = mask["slopes"].repeat(16)
+    check(q2d, *make(2, 250, 250, 64, 64, D, dtype, seed=12), **mask)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(4, 140, 140, 64, 32, 72), (8, 64, 300, 32, 32, 128), (4, 300, 65, 32, 32, 40)], ids=str)
+def test_shapes_of_many_heads(q2d, shape, dtype):
+    check(q2d, *make(*shape, dtype, seed=13))
+
+
 @pytest.mark.parametrize("Lq", [1, 90])
 @pytest.mark.parametrize("name", ["documents", "documents_prefix", "prefix", "window", "slopes"])
 def test_masks_of_last_queries(q2d, name, Lq):
@@ -173,11 +190,12 @@ def test_large_scores(q2d):
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("fill", [math.inf, math.nan])
-def test_unseen_non_finite(q2d, fill, D, dtype):
+@pytest.mark.parametrize("B,H", [(1, 2), (2, 64)], ids=["few heads", "many heads"])
+def test_unseen_non_finite(q2d, B, H, fill, D, dtype):
     """Infinities and NaN in padding, and in keys that only later queries see."""
-    B, L, H = 1, 150, 2
+    L = 150
     q, k, v, dout = make(B, L, L, H, H, D, dtype, seed=8)
-    docs = torch.tensor([[0] * 60 + [-1] * 20 + [1] * 70], dtype=torch.int32)
+    docs = torch.tensor([[0] * 60 + [-1] * 20 + [1] * 70] * B, dtype=torch.int32)
     clean = check(q2d, q, k, v, dout, documents=docs)
     bad = [t.clone() for t in (q, k, v, dout)]
     for t in bad:
