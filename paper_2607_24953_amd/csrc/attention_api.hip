@@ -83,9 +83,15 @@ int64_t ranges_bytes(const q2d_attention *a)
 
 int64_t rows_bytes(const q2d_attention *a) { return up256((int64_t)a->batch * a->heads_q * a->len_q * 4); }
 
+int64_t part_bytes(const q2d_attention *a)
+{
+    const int n = dkv_splits(a->batch, a->len_q, a->len_k, a->heads_q, a->heads_kv, a->documents != nullptr);
+    return n > 1 ? up256((int64_t)n * a->batch * a->len_k * a->heads_kv * a->dim * 8) : 0;
+}
+
 int64_t workspace_of(const q2d_attention *a, bool backward)
 {
-    return ranges_bytes(a) + (backward ? 2 * rows_bytes(a) : 0);
+    return ranges_bytes(a) + (backward ? 2 * rows_bytes(a) + part_bytes(a) : 0);
 }
 
 AttentionArgs make_args(const q2d_attention *a, void *workspace)
@@ -97,6 +103,8 @@ AttentionArgs make_args(const q2d_attention *a, void *workspace)
     r.delta = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + ranges_bytes(a));
     r.lse2 = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(r.delta) + rows_bytes(a));
     r.mask.causal = a->causal;
+    r.part = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(r.lse2) + rows_bytes(a));
+    r.splits = dkv_splits(a->batch, a->len_q, a->len_k, a->heads_q, a->heads_kv, a->documents != nullptr);
     // (no distance reaches 2^30)
     r.mask.window = (int32_t)(a->window > kMaxLen ? kMaxLen : a->window);
     r.mask.scale = a->scale; r.mask.cap = a->softcap;

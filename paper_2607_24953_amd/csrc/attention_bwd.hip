@@ -214,6 +214,39 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
 
 // ---------------------------------------------------------------- dK, dV
 
+// One key's dK or dV: the gradient itself, or a split's part of it
+template <typename T, int DS>
+__device__ __forceinline__ void store_dkv(const AttentionArgs &a, bool dv, int split, int b, int j, int hk, const v16f *x, int h)
+{
+    if (a.splits > 1) {
+        const int64_t at = ((((int64_t)(dv ? a.splits : 0) + split) * a.batch + b) * a.len_k + j) * a.heads_kv + hk;
+        store_columns<float, DS>(a.part + at * a.dim, x, 1.f, h, a.dim);
+        return;
+    }
+    const HeadsView &to = dv ? a.dv : a.dk;
+    store_columns<T, DS>((T *)to.p + b * to.sb + (int64_t)j * to.sl + hk * to.sh, x, dv ? 1.f : a.mask.scale, h, a.dim);
+}
+
+// Sums the splits' parts in order: 4 neighbouring dims a thread
+template <typename T>
+__global__ __launch_bounds__(256) void attention_dkv_sum_kernel(const AttentionArgs a)
+{
+    const int64_t rows = (int64_t)a.batch * a.len_k * a.heads_kv, n = rows * (a.dim / 4);
+    int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (x >= 2 * n) return;
+    const bool dv = x >= n;
+    x -= dv ? n : 0;
+    const float *p = a.part + (dv ? (int64_t)a.splits * n * 4 : 0) + x * 4;
+    v4f sum = *reinterpret_cast<const v4f *>(p);
+    for (int s = 1; s < a.splits; ++s) sum += *reinterpret_cast<const v4f *>(p + (int64_t)s * n * 4);
+    const int d = (int)(x % (a.dim / 4)) * 4;
+    const int64_t r = x / (a.dim / 4);
+    const int hk = (int)(r % a.heads_kv), j = (int)(r / a.heads_kv % a.len_k), b = (int)(r / a.heads_kv / a.len_k);
+    const HeadsView &to = dv ? a.dv : a.dk;
+    const float f = dv ? 1.f : a.mask.scale;
+    store4((T *)to.p + b * to.sb + (int64_t)j * to.sl + hk * to.sh + d, sum[0] * f, sum[1] * f, sum[2] * f, sum[3] * f);
+}
+
 // A workgroup of four waves owns 128 keys and its waves share tiles of 64 (float32: 32)
 // queries; or (NARROW) 32 keys, and each wave takes its quarter of tiles of 128 queries.
 template <typename T, int DC, int MODS, bool NARROW>
@@ -234,7 +267,10 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
     const uint32_t tiles = (a.len_k + BN - 1) / BN;
     uint32_t head, kt;
     head_tile(blockIdx.x, gridDim.x, tiles, head, kt);
-    const int b = head / a.heads_kv, hk = head % a.heads_kv, group = a.heads_q / a.heads_kv;
+    const int split = head % a.splits, b = head / a.splits / a.heads_kv, hk = head / a.splits % a.heads_kv;
+    // this workgroup's query heads [first, last) of those that share the key head
+    const int group = a.heads_q / a.heads_kv, each = (group + a.splits - 1) / a.splits;
+    const int first = split * each, last = min(first + each, group);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, col = lane & 31;
     const int shift = a.len_k - a.len_q, D = a.dim;
@@ -282,7 +318,7 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
     }
     v16f dk[DS] = {}, dv[DS] = {};
     bool spoilt = false;                // an infinity or a NaN among the queries that see this key
-    for (int gh = 0; gh < group; ++gh) {
+    for (int gh = first; gh < last; ++gh) {
         const int hq = hk * group + gh;
         const T *q = (const T *)a.q.p + b * a.q.sb + hq * a.q.sh;
         const T *g = (const T *)a.dout.p + b * a.dout.sb + hq * a.dout.sh;
@@ -387,8 +423,8 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
         if (wave != 0) return;
     }
     if (!key) return;
-    store_columns<T, DS>((T *)a.dk.p + b * a.dk.sb + (int64_t)j * a.dk.sl + hk * a.dk.sh, dk, m.scale, h, D);
-    store_columns<T, DS>((T *)a.dv.p + b * a.dv.sb + (int64_t)j * a.dv.sl + hk * a.dv.sh, dv, 1.f, h, D);
+    store_dkv<T, DS>(a, false, split, b, j, hk, dk, h);
+    store_dkv<T, DS>(a, true, split, b, j, hk, dv, h);
 }
 
 // The same for bfloat16 with more than 64 dims, where the two accumulators of 32 keys and
@@ -414,7 +450,10 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
     const uint32_t tiles = (a.len_k + BN - 1) / BN;
     uint32_t head, kt;
     head_tile(blockIdx.x, gridDim.x, tiles, head, kt);
-    const int b = head / a.heads_kv, hk = head % a.heads_kv, group = a.heads_q / a.heads_kv;
+    const int split = head % a.splits, b = head / a.splits / a.heads_kv, hk = head / a.splits % a.heads_kv;
+    // this workgroup's query heads [first, last) of those that share the key head
+    const int group = a.heads_q / a.heads_kv, each = (group + a.splits - 1) / a.splits;
+    const int first = split * each, last = min(first + each, group);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool second = wave >= 4;
     const int keys = wave & 3;
@@ -461,10 +500,10 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
     // the visited tiles of all query heads, in order
     struct At { int tile, head; bool part, any, all; };
     Schedule sched;
-    int gh = 0;
+    int gh = first;
     auto advance = [&]() __attribute__((always_inline)) {
         int t = sched.next(end, see);
-        while (t < 0 && ++gh < group) {
+        while (t < 0 && ++gh < last) {
             sched = Schedule();
             t = sched.next(end, see);
         }
@@ -607,9 +646,11 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
             parity ^= 1;
         }
         if (!key) return;
-        const HeadsView &to = SECOND ? a.dk : a.dv;
-        store_columns<T, DS>((T *)to.p + b * to.sb + (int64_t)j * to.sl + hk * to.sh, acc,
-                             spoilt ? __builtin_nanf("") : SECOND ? m.scale : 1.f, h, D);
+        if (spoilt) {
+#pragma unroll
+            for (int dt = 0; dt < DS; ++dt) acc[dt] += __builtin_nanf("");
+        }
+        store_dkv<T, DS>(a, !SECOND, split, b, j, hk, acc, h);
     };
     if (second) run(std::true_type{});
     else run(std::false_type{});
@@ -618,16 +659,21 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
 template <typename T, int DC, int MODS>
 hipError_t launch(const AttentionArgs &a, hipStream_t stream)
 {
-    const int64_t hq = (int64_t)a.heads_q * a.batch, hk = (int64_t)a.heads_kv * a.batch;
+    const int64_t hq = (int64_t)a.heads_q * a.batch, hk = (int64_t)a.heads_kv * a.batch * a.splits;
     int64_t nq = hq * ((a.len_q + 127) / 128), nk = hk * ((a.len_k + 127) / 128);
     // 32 rows a workgroup where 128 would leave compute units without one
-    const bool narrow_q = nq < cu_count(), narrow_k = nk < cu_count();
+    const bool narrow_q = nq < kComputeUnits, narrow_k = nk < kComputeUnits;
     if (narrow_q) nq = hq * ((a.len_q + 31) / 32);
     if (narrow_k) nk = hk * ((a.len_k + 31) / 32);
     if (nq > INT32_MAX || nk > INT32_MAX) return hipErrorInvalidConfiguration;
     if (narrow_k) attention_dkv_kernel<T, DC, MODS, true><<<(uint32_t)nk, 256, 0, stream>>>(a);
     else if constexpr (sizeof(T) == 2 && DC > 64) attention_dkv_pair_kernel<DC, MODS><<<(uint32_t)nk, 512, 0, stream>>>(a);
     else attention_dkv_kernel<T, DC, MODS, false><<<(uint32_t)nk, 256, 0, stream>>>(a);
+    if (a.splits > 1) {
+        const int64_t n = (int64_t)a.batch * a.len_k * a.heads_kv * (a.dim / 4) * 2;
+        if ((n + 255) / 256 > INT32_MAX) return hipErrorInvalidConfiguration;
+        attention_dkv_sum_kernel<T><<<(uint32_t)((n + 255) / 256), 256, 0, stream>>>(a);
+    }
     if (narrow_q) attention_dq_kernel<T, DC, MODS, true><<<(uint32_t)nq, 256, 0, stream>>>(a);
     else attention_dq_kernel<T, DC, MODS, false><<<(uint32_t)nq, 256, 0, stream>>>(a);
     return hipGetLastError();

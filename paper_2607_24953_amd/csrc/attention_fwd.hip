@@ -210,7 +210,7 @@ hipError_t launch(const AttentionArgs &a, hipStream_t stream)
 {
     const int64_t heads = (int64_t)a.heads_q * a.batch, n = heads * ((a.len_q + 127) / 128);
     // 32 rows a workgroup where 128 would leave compute units without one
-    const bool narrow = n < cu_count();
+    const bool narrow = n < kComputeUnits;
     const int64_t grid = narrow ? heads * ((a.len_q + 31) / 32) : n;
     if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
     if (narrow) attention_fwd_kernel<T, DC, MODS, true><<<(uint32_t)grid, 256, 0, stream>>>(a);
