@@ -95,7 +95,7 @@ struct CachedArgs {
     AttentionMask mask;
     int32_t heads_q;
     int32_t splits;                              // parts of a sequence's tokens
-    int32_t wide;                                // 64 query rows a workgroup, not 16
+    int32_t wide;                                // 128 query rows a workgroup, not 16
     int64_t tiles;                               // bound of the query tiles of all sequences
     float *part;                                 // workspace: [tile][head][split][rows][dim] sums,
     float *stat;                                 // [tile][head][split][rows] maximum and sum

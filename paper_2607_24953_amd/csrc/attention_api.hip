@@ -182,7 +182,7 @@ struct CachedSplit {
     int64_t tiles, stat_at, bytes;
 };
 
-// Query tiles of 16 rows where the sequences have no more on average (decoding), of 64
+// Query tiles of 16 rows where the sequences have no more on average (decoding), of 128
 // otherwise; and enough parts of the sequences' tokens to give each compute unit a few
 // workgroups, none below four super-blocks of 64 tokens, one a wave.
 CachedSplit split_cached(const q2d_kv_cache *c, const q2d_sequences *s, int32_t heads_q)
@@ -190,7 +190,7 @@ CachedSplit split_cached(const q2d_kv_cache *c, const q2d_sequences *s, int32_t 
     CachedSplit p;
     const int64_t group = heads_q / c->heads;
     p.wide = s->tokens * group > 16 * (int64_t)s->batch;
-    const int64_t rows = p.wide ? 64 : 16;
+    const int64_t rows = p.wide ? 128 : 16;
     if (s->offsets) {
         const int64_t some = s->tokens < s->batch ? s->tokens : s->batch, each = s->tokens * ((group + rows - 1) / rows);
         p.tiles = s->tokens * group / rows + some;
@@ -319,6 +319,7 @@ q2d_status q2d_attention_cached(const q2d_kv_cache *c, const q2d_sequences *s, c
     if (!(a->scale > 0.f) || !isfinite(a->scale) || !(a->softcap >= 0.f) || !isfinite(a->softcap)) return Q2D_EINVAL;
     if (!on4(a->slopes) || !on4(a->prefix)) return Q2D_EINVAL;
     if (s->tokens == 0) return Q2D_OK;
+    if (s->tokens > INT32_MAX / a->heads_q) return Q2D_EUNSUPPORTED;
     r = check_rows(a->q, s->tokens, a->q_stride_token, a->heads_q, a->q_stride_head, c->dim, 8, false);
     if (r == Q2D_OK) r = check_rows(a->out, s->tokens, a->out_stride_token, a->heads_q, a->out_stride_head, c->dim, 8, true);
     if (r != Q2D_OK) return r;

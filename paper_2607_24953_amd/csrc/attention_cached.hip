@@ -76,12 +76,45 @@ __device__ __forceinline__ void fetch(const CachedArgs &a, const Where &w, int l
     c.vs = w.value >= 0 ? a.cache.vs[w.value] : kNoBlock;
 }
 
-// MODS bit 0: capped scores, bit 1: distance bias; NT: 16-column tiles of query rows
-template <int DT, int MODS, int NT>
-__global__ __launch_bounds__(256, 1) void attention_cached_kernel(const CachedArgs a)
+// Where a workgroup of either kernel works: tile of ROWS query rows of a sequence that share key
+// head `head`, and its part of the super-blocks, [from, to)
+struct Place {
+    int b, rt, head, split, rows, prefix, p0, p1, from, to;
+    int64_t tile;
+    Span s;
+};
+
+// false: no such tile.  (ROWS: row r of the tile is token r / group, head r % group.)
+template <int ROWS>
+__device__ __forceinline__ bool place_of(const CachedArgs &a, int group, Place &w)
+{
+    const AttentionMask &m = a.mask;
+    w.split = blockIdx.x % a.splits;
+    const int64_t rest = blockIdx.x / a.splits;
+    w.head = (int)(rest % a.cache.heads);
+    w.tile = rest / a.cache.heads;
+    w.b = find_unit(a.seq, a.cache.page_blocks * kBlockTokens, w.tile,
+                    [&](const Span &x) { return (int)(((int64_t)x.n * group + ROWS - 1) / ROWS); }, w.s, w.rt);
+    if (w.b < 0) return false;
+    w.rows = min(ROWS, (int)((int64_t)w.s.n * group - (int64_t)w.rt * ROWS));
+    w.prefix = m.prefix ? min(max(m.prefix[w.b], 0), w.s.len) : 0;
+    w.p0 = w.s.len - w.s.n + w.rt * ROWS / group;
+    w.p1 = w.s.len - w.s.n + (w.rt * ROWS + w.rows - 1) / group;
+    // tokens that some row sees: [t0, t1)
+    int t1 = max(min(w.p1 + 1, w.s.len), w.prefix), t0 = m.window && !w.prefix ? max(w.p0 - m.window + 1, 0) : 0;
+    if (t1 < t0) t1 = t0;
+    const int sb0 = t0 / kSuper, sbs = (t1 + kSuper - 1) / kSuper - sb0;
+    w.from = sb0 + (int)((int64_t)sbs * w.split / a.splits);
+    w.to = sb0 + (int)((int64_t)sbs * (w.split + 1) / a.splits);
+    return true;
+}
+
+// MODS bit 0: capped scores, bit 1: distance bias
+template <int DT, int MODS>
+__global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedArgs a)
 {
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2;
-    constexpr int KS = DT / 32, VT = DT / 16, ROWS = 16 * NT;
+    constexpr int KS = DT / 32, VT = DT / 16, ROWS = 16;
     // two waves' sums [row][dim] at a time, and all waves' statistics
     __shared__ __align__(16) float osum[2][ROWS * DT];
     __shared__ float stat[2][4][ROWS];
@@ -90,65 +123,39 @@ __global__ __launch_bounds__(256, 1) void attention_cached_kernel(const CachedAr
     const int group = a.heads_q / a.cache.heads, D = a.cache.dim;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x % a.splits;
-    const int64_t rest = blockIdx.x / a.splits;
-    const int head = (int)(rest % a.cache.heads);
-    const int64_t tile = rest / a.cache.heads;
-    Span s;
-    int rt;
-    const int b = find_unit(a.seq, a.cache.page_blocks * kBlockTokens, tile,
-                            [&](const Span &x) { return (int)(((int64_t)x.n * group + ROWS - 1) / ROWS); }, s, rt);
-    if (b < 0) return;
+    Place w;
+    if (!place_of<ROWS>(a, group, w)) return;
+    const Span &s = w.s;
 
-    // this lane's query rows: column c of tile nt
-    const int rows = min(ROWS, (int)((int64_t)s.n * group - (int64_t)rt * ROWS));
-    const int nts = (rows + 15) / 16;
-    int tok[NT], hq[NT], pos[NT];
-    bool row[NT];
-    bf16x8 qf[NT][KS];
-    float slope[NT];
-    ScoreMap sm = score_map(m, 0);
+    // this lane's query row
+    const int r = w.rt * ROWS + col, tok = r / group, hq = w.head * group + r % group, pos = s.len - s.n + tok;
+    const bool row = col < w.rows;
+    const ScoreMap sm = score_map(m, row ? hq : 0);
+    bf16x8 qf[KS];
+    const __bf16 *q = (const __bf16 *)a.q + (s.tok0 + tok) * a.q_st + hq * a.q_sh;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int c = nt * 16 + col, r = rt * ROWS + c;
-        row[nt] = c < rows;
-        tok[nt] = r / group;
-        hq[nt] = head * group + r % group;
-        pos[nt] = s.len - s.n + tok[nt];
-        const __bf16 *q = (const __bf16 *)a.q + (s.tok0 + tok[nt]) * a.q_st + hq[nt] * a.q_sh;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            // the order of dims in which a 16-byte load of codes serves two steps
-            const int d = 64 * (ks >> 1) + 16 * g + 8 * (ks & 1);
-            bf16x8 x = {};
-            if (row[nt] && d < D) x = *reinterpret_cast<const bf16x8 *>(q + d);
-            qf[nt][ks] = x;
-        }
-        slope[nt] = BIAS && row[nt] ? m.slopes[hq[nt]] * kLog2e / sm.c : 0.f;
+    for (int ks = 0; ks < KS; ++ks) {
+        // the order of dims in which a 16-byte load of codes serves two steps
+        const int d = 64 * (ks >> 1) + 16 * g + 8 * (ks & 1);
+        bf16x8 x = {};
+        if (row && d < D) x = *reinterpret_cast<const bf16x8 *>(q + d);
+        qf[ks] = x;
     }
-    const int prefix = m.prefix ? min(max(m.prefix[b], 0), s.len) : 0;
-    const int p0 = s.len - s.n + rt * ROWS / group, p1 = s.len - s.n + (rt * ROWS + rows - 1) / group;
-    // tokens that some row sees: [t0, t1), and this workgroup's super-blocks of them
-    int t1 = max(min(p1 + 1, s.len), prefix), t0 = m.window && !prefix ? max(p0 - m.window + 1, 0) : 0;
-    if (t1 < t0) t1 = t0;
-    const int sb0 = t0 / kSuper, sbs = (t1 + kSuper - 1) / kSuper - sb0;
-    const int from = sb0 + (int)((int64_t)sbs * split / a.splits), to = sb0 + (int)((int64_t)sbs * (split + 1) / a.splits);
+    const Sight sight = query_sight(m, pos, s.len, w.prefix, 0);
 
-    v4f o[VT][NT] = {};
-    float mx[NT], sum[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) { mx[nt] = -INFINITY; sum[nt] = 0.f; }
+    v4f o[VT] = {};
+    float mx = -INFINITY, sum = 0.f;
     const float thr = 8.f / sm.c;
 
     Codes<DT> c;
     Where ahead = {-1, -1};
-    int sb = from + wave;
-    if (sb < to) fetch<DT>(a, locate(a, b, head, sb, s.len, lane), lane, c);
-    if (sb + 4 < to) ahead = locate(a, b, head, sb + 4, s.len, lane);
-    for (; sb < to; sb += 4) {
+    int sb = w.from + wave;
+    if (sb < w.to) fetch<DT>(a, locate(a, w.b, w.head, sb, s.len, lane), lane, c);
+    if (sb + 4 < w.to) ahead = locate(a, w.b, w.head, sb + 4, s.len, lane);
+    for (; sb < w.to; sb += 4) {
         Codes<DT> next;
-        if (sb + 4 < to) fetch<DT>(a, ahead, lane, next);
-        if (sb + 8 < to) ahead = locate(a, b, head, sb + 8, s.len, lane);
+        if (sb + 4 < w.to) fetch<DT>(a, ahead, lane, next);
+        if (sb + 8 < w.to) ahead = locate(a, w.b, w.head, sb + 8, s.len, lane);
 
         const int j0 = sb * kSuper;
         // values past the end: codes of 0 in place of what a page holds there
@@ -163,131 +170,109 @@ __global__ __launch_bounds__(256, 1) void attention_cached_kernel(const CachedAr
             }
         }
         const float ks = c.ks == 255 ? __builtin_nanf("") : ldexpf(CAP ? sm.k1 : 1.f, (int)c.ks - 127);
-        const bool all = j0 + kSuper - 1 <= p0 && j0 + kSuper <= s.len && (!m.window || p1 - j0 < m.window) &&
+        const bool all = j0 + kSuper - 1 <= w.p0 && j0 + kSuper <= s.len && (!m.window || w.p1 - j0 < m.window) &&
                          !__any(c.vs == kNoBlock);
-        bf16x8 pf[NT][2];
+        bf16x8 pf[2];
         // (a value scale of 255 marks a block with a NaN: rows that see it get one)
         const bool bad = __any(c.vs == 255);
+        v4f z[4] = {};
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            if (nt >= nts) continue;
-            v4f z[4] = {};
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int t = 0; t < DT / 64; ++t) {
+                const u4v w = c.k[u][t];
+                z[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_to_bf16(w[0], w[1], 1.f), qf[2 * t], z[u], 0, 0, 0);
+                z[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_to_bf16(w[2], w[3], 1.f), qf[2 * t + 1], z[u], 0, 0, 0);
+            }
+        const int jl = j0 + 16 * g;
+        const float d0 = (float)(pos - jl);
+        float top = -INFINITY;
 #pragma unroll
-                for (int t = 0; t < DT / 64; ++t) {
-                    const u4v w = c.k[u][t];
-                    z[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_to_bf16(w[0], w[1], 1.f), qf[nt][2 * t], z[u], 0, 0, 0);
-                    z[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_to_bf16(w[2], w[3], 1.f), qf[nt][2 * t + 1], z[u], 0, 0, 0);
-                }
-            const int jl = j0 + 16 * g;
-            const float d0 = (float)(pos[nt] - jl);
-            float top = -INFINITY;
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float x = z[u][i] * ks;
+                if constexpr (CAP) x = tanh_of(x, false);
+                if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 - (float)(4 * u + i)), x);
+                z[u][i] = x;
+            }
+        if (!all) {
 #pragma unroll
             for (int u = 0; u < 4; ++u)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float x = z[u][i] * ks;
-                    if constexpr (CAP) x = tanh_of(x, false);
-                    if constexpr (BIAS) x = fmaf(-slope[nt], fabsf(d0 - (float)(4 * u + i)), x);
-                    z[u][i] = x;
+                    const int j = jl + 4 * u + i;
+                    const bool ok = ((j >= sight.lo && j < sight.hi) || j < w.prefix) && c.vs != kNoBlock;
+                    z[u][i] = ok ? z[u][i] : -INFINITY;
                 }
-            if (!all) {
-                const Sight sight = query_sight(m, pos[nt], s.len, prefix, 0);
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int j = jl + 4 * u + i;
-                        const bool ok = ((j >= sight.lo && j < sight.hi) || j < prefix) && c.vs != kNoBlock;
-                        z[u][i] = ok ? z[u][i] : -INFINITY;
-                    }
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, z[u][i]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            // (as in the forward kernel: the maximum moves only where it is passed by 2^8)
-            if (__any(top > mx[nt] + thr)) {
-                const float now = fmaxf(mx[nt], top);
-                const float f = mx[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx[nt] - now) * sm.c);
-#pragma unroll
-                for (int t = 0; t < VT; ++t) o[t][nt] *= f;
-                sum[nt] *= f;
-                mx[nt] = now;
-            }
-            const float off = mx[nt] == -INFINITY ? 0.f : -mx[nt] * sm.c;
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(z[u][i], sm.c, off));
-                    sum[nt] += e;
-                    z[u][i] = e;
-                    if (bad && c.vs == 255 && e != 0.f) z[u][i] = __builtin_nanf("");
-                }
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) pf[nt][k][i] = (__bf16)z[2 * k + (i >> 2)][i & 3];
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, z[u][i]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        // (as in the forward kernel: the maximum moves only where it is passed by 2^8)
+        if (__any(top > mx + thr)) {
+            const float now = fmaxf(mx, top);
+            const float f = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx - now) * sm.c);
+#pragma unroll
+            for (int t = 0; t < VT; ++t) o[t] *= f;
+            sum *= f;
+            mx = now;
+        }
+        const float off = mx == -INFINITY ? 0.f : -mx * sm.c;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(z[u][i], sm.c, off));
+                sum += e;
+                z[u][i] = e;
+                if (bad && c.vs == 255 && e != 0.f) z[u][i] = __builtin_nanf("");
+            }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pf[k][i] = (__bf16)z[2 * k + (i >> 2)][i & 3];
         const float vs = bits_f((c.vs >= 255 ? 127u : c.vs) << 23);
 #pragma unroll
         for (int t = 0; t < VT; ++t)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const bf16x8 x = fp8_to_bf16(c.v[t][2 * k], c.v[t][2 * k + 1], vs);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-                    if (nt < nts) o[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pf[nt][k], o[t][nt], 0, 0, 0);
+                o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pf[k], o[t], 0, 0, 0);
             }
         c = next;
     }
 
     // join the four waves: common maximum, then the sums in two steps
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        sum[nt] += __shfl_xor(sum[nt], 16);
-        sum[nt] += __shfl_xor(sum[nt], 32);
-        if (g == 0) {
-            stat[0][wave][nt * 16 + col] = mx[nt];
-            stat[1][wave][nt * 16 + col] = sum[nt];
-        }
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (g == 0) {
+        stat[0][wave][col] = mx;
+        stat[1][wave][col] = sum;
     }
     __syncthreads();
-    float total[NT], most[NT];
+    float total = 0.f, most = -INFINITY;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int r = nt * 16 + col;
-        most[nt] = -INFINITY;
+    for (int x = 0; x < 4; ++x) most = fmaxf(most, stat[0][x][col]);
+    auto weight = [&](float x, float l) {
+        // (a sum of nothing counts 0, one that is NaN stays)
+        return l == 0.f ? 0.f : x == most ? 1.f : __builtin_amdgcn_exp2f((x - most) * sm.c);
+    };
 #pragma unroll
-        for (int w = 0; w < 4; ++w) most[nt] = fmaxf(most[nt], stat[0][w][r]);
-        total[nt] = 0.f;
+    for (int x = 0; x < 4; ++x) total += weight(stat[0][x][col], stat[1][x][col]) * stat[1][x][col];
+    const float f = weight(mx, sum);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            // (sums of nothing are 0; one that is NaN stays)
-            const float x = stat[1][w][r], y = stat[0][w][r];
-            total[nt] += x == 0.f ? 0.f : x * (y == most[nt] ? 1.f : __builtin_amdgcn_exp2f((y - most[nt]) * sm.c));
-        }
-        const float f = sum[nt] == 0.f ? 0.f : mx[nt] == most[nt] ? 1.f : __builtin_amdgcn_exp2f((mx[nt] - most[nt]) * sm.c);
-#pragma unroll
-        for (int t = 0; t < VT; ++t) o[t][nt] *= f;
-    }
+    for (int t = 0; t < VT; ++t) o[t] *= f;
     auto put = [&](float *dst) {
 #pragma unroll
-        for (int t = 0; t < VT; ++t)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-                *reinterpret_cast<v4f *>(dst + (nt * 16 + col) * DT + 16 * t + 4 * g) = o[t][nt];
+        for (int t = 0; t < VT; ++t) *reinterpret_cast<v4f *>(dst + (t * 64 + lane) * 4) = o[t];
     };
     auto add = [&](const float *src) {
 #pragma unroll
-        for (int t = 0; t < VT; ++t)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-                o[t][nt] += *reinterpret_cast<const v4f *>(src + (nt * 16 + col) * DT + 16 * t + 4 * g);
+        for (int t = 0; t < VT; ++t) o[t] += *reinterpret_cast<const v4f *>(src + (t * 64 + lane) * 4);
     };
     if (wave >= 2) put(osum[wave - 2]);
     __syncthreads();
@@ -295,27 +280,245 @@ __global__ __launch_bounds__(256, 1) void attention_cached_kernel(const CachedAr
     __syncthreads();
     if (wave == 1) put(osum[0]);
     __syncthreads();
-    if (wave != 0) return;
+    if (wave != 0 || !row) return;
     add(osum[0]);
+    if (a.splits == 1) {
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        __bf16 *out = (__bf16 *)a.out + (s.tok0 + tok) * a.out_st + hq * a.out_sh;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        if (!row[nt]) continue;
-        if (a.splits == 1) {
-            const float inv = total[nt] == 0.f ? 0.f : 1.f / total[nt];
-            __bf16 *out = (__bf16 *)a.out + (s.tok0 + tok[nt]) * a.out_st + hq[nt] * a.out_sh;
+        for (int t = 0; t < VT; ++t)
+            if (16 * t < D) store4(out + 16 * t + 4 * g, o[t][0] * inv, o[t][1] * inv, o[t][2] * inv, o[t][3] * inv);
+    } else {
+        const int64_t at = ((w.tile * a.cache.heads + w.head) * a.splits + w.split) * ROWS + col;
 #pragma unroll
-            for (int t = 0; t < VT; ++t)
-                if (16 * t < D)
-                    store4(out + 16 * t + 4 * g, o[t][nt][0] * inv, o[t][nt][1] * inv, o[t][nt][2] * inv, o[t][nt][3] * inv);
-        } else {
-            const int64_t at = ((tile * a.cache.heads + head) * a.splits + split) * ROWS + nt * 16 + col;
+        for (int t = 0; t < VT; ++t)
+            if (16 * t < D) *reinterpret_cast<v4f *>(a.part + at * D + 16 * t + 4 * g) = o[t];
+        if (g == 0) {
+            a.stat[2 * at] = most * sm.c;
+            a.stat[2 * at + 1] = total;
+        }
+    }
+}
+
+// The same for prompts: 128 query rows a workgroup, 32 a wave, as in the forward kernel on whole
+// sequences.  The workgroup converts each super-block once into LDS tiles of bfloat16 (exact:
+// a code times its power of two), keys [token][dim] and values [dim][token], while the codes of
+// the next one are on their way.  With the key rows taken in the order
+// 16 (b / 2) + 8 h + 4 (b % 2) + i for output row 8 b + 4 h + i, a lane ends with 8 neighbouring
+// tokens for each k-step, and value fragments are single 16-byte reads.
+template <int DC, int MODS>
+__global__ __launch_bounds__(256, 2) void attention_cached_rows_kernel(const CachedArgs a)
+{
+    constexpr bool CAP = MODS & 1, BIAS = MODS & 2;
+    constexpr int DT = DC <= 64 ? 64 : 128, KS = DC / 16, DS = DC / 32, ROWS = 128;
+    constexpr int kPasses = kSuper * DT / (16 * 256);          // 16-byte loads of a thread, keys or values
+    typedef Tile<__bf16, DT> Lds;
+    __shared__ __align__(1024) uint8_t ktile[2][kSuper * DT * 2], vtile[2][kSuper * DT * 2];
+
+    const AttentionMask &m = a.mask;
+    const int group = a.heads_q / a.cache.heads, D = a.cache.dim;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int h = lane >> 5, col = lane & 31;
+    Place w;
+    if (!place_of<ROWS>(a, group, w)) return;
+    const Span &s = w.s;
+    const int c = wave * 32 + col, r = w.rt * ROWS + c, tok = r / group, hq = w.head * group + r % group;
+    const int pos = s.len - s.n + tok;
+    const bool row = c < w.rows, some = wave * 32 < w.rows;
+    // positions of the wave's first and last row
+    const int pw0 = s.len - s.n + (w.rt * ROWS + wave * 32) / group;
+    const int pw1 = s.len - s.n + (w.rt * ROWS + min(wave * 32 + 32, w.rows) - 1) / group;
+    const ScoreMap sm = score_map(m, row ? hq : 0);
+    const __bf16 *q = (const __bf16 *)a.q + (s.tok0 + tok) * a.q_st + hq * a.q_sh;
+    bf16x8 qf[KS];
 #pragma unroll
-            for (int t = 0; t < VT; ++t)
-                if (16 * t < D) *reinterpret_cast<v4f *>(a.part + at * D + 16 * t + 4 * g) = o[t][nt];
-            if (g == 0) {
-                a.stat[2 * at] = most[nt] * sm.c;
-                a.stat[2 * at + 1] = total[nt];
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = global_frag<__bf16>(q, row, ks, h, D);
+    const Sight sight = query_sight(m, pos, s.len, w.prefix, 0);
+    const float thr = 8.f / sm.c;
+
+    // the two cache blocks of a super-block (-1: none), and their scale bytes
+    struct Blocks {
+        int64_t at[2];
+        uint32_t ks[2], vs[2];
+    };
+    auto blocks_of = [&](int sb) __attribute__((always_inline)) {
+        Blocks x;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            x.at[i] = -1;
+            x.ks[i] = 0;
+            x.vs[i] = kNoBlock;
+            const int blk = 2 * sb + i;
+            if (sb < w.to && blk * kBlockTokens < s.len) x.at[i] = cache_block(a.cache, a.seq, w.b, blk, w.head);
+            if (x.at[i] >= 0) {
+                x.ks[i] = a.cache.ks[x.at[i]];
+                x.vs[i] = a.cache.vs[x.at[i]];
             }
+        }
+        return x;
+    };
+    u4v kc[kPasses], vc[kPasses];
+    auto fetch = [&](const Blocks &x) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            const int slot = i * 256 + tid;
+            // keys: 16 dims of a token; values: 16 tokens of a dim
+            const int t = slot / (DT / 16), d = slot % (DT / 16) * 16;
+            const int64_t kb = t < kBlockTokens ? x.at[0] : x.at[1];
+            const int blk = slot / (2 * DT), dv = slot % (2 * DT) / 2;
+            const int64_t vb = blk ? x.at[1] : x.at[0];
+            kc[i] = vc[i] = u4v{0, 0, 0, 0};
+            if (kb >= 0 && d < D)
+                kc[i] = *reinterpret_cast<const u4v *>(a.cache.k + (kb * kBlockTokens + t % kBlockTokens) * D + d);
+            if (vb >= 0 && dv < D)
+                vc[i] = *reinterpret_cast<const u4v *>(a.cache.v + (vb * D + dv) * kBlockTokens + slot % 2 * 16);
+        }
+    };
+    auto scale_of = [](uint32_t byte) { return bits_f((byte >= 255 ? 127u : byte) << 23); };
+    // codes at hand (of super-block sb) -> bfloat16 tiles
+    auto convert = [&](int stage, int sb, const Blocks &x) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            const int slot = i * 256 + tid;
+            const int t = slot / (DT / 16), c16 = slot % (DT / 16);
+            const uint32_t kb = t < kBlockTokens ? x.ks[0] : x.ks[1];
+            const float kscale = scale_of(kb);
+            bf16x8 lo = fp8_to_bf16(kc[i][0], kc[i][1], kscale), hi = fp8_to_bf16(kc[i][2], kc[i][3], kscale);
+            if (kb == 255) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) lo[e] = hi[e] = (__bf16)__builtin_nanf("");
+            }
+            *reinterpret_cast<bf16x8 *>(ktile[stage] + Lds::offset(t, 2 * c16)) = lo;
+            *reinterpret_cast<bf16x8 *>(ktile[stage] + Lds::offset(t, 2 * c16 + 1)) = hi;
+
+            const int blk = slot / (2 * DT), d = slot % (2 * DT) / 2, half = slot % 2;
+            u4v v = vc[i];
+            // tokens past the end: codes of 0 in place of what the page holds there
+            const int n = s.len - (sb * kSuper + blk * kBlockTokens + half * 16);
+            if (n < 16) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] &= (uint32_t)((1ull << (8 * min(max(n - 4 * e, 0), 4))) - 1);
+            }
+            const float vscale = scale_of(blk ? x.vs[1] : x.vs[0]);
+            const int chunk = 4 * blk + 2 * half;
+            uint8_t *p = vtile[stage] + d * (kSuper * 2);
+            *reinterpret_cast<bf16x8 *>(p + ((chunk ^ ((d >> 1) & 7)) << 4)) = fp8_to_bf16(v[0], v[1], vscale);
+            *reinterpret_cast<bf16x8 *>(p + (((chunk + 1) ^ ((d >> 1) & 7)) << 4)) = fp8_to_bf16(v[2], v[3], vscale);
+        }
+    };
+
+    v16f o[DS] = {};
+    float mx = -INFINITY, sum = 0.f;
+    auto tile = [&](int stage, int sb, const Blocks &x) __attribute__((always_inline)) {
+        const int j0 = sb * kSuper;
+        if (j0 > pw1 && j0 >= w.prefix) return;
+        const int krow = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
+        const uint32_t kr = Lds::fresh(Lds::address(ktile[stage]) + Lds::offset(krow, h));
+        const uint32_t vr = Lds::fresh(Lds::address(vtile[stage]) + col * (kSuper * 2) + ((h ^ ((col >> 1) & 7)) << 4));
+        v16f z[2] = {};
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) z[t] = mma(Lds::row_frag(kr, t, ks), qf[ks], z[t]);
+        // token of register i: 16 (i / 8) + 8 h + i % 8
+        if constexpr (CAP || BIAS) {
+            const float d0 = (float)(pos - j0 - 8 * h);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float y = z[t][i];
+                    if constexpr (CAP) y = tanh_of(y * sm.k1, false);
+                    if constexpr (BIAS) y = fmaf(-sm.slope, fabsf(d0 - (float)(32 * t + 16 * (i >> 3) + (i & 7))), y);
+                    z[t][i] = y;
+                }
+        }
+        const bool all = j0 + kSuper - 1 <= pw0 && j0 + kSuper <= s.len && (!m.window || pw1 - j0 < m.window) &&
+                         x.at[0] >= 0 && x.at[1] >= 0;
+        if (!all) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const uint32_t seen = x.at[t] >= 0 ? sight.word(j0 + 32 * t, nullptr) >> (8 * h) : 0u;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    z[t][i] = (seen >> (16 * (i >> 3) + (i & 7))) & 1 ? z[t][i] : -INFINITY;
+            }
+        }
+        float top = z[0][0];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, z[t][i]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        // (as in the forward kernel: the maximum moves only where it is passed by 2^8)
+        if (__any(top > mx + thr)) {
+            const float now = fmaxf(mx, top);
+            const float f = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mx - now) * sm.c);
+#pragma unroll
+            for (int dt = 0; dt < DS; ++dt) o[dt] *= f;
+            sum *= f;
+            mx = now;
+        }
+        const float off = mx == -INFINITY ? 0.f : -mx * sm.c;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                z[t][i] = __builtin_amdgcn_exp2f(fmaf(z[t][i], sm.c, off));
+                sum += z[t][i];
+            }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            // (a value scale of 255 marks a block with a NaN: rows that see it get one)
+            if (x.vs[t] == 255) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[t][i] = z[t][i] != 0.f ? __builtin_nanf("") : 0.f;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 pf = to_frag<__bf16>(z[t], k);
+#pragma unroll
+                for (int dt = 0; dt < DS; ++dt)
+                    o[dt] = mma(*Lds::template lds_ptr<bf16x8>((vr ^ (uint32_t)((4 * t + 2 * k) << 4)) + dt * 32 * kSuper * 2),
+                                pf, o[dt]);
+            }
+    };
+
+    Blocks now = blocks_of(w.from), next = blocks_of(w.from + 1);
+    if (w.from < w.to) {
+        fetch(now);
+        convert(0, w.from, now);
+    }
+    fetch(next);
+    int stage = 0;
+    for (int sb = w.from; sb < w.to; ++sb) {
+        __syncthreads();
+        Blocks after = next;
+        if (sb + 1 < w.to) {
+            after = blocks_of(sb + 2);
+            convert(stage ^ 1, sb + 1, next);
+            fetch(after);
+        }
+        if (some) tile(stage, sb, now);
+        now = next;
+        next = after;
+        stage ^= 1;
+    }
+
+    sum += __shfl_xor(sum, 32);
+    if (!row) return;
+    if (a.splits == 1) {
+        __bf16 *out = (__bf16 *)a.out + (s.tok0 + tok) * a.out_st + hq * a.out_sh;
+        store_columns<__bf16, DS>(out, o, sum == 0.f ? 0.f : 1.f / sum, h, D);
+    } else {
+        const int64_t at = ((w.tile * a.cache.heads + w.head) * a.splits + w.split) * ROWS + c;
+        store_columns<float, DS>(a.part + at * D, o, 1.f, h, D);
+        if (h == 0) {
+            a.stat[2 * at] = mx * sm.c;
+            a.stat[2 * at + 1] = sum;
         }
     }
 }
@@ -360,24 +563,26 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const CachedArgs a)
     *reinterpret_cast<bf16x2v *>(out + 2 * lane) = bf16x2v{(__bf16)(x0 * inv), (__bf16)(x1 * inv)};
 }
 
-template <int DT, int MODS, int NT>
+// ROWS: query rows of a workgroup, 128 or 16
+template <int DC, int MODS, int ROWS>
 hipError_t launch(const CachedArgs &a, hipStream_t stream)
 {
     const int64_t heads = a.tiles * a.cache.heads, n = heads * a.splits;
-    if (n > INT32_MAX || heads * (4 * NT) > INT32_MAX) return hipErrorInvalidConfiguration;
-    attention_cached_kernel<DT, MODS, NT><<<(uint32_t)n, 256, 0, stream>>>(a);
-    if (a.splits > 1) attention_join_kernel<16 * NT><<<(uint32_t)(heads * 4 * NT), 256, 0, stream>>>(a);
+    if (n > INT32_MAX || heads * (ROWS / 4) > INT32_MAX) return hipErrorInvalidConfiguration;
+    if constexpr (ROWS == 16) attention_cached_kernel<DC, MODS><<<(uint32_t)n, 256, 0, stream>>>(a);
+    else attention_cached_rows_kernel<DC, MODS><<<(uint32_t)n, 256, 0, stream>>>(a);
+    if (a.splits > 1) attention_join_kernel<ROWS><<<(uint32_t)(heads * (ROWS / 4)), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
-template <int DT, int NT>
+template <int DC, int ROWS>
 hipError_t launch_mods(const CachedArgs &a, hipStream_t stream)
 {
     switch ((a.mask.cap > 0.f ? 1 : 0) | (a.mask.slopes ? 2 : 0)) {
-    case 0: return launch<DT, 0, NT>(a, stream);
-    case 1: return launch<DT, 1, NT>(a, stream);
-    case 2: return launch<DT, 2, NT>(a, stream);
-    default: return launch<DT, 3, NT>(a, stream);
+    case 0: return launch<DC, 0, ROWS>(a, stream);
+    case 1: return launch<DC, 1, ROWS>(a, stream);
+    case 2: return launch<DC, 2, ROWS>(a, stream);
+    default: return launch<DC, 3, ROWS>(a, stream);
     }
 }
 
@@ -386,8 +591,9 @@ hipError_t launch_mods(const CachedArgs &a, hipStream_t stream)
 hipError_t launch_attention_cached(const CachedArgs &a, hipStream_t stream)
 {
     if (a.tiles == 0) return hipSuccess;
-    if (a.cache.dim <= 64) return a.wide ? launch_mods<64, 4>(a, stream) : launch_mods<64, 1>(a, stream);
-    return a.wide ? launch_mods<128, 4>(a, stream) : launch_mods<128, 1>(a, stream);
+    if (!a.wide) return a.cache.dim <= 64 ? launch_mods<64, 16>(a, stream) : launch_mods<128, 16>(a, stream);
+    if (a.cache.dim <= 64) return launch_mods<64, 128>(a, stream);
+    return a.cache.dim <= 96 ? launch_mods<96, 128>(a, stream) : launch_mods<128, 128>(a, stream);
 }
 
 }  // namespace q2d
