@@ -5,11 +5,10 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import math
 
 import torch
 
-from . import Q2DError, _check, _dtype_code, _lib, _same_device, _stream
+from . import Q2DError, _check, _dtype_code, _lib, _norm, _same_device, _stream
 
 
 class _Heads(ctypes.Structure):
@@ -47,10 +46,11 @@ class _CachedAttention(ctypes.Structure):
 
 
 _P, _I64, _I32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
-_AP, _HP = ctypes.POINTER(_Attention), ctypes.POINTER(_Heads)
+_AP = ctypes.POINTER(_Attention)
 _lib.q2d_attention_workspace.argtypes, _lib.q2d_attention_workspace.restype = [_AP, _I32], _I64
 _lib.q2d_attention_fwd.argtypes, _lib.q2d_attention_fwd.restype = [_AP, _P, _I64, _P], _I32
-_lib.q2d_attention_bwd.argtypes, _lib.q2d_attention_bwd.restype = [_AP, _HP, _HP, _HP, _HP, _P, _I64, _P], _I32
+# (the four descriptors stand in one array)
+_lib.q2d_attention_bwd.argtypes, _lib.q2d_attention_bwd.restype = [_AP, _P, _P, _P, _P, _P, _I64, _P], _I32
 
 _CP, _SP = ctypes.POINTER(_Cache), ctypes.POINTER(_Sequences)
 _lib.q2d_kv_cache_init.argtypes = [_CP, _I32, _I32, _I32, _I32, ctypes.POINTER(_I64)]
@@ -63,26 +63,30 @@ _lib.q2d_attention_cached.argtypes = [_CP, _SP, ctypes.POINTER(_CachedAttention)
 _lib.q2d_attention_cached.restype = _I32
 
 
+def _on(device, t):
+    if t.device != device:
+        _same_device(device, t)
+
+
 def _vector(t, n, dtype, device, what):
     """Pointer of an optional contiguous device vector or matrix of n elements."""
     if t is None:
         return None
     if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
         raise Q2DError("%s: a contiguous %s tensor of %d elements is expected" % (what, dtype, n))
-    _same_device(device, t)
+    _on(device, t)
     return t.data_ptr()
 
 
-def _heads(t, shape, dtype, device, what, into=None):
-    """Descriptor of a [batch, length, heads, dim] tensor (any strides, unit along dim)."""
-    if tuple(t.shape) != shape or t.dtype != dtype or (t.stride(3) != 1 and shape[3] > 1):
+def _heads(t, shape, dtype, device, what, d):
+    """Fills descriptor d of a [batch, length, heads, dim] tensor (any strides, unit along dim)."""
+    st = t.stride()
+    if t.shape != shape or t.dtype != dtype or (st[3] != 1 and shape[3] > 1):
         raise Q2DError("%s: a %s tensor of shape %s with unit stride along the last dimension is expected"
-                       % (what, dtype, shape))
-    _same_device(device, t)
-    d = _Heads() if into is None else into
+                       % (what, dtype, tuple(shape)))
+    _on(device, t)
     d.data = t.data_ptr()
-    d.stride_batch, d.stride_length, d.stride_head = t.stride(0), t.stride(1), t.stride(2)
-    return d
+    d.stride_batch, d.stride_length, d.stride_head = st[0], st[1], st[2]
 
 
 @functools.lru_cache(maxsize=1024)
@@ -97,25 +101,30 @@ def _template(dtype, causal, batch, heads_q, heads_kv, dim, len_q, len_k, window
 
 
 def _problem(q, k, v, out, lse, scale, causal, window, softcap, slopes, documents, prefix):
-    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+    if q.dim() != 4 or k.dim() != 4:
         raise Q2DError("expected q, k and v as [batch, length, heads, dim]")
-    B, Lq, Hq, D = q.shape
-    Lk, Hkv = k.shape[1], k.shape[2]
+    qs, ks = q.shape, k.shape
+    B, Lq, Hq, D = qs
+    Lk, Hkv = ks[1], ks[2]
     device, dt = q.device, q.dtype
-    _same_device(device)
+    if device.type != "cuda" or ks[0] != B or ks[3] != D:
+        _same_device(device)
+        raise Q2DError("k: a tensor of shape %s is expected" % ((B, Lk, Hkv, D),))
     if scale is None:
-        scale = 1.0 / math.sqrt(D) if D else 0.0
-    raw, sizes = _template(_dtype_code(dt), int(bool(causal)), B, Hq, Hkv, D, Lq, Lk, int(window), float(scale),
+        scale = D ** -0.5 if D else 0.0
+    raw, sizes = _template(_dtype_code(dt), 1 if causal else 0, B, Hq, Hkv, D, Lq, Lk, int(window), float(scale),
                            float(softcap), documents is not None)
     a = _Attention.from_buffer_copy(raw)
-    kv = (B, Lk, Hkv, D)
-    _heads(q, (B, Lq, Hq, D), dt, device, "q", a.q)
-    _heads(k, kv, dt, device, "k", a.k)
-    _heads(v, kv, dt, device, "v", a.v)
-    _heads(out, (B, Lq, Hq, D), dt, device, "out", a.out)
-    a.slopes = _vector(slopes, Hq, torch.float32, device, "slopes")
-    a.documents = _vector(documents, B * Lk, torch.int32, device, "documents")
-    a.prefix = _vector(prefix, B, torch.int32, device, "prefix")
+    _heads(q, qs, dt, device, "q", a.q)
+    _heads(k, ks, dt, device, "k", a.k)
+    _heads(v, ks, dt, device, "v", a.v)
+    _heads(out, qs, dt, device, "out", a.out)
+    if slopes is not None:
+        a.slopes = _vector(slopes, Hq, torch.float32, device, "slopes")
+    if documents is not None:
+        a.documents = _vector(documents, B * Lk, torch.int32, device, "documents")
+    if prefix is not None:
+        a.prefix = _vector(prefix, B, torch.int32, device, "prefix")
     a.lse = _vector(lse, B * Hq * Lq, torch.float32, device, "lse")
     return a, sizes
 
@@ -141,11 +150,14 @@ def q2d_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: 
     it; documents (int32 [batch, len_k], negative: padding) keeps attention within documents;
     prefix (int32 [batch]) lets every query see the first keys.  lse (float32 [batch,
     heads_q, len_q]) is what q2d_attention_bwd needs, None with need_lse=False."""
+    if q.dim() != 4 or v.dim() != 4 or (out is not None and out.dim() != 4):
+        raise Q2DError("expected q, k and v as [batch, length, heads, dim]")
+    shape = q.shape
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty(shape, dtype=q.dtype, device=q.device)
     lse = None
-    if need_lse and q.dim() == 4:
-        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+    if need_lse:
+        lse = torch.empty((shape[0], shape[2], shape[1]), dtype=torch.float32, device=q.device)
     a, sizes = _problem(q, k, v, out, lse, scale, causal, window, softcap, slopes, documents, prefix)
     keep, ws = _workspace(sizes[0], q.device)
     _check(_lib.q2d_attention_fwd(ctypes.byref(a), ws, max(sizes[0], 0), _stream(q.device)), "q2d_attention_fwd")
@@ -159,15 +171,22 @@ def q2d_attention_bwd(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
                       dk: torch.Tensor | None = None, dv: torch.Tensor | None = None):
     """Gradients (dq, dk, dv) of q2d_attention_fwd with the same arguments, from its out and
     lse and the gradient dout of out."""
+    if v.dim() != 4 or out.dim() != 4:
+        raise Q2DError("expected v and out as [batch, length, heads, dim]")
     a, sizes = _problem(q, k, v, out, lse, scale, causal, window, softcap, slopes, documents, prefix)
     dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
     dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
     dv = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dv is None else dv
-    g = [_heads(t, tuple(s.shape), q.dtype, q.device, n)
-         for t, s, n in ((dout, q, "dout"), (dq, q, "dq"), (dk, k, "dk"), (dv, k, "dv"))]
+    g = (_Heads * 4)()
+    for i, (t, s, n) in enumerate(((dout, q, "dout"), (dq, q, "dq"), (dk, k, "dk"), (dv, k, "dv"))):
+        if t.dim() != 4:
+            raise Q2DError("%s: a [batch, length, heads, dim] tensor is expected" % n)
+        _heads(t, s.shape, q.dtype, q.device, n, g[i])
+    size = ctypes.sizeof(_Heads)
     keep, ws = _workspace(sizes[1], q.device)
-    _check(_lib.q2d_attention_bwd(ctypes.byref(a), *[ctypes.byref(x) for x in g], ws, max(sizes[1], 0),
-                                  _stream(q.device)), "q2d_attention_bwd")
+    _check(_lib.q2d_attention_bwd(ctypes.byref(a), ctypes.byref(g), ctypes.byref(g, size), ctypes.byref(g, 2 * size),
+                                  ctypes.byref(g, 3 * size), ws, max(sizes[1], 0), _stream(q.device)),
+           "q2d_attention_bwd")
     return dq, dk, dv
 
 
@@ -186,7 +205,8 @@ class KVCache:
                "q2d_kv_cache_init")
         self._ref = ctypes.byref(self.desc)
         self.pages, self.heads, self.dim, self.page_size = int(pages), int(heads), int(dim), int(page_size)
-        self.device = torch.device(device)
+        self.device = _norm(device)
+        self.scale = self.dim ** -0.5
         blocks = self.page_size // 32
         shapes = {"k_codes": (pages, heads, page_size, dim), "v_codes_t": (pages, heads, blocks, dim, 32),
                   "k_scales": (pages, heads, blocks), "v_scales": (pages, heads, blocks)}
@@ -196,27 +216,48 @@ class KVCache:
             setattr(self.desc, name, t.data_ptr())
 
 
+@functools.lru_cache(maxsize=1024)
+def _sequences_template(batch, table_pages, tokens, table_stride):
+    return bytes(_Sequences(batch=batch, table_pages=table_pages, tokens=tokens, table_stride=table_stride))
+
+
 def _sequences(cache, table, lens, tokens, offsets):
     if not isinstance(cache, KVCache):
         raise Q2DError("expected a KVCache")
-    if table.dim() != 2 or table.dtype != torch.int32 or (table.shape[1] > 1 and table.stride(1) != 1):
-        raise Q2DError("block_table: an int32 tensor [sequences, pages] with unit column stride is expected")
-    _same_device(cache.device, table)
-    batch = table.shape[0]
-    s = _Sequences(batch=batch, table_pages=table.shape[1], tokens=tokens,
-                   table_stride=table.stride(0) if batch > 1 else max(table.stride(0), table.shape[1]))
+    if table.dim() != 2 or table.dtype != torch.int32:
+        raise Q2DError("block_table: an int32 tensor [sequences, pages] is expected")
+    batch, pages = table.shape
+    stride, one = table.stride()
+    if one != 1 and pages > 1:
+        raise Q2DError("block_table: unit column stride is expected")
+    _on(cache.device, table)
+    s = _Sequences.from_buffer_copy(_sequences_template(batch, pages, tokens, stride if batch > 1 else max(stride, pages)))
     s.table = table.data_ptr()
     s.lens = _vector(lens, batch, torch.int32, cache.device, "lens")
-    s.offsets = _vector(offsets, batch + 1, torch.int64, cache.device, "offsets")
+    if offsets is not None:
+        s.offsets = _vector(offsets, batch + 1, torch.int64, cache.device, "offsets")
     return s
 
 
 def _token_rows(t, heads, dim, device, what):
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.stride(2) != 1:
+    shape, st = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or st[2] != 1:
         raise Q2DError("%s: a [tokens, %d, %d] tensor with unit stride along the last dimension is expected"
                        % (what, heads, dim))
-    _same_device(device, t)
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    _on(device, t)
+    return t.data_ptr(), st[0], st[1]
+
+
+@functools.lru_cache(maxsize=1024)
+def _cached_template(dtype, heads, scale, softcap, window):
+    return bytes(_CachedAttention(dtype=dtype, heads_q=heads, scale=scale, softcap=softcap, window=window))
+
+
+@functools.lru_cache(maxsize=1024)
+def _cached_workspace(pages, heads, dim, page_size, sequences, offsets, heads_q):
+    c, s = _Cache(pages=pages, heads=heads, dim=dim, page_size=page_size), _Sequences.from_buffer_copy(sequences)
+    s.offsets = 256 if offsets else None
+    return _lib.q2d_attention_cached_workspace(ctypes.byref(c), ctypes.byref(s), heads_q)
 
 
 def q2d_kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor,
@@ -264,21 +305,24 @@ def q2d_attention_cached(q: torch.Tensor, cache: KVCache, block_table: torch.Ten
     q2d_attention_fwd."""
     if q.dim() != 3:
         raise Q2DError("expected q as [tokens, heads, dim]")
-    s = _sequences(cache, block_table, lens, q.shape[0], offsets)
-    heads = q.shape[1]
+    tokens, heads, _ = q.shape
+    s = _sequences(cache, block_table, lens, tokens, offsets)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if out.dtype != q.dtype or out.shape != q.shape:
+    elif out.dtype != q.dtype or out.shape != q.shape:
         raise Q2DError("out: the shape and dtype of q are expected")
-    a = _CachedAttention(dtype=_dtype_code(q.dtype), heads_q=heads,
-                         scale=cache.dim ** -0.5 if scale is None else float(scale), softcap=float(softcap),
-                         window=int(window))
-    a.slopes = _vector(slopes, heads, torch.float32, cache.device, "slopes")
-    a.prefix = _vector(prefix, s.batch, torch.int32, cache.device, "prefix")
-    a.q, a.q_stride_token, a.q_stride_head = _token_rows(q, heads, cache.dim, cache.device, "q")
-    a.out, a.out_stride_token, a.out_stride_head = _token_rows(out, heads, cache.dim, cache.device, "out")
-    size = _lib.q2d_attention_cached_workspace(cache._ref, ctypes.byref(s), heads)
-    keep, ws = _workspace(size, cache.device)
-    _check(_lib.q2d_attention_cached(cache._ref, ctypes.byref(s), ctypes.byref(a), ws, max(size, 0),
-                                     _stream(cache.device)), "q2d_attention_cached")
+    device = cache.device
+    a = _CachedAttention.from_buffer_copy(_cached_template(
+        _dtype_code(q.dtype), heads, cache.scale if scale is None else float(scale), float(softcap), int(window)))
+    if slopes is not None:
+        a.slopes = _vector(slopes, heads, torch.float32, device, "slopes")
+    if prefix is not None:
+        a.prefix = _vector(prefix, s.batch, torch.int32, device, "prefix")
+    a.q, a.q_stride_token, a.q_stride_head = _token_rows(q, heads, cache.dim, device, "q")
+    a.out, a.out_stride_token, a.out_stride_head = _token_rows(out, heads, cache.dim, device, "out")
+    size = _cached_workspace(cache.pages, cache.heads, cache.dim, cache.page_size,
+                             _sequences_template(s.batch, s.table_pages, tokens, s.table_stride), offsets is not None, heads)
+    keep, ws = _workspace(size, device)
+    _check(_lib.q2d_attention_cached(cache._ref, ctypes.byref(s), ctypes.byref(a), ws, max(size, 0), _stream(device)),
+           "q2d_attention_cached")
     return out

@@ -101,6 +101,8 @@ struct CachedArgs {
     float *stat;                                 // [tile][head][split][rows] maximum and sum
 };
 
+constexpr int kMaxSplits = 64;                   // parts of a sequence's tokens: a lane each in the join
+
 hipError_t launch_kv_write(const CacheCopyArgs &a, bool f32, hipStream_t stream);
 hipError_t launch_kv_read(const CacheCopyArgs &a, bool f32, hipStream_t stream);
 hipError_t launch_attention_cached(const CachedArgs &a, hipStream_t stream);

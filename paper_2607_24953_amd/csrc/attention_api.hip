@@ -201,7 +201,7 @@ CachedSplit split_cached(const q2d_kv_cache *c, const q2d_sequences *s, int32_t 
     const int64_t units = p.tiles * c->heads, longest = (int64_t)s->table_pages * c->page_size;
     int64_t n = units > 0 ? (1024 + units - 1) / units : 1;
     if (n > (longest + 255) / 256) n = (longest + 255) / 256;
-    if (n > 64) n = 64;
+    if (n > kMaxSplits) n = kMaxSplits;
     p.splits = (int32_t)(n < 1 ? 1 : n);
     const int64_t parts = p.splits > 1 ? units * p.splits * rows : 0;
     p.stat_at = up256(parts * c->dim * 4);

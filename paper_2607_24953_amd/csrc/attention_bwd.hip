@@ -146,13 +146,27 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
         const int j0 = at.tile * BN + jw;
         const uint8_t *kt = smem[stage][0] + jw * Lds::kRowBytes, *vt = smem[stage][1] + jw * Lds::kRowBytes;
         const uint32_t kr = Lds::row_base(kt, lane), vr = Lds::row_base(vt, lane), kc = Lds::column_base(kt, lane);
-#pragma unroll
-        for (int t = 0; t < WN / 32; ++t) {
+        // the order of the reads as in the forward kernel; a step of 32 keys is 2 KS products for
+        // S and dP and 2 DS for dQ
+        constexpr int kFirst = 2 * KS, kStep = kFirst + 2 * DS, kAll = WN / 32 * kStep, kAhead = F32 ? 2 : DC <= 64 ? 1 : 6;
+        Frag<T> ring[kAhead];
+        auto read = [&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value, t = i / kStep, x = i % kStep, y = x - kFirst;
+            if constexpr (i >= kAll) return;
+            else if constexpr (x < kFirst) ring[i % kAhead] = Lds::row_frag(x % 2 ? vr : kr, t, x / 2);
+            else ring[i % kAhead] = Lds::column_frag(kc, 32 * t + 16 * (y / DS), y % DS);
+        };
+        unroll<kAhead>(read);
+        unroll<WN / 32>([&](auto tc) __attribute__((always_inline)) {
+            constexpr int t = decltype(tc)::value;
             v16f z = {}, e = {};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(kr, t, ks), qf[ks], z);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(vr, t, ks), gf[ks], e);
+            unroll<kFirst>([&](auto xc) __attribute__((always_inline)) {
+                constexpr int x = decltype(xc)::value, i = t * kStep + x;
+                if constexpr (x % 2) e = mma(ring[i % kAhead], gf[x / 2], e);
+                else z = mma(ring[i % kAhead], qf[x / 2], z);
+                read(std::integral_constant<int, i + kAhead>{});
+                pin<(DC > 64)>();
+            });
             const float d0 = pos - (float)(j0 + 32 * t) - (float)(4 * h);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -166,18 +180,19 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
                 e[r] = pr * (e[r] - delta) * u;
             }
             if (!at.all) {
-                const uint32_t w = sight.word(j0 + 32 * t, docs ? &doc_of[stage][jw + 32 * t] : nullptr) >> (4 * h);
+                const uint32_t w = sight.word(j0 + 32 * t, docs && !at.same ? &doc_of[stage][jw + 32 * t] : nullptr) >> (4 * h);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) e[r] = word_bit(w, r) ? e[r] : 0.f;
             }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const Frag<T> ef = to_frag<T>(e, s);
-#pragma unroll
-                for (int dt = 0; dt < DS; ++dt)
-                    dq[dt] = mma(Lds::column_frag(kc, 32 * t + 16 * s, dt), ef, dq[dt]);
-            }
-        }
+            Frag<T> ef;
+            unroll<2 * DS>([&](auto yc) __attribute__((always_inline)) {
+                constexpr int y = decltype(yc)::value, i = t * kStep + kFirst + y;
+                if constexpr (y % DS == 0) ef = to_frag<T>(e, y / DS);
+                dq[y % DS] = mma(ring[i % kAhead], ef, dq[y % DS]);
+                read(std::integral_constant<int, i + kAhead>{});
+                pin<(DC > 64)>();
+            });
+        });
     };
     auto check = [&](const Visit &at, int stage) __attribute__((always_inline)) {
         uint32_t bad[BN / 32], some = 0;
@@ -187,7 +202,7 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
         if (!some) return;
 #pragma unroll
         for (int t = 0; t < WN / 32; ++t) {
-            const uint32_t w = sight.word(at.tile * BN + jw + 32 * t, docs ? &doc_of[stage][jw + 32 * t] : nullptr);
+            const uint32_t w = sight.word(at.tile * BN + jw + 32 * t, docs && !at.same ? &doc_of[stage][jw + 32 * t] : nullptr);
             spoilt = spoilt || (at.any && ((at.all ? ~0u : w) & pick<BN / 32>(bad, NARROW ? wave : t)));
         }
         Lds::template clean<BN, NW * 64>(smem[stage][0]);
@@ -357,7 +372,7 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
                     }
                 }
                 if (!at.all) {
-                    const uint32_t w = sight.word(p0, docs ? &doc_of[stage][iw + 32 * t] : nullptr) >> (4 * h);
+                    const uint32_t w = sight.word(p0, docs && !at.same ? &doc_of[stage][iw + 32 * t] : nullptr) >> (4 * h);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         z[r] = word_bit(w, r) ? z[r] : 0.f;
@@ -388,7 +403,7 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
 #pragma unroll
             for (int t = 0; t < WQ / 32; ++t) {
                 const uint32_t w =
-                    sight.word(at.tile * BQ + iw + 32 * t + shift, docs ? &doc_of[stage][iw + 32 * t] : nullptr);
+                    sight.word(at.tile * BQ + iw + 32 * t + shift, docs && !at.same ? &doc_of[stage][iw + 32 * t] : nullptr);
                 spoilt = spoilt || (at.any && ((at.all ? ~0u : w) & pick<BQ / 32>(bq, NARROW ? wave : t)));
             }
             Lds::template clean<BQ, NW * 64>(smem[stage][0]);
@@ -498,7 +513,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
     }
 
     // the visited tiles of all query heads, in order
-    struct At { int tile, head; bool part, any, all; };
+    struct At { int tile, head; bool part, any, all, same; };
     Schedule sched;
     int gh = first;
     auto advance = [&]() __attribute__((always_inline)) {
@@ -507,7 +522,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
             sched = Schedule();
             t = sched.next(end, see);
         }
-        return At{t, gh, sched.part, sched.wave_any, sched.wave_all};
+        return At{t, gh, sched.part, sched.wave_any, sched.wave_all, sched.wave_same};
     };
     auto fetch = [&](int st, const At &at) __attribute__((always_inline)) {
         const int hq = hk * group + at.head, i0 = at.tile * BQ;
@@ -530,22 +545,38 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
 #pragma unroll
         for (int t = 0; t < BQ / 32; ++t) {
             const uint32_t w =
-                at.all ? ~0u : sight.word(at.tile * BQ + 32 * t + shift, docs ? &doc_of[stage][32 * t] : nullptr);
+                at.all ? ~0u : sight.word(at.tile * BQ + 32 * t + shift, docs && !at.same ? &doc_of[stage][32 * t] : nullptr);
             spoilt = spoilt || (at.any && (w & (bq[t] | bg[t])));
         }
         Lds::template clean<BQ, NW * 64>(smem[stage][0]);
         Lds::template clean<BQ, NW * 64>(smem[stage][1]);
     };
 
+    // Both waves' steps of 32 queries are KS products with rows of one operand and 2 DS with
+    // columns of the other; reads are kAhead products ahead, as in the forward kernel.
+    constexpr int kStep = KS + 2 * DS, kAhead = 6;
+    auto read_pair = [&](auto ic, Frag<T> *ring, uint32_t row, uint32_t column) __attribute__((always_inline)) {
+        constexpr int i = decltype(ic)::value, t = i / kStep, x = i % kStep, y = x - KS;
+        if constexpr (i >= BQ / 32 * kStep) return;
+        else if constexpr (x < KS) ring[i % kAhead] = Lds::row_frag(row, t, x);
+        else ring[i % kAhead] = Lds::column_frag(column, 32 * t + 16 * (y / DS), y % DS);
+    };
     // The first wave on a tile: P, and its product with dO
     auto probabilities = [&](v16f *acc, int stage, int parity, const At &at) __attribute__((always_inline)) {
         const uint32_t qr = Lds::row_base(smem[stage][0], lane), gc = Lds::column_base(smem[stage][1], lane);
         const ScoreMap sm = score_map(m, hk * group + at.head);
-#pragma unroll
-        for (int t = 0; t < BQ / 32; ++t) {
+        Frag<T> ring[kAhead];
+        auto read = [&](auto ic) __attribute__((always_inline)) { read_pair(ic, ring, qr, gc); };
+        unroll<kAhead>(read);
+        unroll<BQ / 32>([&](auto tc) __attribute__((always_inline)) {
+            constexpr int t = decltype(tc)::value;
             v16f z = {};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) z = mma(Lds::row_frag(qr, t, ks), f[ks], z);
+            unroll<KS>([&](auto xc) __attribute__((always_inline)) {
+                constexpr int x = decltype(xc)::value, i = t * kStep + x;
+                z = mma(ring[i % kAhead], f[x], z);
+                read(std::integral_constant<int, i + kAhead>{});
+                pin();
+            });
             const int p0 = at.tile * BQ + 32 * t + shift;
             const float d0 = BIAS ? (float)(p0 + 4 * h) - (float)j : 0.f;
             v16f pu;
@@ -566,30 +597,41 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
                 }
             }
             if (!at.all) {
-                const uint32_t w = sight.word(p0, docs ? &doc_of[stage][32 * t] : nullptr) >> (4 * h);
+                const uint32_t w = sight.word(p0, docs && !at.same ? &doc_of[stage][32 * t] : nullptr) >> (4 * h);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     z[r] = word_bit(w, r) ? z[r] : 0.f;
                     if constexpr (CAP) pu[r] = word_bit(w, r) ? pu[r] : 0.f;
                 }
             }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const Frag<T> pf = to_frag<T>(z, s);
-                shared_p[parity][keys][t][s][lane] = __builtin_bit_cast(u4v, CAP ? to_frag<T>(pu, s) : pf);
-#pragma unroll
-                for (int dt = 0; dt < DS; ++dt) acc[dt] = mma(Lds::column_frag(gc, 32 * t + 16 * s, dt), pf, acc[dt]);
-            }
-        }
+            Frag<T> pf;
+            unroll<2 * DS>([&](auto yc) __attribute__((always_inline)) {
+                constexpr int y = decltype(yc)::value, i = t * kStep + KS + y, s = y / DS;
+                if constexpr (y % DS == 0) {
+                    pf = to_frag<T>(z, s);
+                    shared_p[parity][keys][t][s][lane] = __builtin_bit_cast(u4v, CAP ? to_frag<T>(pu, s) : pf);
+                }
+                acc[y % DS] = mma(ring[i % kAhead], pf, acc[y % DS]);
+                read(std::integral_constant<int, i + kAhead>{});
+                pin();
+            });
+        });
     };
     // The second wave on the tile before: dS, and its product with Q
     auto gradients = [&](v16f *acc, int stage, int parity, const At &at) __attribute__((always_inline)) {
         const uint32_t gr = Lds::row_base(smem[stage][1], lane), qc = Lds::column_base(smem[stage][0], lane);
-#pragma unroll
-        for (int t = 0; t < BQ / 32; ++t) {
+        Frag<T> ring[kAhead];
+        auto read = [&](auto ic) __attribute__((always_inline)) { read_pair(ic, ring, gr, qc); };
+        unroll<kAhead>(read);
+        unroll<BQ / 32>([&](auto tc) __attribute__((always_inline)) {
+            constexpr int t = decltype(tc)::value;
             v16f e = {};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(gr, t, ks), f[ks], e);
+            unroll<KS>([&](auto xc) __attribute__((always_inline)) {
+                constexpr int x = decltype(xc)::value, i = t * kStep + x;
+                e = mma(ring[i % kAhead], f[x], e);
+                read(std::integral_constant<int, i + kAhead>{});
+                pin();
+            });
             u4v pw[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s) pw[s] = shared_p[parity][keys][t][s][lane];
@@ -608,20 +650,22 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
 #pragma unroll
                 for (int r = 0; r < 16; ++r) e[r] = p_of(r) != 0.f ? e[r] : 0.f;
             }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const Frag<T> ef = to_frag<T>(e, s);
-#pragma unroll
-                for (int dt = 0; dt < DS; ++dt) acc[dt] = mma(Lds::column_frag(qc, 32 * t + 16 * s, dt), ef, acc[dt]);
-            }
-        }
+            Frag<T> ef;
+            unroll<2 * DS>([&](auto yc) __attribute__((always_inline)) {
+                constexpr int y = decltype(yc)::value, i = t * kStep + KS + y;
+                if constexpr (y % DS == 0) ef = to_frag<T>(e, y / DS);
+                acc[y % DS] = mma(ring[i % kAhead], ef, acc[y % DS]);
+                read(std::integral_constant<int, i + kAhead>{});
+                pin();
+            });
+        });
     };
 
     // (a loop for each of the two: they share nothing but the barriers)
     auto run = [&](auto second) __attribute__((always_inline)) {
         constexpr bool SECOND = decltype(second)::value;
         v16f acc[DS] = {};                               // dV, or dK
-        At cur = advance(), before = {-1, 0, false, false, false};
+        At cur = advance(), before = {-1, 0, false, false, false, false};
         int stage = 0, parity = 0;
         if (cur.tile >= 0) fetch(0, cur);
         while (cur.tile >= 0 || before.tile >= 0) {

@@ -540,21 +540,31 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const CachedArgs a)
     const int64_t i = (int64_t)rt * ROWS + r;
     if (i >= (int64_t)s.n * group) return;
     const int64_t at = (tile * a.cache.heads + head) * a.splits * ROWS + r;
-    float most = -INFINITY;
-    for (int k = lane; k < a.splits; k += 64) most = fmaxf(most, a.stat[2 * (at + (int64_t)k * ROWS)]);
+    // lane k: split k's maximum and sum (there are at most kMaxSplits)
+    float l = 0.f, y = -INFINITY;
+    if (lane < a.splits) {
+        const v2f x = *reinterpret_cast<const v2f *>(a.stat + 2 * (at + (int64_t)lane * ROWS));
+        y = x[0];
+        l = x[1];
+    }
+    float most = y;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
-    float total = 0.f, x0 = 0.f, x1 = 0.f;
-    for (int k = 0; k < a.splits; ++k) {
-        const int64_t e = at + (int64_t)k * ROWS;
-        const float l = a.stat[2 * e + 1], y = a.stat[2 * e];
-        if (l == 0.f) continue;
-        const float f = y == most ? 1.f : __builtin_amdgcn_exp2f(y - most);
-        total += l * f;
-        if (2 * lane < D) {
-            const v2f v = *reinterpret_cast<const v2f *>(a.part + e * D + 2 * lane);
-            x0 += v[0] * f;
-            x1 += v[1] * f;
+    const float f = l == 0.f ? 0.f : y == most ? 1.f : __builtin_amdgcn_exp2f(y - most);
+    float total = l * f, x0 = 0.f, x1 = 0.f;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+    const float *p = a.part + at * D + min(2 * lane, D - 2);
+    // (a split without tokens has sums of 0, lanes past the last split a weight of 0)
+    for (int k = 0; k < a.splits; k += 8) {
+        v2f v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const v2f *>(p + (int64_t)min(k + i, a.splits - 1) * ROWS * D);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float g = bits_f(__builtin_amdgcn_readlane(f_bits(f), k + i));
+            x0 += v[i][0] * g;
+            x1 += v[i][1] * g;
         }
     }
     if (2 * lane >= D) return;

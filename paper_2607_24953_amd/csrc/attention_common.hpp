@@ -343,8 +343,8 @@ __device__ __forceinline__ void add_non_finite(v16f *acc, uint32_t seen, uint32_
 // ---------------------------------------------------------------- masks
 
 // What the masks leave between query positions [p0, p1] and keys [j0, j1]: nothing, some
-// or all pairs.
-struct Seen { bool any, all; };
+// or all pairs; same: all are of one document.
+struct Seen { bool any, all, same; };
 
 // Range of the document numbers of some positions, and whether there is padding among them
 // (negative numbers, which the range leaves out).  In memory: {lo, or ~lo with padding; hi}.
@@ -356,7 +356,7 @@ struct Documents {
 __device__ __forceinline__ Seen classify(const AttentionMask &m, int prefix, int p0, int p1, int j0, int j1,
                                          const Documents &q, const Documents &k)
 {
-    bool any = true, all = true;
+    bool any = true, all = true, same = true;
     if (m.causal) {
         any = j0 <= p1;
         all = j1 <= p0;
@@ -373,26 +373,27 @@ __device__ __forceinline__ Seen classify(const AttentionMask &m, int prefix, int
     all = all || j1 < prefix;
     if (m.documents) {
         any = any && q.lo <= k.hi && k.lo <= q.hi;
-        all = all && q.lo == q.hi && k.lo == k.hi && q.lo == k.lo && !q.padding && !k.padding;
+        same = q.lo == q.hi && k.lo == k.hi && q.lo == k.lo && !q.padding && !k.padding;
+        all = all && same;
     }
-    return {any, all && any};
+    return {any, all && any, same};
 }
 
 // A visited tile (-1: none): whether some pair of the workgroup is masked, whether this wave
-// sees some and all pairs
+// sees some and all pairs, and whether its pairs are of one document
 struct Visit {
     int tile;
-    bool part, any, all;
+    bool part, any, all, same;
 };
 
 // Tiles of one loop axis that a workgroup visits, 64 at a time: lane t classifies tile
 // base + t, and ballots hold what the workgroup and this wave see of them.
 struct Schedule {
-    uint64_t visit = 0, whole = 0, any = 0, all = 0;
+    uint64_t visit = 0, whole = 0, any = 0, all = 0, same = 0;
     int base = -64;
     // of the tile that next() gave: whether some pair of the workgroup is masked, whether this
     // wave sees some and all pairs
-    bool part = false, wave_any = false, wave_all = false;
+    bool part = false, wave_any = false, wave_all = false, wave_same = false;
 
 
     // next visited tile below `end`, or -1 (the same in all waves); f(tile) -> {of the
@@ -404,31 +405,40 @@ struct Schedule {
             base += 64;
             if (base >= end) return -1;
             const int t = base + (threadIdx.x & 63);
-            Seen g = {false, false}, w = {false, false};
+            Seen g = {}, w = {};
             if (t < end) f(t, g, w);
             visit = __ballot(g.any);
             whole = __ballot(g.all);
             any = __ballot(w.any);
             all = __ballot(w.all);
+            same = __ballot(w.same);
         }
         const int b = __builtin_ctzll(visit);
         visit &= visit - 1;
         part = !((whole >> b) & 1);
         wave_any = (any >> b) & 1;
         wave_all = (all >> b) & 1;
+        wave_same = (same >> b) & 1;
         return base + b;
     }
     template <typename F>
     __device__ __forceinline__ Visit take(int end, F &&f)
     {
         const int t = next(end, f);
-        return {t, part, wave_any, wave_all};
+        return {t, part, wave_any, wave_all, wave_same};
     }
 };
 
 // LDS stages of a tile loop for tiles of so many bytes (both operands): three where they leave
 // room for two workgroups a compute unit, two, or one
 constexpr int stages_of(int bytes) { return 3 * bytes <= 49152 ? 3 : 2 * bytes <= 131072 ? 2 : 1; }
+
+// Keeps the order of the instructions before and after it
+template <bool ON = true>
+__device__ __forceinline__ void pin()
+{
+    if constexpr (ON) __builtin_amdgcn_sched_barrier(0);
+}
 
 // The loop over a workgroup's tiles: body(visit, stage) on each visited one, with fetch(stage,
 // tile) two tiles ahead where there are three stages, one ahead with two, and after use with
