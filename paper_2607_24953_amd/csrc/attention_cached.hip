@@ -415,11 +415,23 @@ __global__ __launch_bounds__(256, 2) void attention_cached_rows_kernel(const Cac
         const int krow = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
         const uint32_t kr = Lds::fresh(Lds::address(ktile[stage]) + Lds::offset(krow, h));
         const uint32_t vr = Lds::fresh(Lds::address(vtile[stage]) + col * (kSuper * 2) + ((h ^ ((col >> 1) & 7)) << 4));
+        // (reads ahead of the products as in the forward kernel)
+        constexpr int kScores = 2 * KS, kValues = 4 * DS, kAhead = DC <= 64 ? 1 : 6;
+        bf16x8 ring[kAhead];
+        auto read = [&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value, y = i - kScores;
+            if constexpr (i < kScores) ring[i % kAhead] = Lds::row_frag(kr, i % 2, i / 2);
+            else if constexpr (y < kValues)
+                ring[i % kAhead] = *Lds::template lds_ptr<bf16x8>((vr ^ (uint32_t)(2 * (y / DS) << 4)) + y % DS * 32 * kSuper * 2);
+        };
         v16f z[2] = {};
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) z[t] = mma(Lds::row_frag(kr, t, ks), qf[ks], z[t]);
+        unroll<kAhead>(read);
+        unroll<kScores>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value;
+            z[i % 2] = mma(ring[i % kAhead], qf[i / 2], z[i % 2]);
+            read(std::integral_constant<int, i + kAhead>{});
+            pin<(DC > 64)>();
+        });
         // token of register i: 16 (i / 8) + 8 h + i % 8
         if constexpr (CAP || BIAS) {
             const float d0 = (float)(pos - j0 - 8 * h);
@@ -475,16 +487,14 @@ __global__ __launch_bounds__(256, 2) void attention_cached_rows_kernel(const Cac
                 for (int i = 0; i < 16; ++i) z[t][i] = z[t][i] != 0.f ? __builtin_nanf("") : 0.f;
             }
         }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const bf16x8 pf = to_frag<__bf16>(z[t], k);
-#pragma unroll
-                for (int dt = 0; dt < DS; ++dt)
-                    o[dt] = mma(*Lds::template lds_ptr<bf16x8>((vr ^ (uint32_t)((4 * t + 2 * k) << 4)) + dt * 32 * kSuper * 2),
-                                pf, o[dt]);
-            }
+        bf16x8 pf;
+        unroll<kValues>([&](auto yc) __attribute__((always_inline)) {
+            constexpr int y = decltype(yc)::value, i = kScores + y;
+            if constexpr (y % DS == 0) pf = to_frag<__bf16>(z[y / (2 * DS)], y / DS % 2);
+            o[y % DS] = mma(ring[i % kAhead], pf, o[y % DS]);
+            read(std::integral_constant<int, i + kAhead>{});
+            pin<(DC > 64)>();
+        });
     };
 
     Blocks now = blocks_of(w.from), next = blocks_of(w.from + 1);

@@ -78,12 +78,13 @@ struct Unit {
 __device__ __forceinline__ bool take_unit(const CacheCopyArgs &a, Unit &u)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // blockIdx.x: touched block; the heads' keys and values over blockIdx.y and the waves
-    const int part = blockIdx.y * 4 + wave;
+    // neighbouring workgroups take the heads of one block: a token's heads lie side by side
+    const uint32_t parts = (2 * a.cache.heads + 3) / 4;
+    const int part = blockIdx.x % parts * 4 + wave;
     if (part >= 2 * a.cache.heads) return false;
     Span s;
     int i;
-    const int b = find_unit(a.seq, a.cache.page_blocks * kBlockTokens, blockIdx.x, touched, s, i);
+    const int b = find_unit(a.seq, a.cache.page_blocks * kBlockTokens, blockIdx.x / parts, touched, s, i);
     if (b < 0) return false;
     const int n = min(s.n, s.len), first = s.len - n, block = first / kBlockTokens + i;
     u.head = part >> 1;
@@ -208,8 +209,8 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const CacheCopyArgs a)
         if (s0 + i >= u.lo && s0 + i < u.hi) store8(x + (u.row0 + s0 + i) * st, e[i]);
 }
 
-// a sequence's n tokens lie in at most (n + 30) / 32 + 1 blocks
-bool grid_of(const CacheCopyArgs &a, dim3 &grid)
+// workgroups: a sequence's n tokens lie in at most (n + 30) / 32 + 1 blocks
+int64_t grid_of(const CacheCopyArgs &a)
 {
     int64_t blocks;
     if (a.seq.offsets) {
@@ -220,29 +221,28 @@ bool grid_of(const CacheCopyArgs &a, dim3 &grid)
         const int64_t n = a.seq.tokens / a.seq.batch;
         blocks = n == 0 ? 0 : a.seq.batch * ((n + 30) / kBlockTokens + 1);
     }
-    grid = dim3((uint32_t)blocks, (2 * a.cache.heads + 3) / 4);
-    return blocks <= INT32_MAX;
+    return blocks * ((2 * a.cache.heads + 3) / 4);
 }
 
 }  // namespace
 
 hipError_t launch_kv_write(const CacheCopyArgs &a, bool f32, hipStream_t stream)
 {
-    dim3 grid;
-    if (!grid_of(a, grid)) return hipErrorInvalidConfiguration;
-    if (grid.x == 0) return hipSuccess;
-    if (f32) kv_write_kernel<float><<<grid, 256, 0, stream>>>(a);
-    else kv_write_kernel<__bf16><<<grid, 256, 0, stream>>>(a);
+    const int64_t grid = grid_of(a);
+    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (grid == 0) return hipSuccess;
+    if (f32) kv_write_kernel<float><<<(uint32_t)grid, 256, 0, stream>>>(a);
+    else kv_write_kernel<__bf16><<<(uint32_t)grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const CacheCopyArgs &a, bool f32, hipStream_t stream)
 {
-    dim3 grid;
-    if (!grid_of(a, grid)) return hipErrorInvalidConfiguration;
-    if (grid.x == 0) return hipSuccess;
-    if (f32) kv_read_kernel<float><<<grid, 256, 0, stream>>>(a);
-    else kv_read_kernel<__bf16><<<grid, 256, 0, stream>>>(a);
+    const int64_t grid = grid_of(a);
+    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (grid == 0) return hipSuccess;
+    if (f32) kv_read_kernel<float><<<(uint32_t)grid, 256, 0, stream>>>(a);
+    else kv_read_kernel<__bf16><<<(uint32_t)grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
