@@ -94,11 +94,11 @@ struct CachedArgs {
     int64_t q_st, q_sh, out_st, out_sh;
     AttentionMask mask;
     int32_t heads_q;
-    int32_t splits;                              // parts of a sequence's tokens
+    int32_t units;                               // work units a head to cut long sequences for, 0: do not
     int32_t wide;                                // 128 query rows a workgroup, not 16
     int64_t tiles;                               // bound of the query tiles of all sequences
-    float *part;                                 // workspace: [tile][head][split][rows][dim] sums,
-    float *stat;                                 // [tile][head][split][rows] maximum and sum
+    float *part;                                 // workspace: [unit][head][rows][dim] sums,
+    float *stat;                                 // [unit][head][rows] maximum and sum
 };
 
 constexpr int kMaxSplits = 64;                   // parts of a sequence's tokens: a lane each in the join

@@ -178,13 +178,13 @@ SequencesView sequences_view(const q2d_sequences *s)
 }
 
 struct CachedSplit {
-    int32_t splits, wide;
+    int32_t units, wide;
     int64_t tiles, stat_at, bytes;
 };
 
 // Query tiles of 16 rows where the sequences have no more on average (decoding), of 128
-// otherwise; and enough parts of the sequences' tokens to give each compute unit a few
-// workgroups, none below four super-blocks of 64 tokens, one a wave.
+// otherwise.  Sequences' tokens are cut into parts where the tiles alone would leave compute
+// units short of four workgroups.
 CachedSplit split_cached(const q2d_kv_cache *c, const q2d_sequences *s, int32_t heads_q)
 {
     CachedSplit p;
@@ -198,12 +198,11 @@ CachedSplit split_cached(const q2d_kv_cache *c, const q2d_sequences *s, int32_t 
     } else {
         p.tiles = s->batch * ((s->tokens / s->batch * group + rows - 1) / rows);
     }
-    const int64_t units = p.tiles * c->heads, longest = (int64_t)s->table_pages * c->page_size;
-    int64_t n = units > 0 ? (1024 + units - 1) / units : 1;
-    if (n > (longest + 255) / 256) n = (longest + 255) / 256;
-    if (n > kMaxSplits) n = kMaxSplits;
-    p.splits = (int32_t)(n < 1 ? 1 : n);
-    const int64_t parts = p.splits > 1 ? units * p.splits * rows : 0;
+    // (never for tables that hold less than two parts)
+    const int64_t longest = (int64_t)s->table_pages * c->page_size, least = p.wide ? 1024 : 512;
+    const int64_t want = (4 * kComputeUnits + c->heads - 1) / c->heads;
+    p.units = (int32_t)(p.tiles < want && longest >= least ? want : 0);
+    const int64_t parts = p.units > 0 ? (p.tiles + p.units) * c->heads * rows : 0;
     p.stat_at = up256(parts * c->dim * 4);
     p.bytes = p.stat_at + up256(parts * 8);
     return p;
@@ -336,7 +335,7 @@ q2d_status q2d_attention_cached(const q2d_kv_cache *c, const q2d_sequences *s, c
     g.mask.scale = a->scale; g.mask.cap = a->softcap;
     g.mask.slopes = a->slopes; g.mask.prefix = a->prefix;
     g.heads_q = a->heads_q;
-    g.splits = p.splits; g.wide = p.wide; g.tiles = p.tiles;
+    g.units = p.units; g.wide = p.wide; g.tiles = p.tiles;
     g.part = reinterpret_cast<float *>(workspace);
     g.stat = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + p.stat_at);
     if (launch_attention_cached(g, stream) != hipSuccess) return Q2D_ELAUNCH;

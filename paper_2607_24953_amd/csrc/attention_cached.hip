@@ -76,27 +76,96 @@ __device__ __forceinline__ void fetch(const CachedArgs &a, const Where &w, int l
     c.vs = w.value >= 0 ? a.cache.vs[w.value] : kNoBlock;
 }
 
-// Where a workgroup of either kernel works: tile of ROWS query rows of a sequence that share key
-// head `head`, and its part of the super-blocks, [from, to)
+// Work is handed out per key head in units: a tile of ROWS query rows of a sequence (row r of it
+// is token r / group, query head r % group) and one of `parts` equal shares of the super-blocks
+// that the tile sees.  A sequence's tiles have as many parts as its length asks for, so that
+// long and short sequences of a call end together: with W super-blocks to visit over all tiles,
+// a part has about W / a.units of them, and at least kLeast.
+template <int ROWS>
+constexpr int kLeast = ROWS == 16 ? 4 : 8;
+
 struct Place {
-    int b, rt, head, split, rows, prefix, p0, p1, from, to;
-    int64_t tile;
+    int b, rt, head, part, parts, rows, prefix, p0, p1, from, to;
+    int64_t unit;                  // number of the unit (BY_TILE: of the tile's first)
     Span s;
 };
 
-// false: no such tile.  (ROWS: row r of the tile is token r / group, head r % group.)
+// Unit (BY_TILE: tile) `index` of a head; false: past the last.  One full wave, the same in all lanes.
+template <int ROWS, bool BY_TILE>
+__device__ __forceinline__ bool find_place(const CachedArgs &a, int group, int64_t index, Place &w)
+{
+    const AttentionMask &m = a.mask;
+    const SequencesView &q = a.seq;
+    const int lane = threadIdx.x & 63, page = a.cache.page_blocks * kBlockTokens;
+    auto tiles_of = [&](const Span &x) { return (int)(((int64_t)x.n * group + ROWS - 1) / ROWS); };
+    auto blocks_of = [&](const Span &x) {
+        const int64_t seen = m.window && !m.prefix ? min((int64_t)x.len, (int64_t)m.window + ROWS) : x.len;
+        return (int)((seen + kSuper - 1) / kSuper);
+    };
+    // (the first 64 sequences' spans stay in registers over the two passes)
+    Span first = {0, 0, 0};
+    if (lane < q.batch) first = span_of(q, page, lane);
+    int64_t share = INT32_MAX;
+    if (a.units > 0) {
+        int64_t work = (int64_t)tiles_of(first) * blocks_of(first);
+        for (int b = 64 + lane; b < q.batch; b += 64) {
+            const Span x = span_of(q, page, b);
+            work += (int64_t)tiles_of(x) * blocks_of(x);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
+        share = max((work + a.units - 1) / a.units, (int64_t)kLeast<ROWS>);
+    }
+    int64_t carry = 0, units = 0;
+    for (int base = 0; base < q.batch; base += 64) {
+        const int b = base + lane;
+        Span x = first;
+        if (base > 0) {
+            x = {0, 0, 0};
+            if (b < q.batch) x = span_of(q, page, b);
+        }
+        const int tiles = tiles_of(x);
+        const int parts = (int)min(max((blocks_of(x) + share - 1) / share, (int64_t)1), (int64_t)kMaxSplits);
+        const int64_t all = (int64_t)tiles * parts, count = BY_TILE ? tiles : all;
+        int64_t upto = count, units_upto = all;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t below = __shfl_up(upto, d);
+            if (lane >= d) upto += below;
+            if constexpr (BY_TILE) {
+                const int64_t y = __shfl_up(units_upto, d);
+                if (lane >= d) units_upto += y;
+            }
+        }
+        const uint64_t past = __ballot(carry + upto > index);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            w.b = base + at;
+            w.s.n = __builtin_amdgcn_readlane(x.n, at);
+            w.s.len = __builtin_amdgcn_readlane(x.len, at);
+            w.s.tok0 = (int64_t)uniform64(__shfl((uint64_t)x.tok0, at));
+            w.parts = __builtin_amdgcn_readlane(parts, at);
+            const int local = __builtin_amdgcn_readfirstlane((int)(index - carry - __shfl(upto - count, at)));
+            w.rt = BY_TILE ? local : local / w.parts;
+            w.part = BY_TILE ? 0 : local % w.parts;
+            w.unit = index;
+            if (BY_TILE) w.unit = (int64_t)uniform64((uint64_t)(units + __shfl(units_upto - all, at))) + (int64_t)w.rt * w.parts;
+            w.rows = min(ROWS, (int)((int64_t)w.s.n * group - (int64_t)w.rt * ROWS));
+            return true;
+        }
+        carry += __shfl(upto, 63);
+        if constexpr (BY_TILE) units += __shfl(units_upto, 63);
+    }
+    return false;
+}
+
+// The unit of this workgroup, and its super-blocks [from, to)
 template <int ROWS>
 __device__ __forceinline__ bool place_of(const CachedArgs &a, int group, Place &w)
 {
     const AttentionMask &m = a.mask;
-    w.split = blockIdx.x % a.splits;
-    const int64_t rest = blockIdx.x / a.splits;
-    w.head = (int)(rest % a.cache.heads);
-    w.tile = rest / a.cache.heads;
-    w.b = find_unit(a.seq, a.cache.page_blocks * kBlockTokens, w.tile,
-                    [&](const Span &x) { return (int)(((int64_t)x.n * group + ROWS - 1) / ROWS); }, w.s, w.rt);
-    if (w.b < 0) return false;
-    w.rows = min(ROWS, (int)((int64_t)w.s.n * group - (int64_t)w.rt * ROWS));
+    if (!find_place<ROWS, false>(a, group, blockIdx.x / a.cache.heads, w)) return false;
+    w.head = blockIdx.x % a.cache.heads;
     w.prefix = m.prefix ? min(max(m.prefix[w.b], 0), w.s.len) : 0;
     w.p0 = w.s.len - w.s.n + w.rt * ROWS / group;
     w.p1 = w.s.len - w.s.n + (w.rt * ROWS + w.rows - 1) / group;
@@ -104,8 +173,8 @@ __device__ __forceinline__ bool place_of(const CachedArgs &a, int group, Place &
     int t1 = max(min(w.p1 + 1, w.s.len), w.prefix), t0 = m.window && !w.prefix ? max(w.p0 - m.window + 1, 0) : 0;
     if (t1 < t0) t1 = t0;
     const int sb0 = t0 / kSuper, sbs = (t1 + kSuper - 1) / kSuper - sb0;
-    w.from = sb0 + (int)((int64_t)sbs * w.split / a.splits);
-    w.to = sb0 + (int)((int64_t)sbs * (w.split + 1) / a.splits);
+    w.from = sb0 + (int)((int64_t)sbs * w.part / w.parts);
+    w.to = sb0 + (int)((int64_t)sbs * (w.part + 1) / w.parts);
     return true;
 }
 
@@ -282,14 +351,14 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
     __syncthreads();
     if (wave != 0 || !row) return;
     add(osum[0]);
-    if (a.splits == 1) {
+    if (w.parts == 1) {
         const float inv = total == 0.f ? 0.f : 1.f / total;
         __bf16 *out = (__bf16 *)a.out + (s.tok0 + tok) * a.out_st + hq * a.out_sh;
 #pragma unroll
         for (int t = 0; t < VT; ++t)
             if (16 * t < D) store4(out + 16 * t + 4 * g, o[t][0] * inv, o[t][1] * inv, o[t][2] * inv, o[t][3] * inv);
     } else {
-        const int64_t at = ((w.tile * a.cache.heads + w.head) * a.splits + w.split) * ROWS + col;
+        const int64_t at = (w.unit * a.cache.heads + w.head) * ROWS + col;
 #pragma unroll
         for (int t = 0; t < VT; ++t)
             if (16 * t < D) *reinterpret_cast<v4f *>(a.part + at * D + 16 * t + 4 * g) = o[t];
@@ -520,11 +589,11 @@ __global__ __launch_bounds__(256, 2) void attention_cached_rows_kernel(const Cac
 
     sum += __shfl_xor(sum, 32);
     if (!row) return;
-    if (a.splits == 1) {
+    if (w.parts == 1) {
         __bf16 *out = (__bf16 *)a.out + (s.tok0 + tok) * a.out_st + hq * a.out_sh;
         store_columns<__bf16, DS>(out, o, sum == 0.f ? 0.f : 1.f / sum, h, D);
     } else {
-        const int64_t at = ((w.tile * a.cache.heads + w.head) * a.splits + w.split) * ROWS + c;
+        const int64_t at = (w.unit * a.cache.heads + w.head) * ROWS + c;
         store_columns<float, DS>(a.part + at * D, o, 1.f, h, D);
         if (h == 0) {
             a.stat[2 * at] = mx * sm.c;
@@ -533,27 +602,23 @@ __global__ __launch_bounds__(256, 2) void attention_cached_rows_kernel(const Cac
     }
 }
 
-// Joins the splits of a query row: one wave a row, two dims a lane
+// Joins the parts of a tile's query rows: one wave a row, two dims a lane
 template <int ROWS>
 __global__ __launch_bounds__(256) void attention_join_kernel(const CachedArgs a)
 {
     const int group = a.heads_q / a.cache.heads, D = a.cache.dim, lane = threadIdx.x & 63;
-    const int r = (blockIdx.x % (ROWS / 4)) * 4 + (threadIdx.x >> 6);
+    const int r = blockIdx.x % (ROWS / 4) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t rest = blockIdx.x / (ROWS / 4);
     const int head = (int)(rest % a.cache.heads);
-    const int64_t tile = rest / a.cache.heads;
-    Span s;
-    int rt;
-    const int b = find_unit(a.seq, a.cache.page_blocks * kBlockTokens, tile,
-                            [&](const Span &x) { return (int)(((int64_t)x.n * group + ROWS - 1) / ROWS); }, s, rt);
-    if (b < 0) return;
-    const int64_t i = (int64_t)rt * ROWS + r;
-    if (i >= (int64_t)s.n * group) return;
-    const int64_t at = (tile * a.cache.heads + head) * a.splits * ROWS + r;
-    // lane k: split k's maximum and sum (there are at most kMaxSplits)
+    Place w;
+    if (!find_place<ROWS, true>(a, group, rest / a.cache.heads, w) || w.parts == 1 || r >= w.rows) return;
+    // (the host's bound, which offsets that do not ascend could pass)
+    if (w.unit + w.parts > a.tiles + a.units) return;
+    const int64_t step = (int64_t)a.cache.heads * ROWS, at = (w.unit * a.cache.heads + head) * ROWS + r;
+    // lane k: part k's maximum and sum (there are at most kMaxSplits)
     float l = 0.f, y = -INFINITY;
-    if (lane < a.splits) {
-        const v2f x = *reinterpret_cast<const v2f *>(a.stat + 2 * (at + (int64_t)lane * ROWS));
+    if (lane < w.parts) {
+        const v2f x = *reinterpret_cast<const v2f *>(a.stat + 2 * (at + lane * step));
         y = x[0];
         l = x[1];
     }
@@ -565,11 +630,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const CachedArgs a)
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
     const float *p = a.part + at * D + min(2 * lane, D - 2);
-    // (a split without tokens has sums of 0, lanes past the last split a weight of 0)
-    for (int k = 0; k < a.splits; k += 8) {
+    // (a part without tokens has sums of 0, lanes past the last part a weight of 0)
+    for (int k = 0; k < w.parts; k += 8) {
         v2f v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const v2f *>(p + (int64_t)min(k + i, a.splits - 1) * ROWS * D);
+        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const v2f *>(p + min(k + i, w.parts - 1) * step * D);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float g = bits_f(__builtin_amdgcn_readlane(f_bits(f), k + i));
@@ -579,7 +644,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const CachedArgs a)
     }
     if (2 * lane >= D) return;
     const float inv = total == 0.f ? 0.f : 1.f / total;
-    __bf16 *out = (__bf16 *)a.out + (s.tok0 + i / group) * a.out_st + (head * group + (int)(i % group)) * a.out_sh;
+    const int64_t i = (int64_t)w.rt * ROWS + r;
+    __bf16 *out = (__bf16 *)a.out + (w.s.tok0 + i / group) * a.out_st + (head * group + (int)(i % group)) * a.out_sh;
     *reinterpret_cast<bf16x2v *>(out + 2 * lane) = bf16x2v{(__bf16)(x0 * inv), (__bf16)(x1 * inv)};
 }
 
@@ -587,11 +653,12 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const CachedArgs a)
 template <int DC, int MODS, int ROWS>
 hipError_t launch(const CachedArgs &a, hipStream_t stream)
 {
-    const int64_t heads = a.tiles * a.cache.heads, n = heads * a.splits;
-    if (n > INT32_MAX || heads * (ROWS / 4) > INT32_MAX) return hipErrorInvalidConfiguration;
+    // (every tile has a unit, and the parts of W / units super-blocks are no more than units)
+    const int64_t tiles = a.tiles * a.cache.heads, n = (a.tiles + a.units) * a.cache.heads;
+    if (n > INT32_MAX || tiles * (ROWS / 4) > INT32_MAX) return hipErrorInvalidConfiguration;
     if constexpr (ROWS == 16) attention_cached_kernel<DC, MODS><<<(uint32_t)n, 256, 0, stream>>>(a);
     else attention_cached_rows_kernel<DC, MODS><<<(uint32_t)n, 256, 0, stream>>>(a);
-    if (a.splits > 1) attention_join_kernel<ROWS><<<(uint32_t)(heads * (ROWS / 4)), 256, 0, stream>>>(a);
+    if (a.units > 0) attention_join_kernel<ROWS><<<(uint32_t)(tiles * (ROWS / 4)), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
