@@ -224,6 +224,8 @@ def _sequences_template(batch, table_pages, tokens, table_stride):
 def _sequences(cache, table, lens, tokens, offsets):
     if not isinstance(cache, KVCache):
         raise Q2DError("expected a KVCache")
+    if cache.device.type != "cuda":
+        _same_device(cache.device)
     if table.dim() != 2 or table.dtype != torch.int32:
         raise Q2DError("block_table: an int32 tensor [sequences, pages] is expected")
     batch, pages = table.shape

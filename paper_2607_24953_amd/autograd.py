@@ -1,4 +1,4 @@
-"""PyTorch autograd form of the quantized linear layer (Sec. 3; App. C, App. E).
+"""PyTorch autograd forms: the quantized linear layer (Sec. 3; App. C, App. E) and attention.
 
 ``Q2DLinear`` is a bias-free linear layer y = x W^T whose forward and backward
 GEMMs run on quantized operands through ``q2d_linear_fwd`` / ``q2d_linear_bwd``:
@@ -21,6 +21,8 @@ layers the same random bits at the same storage indices).  The weight
 bfloat16) before quantization; Y and dX have the input's dtype, dW is computed
 in float32 and cast to the weight's dtype.
 
+``attention`` is q2d_attention_fwd with q2d_attention_bwd as its gradient.
+
 Options mirror the paper's ablations: ``mode_*`` "rtn" / "sr" choose the
 rounding per operand, the "-floor" variants the scale rule that the
 truncation-free ablation goes back to; ``activations="1d"`` quantizes X in 1D
@@ -33,7 +35,8 @@ import math
 
 import torch
 
-from . import FP4_1D, FP4_2D, Q2DError, q2d_linear_bwd, q2d_linear_fwd
+from . import (FP4_1D, FP4_2D, Q2DError, q2d_attention_bwd, q2d_attention_fwd, q2d_linear_bwd,
+               q2d_linear_fwd)
 
 _DTYPES = (torch.float32, torch.bfloat16)
 
@@ -101,3 +104,27 @@ class Q2DLinear(torch.nn.Module):
         return "in=%d, out=%d, x=%s, w=%s, dy=%s, activations=%s, block=%d, seed=%#x" % (
             self.in_features, self.out_features, self.mode_x, self.mode_w, self.mode_dy,
             self.activations, self.block, self.seed)
+
+
+class _AttentionFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, mask):
+        out, lse = q2d_attention_fwd(q, k, v, **mask)
+        ctx.save_for_backward(q, k, v, out, lse)
+        ctx.mask = mask
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        q, k, v, out, lse = ctx.saved_tensors
+        if dout.stride(-1) != 1 or any(s % 8 for s in dout.stride()[:-1]) or dout.data_ptr() % 16:
+            dout = dout.contiguous()
+        dq, dk, dv = q2d_attention_bwd(dout, q, k, v, out, lse, **ctx.mask)
+        return dq, dk, dv, None
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, **mask) -> torch.Tensor:
+    """Attention of q [batch, len_q, heads_q, dim] on k, v [batch, len_k, heads_kv, dim] with
+    gradients for q, k and v; ``mask``: scale, causal, window, softcap, slopes, documents and
+    prefix as in q2d_attention_fwd (slopes get no gradient)."""
+    return _AttentionFunction.apply(q, k, v, mask)

@@ -10,7 +10,7 @@ namespace {
 using namespace q2d;
 
 constexpr int64_t kMaxLen = int64_t(1) << 30;
-constexpr int64_t kMaxPitch = int64_t(1) << 24;    // the tile loads' 32-bit row offsets
+constexpr int64_t kMaxPitch = int64_t(1) << 22;    // the tile loads' 32-bit row offsets
 
 inline bool on16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 inline int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }

@@ -159,7 +159,7 @@ struct Tile {
     }
 
     // Fills ROWS rows from row r0 of a matrix of n rows (base; stride in elements, below
-    // 2^24) and D columns with NT threads, asynchronously (wait_vmcnt).  Rows from n on
+    // 2^22) and D columns with NT threads, asynchronously (wait_vmcnt).  Rows from n on
     // repeat row n - 1; columns from D on keep what the tile holds (clear).
     template <int ROWS, int NT>
     static __device__ __forceinline__ void load(uint8_t *t, const T *base, int64_t stride, int r0, int n, int D)

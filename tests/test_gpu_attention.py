@@ -240,6 +240,22 @@ def test_views_and_streams(q2d):
     check(q2d, q, kb, vb, dout)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_long_strides(q2d, dtype):
+    """Rows 2^22 - 8 elements apart: offsets within a tile of 128 rows pass 2^31 bytes, and those
+    of the whole tensor 2^32."""
+    step, L = 2 ** 22 - 8, 150
+    q, k, v, dout = make(1, L, L, 2, 1, 64, dtype, seed=14)
+    far = torch.empty((L - 1) * step + 2048, dtype=dtype, device="cuda")
+    args = []
+    for i, t in enumerate((q, k, v, dout)):
+        w = far.as_strided(t.shape, (0, step, 64, 1), 256 * i)
+        w.copy_(t)
+        args.append(w)
+    base, got = check(q2d, q, k, v, dout), check(q2d, *args)
+    assert torch.equal(base[0], got[0]) and all(torch.equal(a, b) for a, b in zip(base[2], got[2]))
+
+
 def test_same_results_each_time(q2d):
     args = make(2, 300, 300, 8, 2, 128, torch.bfloat16, seed=10)
     first = check(q2d, *args, softcap=20.0)
