@@ -15,6 +15,11 @@ namespace q2d {
 
 namespace {
 
+// Probabilities and dS are formed times 2^kShift, which the final scaling takes back exactly:
+// where probabilities pass through LDS as float16 (attention_dkv_pair_kernel) all of those that
+// count are then normal numbers, the largest below 2^16.
+constexpr float kShift = 15.f, kUnshift = 1.f / 32768.f;
+
 // delta of 4 rows a wave: 16 lanes a row
 template <typename T>
 __global__ __launch_bounds__(256) void attention_delta_kernel(const AttentionArgs a)
@@ -41,7 +46,7 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(const AttentionArg
     if (l != 0) return;
     const int64_t at = ((int64_t)b * a.heads_q + hq) * a.len_q + i;
     a.delta[at] = s;
-    a.lse2[at] = a.lse[at] * kLog2e;
+    a.lse2[at] = a.lse[at] * kLog2e - kShift;
 }
 
 // Documents of 64 positions at a time (struct Documents)
@@ -224,7 +229,7 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
     }
     if (!row) return;
     T *out = (T *)a.dq.p + b * a.dq.sb + (int64_t)i * a.dq.sl + hq * a.dq.sh;
-    store_columns<T, DS>(out, dq, m.scale, h, D);
+    store_columns<T, DS>(out, dq, m.scale * kUnshift, h, D);
 }
 
 // ---------------------------------------------------------------- dK, dV
@@ -239,7 +244,7 @@ __device__ __forceinline__ void store_dkv(const AttentionArgs &a, bool dv, int s
         return;
     }
     const HeadsView &to = dv ? a.dv : a.dk;
-    store_columns<T, DS>((T *)to.p + b * to.sb + (int64_t)j * to.sl + hk * to.sh, x, dv ? 1.f : a.mask.scale, h, a.dim);
+    store_columns<T, DS>((T *)to.p + b * to.sb + (int64_t)j * to.sl + hk * to.sh, x, dv ? kUnshift : a.mask.scale * kUnshift, h, a.dim);
 }
 
 // Sums the splits' parts in order: 4 neighbouring dims a thread
@@ -258,7 +263,7 @@ __global__ __launch_bounds__(256) void attention_dkv_sum_kernel(const AttentionA
     const int64_t r = x / (a.dim / 4);
     const int hk = (int)(r % a.heads_kv), j = (int)(r / a.heads_kv % a.len_k), b = (int)(r / a.heads_kv / a.len_k);
     const HeadsView &to = dv ? a.dv : a.dk;
-    const float f = dv ? 1.f : a.mask.scale;
+    const float f = dv ? kUnshift : a.mask.scale * kUnshift;
     store4((T *)to.p + b * to.sb + (int64_t)j * to.sl + hk * to.sh + d, sum[0] * f, sum[1] * f, sum[2] * f, sum[3] * f);
 }
 
@@ -442,12 +447,25 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
     store_dkv<T, DS>(a, true, split, b, j, hk, dv, h);
 }
 
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+
+// registers 8 s .. 8 s + 7 of an output tile as float16
+__device__ __forceinline__ u4v to_half(const v16f &x, int s)
+{
+    u4v w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{x[8 * s + 2 * j], x[8 * s + 2 * j + 1]}), half2v));
+    return w;
+}
+
 // The same for bfloat16 with more than 64 dims, where the two accumulators of 32 keys and
 // their K and V fragments take 192 registers: one wave a SIMD could hold them, and would then
 // be bound by issuing one instruction after the other.  So two waves share 32 keys: the first
 // keeps K and dV, forms S and P, and leaves P in LDS; the second keeps V and dK, forms dP and,
-// one tile later, dS.  P passes in the registers' own order (operand fragments), rounded to
-// bfloat16 as the product with dO takes it, and with the cap's derivative multiplied in.
+// one tile later, dS.  P passes in the registers' own order (operand fragments) as float16, with
+// the cap's derivative multiplied in: as bfloat16 its rounding would add to that of dS (dK off by
+// 0.0030 of its norm in place of 0.0024, 0.0017 of it the rounding of dK itself).
 template <int DC, int MODS>
 __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const AttentionArgs a)
 {
@@ -579,7 +597,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
             });
             const int p0 = at.tile * BQ + 32 * t + shift;
             const float d0 = BIAS ? (float)(p0 + 4 * h) - (float)j : 0.f;
-            v16f pu;
+            v16f pu;                                     // P times the cap's derivative
 #pragma unroll
             for (int x4 = 0; x4 < 4; ++x4) {
                 const v4f l4 = *reinterpret_cast<const v4f *>(&rows[stage][0][32 * t + tile_row(4 * x4, h)]);
@@ -609,7 +627,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
                 constexpr int y = decltype(yc)::value, i = t * kStep + KS + y, s = y / DS;
                 if constexpr (y % DS == 0) {
                     pf = to_frag<T>(z, s);
-                    shared_p[parity][keys][t][s][lane] = __builtin_bit_cast(u4v, CAP ? to_frag<T>(pu, s) : pf);
+                    shared_p[parity][keys][t][s][lane] = to_half(CAP ? pu : z, s);
                 }
                 acc[y % DS] = mma(ring[i % kAhead], pf, acc[y % DS]);
                 read(std::integral_constant<int, i + kAhead>{});
@@ -637,7 +655,8 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
             for (int s = 0; s < 2; ++s) pw[s] = shared_p[parity][keys][t][s][lane];
             auto p_of = [&](int r) __attribute__((always_inline)) {
                 const uint32_t w = pw[r / 8][r % 8 / 2];
-                return bits_f(r % 2 ? w & 0xffff0000u : w << 16);
+                const half2v x = __builtin_bit_cast(half2v, w);
+                return (float)(r % 2 ? x[1] : x[0]);
             };
 #pragma unroll
             for (int x4 = 0; x4 < 4; ++x4) {
