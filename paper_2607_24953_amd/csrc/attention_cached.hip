@@ -602,51 +602,64 @@ __global__ __launch_bounds__(256, 2) void attention_cached_rows_kernel(const Cac
     }
 }
 
-// Joins the parts of a tile's query rows: one wave a row, two dims a lane
+// Joins the parts of a tile's query rows: two dims a lane, a wave takes kJoinRows rows of it.
+// Bound by the latency of finding its tile (two scans over the sequences) and of one pass of
+// loads: tiles of 16 rows one row a wave (64 sequences, 2048 rows of 128 dims: 11 us), tiles of
+// 128 rows, where the finding counts more, four (8 unequal prompts, 12644 rows: the whole call
+// 417 us with one, 384 with four, 387 with eight).
+template <int ROWS>
+constexpr int kJoinRows = ROWS == 16 ? 1 : 4;
+
 template <int ROWS>
 __global__ __launch_bounds__(256) void attention_join_kernel(const CachedArgs a)
 {
+    constexpr int kGroups = ROWS / (4 * kJoinRows<ROWS>);
     const int group = a.heads_q / a.cache.heads, D = a.cache.dim, lane = threadIdx.x & 63;
-    const int r = blockIdx.x % (ROWS / 4) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t rest = blockIdx.x / (ROWS / 4);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t rest = blockIdx.x / kGroups;
     const int head = (int)(rest % a.cache.heads);
     Place w;
-    if (!find_place<ROWS, true>(a, group, rest / a.cache.heads, w) || w.parts == 1 || r >= w.rows) return;
+    if (!find_place<ROWS, true>(a, group, rest / a.cache.heads, w) || w.parts == 1) return;
     // (the host's bound, which offsets that do not ascend could pass)
     if (w.unit + w.parts > a.tiles + a.units) return;
-    const int64_t step = (int64_t)a.cache.heads * ROWS, at = (w.unit * a.cache.heads + head) * ROWS + r;
-    // lane k: part k's maximum and sum (there are at most kMaxSplits)
-    float l = 0.f, y = -INFINITY;
-    if (lane < w.parts) {
-        const v2f x = *reinterpret_cast<const v2f *>(a.stat + 2 * (at + lane * step));
-        y = x[0];
-        l = x[1];
-    }
-    float most = y;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
-    const float f = l == 0.f ? 0.f : y == most ? 1.f : __builtin_amdgcn_exp2f(y - most);
-    float total = l * f, x0 = 0.f, x1 = 0.f;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
-    const float *p = a.part + at * D + min(2 * lane, D - 2);
-    // (a part without tokens has sums of 0, lanes past the last part a weight of 0)
-    for (int k = 0; k < w.parts; k += 8) {
-        v2f v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const v2f *>(p + min(k + i, w.parts - 1) * step * D);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float g = bits_f(__builtin_amdgcn_readlane(f_bits(f), k + i));
-            x0 += v[i][0] * g;
-            x1 += v[i][1] * g;
+    const int64_t step = (int64_t)a.cache.heads * ROWS;
+#pragma unroll 2
+    for (int n = 0; n < kJoinRows<ROWS>; ++n) {
+        const int r = (blockIdx.x % kGroups * 4 + wave) * kJoinRows<ROWS> + n;
+        if (r >= w.rows) return;
+        const int64_t at = (w.unit * a.cache.heads + head) * ROWS + r;
+        // lane k: part k's maximum and sum (there are at most kMaxSplits)
+        float l = 0.f, y = -INFINITY;
+        if (lane < w.parts) {
+            const v2f x = *reinterpret_cast<const v2f *>(a.stat + 2 * (at + lane * step));
+            y = x[0];
+            l = x[1];
         }
+        float most = y;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+        const float f = l == 0.f ? 0.f : y == most ? 1.f : __builtin_amdgcn_exp2f(y - most);
+        float total = l * f, x0 = 0.f, x1 = 0.f;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+        const float *p = a.part + at * D + min(2 * lane, D - 2);
+        // (a part without tokens has sums of 0, lanes past the last part a weight of 0)
+        for (int k = 0; k < w.parts; k += 8) {
+            v2f v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const v2f *>(p + min(k + i, w.parts - 1) * step * D);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float g = bits_f(__builtin_amdgcn_readlane(f_bits(f), k + i));
+                x0 += v[i][0] * g;
+                x1 += v[i][1] * g;
+            }
+        }
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        const int64_t i = (int64_t)w.rt * ROWS + r;
+        __bf16 *out = (__bf16 *)a.out + (w.s.tok0 + i / group) * a.out_st + (head * group + (int)(i % group)) * a.out_sh;
+        if (2 * lane < D) *reinterpret_cast<bf16x2v *>(out + 2 * lane) = bf16x2v{(__bf16)(x0 * inv), (__bf16)(x1 * inv)};
     }
-    if (2 * lane >= D) return;
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    const int64_t i = (int64_t)w.rt * ROWS + r;
-    __bf16 *out = (__bf16 *)a.out + (w.s.tok0 + i / group) * a.out_st + (head * group + (int)(i % group)) * a.out_sh;
-    *reinterpret_cast<bf16x2v *>(out + 2 * lane) = bf16x2v{(__bf16)(x0 * inv), (__bf16)(x1 * inv)};
 }
 
 // ROWS: query rows of a workgroup, 128 or 16
@@ -654,11 +667,12 @@ template <int DC, int MODS, int ROWS>
 hipError_t launch(const CachedArgs &a, hipStream_t stream)
 {
     // (every tile has a unit, and the parts of W / units super-blocks are no more than units)
+    constexpr int groups = ROWS / (4 * kJoinRows<ROWS>);
     const int64_t tiles = a.tiles * a.cache.heads, n = (a.tiles + a.units) * a.cache.heads;
-    if (n > INT32_MAX || tiles * (ROWS / 4) > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (n > INT32_MAX || tiles * groups > INT32_MAX) return hipErrorInvalidConfiguration;
     if constexpr (ROWS == 16) attention_cached_kernel<DC, MODS><<<(uint32_t)n, 256, 0, stream>>>(a);
     else attention_cached_rows_kernel<DC, MODS><<<(uint32_t)n, 256, 0, stream>>>(a);
-    if (a.units > 0) attention_join_kernel<ROWS><<<(uint32_t)(tiles * (ROWS / 4)), 256, 0, stream>>>(a);
+    if (a.units > 0) attention_join_kernel<ROWS><<<(uint32_t)(tiles * groups), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
