@@ -395,7 +395,6 @@ struct Schedule {
     // wave sees some and all pairs
     bool part = false, wave_any = false, wave_all = false, wave_same = false;
 
-
     // next visited tile below `end`, or -1 (the same in all waves); f(tile) -> {of the
     // workgroup, of this wave}
     template <typename F>
@@ -430,7 +429,9 @@ struct Schedule {
 };
 
 // LDS stages of a tile loop for tiles of so many bytes (both operands): three where they leave
-// room for two workgroups a compute unit, two, or one
+// room for three workgroups a compute unit (loads then have two tiles' time: tiles of 64 keys and
+// 64 dims in bfloat16 or 32 keys in float32), two, or one (float32, NARROW, more than 64 dims:
+// the tiles of 128 rows fill the LDS)
 constexpr int stages_of(int bytes) { return 3 * bytes <= 49152 ? 3 : 2 * bytes <= 131072 ? 2 : 1; }
 
 // Keeps the order of the instructions before and after it

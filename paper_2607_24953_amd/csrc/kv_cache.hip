@@ -1,6 +1,12 @@
 // Writing new tokens into the paged 8-bit cache, and reading tokens back as values.
 //
-// Both are memory-bound.  A wave takes one block of 32 tokens of one head, keys or values:
+// Both are memory-bound: 16384 tokens of 32 heads and 128 dims, bfloat16, keys and values, are
+// written (403 MB read and written) in 106 us, 3.8 TB/s, and read back in 71 us, 5.7 TB/s,
+// where a large copy reaches 4.9.  One token of each of 64 sequences takes 7 and 6 us, a launch and
+// the chain offsets, page table, block.  The write gains nothing from more bytes under way: a
+// lane's 8 rows are loaded at once, and the scale needs all of them.
+//
+// A wave takes one block of 32 tokens of one head, keys or values:
 // lane (tg, dg) holds the 8 x 8 elements of tokens 8 tg .. and dims 8 dg .., loaded as 16 or
 // 32 bytes a token.  The E4M3 codes come from v_cvt_scalef32_pk_fp8_f32, pairs along dims for
 // keys and along tokens for the transposed values, so that both leave in 8-byte stores with
@@ -122,7 +128,8 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const CacheCopyArgs a)
     uint32_t byte = top >= 0x7F800000u ? 255u : (uint32_t)(fp8_block_exponent(top) + 127);
     uint8_t *scale_at = (u.values ? a.cache.vs : a.cache.ks) + u.at;
     const uint32_t before = u.lo > 0 ? *scale_at : byte;
-    // the scale of tokens already there only grows; their codes are then rounded to the new one
+    // The scale of tokens already there only grows; their codes are then rounded to the new one
+    // (to nearest even, a second rounding: the values they came from are gone)
     byte = max(byte, before);
     const bool redo = u.lo > 0 && byte != before;
     const float scale = bits_f((byte == 255 ? 127u : byte) << 23);
