@@ -248,8 +248,6 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
         const bool all = j0 + kSuper - 1 <= w.p0 && j0 + kSuper <= s.len && (!m.window || w.p1 - j0 < m.window) &&
                          !__any(c.vs == kNoBlock);
         bf16x8 pf[2];
-        // (a value scale of 255 marks a block with a NaN: rows that see it get one)
-        const bool bad = __any(c.vs == 255);
         v4f z[4] = {};
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -281,6 +279,15 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
                     z[u][i] = ok ? z[u][i] : -INFINITY;
                 }
         }
+        // A value scale of 255 marks a block with a NaN: rows that see it become NaN, however small
+        // their weight of it (the maximum passes NaN scores over)
+        if (__any(c.vs == 255)) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (c.vs == 255 && z[u][i] != -INFINITY) z[u][i] = __builtin_nanf("");
+        }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -304,7 +311,6 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
                 const float e = __builtin_amdgcn_exp2f(fmaf(z[u][i], sm.c, off));
                 sum += e;
                 z[u][i] = e;
-                if (bad && c.vs == 255 && e != 0.f) z[u][i] = __builtin_nanf("");
             }
 #pragma unroll
         for (int k = 0; k < 2; ++k)
@@ -534,6 +540,14 @@ __global__ __launch_bounds__(256, 2) void attention_cached_rows_kernel(const Cac
                     z[t][i] = (seen >> (16 * (i >> 3) + (i & 7))) & 1 ? z[t][i] : -INFINITY;
             }
         }
+        // (blocks with a NaN among the values, as in the kernel above)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            if (x.vs[t] == 255) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[t][i] = z[t][i] != -INFINITY ? __builtin_nanf("") : z[t][i];
+            }
+        }
         float top = z[0][0];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -557,14 +571,6 @@ __global__ __launch_bounds__(256, 2) void attention_cached_rows_kernel(const Cac
                 z[t][i] = __builtin_amdgcn_exp2f(fmaf(z[t][i], sm.c, off));
                 sum += z[t][i];
             }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            // (a value scale of 255 marks a block with a NaN: rows that see it get one)
-            if (x.vs[t] == 255) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) z[t][i] = z[t][i] != 0.f ? __builtin_nanf("") : 0.f;
-            }
-        }
         bf16x8 pf;
         unroll<kValues>([&](auto yc) __attribute__((always_inline)) {
             constexpr int y = decltype(yc)::value, i = kScores + y;

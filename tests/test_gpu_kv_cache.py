@@ -245,6 +245,21 @@ def test_blocks_with_nan(q2d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("take", [1, 150])
+def test_blocks_with_nan_of_vanishing_weight(q2d, take, dim):
+    """Values that are NaN reach a query that sees them also where their weight underflows."""
+    p = Paged(q2d, 1, 1, dim, 32)
+    k, v = tokens(150, 1, dim, seed=12, spread=80.0)
+    k[96:128], v[100, 0, 3] = 0.0, math.nan                 # scores of 0 beside ones of some hundreds
+    p.append(k, v, [150])
+    q = torch.randn((take, 4, dim), generator=torch.Generator().manual_seed(13)).to(torch.bfloat16).cuda()
+    out = q2d.q2d_attention_cached(q, p.cache, p.table.cuda(), p.lens().cuda())
+    sees = torch.arange(150 - take, 150).cuda() >= 96
+    assert torch.equal(torch.isnan(out), sees[:, None, None].expand_as(out))
+
+
+@pytest.mark.gpu
 def test_missing_pages(q2d):
     """A table entry that names no page: its tokens are not seen."""
     p = filled(q2d, [200], 1, 64, 64, 256)
