@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
             for (int r = 0; r < 16; ++r) {
                 float x = z[r], u = 1.f;
                 if constexpr (CAP) {
-                    x = tanh_of(x * sm.k1, F32);
+                    x = tanh_of<F32, MODS>(x * sm.k1);
                     u = 1.f - x * x;
                 }
                 if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 - (float)tile_row(r, 0)), x);
@@ -385,7 +385,7 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
                         const int r = 4 * x4 + y;
                         float x = z[r], u = 1.f;
                         if constexpr (CAP) {
-                            x = tanh_of(x * sm.k1, F32);
+                            x = tanh_of<F32, MODS>(x * sm.k1);
                             u = 1.f - x * x;
                         }
                         if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 + (float)tile_row(r, 0)), x);
@@ -627,7 +627,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
                     const int r = 4 * x4 + y;
                     float x = z[r], u = 1.f;
                     if constexpr (CAP) {
-                        x = tanh_of(x * sm.k1, false);
+                        x = tanh_of<false, MODS>(x * sm.k1);
                         u = 1.f - x * x;
                     }
                     if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 + (float)tile_row(r, 0)), x);
@@ -766,11 +766,13 @@ hipError_t launch(const AttentionArgs &a, hipStream_t stream)
 template <typename T, int DC>
 hipError_t launch_mods(const AttentionArgs &a, hipStream_t stream)
 {
-    switch ((a.mask.cap > 0.f ? 1 : 0) | (a.mask.slopes ? 2 : 0)) {
+    constexpr bool f32 = sizeof(T) == 4;
+    switch (mods_of(a.mask, f32)) {
     case 0: return launch<T, DC, 0>(a, stream);
     case 1: return launch<T, DC, 1>(a, stream);
     case 2: return launch<T, DC, 2>(a, stream);
-    default: return launch<T, DC, 3>(a, stream);
+    case 3: return launch<T, DC, 3>(a, stream);
+    default: return launch<T, DC, f32 ? 3 : kAnyCap>(a, stream);
     }
 }
 

@@ -184,7 +184,6 @@ __device__ __forceinline__ bool place_of(const CachedArgs &a, int group, Place &
     return true;
 }
 
-// MODS bit 0: capped scores, bit 1: distance bias
 template <int DT, int MODS>
 __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedArgs a)
 {
@@ -265,7 +264,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float x = z[u][i] * ks;
-                if constexpr (CAP) x = tanh_of(x, false);
+                if constexpr (CAP) x = tanh_of<false, MODS>(x);
                 if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 - (float)(4 * u + i)), x);
                 z[u][i] = x;
             }
@@ -524,7 +523,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_rows_kernel(const Cac
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     float y = z[t][i];
-                    if constexpr (CAP) y = tanh_of(y * sm.k1, false);
+                    if constexpr (CAP) y = tanh_of<false, MODS>(y * sm.k1);
                     if constexpr (BIAS) y = fmaf(-sm.slope, fabsf(d0 - (float)(32 * t + 16 * (i >> 3) + (i & 7))), y);
                     z[t][i] = y;
                 }
@@ -694,11 +693,12 @@ hipError_t launch(const CachedArgs &a, hipStream_t stream)
 template <int DC, int ROWS>
 hipError_t launch_mods(const CachedArgs &a, hipStream_t stream)
 {
-    switch ((a.mask.cap > 0.f ? 1 : 0) | (a.mask.slopes ? 2 : 0)) {
+    switch (mods_of(a.mask, false)) {
     case 0: return launch<DC, 0, ROWS>(a, stream);
     case 1: return launch<DC, 1, ROWS>(a, stream);
     case 2: return launch<DC, 2, ROWS>(a, stream);
-    default: return launch<DC, 3, ROWS>(a, stream);
+    case 3: return launch<DC, 3, ROWS>(a, stream);
+    default: return launch<DC, kAnyCap, ROWS>(a, stream);
     }
 }
 

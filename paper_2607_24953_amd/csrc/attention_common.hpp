@@ -600,11 +600,19 @@ __device__ __forceinline__ ScoreMap score_map(const AttentionMask &m, int hq)
     return s;
 }
 
-__device__ __forceinline__ float tanh_of(float x, bool precise)
+template <bool F32, int MODS>
+__device__ __forceinline__ float tanh_of(float x)
 {
-    if (precise) return tanhf(x);
-    // 1 - 2 / (e^2x + 1): off by about 2^-23 of 1, far below the bf16 operands' rounding
-    return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
+    if constexpr (F32) return tanhf(x);
+    // off by 2^-23 of 1
+    const float t = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
+    if constexpr (MODS != kAnyCap) return t;
+    // off by 2^-22 of itself: below 0.55 an odd polynomial (least relative error on that interval,
+    // 2^-24.7, fitted to tanh(x) / x at Chebyshev points); above it the form above, which is there
+    // more than half of 1
+    const float y = x * x;
+    const float p = fmaf(fmaf(fmaf(0.016458744f, y, -0.052684136f), y, 0.13320942f), y, -0.33332959f);
+    return fabsf(x) < 0.55f ? fmaf(x, y * p, x) : t;
 }
 
 // 4 neighbouring elements to memory, rounded to nearest even for bf16

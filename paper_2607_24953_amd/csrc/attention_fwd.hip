@@ -28,7 +28,7 @@ namespace q2d {
 
 namespace {
 
-// MODS bit 0: capped scores, bit 1: distance bias.  A workgroup of four waves owns 128
+// A workgroup of four waves owns 128
 // queries and its waves share tiles of 64 (float32: 32) keys; or (NARROW) 32 queries, and
 // each wave takes its quarter of tiles of 128 keys, joined at the end.  DC is 64, 96 or 128: dims
 // round up to whole 32s of O's tiles (fewer than 33 run as 64).  Three waves a SIMD where their
@@ -132,7 +132,7 @@ void attention_fwd_kernel(const AttentionArgs a)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     float x = z[t][r];
-                    if constexpr (CAP) x = tanh_of(x * sm.k1, F32);
+                    if constexpr (CAP) x = tanh_of<F32, MODS>(x * sm.k1);
                     if constexpr (BIAS) x = fmaf(-sm.slope, fabsf(d0 - (float)(32 * t + tile_row(r, 0))), x);
                     z[t][r] = x;
                 }
@@ -256,11 +256,13 @@ hipError_t launch(const AttentionArgs &a, hipStream_t stream)
 template <typename T, int DC>
 hipError_t launch_mods(const AttentionArgs &a, hipStream_t stream)
 {
-    switch ((a.mask.cap > 0.f ? 1 : 0) | (a.mask.slopes ? 2 : 0)) {
+    constexpr bool f32 = sizeof(T) == 4;
+    switch (mods_of(a.mask, f32)) {
     case 0: return launch<T, DC, 0>(a, stream);
     case 1: return launch<T, DC, 1>(a, stream);
     case 2: return launch<T, DC, 2>(a, stream);
-    default: return launch<T, DC, 3>(a, stream);
+    case 3: return launch<T, DC, 3>(a, stream);
+    default: return launch<T, DC, f32 ? 3 : kAnyCap>(a, stream);
     }
 }
 
