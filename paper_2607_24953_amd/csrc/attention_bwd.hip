@@ -138,7 +138,6 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
         my_doc = row && p >= 0 ? docs[p] : -1;
     }
     const ScoreMap sm = score_map(m, hq);
-    const float pos = (float)p;
     const Sight sight = query_sight(m, p, a.len_k, prefix, my_doc);
 
     int end = (a.len_k + BN - 1) / BN;
@@ -184,7 +183,7 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
                 read(std::integral_constant<int, i + kAhead>{});
                 pin<(DC > 64)>();
             });
-            const float d0 = pos - (float)(j0 + 32 * t) - (float)(4 * h);
+            const float d0 = (float)(p - (j0 + 32 * t) - 4 * h);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 float x = z[r], u = 1.f;
@@ -375,7 +374,7 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) e = mma(Lds::row_frag(gr, t, ks), vf[ks], e);
                 const int p0 = i0 + 32 * t + shift;
-                const float d0 = (float)(p0 + 4 * h) - (float)j;
+                const float d0 = (float)(p0 + 4 * h - j);
 #pragma unroll
                 for (int x4 = 0; x4 < 4; ++x4) {
                     const v4f l4 = *reinterpret_cast<const v4f *>(&rows[stage][0][iw + 32 * t + tile_row(4 * x4, h)]);
@@ -617,7 +616,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
                 pin();
             });
             const int p0 = at.tile * BQ + 32 * t + shift;
-            const float d0 = BIAS ? (float)(p0 + 4 * h) - (float)j : 0.f;
+            const float d0 = BIAS ? (float)(p0 + 4 * h - j) : 0.f;
             v16f pu;                                     // P times the cap's derivative
 #pragma unroll
             for (int x4 = 0; x4 < 4; ++x4) {

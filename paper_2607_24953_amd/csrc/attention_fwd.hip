@@ -82,7 +82,7 @@ void attention_fwd_kernel(const AttentionArgs a)
         my_doc = row && p >= 0 ? docs[p] : -1;
     }
     const ScoreMap sm = score_map(m, hq);
-    const float thr = 8.f / sm.c, pos = (float)p;
+    const float thr = 8.f / sm.c;
     const Sight sight = query_sight(m, p, a.len_k, prefix, my_doc);
 
     int end = (a.len_k + BN - 1) / BN;
@@ -126,7 +126,7 @@ void attention_fwd_kernel(const AttentionArgs a)
             pin<(DC > 64)>();
         });
         if constexpr (CAP || BIAS) {
-            const float d0 = pos - (float)j0 - (float)(4 * h);
+            const float d0 = (float)(p - j0 - 4 * h);        // (positions do not fit float32)
 #pragma unroll
             for (int t = 0; t < WN / 32; ++t)
 #pragma unroll
