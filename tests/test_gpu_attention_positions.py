@@ -10,7 +10,7 @@ from test_gpu_attention import U, limits, q2d  # noqa: F401  (q2d: the fixture)
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("D,dtype", [(8, torch.bfloat16), (8, torch.float32)], ids=str)
+@pytest.mark.parametrize("D,dtype", [(8, torch.bfloat16), (8, torch.float32), (72, torch.bfloat16)], ids=str)
 def test_distances_past_2_24(q2d, D, dtype):
     Lq, Lk, W, tail = 200, 2 ** 24 + 301, 150, 512
     g = torch.Generator().manual_seed(41)
