@@ -90,6 +90,7 @@ void attention_fwd_kernel(const AttentionArgs a)
     auto see = [&](int t, Seen &g, Seen &w) __attribute__((always_inline)) {
         const int j0 = t * BN, j1 = min(j0 + BN, a.len_k) - 1, k0 = j0 + jw, k1 = min(k0 + WN, a.len_k) - 1;
         g = classify(m, prefix, p0, p1, j0, j1, dg, docs ? range_of(ranges, j0, j1) : Documents{});
+        g.all = g.all && j0 + BN <= a.len_k;                   // (the copies behind the last key are masked)
         if (pw1 >= pw0 && k1 >= k0) {
             w = classify(m, prefix, pw0, pw1, k0, k1, dw, docs ? range_of(ranges, k0, k1) : Documents{});
             w.all = w.all && k0 + WN <= a.len_k;
