@@ -380,7 +380,10 @@ q2d_status q2d_grouped_gemm(const q2d_tensor *A, int transA, const q2d_tensor *B
  *   lse_i = log sum_j exp s_ij.
  * A query that sees no key has out = 0, lse = -infinity and adds nothing to any gradient.
  * Keys and values that a query does not see have no influence on its results, whatever
- * they hold (infinities and NaN included), and likewise in the gradients.
+ * they hold (infinities and NaN included), and likewise in the gradients.  Infinities and NaN
+ * that are seen reach the results that the formulas lead them to, and no others (an infinity in
+ * one element of dout: that element of dv); a weight too small for float32 may count as 0, and
+ * its product with an infinity then as NaN.
  *
  * heads_q is a multiple of heads_kv; query head h reads key head h / (heads_q / heads_kv).
  * dim is a multiple of 8 up to 128 (Q2D_EUNSUPPORTED otherwise).  Lengths are 1 to 2^30.

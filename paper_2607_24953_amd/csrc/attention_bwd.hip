@@ -77,6 +77,78 @@ __global__ __launch_bounds__(64) void document_ranges_kernel(const int32_t *docs
     if (threadIdx.x == 0) ranges[blockIdx.x] = make_int2(padding ? ~lo : lo, hi);
 }
 
+// ---------------------------------------------------------------- rows that are not finite
+//
+// Rows with an infinity or a NaN among their numbers, in tiles with masked pairs.  The products
+// leave them out (`skip`); behind the loop, where its registers are free, the pairs that see
+// them are added in plain arithmetic on the rows in memory.
+
+// The tiles of a loop that have masked pairs, and their rows of x (and y) that are not finite:
+// f(row), for a wave
+template <int ROWS, int WIDTH, typename T, typename See, typename F>
+__device__ __forceinline__ void add_rows(int end, See &&see, int first, int n, const T *x, int64_t sx, const T *y, int64_t sy, int D,
+                                         F &&f)
+{
+    Schedule sched;
+    for (Visit at = sched.take(end, see); at.tile >= 0; at = sched.take(end, see)) {
+        if (!at.part || !at.any) continue;
+        const int r0 = at.tile * ROWS + first, r1 = min(r0 + WIDTH, n);
+#pragma unroll 1
+        for (int r = r0; r < r1; ++r) {
+            bool bad = false;
+            for (int d = threadIdx.x & 63; d < D; d += 64)
+                bad = bad || !(fabsf((float)x[r * sx + d]) < INFINITY) || !(fabsf((float)y[r * sy + d]) < INFINITY);
+            if (__any(bad)) f(r);
+        }
+    }
+}
+
+// product of a lane pair's own row with a row that all lanes share, in both lanes
+template <typename T>
+__device__ __forceinline__ float row_dot(const T *own, bool valid, const T *row, int h, int D)
+{
+    float s = 0.f;
+#pragma unroll 1
+    for (int d = valid ? 8 * h : D; d < D; d += 16) {
+        const Frag<T> x = global_frag<T>(own + d, true, 0, 0, 8), y = global_frag<T>(row + d, true, 0, 0, 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf((float)x[e], (float)y[e], s);
+    }
+    return s + __shfl_xor(s, 32);
+}
+
+struct PairWeights { float p, ds; };
+
+// P and dS of a pair from its products q.k and dO.v and its distance
+template <typename T, int MODS>
+__device__ __forceinline__ PairWeights pair_weights(const ScoreMap &sm, float qk, float dp, int distance, float lse2, float delta)
+{
+    float u = 1.f;
+    if constexpr (MODS & 1) {
+        qk = tanh_of<sizeof(T) == 4, MODS>(qk * sm.k1);
+        u = 1.f - qk * qk;
+    }
+    if constexpr (MODS & 2) qk = fmaf(-sm.slope, fabsf((float)distance), qk);
+    const float p = __builtin_amdgcn_exp2f(fmaf(qk, sm.c, -lse2));
+    return {p, p * (dp - delta) * u};
+}
+
+// accumulators (rows d, a column a lane pair) += w times a row of memory, in the columns that see it
+template <typename T, int DS>
+__device__ __forceinline__ void add_row(v16f *acc, const T *row, float w, bool sees, int h, int D)
+{
+#pragma unroll
+    for (int dt = 0; dt < DS; ++dt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * dt + 8 * g + 4 * h;
+            if (sees && d < D) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[dt][4 * g + i] = fmaf(w, (float)row[d + i], acc[dt][4 * g + i]);
+            }
+        }
+}
+
 // ---------------------------------------------------------------- dQ
 
 // A workgroup's layout and NARROW are the forward kernel's.  Three products a tile, S, dP and
@@ -145,6 +217,7 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
     auto see = [&](int t, Seen &g, Seen &w) __attribute__((always_inline)) {
         const int j0 = t * BN, j1 = min(j0 + BN, a.len_k) - 1, k0 = j0 + jw, k1 = min(k0 + WN, a.len_k) - 1;
         g = classify(m, prefix, p0, p1, j0, j1, dg, docs ? range_of(ranges, j0, j1) : Documents{});
+        g.all = g.all && j0 + BN <= a.len_k;
         if (pw1 >= pw0 && k1 >= k0) {
             w = classify(m, prefix, pw0, pw1, k0, k1, dw, docs ? range_of(ranges, k0, k1) : Documents{});
             w.all = w.all && k0 + WN <= a.len_k;
@@ -156,7 +229,8 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
     }
     v16f dq[DS] = {};
 
-    bool spoilt = false;                // this query sees an infinity or a NaN among the keys
+    uint32_t skip[WN / 32] = {};        // keys of the tile that the products leave out
+    bool left_out = false;
 
     auto tile = [&](const Visit &at, int stage) __attribute__((always_inline)) {
         const int j0 = at.tile * BN + jw;
@@ -196,7 +270,8 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
                 e[r] = pr * (e[r] - delta) * u;
             }
             if (!at.all) {
-                const uint32_t w = sight.word(j0 + 32 * t, docs && !at.same ? &doc_of[stage][jw + 32 * t] : nullptr) >> (4 * h);
+                const uint32_t w =
+                    (sight.word(j0 + 32 * t, docs && !at.same ? &doc_of[stage][jw + 32 * t] : nullptr) & ~skip[t]) >> (4 * h);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) e[r] = word_bit(w, r) ? e[r] : 0.f;
             }
@@ -210,17 +285,16 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
             });
         });
     };
-    auto check = [&](const Visit &at, int stage) __attribute__((always_inline)) {
+    auto check = [&](Visit &at, int stage) __attribute__((always_inline)) {
         uint32_t bad[BN / 32], some = 0;
         non_finite<Lds, BN, NW>(smem[stage][0], &found[0][0], bad);
 #pragma unroll
         for (int t = 0; t < BN / 32; ++t) some |= bad[t];
-        if (!some) return;
 #pragma unroll
-        for (int t = 0; t < WN / 32; ++t) {
-            const uint32_t w = sight.word(at.tile * BN + jw + 32 * t, docs && !at.same ? &doc_of[stage][jw + 32 * t] : nullptr);
-            spoilt = spoilt || (at.any && ((at.all ? ~0u : w) & pick<BN / 32>(bad, NARROW ? wave : t)));
-        }
+        for (int t = 0; t < WN / 32; ++t) skip[t] = pick<BN / 32>(bad, NARROW ? wave : t);
+        if (!some) return;
+        at.all = false;
+        left_out = true;
         Lds::template clean<BN, NW * 64>(smem[stage][0]);
     };
     auto fetch = [&](int stage, int t) __attribute__((always_inline)) {
@@ -229,10 +303,13 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
         if (docs && wave < (BN + 63) / 64) load_words64(&doc_of[stage][64 * wave], docs, t * BN + 64 * wave, a.len_k);
     };
     tile_loop<NS, 2 * kBytes / (NW * 1024)>(end, see, fetch, check, tile);
-    if (spoilt) {
-#pragma unroll
-        for (int dt = 0; dt < DS; ++dt) dq[dt] += __builtin_nanf("");
-    }
+    if (left_out)
+        add_rows<BN, WN>(end, see, jw, a.len_k, k, a.k.sl, k, a.k.sl, D, [&](int j) __attribute__((always_inline)) {
+            const T *kj = k + (int64_t)j * a.k.sl, *vj = v + (int64_t)j * a.v.sl;
+            const float qk = row_dot(q, row, kj, h, D), dp = row_dot(g, row, vj, h, D);
+            const bool sees = sight.sees(j, docs, docs ? docs[j] : 0);
+            add_row<T, DS>(dq, kj, pair_weights<T, MODS>(sm, qk, dp, p - j, lse2, delta).ds, sees, h, D);
+        });
     if constexpr (NARROW) {
         __syncthreads();                       // no wave reads a tile any more
         join_waves<DS>(dq, smem[0][0]);
@@ -342,6 +419,7 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
         const int i0 = t * BQ, i1 = min(i0 + BQ, a.len_q) - 1, k0 = i0 + iw, k1 = min(k0 + WQ, a.len_q) - 1;
         g = classify(m, prefix, i0 + shift, i1 + shift, j0, j1,
                      docs ? range_of(ranges, i0 + shift, i1 + shift) : Documents{}, dg);
+        g.all = g.all && i0 + BQ <= a.len_q;
         if (jw1 >= jw && k1 >= k0) {
             w = classify(m, prefix, k0 + shift, k1 + shift, jw, jw1,
                          docs ? range_of(ranges, k0 + shift, k1 + shift) : Documents{}, dw);
@@ -353,7 +431,8 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
         __syncthreads();
     }
     v16f dk[DS] = {}, dv[DS] = {};
-    bool spoilt = false;                // an infinity or a NaN among the queries that see this key
+    uint32_t skip[WQ / 32] = {};        // queries of the tile that the products leave out
+    bool left_out = false;
     for (int gh = first; gh < last; ++gh) {
         const int hq = hk * group + gh;
         const T *q = (const T *)a.q.p + b * a.q.sb + hq * a.q.sh;
@@ -393,7 +472,8 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
                     }
                 }
                 if (!at.all) {
-                    const uint32_t w = sight.word(p0, docs && !at.same ? &doc_of[stage][iw + 32 * t] : nullptr) >> (4 * h);
+                    const uint32_t w =
+                        (sight.word(p0, docs && !at.same ? &doc_of[stage][iw + 32 * t] : nullptr) & ~skip[t]) >> (4 * h);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         z[r] = word_bit(w, r) ? z[r] : 0.f;
@@ -411,7 +491,7 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
                 }
             }
         };
-        auto check = [&](const Visit &at, int stage) __attribute__((always_inline)) {
+        auto check = [&](Visit &at, int stage) __attribute__((always_inline)) {
             uint32_t bq[BQ / 32], bg[BQ / 32], some = 0;
             non_finite<Lds, BQ, NW>(smem[stage][0], &found[0][0][0], bq);
             non_finite<Lds, BQ, NW>(smem[stage][1], &found[1][0][0], bg);
@@ -420,13 +500,11 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
                 bq[t] |= bg[t];
                 some |= bq[t];
             }
-            if (!some) return;
 #pragma unroll
-            for (int t = 0; t < WQ / 32; ++t) {
-                const uint32_t w =
-                    sight.word(at.tile * BQ + iw + 32 * t + shift, docs && !at.same ? &doc_of[stage][iw + 32 * t] : nullptr);
-                spoilt = spoilt || (at.any && ((at.all ? ~0u : w) & pick<BQ / 32>(bq, NARROW ? wave : t)));
-            }
+            for (int t = 0; t < WQ / 32; ++t) skip[t] = pick<BQ / 32>(bq, NARROW ? wave : t);
+            if (!some) return;
+            at.all = false;
+            left_out = true;
             Lds::template clean<BQ, NW * 64>(smem[stage][0]);
             Lds::template clean<BQ, NW * 64>(smem[stage][1]);
         };
@@ -445,12 +523,20 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
         tile_loop<NS, 2 * kBytes / (NW * 1024)>(end, see, fetch, check, tile);
         block_barrier();           // the next head's first tile takes stage 0
     }
-    if (spoilt) {
-#pragma unroll
-        for (int dt = 0; dt < DS; ++dt) {
-            dk[dt] += __builtin_nanf("");
-            dv[dt] += __builtin_nanf("");
-        }
+    for (int gh = first; left_out && gh < last; ++gh) {
+        const int hq = hk * group + gh;
+        const T *q = (const T *)a.q.p + b * a.q.sb + hq * a.q.sh;
+        const T *g = (const T *)a.dout.p + b * a.dout.sb + hq * a.dout.sh;
+        const int64_t at = ((int64_t)b * a.heads_q + hq) * a.len_q;
+        const ScoreMap sm = score_map(m, hq);
+        add_rows<BQ, WQ>(end, see, iw, a.len_q, q, a.q.sl, g, a.dout.sl, D, [&](int i) __attribute__((always_inline)) {
+            const T *qi = q + (int64_t)i * a.q.sl, *gi = g + (int64_t)i * a.dout.sl;
+            const float qk = row_dot(k, key, qi, h, D), dp = row_dot(v, key, gi, h, D);
+            const PairWeights x = pair_weights<T, MODS>(sm, qk, dp, i + shift - j, a.lse2[at + i], a.delta[at + i]);
+            const bool sees = sight.sees(i + shift, docs, docs ? docs[max(i + shift, 0)] : 0);
+            add_row<T, DS>(dv, gi, x.p, sees, h, D);
+            add_row<T, DS>(dk, qi, x.ds, sees, h, D);
+        });
     }
     if constexpr (NARROW) {
         join_waves<DS>(dk, smem[0][0]);
@@ -541,6 +627,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
         const int p0 = t * BQ + shift, p1 = min(t * BQ + BQ, a.len_q) - 1 + shift;
         const Documents dq = docs ? range_of(ranges, p0, p1) : Documents{};
         s = classify(m, prefix, p0, p1, j0, j1, dq, dg);
+        s.all = s.all && t * BQ + BQ <= a.len_q;
         if (jw1 >= jw) {
             w = classify(m, prefix, p0, p1, jw, jw1, dq, dw);
             w.all = w.all && t * BQ + BQ <= a.len_q;
@@ -573,20 +660,20 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
             load_words64(rows[st][wave], (wave ? a.delta : a.lse2) + ((int64_t)b * a.heads_q + hq) * a.len_q, i0, a.len_q);
         if (docs && wave == 2) load_words64(doc_of[st], docs, i0 + shift, a.len_k);
     };
-    bool spoilt = false;                // an infinity or a NaN among the queries that see this key
-    auto check = [&](int stage, const At &at) __attribute__((always_inline)) {
+    uint32_t skip[BQ / 32] = {};        // queries of the tile that the products leave out
+    bool left_out = false;
+    auto check = [&](int stage, At &at) __attribute__((always_inline)) {
         uint32_t bq[BQ / 32], bg[BQ / 32], some = 0;
         non_finite<Lds, BQ, NW>(smem[stage][0], &found[0][0][0], bq);
         non_finite<Lds, BQ, NW>(smem[stage][1], &found[1][0][0], bg);
 #pragma unroll
-        for (int t = 0; t < BQ / 32; ++t) some |= bq[t] | bg[t];
-        if (!some) return;
-#pragma unroll
         for (int t = 0; t < BQ / 32; ++t) {
-            const uint32_t w =
-                at.all ? ~0u : sight.word(at.tile * BQ + 32 * t + shift, docs && !at.same ? &doc_of[stage][32 * t] : nullptr);
-            spoilt = spoilt || (at.any && (w & (bq[t] | bg[t])));
+            skip[t] = bq[t] | bg[t];
+            some |= skip[t];
         }
+        if (!some) return;
+        at.all = false;
+        left_out = true;
         Lds::template clean<BQ, NW * 64>(smem[stage][0]);
         Lds::template clean<BQ, NW * 64>(smem[stage][1]);
     };
@@ -636,7 +723,8 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
                 }
             }
             if (!at.all) {
-                const uint32_t w = sight.word(p0, docs && !at.same ? &doc_of[stage][32 * t] : nullptr) >> (4 * h);
+                const uint32_t w =
+                    (sight.word(p0, docs && !at.same ? &doc_of[stage][32 * t] : nullptr) & ~skip[t]) >> (4 * h);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     z[r] = word_bit(w, r) ? z[r] : 0.f;
@@ -751,11 +839,23 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
             stage = stage == 2 ? 0 : stage + 1;
             parity ^= 1;
         }
-        if (!key) return;
-        if (spoilt) {
-#pragma unroll
-            for (int dt = 0; dt < DS; ++dt) acc[dt] += __builtin_nanf("");
+        const T *kj = (const T *)a.k.p + b * a.k.sb + (int64_t)j * a.k.sl + hk * a.k.sh;
+        const T *vj = (const T *)a.v.p + b * a.v.sb + (int64_t)j * a.v.sl + hk * a.v.sh;
+        for (int gh = first; left_out && gh < last; ++gh) {
+            const int hq = hk * group + gh;
+            const T *q = (const T *)a.q.p + b * a.q.sb + hq * a.q.sh;
+            const T *g = (const T *)a.dout.p + b * a.dout.sb + hq * a.dout.sh;
+            const int64_t at = ((int64_t)b * a.heads_q + hq) * a.len_q;
+            const ScoreMap sm = score_map(m, hq);
+            add_rows<BQ, BQ>(end, see, 0, a.len_q, q, a.q.sl, g, a.dout.sl, D, [&](int i) __attribute__((always_inline)) {
+                const T *qi = q + (int64_t)i * a.q.sl, *gi = g + (int64_t)i * a.dout.sl;
+                const float qk = row_dot(kj, key, qi, h, D), dp = SECOND ? row_dot(vj, key, gi, h, D) : 0.f;
+                const PairWeights x = pair_weights<T, MODS>(sm, qk, dp, i + shift - j, a.lse2[at + i], a.delta[at + i]);
+                const bool sees = sight.sees(i + shift, docs, docs ? docs[max(i + shift, 0)] : 0);
+                add_row<T, DS>(acc, SECOND ? qi : gi, SECOND ? x.ds : x.p, sees, h, D);
+            });
         }
+        if (!key) return;
         store_dkv<T, DS>(a, !SECOND, split, b, j, hk, acc, h);
     };
     if (second) run(std::true_type{});

@@ -262,7 +262,9 @@ __device__ __forceinline__ Frag<T> global_frag(const T *row, bool valid, int ks,
 // Weights of pairs that are not seen are 0, and 0 times an infinity or a NaN is NaN in a
 // matrix product.  So where a workgroup has masked pairs in a tile, its waves first look
 // through the tile that meets those weights (non_finite), and in the rare case take what is
-// not finite out of it (Tile::clean) and put it back for the pairs that are seen.
+// not finite out of it (Tile::clean) and put it back for the pairs that are seen: the forward
+// kernel by what an infinity or a NaN does to a sum (add_non_finite), the backward kernels,
+// whose tile enters the weights as well, a row at a time behind their loop (add_rows).
 
 // Row bits of the tile's rows with an infinity or a NaN, the same in all waves of the
 // workgroup.  words: LDS, [NW][ROWS / 32]; one barrier.
@@ -540,6 +542,11 @@ struct Sight {
             w = doc >= 0 ? w & same : 0u;
         }
         return w;
+    }
+    // whether it sees position x, of document d
+    __device__ __forceinline__ bool sees(int x, bool docs, int d) const
+    {
+        return ((x >= lo && x < hi) || x < prefix) && (!docs || (doc >= 0 && d == doc));
     }
 };
 
