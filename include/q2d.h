@@ -395,7 +395,8 @@ q2d_status q2d_grouped_gemm(const q2d_tensor *A, int transA, const q2d_tensor *B
 
 /* A [batch][length][heads][dim] tensor: strides in elements, unit stride along dim; rows
  * start on 16-byte boundaries (the pointer, and every stride whose extent exceeds 1).
- * A length stride is below 2^22 elements. */
+ * A length stride is below 2^22 elements.  Rows of an output share no memory (each stride
+ * passes what the smaller ones span; Q2D_EINVAL otherwise). */
 typedef struct {
     void *data;
     int64_t stride_batch, stride_length, stride_head;

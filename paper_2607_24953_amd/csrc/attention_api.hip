@@ -32,13 +32,24 @@ q2d_status check_heads(const q2d_heads &t, int64_t batch, int64_t length, int64_
     return Q2D_OK;
 }
 
-// (an output's rows must not share memory)
+// (an output's rows must not share memory: each stride passes what the smaller ones span)
 q2d_status check_output(const q2d_heads &t, int64_t batch, int64_t length, int64_t heads, int64_t dim, int per)
 {
     const q2d_status s = check_heads(t, batch, length, heads, dim, per);
     if (s != Q2D_OK) return s;
-    if ((batch > 1 && t.stride_batch < dim) || (length > 1 && t.stride_length < dim) || (heads > 1 && t.stride_head < dim))
-        return Q2D_EINVAL;
+    struct { int64_t n, stride; } axis[3] = {{heads, t.stride_head}, {length, t.stride_length}, {batch, t.stride_batch}};
+    auto order = [&](int i, int j) {
+        if (axis[j].stride < axis[i].stride) { const auto x = axis[i]; axis[i] = axis[j]; axis[j] = x; }
+    };
+    for (auto &x : axis)
+        if (x.n == 1) x.stride = 0;
+    order(0, 1); order(1, 2); order(0, 1);
+    int64_t span = dim;
+    for (const auto &x : axis) {
+        if (x.n == 1) continue;
+        if (x.stride < span) return Q2D_EINVAL;
+        span += (x.n - 1) * x.stride;
+    }
     return Q2D_OK;
 }
 
