@@ -422,12 +422,15 @@ typedef struct {
 int64_t q2d_attention_workspace(const q2d_attention *a, int backward);
 
 /* Forward: writes out and, where set, lse.  workspace: at least q2d_attention_workspace
- * bytes, 256-byte aligned (may be NULL for 0 bytes); free for reuse in stream order. */
+ * bytes, 256-byte aligned (may be NULL for 0 bytes); free for reuse in stream order.  out
+ * shares no memory with k and v, and with q all of its rows or none (Q2D_EINVAL). */
 q2d_status q2d_attention_fwd(const q2d_attention *a, void *workspace, int64_t workspace_bytes, hipStream_t stream);
 
 /* Backward: from dout and the forward call's inputs, out and lse, writes dq, dk and dv
  * (the shared key and value heads' gradients summed over their query heads).  slopes get no
- * gradient.  Results do not depend on the order in which workgroups run. */
+ * gradient.  Results do not depend on the order in which workgroups run.  dq, dk and dv share
+ * no memory with one another or with q, k, v and dout, but dq may be q or dout itself
+ * (Q2D_EINVAL otherwise). */
 q2d_status q2d_attention_bwd(const q2d_attention *a, const q2d_heads *dout, const q2d_heads *dq, const q2d_heads *dk,
                              const q2d_heads *dv, void *workspace, int64_t workspace_bytes, hipStream_t stream);
 
@@ -487,7 +490,8 @@ q2d_status q2d_kv_write(const q2d_kv_cache *c, const q2d_sequences *s, q2d_dtype
                         hipStream_t stream);
 
 /* Read back: the values of the tokens at positions [lens[b] - n_b, lens[b]) into k and v
- * (layouts as in q2d_kv_write; exact in Q2D_F32 and, within its range, in Q2D_BF16). */
+ * (layouts as in q2d_kv_write; exact in Q2D_F32 and, within its range, in Q2D_BF16), which
+ * share no memory (Q2D_EINVAL). */
 q2d_status q2d_kv_read(const q2d_kv_cache *c, const q2d_sequences *s, q2d_dtype dt, void *k, int64_t k_stride_token,
                        int64_t k_stride_head, void *v, int64_t v_stride_token, int64_t v_stride_head,
                        hipStream_t stream);
@@ -499,7 +503,8 @@ q2d_status q2d_kv_read(const q2d_kv_cache *c, const q2d_sequences *s, q2d_dtype 
  * prefix as in q2d_attention, with the values that the codes stand for.  The call's own
  * keys and values have to be in the cache (q2d_kv_write).  q and out are bfloat16
  * (Q2D_EUNSUPPORTED otherwise); sums and statistics are float32, probabilities are rounded
- * to bfloat16 for the second product.
+ * to bfloat16 for the second product.  out shares all of its rows with q or no memory
+ * (Q2D_EINVAL).
  */
 typedef struct {
     int32_t dtype, heads_q;

@@ -53,6 +53,63 @@ q2d_status check_output(const q2d_heads &t, int64_t batch, int64_t length, int64
     return Q2D_OK;
 }
 
+// A checked tensor's rows in memory: dim elements each, along up to three axes
+struct Rows {
+    uintptr_t at;
+    int64_t n[3], s[3], dim, size;       // strides and dim in elements of `size` bytes, 0 for an extent of 1
+};
+
+Rows rows_of(const q2d_heads &t, int64_t batch, int64_t length, int64_t heads, int64_t dim, int per)
+{
+    Rows r = {reinterpret_cast<uintptr_t>(t.data), {batch, length, heads}, {t.stride_batch, t.stride_length, t.stride_head}, dim,
+              16 / per};
+    for (int i = 0; i < 3; ++i)
+        if (r.n[i] == 1) r.s[i] = 0;
+    return r;
+}
+
+// whether some row of b starts within dim of one of a: off + sum d[i] s[i] for d[i] in
+// (-a.n[i], b.n[i]), the axes by falling stride (`axis`: the order)
+bool rows_meet(const Rows &a, const Rows &b, const int64_t s[3], const int axis[3], int level, int64_t off)
+{
+    if (level == 3) return off > -a.dim && off < a.dim;
+    const int i = axis[level];
+    if (s[i] == 0) return rows_meet(a, b, s, axis, level + 1, off);
+    // (smaller strides reach no further than this one)
+    for (int64_t d = -off / s[i] - 1; d <= -off / s[i] + 1; ++d)
+        if (d > -a.n[i] && d < b.n[i] && rows_meet(a, b, s, axis, level + 1, off + d * s[i])) return true;
+    return false;
+}
+
+// Whether an output may share memory with another tensor of the call: rows of one system of
+// strides between one another (heads of one tensor), or none.
+bool apart(const Rows &a, const Rows &b)
+{
+    int64_t last_a = a.dim, last_b = b.dim, s[3];
+    bool one = true;
+    for (int i = 0; i < 3; ++i) {
+        last_a += (a.n[i] - 1) * a.s[i];
+        last_b += (b.n[i] - 1) * b.s[i];
+        one = one && (a.s[i] == b.s[i] || a.n[i] == 1 || b.n[i] == 1);
+        s[i] = a.n[i] == 1 ? b.s[i] : a.s[i];
+    }
+    if (a.at + last_a * a.size <= b.at || b.at + last_b * b.size <= a.at) return true;
+    if (!one) return false;
+    int axis[3] = {0, 1, 2};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (s[axis[j]] < s[axis[j + 1]]) { const int x = axis[j]; axis[j] = axis[j + 1]; axis[j + 1] = x; }
+    return !rows_meet(a, b, s, axis, 0, ((int64_t)b.at - (int64_t)a.at) / a.size);
+}
+
+// the same rows: an output in the place of an input that only its own workgroup reads
+bool same_rows(const Rows &a, const Rows &b)
+{
+    bool r = a.at == b.at;
+    for (int i = 0; i < 3; ++i) r = r && a.n[i] == b.n[i] && a.s[i] == b.s[i];
+    return r;
+}
+
 q2d_status check_sizes(const q2d_attention *a)
 {
     if (!a) return Q2D_EINVAL;
@@ -83,6 +140,16 @@ q2d_status check(const q2d_attention *a)
     auto word = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; };
     if (!word(a->slopes) || !word(a->documents) || !word(a->prefix) || !word(a->lse)) return Q2D_EINVAL;
     return Q2D_OK;
+}
+
+Rows query_rows(const q2d_attention *a, const q2d_heads &t)
+{
+    return rows_of(t, a->batch, a->len_q, a->heads_q, a->dim, a->dtype == Q2D_F32 ? 4 : 8);
+}
+
+Rows key_rows(const q2d_attention *a, const q2d_heads &t)
+{
+    return rows_of(t, a->batch, a->len_k, a->heads_kv, a->dim, a->dtype == Q2D_F32 ? 4 : 8);
 }
 
 HeadsView view(const q2d_heads &t) { return {t.data, t.stride_batch, t.stride_length, t.stride_head}; }
@@ -178,6 +245,11 @@ q2d_status check_rows(const void *p, int64_t tokens, int64_t st, int64_t heads, 
     return output ? check_output(u, tokens, 1, heads, dim, per) : check_heads(u, tokens, 1, heads, dim, per);
 }
 
+Rows token_rows(const void *p, int64_t tokens, int64_t st, int64_t heads, int64_t sh, int64_t dim, int per)
+{
+    return rows_of({const_cast<void *>(p), st, 0, sh}, tokens, 1, heads, dim, per);
+}
+
 CacheView cache_view(const q2d_kv_cache *c)
 {
     return {c->k_codes, c->v_codes_t, c->k_scales, c->v_scales, c->pages, c->heads, c->dim, c->page_size / 32};
@@ -237,6 +309,9 @@ q2d_status q2d_attention_fwd(const q2d_attention *a, void *workspace, int64_t wo
     q2d_status s = check(a);
     if (s == Q2D_OK) s = check_workspace(workspace_of(a, false), workspace, workspace_bytes);
     if (s != Q2D_OK) return s;
+    const Rows q = query_rows(a, a->q), out = query_rows(a, a->out);
+    if (!apart(out, key_rows(a, a->k)) || !apart(out, key_rows(a, a->v)) || !(same_rows(out, q) || apart(out, q)))
+        return Q2D_EINVAL;
     if (launch_attention_fwd(make_args(a, workspace), a->dtype == Q2D_F32, stream) != hipSuccess) return Q2D_ELAUNCH;
     return Q2D_OK;
 }
@@ -254,6 +329,16 @@ q2d_status q2d_attention_bwd(const q2d_attention *a, const q2d_heads *dout, cons
     if (s == Q2D_OK) s = check_output(*dv, a->batch, a->len_k, a->heads_kv, a->dim, per);
     if (s == Q2D_OK) s = check_workspace(workspace_of(a, true), workspace, workspace_bytes);
     if (s != Q2D_OK) return s;
+    // dK and dV are written before dQ's kernel reads q, k, v and dout; a workgroup of that writes
+    // the rows whose q and dout it alone has read
+    const Rows q = query_rows(a, a->q), k = key_rows(a, a->k), v = key_rows(a, a->v), g = query_rows(a, *dout);
+    const Rows rq = query_rows(a, *dq), rk = key_rows(a, *dk), rv = key_rows(a, *dv);
+    for (const Rows *x : {&rk, &rv})
+        for (const Rows *y : {&q, &k, &v, &g, &rq})
+            if (!apart(*x, *y)) return Q2D_EINVAL;
+    if (!apart(rk, rv) || !apart(rq, k) || !apart(rq, v) || !(same_rows(rq, q) || apart(rq, q)) ||
+        !(same_rows(rq, g) || apart(rq, g)))
+        return Q2D_EINVAL;
     AttentionArgs r = make_args(a, workspace);
     r.dout = view(*dout); r.dq = view(*dq); r.dk = view(*dk); r.dv = view(*dv);
     if (launch_attention_bwd(r, a->dtype == Q2D_F32, stream) != hipSuccess) return Q2D_ELAUNCH;
@@ -289,6 +374,9 @@ static q2d_status kv_copy(const q2d_kv_cache *c, const q2d_sequences *s, q2d_dty
     r = check_rows(k, s->tokens, kst, c->heads, ksh, c->dim, per, !write);
     if (r == Q2D_OK) r = check_rows(v, s->tokens, vst, c->heads, vsh, c->dim, per, !write);
     if (r != Q2D_OK) return r;
+    if (!write && !apart(token_rows(k, s->tokens, kst, c->heads, ksh, c->dim, per),
+                         token_rows(v, s->tokens, vst, c->heads, vsh, c->dim, per)))
+        return Q2D_EINVAL;
     CacheCopyArgs a = {};
     a.cache = cache_view(c);
     a.seq = sequences_view(s);
@@ -339,6 +427,9 @@ q2d_status q2d_attention_cached(const q2d_kv_cache *c, const q2d_sequences *s, c
     const CachedSplit p = split_cached(c, s, a->heads_q);
     r = check_workspace(p.bytes, workspace, workspace_bytes);
     if (r != Q2D_OK) return r;
+    const Rows rows = token_rows(a->q, s->tokens, a->q_stride_token, a->heads_q, a->q_stride_head, c->dim, 8);
+    const Rows out = token_rows(a->out, s->tokens, a->out_stride_token, a->heads_q, a->out_stride_head, c->dim, 8);
+    if (!same_rows(out, rows) && !apart(out, rows)) return Q2D_EINVAL;
     CachedArgs g = {};
     g.cache = cache_view(c);
     g.seq = sequences_view(s);
