@@ -304,7 +304,7 @@ def q2d_attention_cached(q: torch.Tensor, cache: KVCache, block_table: torch.Ten
     """Causal attention of each sequence's last tokens, q [tokens, heads_q, dim] in bfloat16,
     over its keys and values in the cache, these tokens' own among them.  offsets, lens and
     block_table as in q2d_kv_write; scale, window, softcap, slopes and prefix as in
-    q2d_attention_fwd."""
+    q2d_attention_fwd.  Rows outside offsets[0] .. offsets[-1] (a padded batch) are zeros."""
     if q.dim() != 3:
         raise Q2DError("expected q as [tokens, heads, dim]")
     tokens, heads, _ = q.shape

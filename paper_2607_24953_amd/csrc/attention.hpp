@@ -114,6 +114,7 @@ struct CachedArgs {
     int32_t heads_q;
     int32_t units;                               // work units a head to cut long sequences for, 0: do not
     int32_t wide;                                // 128 query rows a workgroup, not 16
+    int32_t grid;                                // workgroups of the units; those past them clear (zero_rows)
     int64_t tiles;                               // bound of the query tiles of all sequences
     float *part;                                 // workspace: [unit][head][rows][dim] sums,
     float *stat;                                 // [unit][head][rows] maximum and sum

@@ -184,9 +184,21 @@ __device__ __forceinline__ bool place_of(const CachedArgs &a, int group, Place &
     return true;
 }
 
+// rows of no sequence: zeros (whoever works on the whole tensor next, as in blocks of rows that share
+// a scale, would otherwise meet what the memory held)
+__device__ __forceinline__ void clear_outside(const CachedArgs &a)
+{
+    const Outside x = outside_of(a.seq);
+    const int64_t first = (int64_t)(blockIdx.x - a.grid) * 256 + threadIdx.x, step = (int64_t)(gridDim.x - a.grid) * 256;
+    __bf16 *out = (__bf16 *)a.out;
+    zero_rows(out, a.out_st, a.out_sh, x.lo, a.heads_q, a.cache.dim, first, step);
+    zero_rows(out + x.hi * a.out_st, a.out_st, a.out_sh, a.seq.tokens - x.hi, a.heads_q, a.cache.dim, first, step);
+}
+
 template <int DT, int MODS>
 __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedArgs a)
 {
+    if (blockIdx.x >= (uint32_t)a.grid) return clear_outside(a);
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2;
     constexpr int KS = DT / 32, VT = DT / 16, ROWS = 16;
     // two waves' sums [row][dim] at a time, and all waves' statistics
@@ -392,6 +404,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
 template <int DC, int MODS>
 __global__ __launch_bounds__(256, 2) void attention_cached_rows_kernel(const CachedArgs a)
 {
+    if (blockIdx.x >= (uint32_t)a.grid) return clear_outside(a);
     constexpr bool CAP = MODS & 1, BIAS = MODS & 2;
     constexpr int DT = DC <= 64 ? 64 : 128, KS = DC / 16, DS = DC / 32, ROWS = 128;
     constexpr int kPasses = kSuper * DT / (16 * 256);          // 16-byte loads of a thread, keys or values
@@ -678,12 +691,14 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const CachedArgs a)
 
 // ROWS: query rows of a workgroup, 128 or 16
 template <int DC, int MODS, int ROWS>
-hipError_t launch(const CachedArgs &a, hipStream_t stream)
+hipError_t launch(CachedArgs a, hipStream_t stream)
 {
     // (every tile has a unit, and the parts of W / units super-blocks are no more than units)
     constexpr int groups = ROWS / (4 * kJoinRows<ROWS>);
-    const int64_t tiles = a.tiles * a.cache.heads, n = (a.tiles + a.units) * a.cache.heads;
+    const int64_t tiles = a.tiles * a.cache.heads, units = (a.tiles + a.units) * a.cache.heads;
+    const int64_t n = units + (a.seq.offsets ? zero_groups(a.seq.tokens) : 0);
     if (n > INT32_MAX || tiles * groups > INT32_MAX) return hipErrorInvalidConfiguration;
+    a.grid = (int32_t)units;
     if constexpr (ROWS == 16) attention_cached_kernel<DC, MODS><<<(uint32_t)n, 256, 0, stream>>>(a);
     else attention_cached_rows_kernel<DC, MODS><<<(uint32_t)n, 256, 0, stream>>>(a);
     if (a.units > 0) attention_join_kernel<ROWS><<<(uint32_t)(tiles * groups), 256, 0, stream>>>(a);

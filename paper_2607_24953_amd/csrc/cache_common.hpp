@@ -33,6 +33,34 @@ __device__ __forceinline__ Span span_of(const SequencesView &s, int page_tokens,
     return r;
 }
 
+// Rows of the token tensors that belong to no sequence: [0, lo) and [hi, tokens)
+struct Outside { int64_t lo, hi; };
+
+__device__ __forceinline__ Outside outside_of(const SequencesView &s)
+{
+    Outside r = {0, s.tokens};
+    if (s.offsets) {
+        r.lo = min(max(s.offsets[0], (int64_t)0), s.tokens);
+        r.hi = min(max(s.offsets[s.batch], r.lo), s.tokens);
+    }
+    return r;
+}
+
+// Zeros in n rows [heads][dim] from x on (strides in elements), by threads first, first + step, ..
+template <typename T>
+__device__ __forceinline__ void zero_rows(T *x, int64_t st, int64_t sh, int64_t n, int heads, int dim, int64_t first, int64_t step)
+{
+    const int chunks = dim * (int)sizeof(T) / 16, row = heads * chunks;
+    for (int64_t i = first; i < n * row; i += step) {
+        const int64_t r = i / row;
+        const int c = (int)(i % row);
+        *reinterpret_cast<u4v *>(x + r * st + c / chunks * sh + c % chunks * (16 / (int)sizeof(T))) = u4v{0, 0, 0, 0};
+    }
+}
+
+// workgroups that do so beside a call's own: a call that leaves no such rows has them look once
+inline int zero_groups(int64_t tokens) { return tokens < 256 ? 1 : tokens > 65536 ? 256 : (int)(tokens / 256); }
+
 // Unit `index` of all sequences' units, sequence b having count(span) of them: its
 // sequence, its number there and the span; b = -1 past the last.  One full wave, the same
 // answer in all lanes.
