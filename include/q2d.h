@@ -468,9 +468,9 @@ q2d_status q2d_kv_cache_init(q2d_kv_cache *c, int32_t pages, int32_t heads, int3
  * All three arrays are read on the device, where they cannot be checked before a launch:
  * offsets are clamped to [0, tokens] and each to the one before it, lens to [0, table_pages *
  * page_size], and a table entry outside [0, pages) names no page: its tokens are not
- * written, read back as nothing and not seen.  Rows of the token tensors outside [offsets[0],
+ * written, read back as zeros and not seen.  Rows of the token tensors outside [offsets[0],
  * offsets[batch]) belong to no sequence, and of more rows than lens[b] the first ones lie before
- * the sequence: nothing is written for them, and attention gives zeros.
+ * the sequence: nothing is written for them, and what is read or attended for them is zeros.
  */
 typedef struct {
     int32_t batch, table_pages;  /* table_pages: entries of a table row */

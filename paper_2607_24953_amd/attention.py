@@ -283,7 +283,8 @@ def q2d_kv_read(cache: KVCache, block_table: torch.Tensor, lens: torch.Tensor, t
                 offsets: torch.Tensor | None = None, out_dtype=torch.float32,
                 k: torch.Tensor | None = None, v: torch.Tensor | None = None):
     """Values (k, v) [tokens, heads, dim] of each sequence's last tokens (offsets as in
-    q2d_kv_write, ``tokens`` in all)."""
+    q2d_kv_write, ``tokens`` in all); zeros in rows of no sequence, before a sequence's first
+    token and on pages that the table does not name."""
     shape = (int(tokens), cache.heads, cache.dim)
     k = torch.empty(shape, dtype=out_dtype, device=cache.device) if k is None else k
     v = torch.empty(shape, dtype=k.dtype, device=cache.device) if v is None else v

@@ -74,7 +74,8 @@ __device__ __forceinline__ int touched(const Span &s)
     return n == 0 ? 0 : (s.len + kBlockTokens - 1) / kBlockTokens - (s.len - n) / kBlockTokens;
 }
 
-// One wave's work: block `block` of sequence b, slots [lo, hi) of it, rows `row0` + slot
+// One wave's work: block `block` of sequence b (at: its number, -1 on no page), slots [lo, hi)
+// of it, rows `row0` + slot
 struct Unit {
     int64_t at, row0;
     int lo, hi, head;
@@ -99,14 +100,14 @@ __device__ __forceinline__ bool take_unit(const CacheCopyArgs &a, Unit &u)
     u.hi = min(s.len - block * kBlockTokens, kBlockTokens);
     u.row0 = s.tok0 + (s.n - n) + (int64_t)block * kBlockTokens - first;
     u.at = cache_block(a.cache, a.seq, b, block, u.head);
-    return u.at >= 0;
+    return true;
 }
 
 template <typename T>
 __global__ __launch_bounds__(256) void kv_write_kernel(const CacheCopyArgs a)
 {
     Unit u;
-    if (!take_unit(a, u)) return;
+    if (!take_unit(a, u) || u.at < 0) return;
     const int lane = threadIdx.x & 63, tg = lane >> 4, dg = lane & 15, D = a.cache.dim, s0 = 8 * tg;
     const bool on = 8 * dg < D;
     const T *x = (const T *)(u.values ? a.v : a.k) + u.head * (u.values ? a.v_sh : a.k_sh) + 8 * dg;
@@ -180,18 +181,46 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const CacheCopyArgs a)
     if (lane == 0) *scale_at = (uint8_t)byte;
 }
 
+// Rows that no token stands behind are zeros: those of no sequence, and a sequence's before its
+// first position
 template <typename T>
-__global__ __launch_bounds__(256) void kv_read_kernel(const CacheCopyArgs a)
+__device__ __forceinline__ void clear_rows(const CacheCopyArgs &a, int group, int groups)
 {
+    T *k = (T *)a.k, *v = (T *)a.v;
+    auto clear = [&](int64_t row, int64_t n, int64_t first, int64_t step) {
+        zero_rows(k + row * a.k_st, a.k_st, a.k_sh, n, a.cache.heads, a.cache.dim, first, step);
+        zero_rows(v + row * a.v_st, a.v_st, a.v_sh, n, a.cache.heads, a.cache.dim, first, step);
+    };
+    const int64_t thread = group * 256 + threadIdx.x, threads = groups * 256;
+    const Outside x = outside_of(a.seq);
+    clear(0, x.lo, thread, threads);
+    clear(x.hi, a.seq.tokens - x.hi, thread, threads);
+    const int lane = threadIdx.x & 63;
+    for (int64_t base = thread - lane; base < a.seq.batch; base += threads) {
+        Span s = {0, 0, 0};
+        if (base + lane < a.seq.batch) s = span_of(a.seq, a.cache.page_blocks * kBlockTokens, (int)base + lane);
+        for (uint64_t some = __ballot(s.n > s.len); some; some &= some - 1) {
+            const int at = __builtin_ctzll(some);
+            clear(__shfl(s.tok0, at), __shfl(s.n - s.len, at), lane, 64);
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void kv_read_kernel(const CacheCopyArgs a, int grid)
+{
+    if (blockIdx.x >= (uint32_t)grid) return clear_rows<T>(a, blockIdx.x - grid, gridDim.x - grid);
     Unit u;
     if (!take_unit(a, u)) return;
     const int lane = threadIdx.x & 63, tg = lane >> 4, dg = lane & 15, D = a.cache.dim, s0 = 8 * tg;
     if (8 * dg >= D) return;
     T *x = (T *)(u.values ? a.v : a.k) + u.head * (u.values ? a.v_sh : a.k_sh) + 8 * dg;
     const int64_t st = u.values ? a.v_st : a.k_st, base = u.at * kBlockTokens * D;
-    const uint32_t byte = *((u.values ? a.cache.vs : a.cache.ks) + u.at);
-    float e[8][8];
-    if (!u.values) {
+    float e[8][8] = {};
+    const uint32_t byte = u.at < 0 ? 0 : *((u.values ? a.cache.vs : a.cache.ks) + u.at);
+    if (u.at < 0) {
+        // (no page: zeros)
+    } else if (!u.values) {
         const uint8_t *p = a.cache.k + base + 8 * dg;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -246,10 +275,11 @@ hipError_t launch_kv_write(const CacheCopyArgs &a, bool f32, hipStream_t stream)
 hipError_t launch_kv_read(const CacheCopyArgs &a, bool f32, hipStream_t stream)
 {
     const int64_t grid = grid_of(a);
-    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    const uint32_t all = (uint32_t)grid + zero_groups(a.seq.tokens > a.seq.batch ? a.seq.tokens : a.seq.batch);
+    if (grid > INT32_MAX - 256) return hipErrorInvalidConfiguration;
     if (grid == 0) return hipSuccess;
-    if (f32) kv_read_kernel<float><<<(uint32_t)grid, 256, 0, stream>>>(a);
-    else kv_read_kernel<__bf16><<<(uint32_t)grid, 256, 0, stream>>>(a);
+    if (f32) kv_read_kernel<float><<<all, 256, 0, stream>>>(a, (int)grid);
+    else kv_read_kernel<__bf16><<<all, 256, 0, stream>>>(a, (int)grid);
     return hipGetLastError();
 }
 

@@ -1,4 +1,5 @@
-"""Rows of no sequence (a padded batch) are zeros."""
+"""Rows that no token of a sequence stands behind are zeros: rows of no sequence (a padded batch),
+and for reads also tokens on missing pages and rows before a sequence's first position."""
 import math
 
 import pytest
@@ -41,3 +42,45 @@ def test_attention_leaves_the_gaps_of_a_strided_output(q2d):
     q2d.q2d_attention_cached(torch.ones((9, 4, 64), dtype=torch.bfloat16, device="cuda"), p.cache, p.table.cuda(),
                              p.lens().cuda(), torch.tensor([1, 3]).cuda(), out=out[..., :64])
     assert bool((out[..., 64:] == 7).all()) and not out[3:, :, :64].any() and not out[:1, :, :64].any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("heads,dim", [(1, 16), (3, 80), (2, 128)])
+def test_read(q2d, heads, dim, dtype):
+    p = filled(q2d, [200, 65, 3], heads, dim)
+    table = p.table.clone()
+    table[0, 1], table[1, 0] = -1, p.cache.pages          # tokens 64 .. 127 and 0 .. 63 are on no page
+    off = torch.tensor([2, 152, 217, 227])                # of 3 tokens, 10 rows
+    k, v = (torch.full((240, heads, dim), math.nan, dtype=dtype, device="cuda") for _ in range(2))
+    q2d.q2d_kv_read(p.cache, table.cuda(), p.lens().cuda(), 240, off.cuda(), k=k, v=v)
+    for got, which in ((k, 0), (v, 1)):
+        want = torch.zeros((240, heads, dim), dtype=torch.float64)
+        for b, (lo, hi, n) in enumerate(((2, 152, 200), (152, 217, 65), (217, 227, 3))):
+            x = p.dense(b)[which]
+            m = min(hi - lo, n)
+            want[hi - m:hi] = x[n - m:]
+        want[2 + 14:2 + 78] = 0                           # positions 50 .. 199 in rows 2 .. 151
+        want[152:152 + 64] = 0
+        assert torch.equal(got.cpu().double(), want)
+
+
+@pytest.mark.parametrize("name", sorted(OFFSETS))
+def test_read_of_no_sequence(q2d, name):
+    p = filled(q2d, [70, 65, 60], 2, 64)
+    k, v = (torch.full((12, 2, 64), math.nan, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    off = torch.tensor(OFFSETS[name])
+    q2d.q2d_kv_read(p.cache, p.table.cuda(), p.lens().cuda(), 12, off.cuda(), k=k, v=v)
+    lo, hi = int(off[0].clamp(0, 12)), int(off[-1].clamp(0, 12))
+    for x in (k, v):
+        assert not x[:lo].any() and not x[hi:].any() and bool(x[lo:hi].any(-1).all()) and torch.isfinite(x).all()
+
+
+def test_read_without_offsets(q2d):
+    """Equally many rows each, more than the sequences have tokens."""
+    p = filled(q2d, [5, 1, 0], 2, 64)
+    k, v = (torch.full((24, 2, 64), math.nan, dtype=torch.float32, device="cuda") for _ in range(2))
+    q2d.q2d_kv_read(p.cache, p.table.cuda(), p.lens().cuda(), 24, k=k, v=v)
+    for x, which in ((k, 0), (v, 1)):
+        want = torch.zeros((24, 2, 64), dtype=torch.float64)
+        want[3:8], want[15:16] = p.dense(0)[which], p.dense(1)[which]
+        assert torch.equal(x.cpu().double(), want)
