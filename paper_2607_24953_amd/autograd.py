@@ -108,23 +108,26 @@ class Q2DLinear(torch.nn.Module):
 
 class _AttentionFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, mask):
-        out, lse = q2d_attention_fwd(q, k, v, **mask)
-        ctx.save_for_backward(q, k, v, out, lse)
-        ctx.mask = mask
+    def forward(ctx, q, k, v, scalars, slopes, documents, prefix):
+        out, lse = q2d_attention_fwd(q, k, v, *scalars, slopes, documents, prefix)
+        # (the masks too: backward has to meet those of the forward call)
+        ctx.save_for_backward(q, k, v, out, lse, slopes, documents, prefix)
+        ctx.scalars = scalars
         return out
 
     @staticmethod
     def backward(ctx, dout):
-        q, k, v, out, lse = ctx.saved_tensors
+        q, k, v, out, lse, *masks = ctx.saved_tensors
         if dout.stride(-1) != 1 or any(s % 8 for s in dout.stride()[:-1]) or dout.data_ptr() % 16:
             dout = dout.contiguous()
-        dq, dk, dv = q2d_attention_bwd(dout, q, k, v, out, lse, **ctx.mask)
-        return dq, dk, dv, None
+        dq, dk, dv = q2d_attention_bwd(dout, q, k, v, out, lse, *ctx.scalars, *masks)
+        return dq, dk, dv, None, None, None, None
 
 
-def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, **mask) -> torch.Tensor:
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float | None = None, causal: bool = True,
+              window: int = 0, softcap: float = 0.0, slopes: torch.Tensor | None = None,
+              documents: torch.Tensor | None = None, prefix: torch.Tensor | None = None) -> torch.Tensor:
     """Attention of q [batch, len_q, heads_q, dim] on k, v [batch, len_k, heads_kv, dim] with
-    gradients for q, k and v; ``mask``: scale, causal, window, softcap, slopes, documents and
-    prefix as in q2d_attention_fwd (slopes get no gradient)."""
-    return _AttentionFunction.apply(q, k, v, mask)
+    gradients for q, k and v; the other arguments as in
+    q2d_attention_fwd (slopes get no gradient)."""
+    return _AttentionFunction.apply(q, k, v, (scale, causal, window, softcap), slopes, documents, prefix)
