@@ -34,6 +34,7 @@ import itertools
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import (FP4_1D, FP4_2D, Q2DError, q2d_attention_bwd, q2d_attention_fwd, q2d_linear_bwd,
                q2d_linear_fwd)
@@ -116,6 +117,7 @@ class _AttentionFunction(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q, k, v, out, lse, *masks = ctx.saved_tensors
         if dout.stride(-1) != 1 or any(s % 8 for s in dout.stride()[:-1]) or dout.data_ptr() % 16:
@@ -128,6 +130,6 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float | 
               window: int = 0, softcap: float = 0.0, slopes: torch.Tensor | None = None,
               documents: torch.Tensor | None = None, prefix: torch.Tensor | None = None) -> torch.Tensor:
     """Attention of q [batch, len_q, heads_q, dim] on k, v [batch, len_k, heads_kv, dim] with
-    gradients for q, k and v; the other arguments as in
+    gradients for q, k and v (once: these have none of their own); the other arguments as in
     q2d_attention_fwd (slopes get no gradient)."""
     return _AttentionFunction.apply(q, k, v, (scale, causal, window, softcap), slopes, documents, prefix)

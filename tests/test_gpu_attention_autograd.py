@@ -25,6 +25,14 @@ def test_masks_changed_in_place(name):
         out.sum().backward()
 
 
+def test_no_second_derivative():
+    """The gradients are computed outside of autograd: asking for their own is an error."""
+    out, inputs = make()
+    grads = torch.autograd.grad(out.float().square().sum(), inputs, create_graph=True)
+    with pytest.raises(RuntimeError):
+        (out.float().sum() + sum(g.float().sum() for g in grads)).backward()
+
+
 def test_arguments_are_refused_in_forward():
     for kw in (dict(out=None), dict(need_lse=False), dict(caual=True)):
         with pytest.raises(TypeError):
