@@ -120,8 +120,10 @@ class _AttentionFunction(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dout):
         q, k, v, out, lse, *masks = ctx.saved_tensors
-        if dout.stride(-1) != 1 or any(s % 8 for s in dout.stride()[:-1]) or dout.data_ptr() % 16:
-            dout = dout.contiguous()
+        # (a copy of what q2d_attention_bwd does not take; contiguous() keeps an offset)
+        *strides, last = dout.stride()
+        if last != 1 or any(s % 8 for s in strides) or strides[1] >= 1 << 22 or dout.data_ptr() % 16:
+            dout = dout.clone(memory_format=torch.contiguous_format)
         dq, dk, dv = q2d_attention_bwd(dout, q, k, v, out, lse, *ctx.scalars, *masks)
         return dq, dk, dv, None, None, None, None
 

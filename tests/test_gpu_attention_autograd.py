@@ -37,3 +37,20 @@ def test_arguments_are_refused_in_forward():
     for kw in (dict(out=None), dict(need_lse=False), dict(caual=True)):
         with pytest.raises(TypeError):
             make(**kw)
+
+
+def test_gradient_off_16_bytes():
+    """A gradient that is a contiguous slice at any offset (attention's output behind others in one
+    tensor), and one whose rows lie 2^22 elements apart."""
+    from paper_2607_24953_amd.autograd import attention
+    g = torch.Generator().manual_seed(82)
+    q, k, v, w = (torch.randn((1, 70, 2, 64), generator=g).to(torch.bfloat16).cuda().requires_grad_() for _ in range(4))
+    want = torch.autograd.grad(attention(q, k, v), (q, k, v), w.detach())
+    lead = torch.zeros(3, dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    out = torch.cat((lead, attention(q, k, v).flatten()))
+    got = torch.autograd.grad(out, (q, k, v), torch.cat((lead.detach(), w.detach().flatten())))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    far = torch.empty(69 * 2 ** 22 + 128, dtype=torch.bfloat16, device="cuda").as_strided((1, 70, 2, 64), (0, 2 ** 22, 64, 1))
+    far.copy_(w.detach())
+    got = torch.autograd.grad(attention(q, k, v), (q, k, v), far)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
