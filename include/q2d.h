@@ -388,6 +388,7 @@ q2d_status q2d_grouped_gemm(const q2d_tensor *A, int transA, const q2d_tensor *B
  * heads_q is a multiple of heads_kv; query head h reads key head h / (heads_q / heads_kv).
  * dim is a multiple of 8 up to 128 (Q2D_EUNSUPPORTED otherwise).  Lengths are 1 to 2^30.
  *
+ * Scores are float32: of ones beyond 2^24 the weights lose their digits, as lse does.
  * Sums, softmax statistics and the gradients' accumulators are float32.  bfloat16 operands
  * run on bf16 MFMA with the probabilities (and dS) rounded to bfloat16 for the second
  * products; float32 operands on float32 MFMA.
@@ -408,8 +409,8 @@ typedef struct {
     int32_t batch, heads_q, heads_kv, dim;
     int64_t len_q, len_k;
     int64_t window;          /* 0: no window */
-    float scale;             /* > 0 */
-    float softcap;           /* 0: no cap; > 0 otherwise */
+    float scale;             /* > 0, 2^-60 to 2^60 (Q2D_EUNSUPPORTED beyond) */
+    float softcap;           /* 0: no cap; > 0 otherwise, the same range */
     const float *slopes;     /* device [heads_q], or NULL: no distance bias */
     const int32_t *documents;/* device [batch][len_k], or NULL; a negative number is padding */
     const int32_t *prefix;   /* device [batch], or NULL; clamped to [0, len_k] */

@@ -15,6 +15,15 @@ constexpr int64_t kMaxPitch = int64_t(1) << 22;    // the tile loads' 32-bit row
 inline bool on16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 inline int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 
+// scale > 0, softcap >= 0; both within 2^-60 .. 2^60, where what the kernels form of them (their
+// quotient, and scores' units by either) stays within float32
+q2d_status check_scale(float scale, float softcap)
+{
+    if (!(scale > 0.f) || !isfinite(scale) || !(softcap >= 0.f) || !isfinite(softcap)) return Q2D_EINVAL;
+    auto fits = [](float x) { return x >= 0x1p-60f && x <= 0x1p60f; };
+    return fits(scale) && (softcap == 0.f || fits(softcap)) ? Q2D_OK : Q2D_EUNSUPPORTED;
+}
+
 // whole 16-byte rows, and a last element within 2^47
 q2d_status check_heads(const q2d_heads &t, int64_t batch, int64_t length, int64_t heads, int64_t dim, int per)
 {
@@ -118,7 +127,8 @@ q2d_status check_sizes(const q2d_attention *a)
         a->len_q <= 0 || a->len_k <= 0 || a->window < 0)
         return Q2D_EINVAL;
     if (a->heads_q % a->heads_kv != 0) return Q2D_EINVAL;
-    if (!(a->scale > 0.f) || !isfinite(a->scale) || !(a->softcap >= 0.f) || !isfinite(a->softcap)) return Q2D_EINVAL;
+    const q2d_status s = check_scale(a->scale, a->softcap);
+    if (s != Q2D_OK) return s;
     if (a->dim % 8 != 0 || a->dim > 128 || a->len_q > kMaxLen || a->len_k > kMaxLen) return Q2D_EUNSUPPORTED;
     int64_t rows, n;
     if (__builtin_mul_overflow((int64_t)a->batch * a->heads_q, a->len_q > a->len_k ? a->len_q : a->len_k, &rows) ||
@@ -417,7 +427,8 @@ q2d_status q2d_attention_cached(const q2d_kv_cache *c, const q2d_sequences *s, c
     if (a->dtype != Q2D_F32 && a->dtype != Q2D_BF16) return Q2D_EINVAL;
     if (a->dtype != Q2D_BF16) return Q2D_EUNSUPPORTED;
     if (a->heads_q <= 0 || a->heads_q % c->heads != 0 || a->window < 0) return Q2D_EINVAL;
-    if (!(a->scale > 0.f) || !isfinite(a->scale) || !(a->softcap >= 0.f) || !isfinite(a->softcap)) return Q2D_EINVAL;
+    r = check_scale(a->scale, a->softcap);
+    if (r != Q2D_OK) return r;
     if (!on4(a->slopes) || !on4(a->prefix)) return Q2D_EINVAL;
     if (s->tokens == 0) return Q2D_OK;
     if (s->tokens > INT32_MAX / a->heads_q) return Q2D_EUNSUPPORTED;
