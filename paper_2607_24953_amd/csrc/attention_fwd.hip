@@ -230,6 +230,10 @@ void attention_fwd_kernel(const AttentionArgs a)
         sum = total;
     }
     if (!row) return;
+    // (a row that sees keys sees its own position, or keys below and beside it; of scores that are
+    // all -infinity the softmax is NaN)
+    const bool sees = docs ? my_doc >= 0 : p >= 0 || prefix > 0 || sight.hi > max(sight.lo, 0);
+    if (sum == 0.f && sees) sum = __builtin_nanf("");
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T *out = (T *)a.out.p + b * a.out.sb + (int64_t)i * a.out.sl + hq * a.out.sh;
     store_columns<T, DS>(out, o, inv, h, D);

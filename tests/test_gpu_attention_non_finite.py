@@ -133,3 +133,31 @@ def test_shared_heads_in_parts(q2d, D, dtype):
     assert torch.isfinite(dv).all()
     assert torch.equal(torch.isfinite(dk[0, :, 0]).all(-1), ~sees)
     assert torch.isfinite(dq[:, :, [0, 1, 3]]).all()
+
+
+@DTYPES
+@HEADS
+@DIMS
+@pytest.mark.parametrize("name", ["causal", "documents", "window"])
+def test_rows_with_scores_of_minus_infinity_alone(q2d, name, D, H, dtype):
+    """A softmax over nothing but -infinity is NaN, not the zeros of a row that sees nothing."""
+    args = make(1, 160, 160, H, H, D, dtype, seed=58)
+    args[0][..., 5] = -1.0 - args[0][..., 5].abs()
+    args[1][:, 0, :, 5] = args[1][:, 59, :, 5] = math.inf
+    out = pattern(q2d, args, **MASKS[name])[0]
+    assert torch.isnan(out[:, 0]).all() and torch.isfinite(out[:, 1]).all()
+    if name == "documents":
+        assert not out[:, 50:59].any() and torch.isnan(out[:, 59]).all()
+
+
+def test_more_queries_than_keys_see_nothing(q2d):
+    """Rows before the first key, with and without a prefix."""
+    q, k, v, _ = make(1, 100, 40, 2, 2, 64, torch.bfloat16, seed=59)
+    out, lse = q2d.q2d_attention_fwd(q, k, v)
+    assert not out[:, :60].any() and bool((lse[:, :, :60] == -math.inf).all()) and torch.isfinite(lse[:, :, 60:]).all()
+    out, lse = q2d.q2d_attention_fwd(q, k, v, window=7)
+    assert not out[:, :60].any() and bool((lse[:, :, :60] == -math.inf).all()) and torch.isfinite(lse[:, :, 60:]).all()
+    for mask in (dict(prefix=torch.tensor([3], dtype=torch.int32).cuda()), dict(causal=False)):
+        assert torch.isfinite(q2d.q2d_attention_fwd(q, k, v, **mask)[1]).all()
+    lse = q2d.q2d_attention_fwd(q, k, v, causal=False, window=20)[1]      # |p - j| < 20: from position -19 on
+    assert bool((lse[:, :, :41] == -math.inf).all()) and torch.isfinite(lse[:, :, 41:]).all()
