@@ -474,7 +474,7 @@ q2d_status q2d_kv_cache_init(q2d_kv_cache *c, int32_t pages, int32_t heads, int3
  * the sequence: nothing is written for them, and what is read or attended for them is zeros.
  */
 typedef struct {
-    int32_t batch, table_pages;  /* table_pages: entries of a table row */
+    int32_t batch, table_pages;  /* entries of a table row; table_pages * page_size <= 2^30 */
     int64_t tokens, table_stride;
     const int64_t *offsets;      /* device [batch + 1], ascending, or NULL */
     const int32_t *lens;         /* device [batch] */

@@ -231,17 +231,19 @@ q2d_status check_cache(const q2d_kv_cache *c)
     return Q2D_OK;
 }
 
-q2d_status check_sequence_sizes(const q2d_sequences *s)
+// (a sequence's positions, sums of two of them and a tile's beyond its end stay within 32 bits)
+q2d_status check_sequence_sizes(const q2d_kv_cache &c, const q2d_sequences *s)
 {
     if (!s || s->batch <= 0 || s->tokens < 0 || s->table_pages <= 0 || s->table_stride < s->table_pages) return Q2D_EINVAL;
     if (!s->offsets && s->tokens % s->batch != 0) return Q2D_EINVAL;
     if (s->tokens > kMaxLen || s->batch > (1 << 20) || s->table_stride > kMaxLen) return Q2D_EUNSUPPORTED;
+    if ((int64_t)s->table_pages * c.page_size > kMaxLen) return Q2D_EUNSUPPORTED;
     return Q2D_OK;
 }
 
-q2d_status check_sequences(const q2d_sequences *s)
+q2d_status check_sequences(const q2d_kv_cache &c, const q2d_sequences *s)
 {
-    const q2d_status r = check_sequence_sizes(s);
+    const q2d_status r = check_sequence_sizes(c, s);
     if (r != Q2D_OK) return r;
     if (!s->lens || !s->table || !on4(s->lens) || !on4(s->table) || (reinterpret_cast<uintptr_t>(s->offsets) & 7) != 0)
         return Q2D_EINVAL;
@@ -376,7 +378,7 @@ static q2d_status kv_copy(const q2d_kv_cache *c, const q2d_sequences *s, q2d_dty
                           int64_t ksh, const void *v, int64_t vst, int64_t vsh, bool write, hipStream_t stream)
 {
     q2d_status r = check_cache(c);
-    if (r == Q2D_OK) r = check_sequences(s);
+    if (r == Q2D_OK) r = check_sequences(*c, s);
     if (r != Q2D_OK) return r;
     if (dt != Q2D_F32 && dt != Q2D_BF16) return Q2D_EINVAL;
     const int per = dt == Q2D_F32 ? 4 : 8;
@@ -412,7 +414,7 @@ q2d_status q2d_kv_read(const q2d_kv_cache *c, const q2d_sequences *s, q2d_dtype 
 
 int64_t q2d_attention_cached_workspace(const q2d_kv_cache *c, const q2d_sequences *s, int32_t heads_q)
 {
-    if (!c || !s || check_cache_sizes(*c) != Q2D_OK || check_sequence_sizes(s) != Q2D_OK) return -1;
+    if (!c || !s || check_cache_sizes(*c) != Q2D_OK || check_sequence_sizes(*c, s) != Q2D_OK) return -1;
     if (heads_q <= 0 || heads_q % c->heads != 0) return -1;
     return split_cached(c, s, heads_q).bytes;
 }
@@ -421,7 +423,7 @@ q2d_status q2d_attention_cached(const q2d_kv_cache *c, const q2d_sequences *s, c
                                 void *workspace, int64_t workspace_bytes, hipStream_t stream)
 {
     q2d_status r = check_cache(c);
-    if (r == Q2D_OK) r = check_sequences(s);
+    if (r == Q2D_OK) r = check_sequences(*c, s);
     if (r != Q2D_OK) return r;
     if (!a) return Q2D_EINVAL;
     if (a->dtype != Q2D_F32 && a->dtype != Q2D_BF16) return Q2D_EINVAL;

@@ -26,3 +26,23 @@ def test_scale_and_cap(q2d, bad):
 def test_ends_of_the_range(q2d):
     for ok in (dict(scale=2.0 ** -60), dict(scale=2.0 ** 60), dict(softcap=2.0 ** -60), dict(softcap=2.0 ** 60)):
         assert q2d._lib.q2d_attention_workspace(ctypes.byref(problem(q2d, **ok)), 0) == 0
+
+
+@pytest.mark.parametrize("page_size,table_pages", [(65536, 2 ** 14 + 1), (65536, 2 ** 15), (64, 2 ** 24 + 1), (1024, 2 ** 22)], ids=str)
+def test_tables_of_too_many_tokens(q2d, page_size, table_pages):
+    """A sequence's tokens are counted in 32 bits, with sums of two positions among them: its
+    table may name 2^30."""
+    from paper_2607_24953_amd import attention as A
+    c, s = cache_of(q2d, page_size=page_size, table_pages=table_pages, table_stride=table_pages)
+    L = q2d._lib
+    for f in (L.q2d_kv_write, L.q2d_kv_read):
+        assert f(ctypes.byref(c), ctypes.byref(s), 1, FAKE, 128, 64, FAKE + (1 << 20), 128, 64, None) == 2
+    a = A._CachedAttention(dtype=1, heads_q=8, scale=0.1, q=FAKE, q_stride_token=512, q_stride_head=64, out=FAKE + (1 << 20),
+                           out_stride_token=512, out_stride_head=64)
+    assert L.q2d_attention_cached(ctypes.byref(c), ctypes.byref(s), ctypes.byref(a), FAKE, 1 << 40, None) == 2
+    assert L.q2d_attention_cached_workspace(ctypes.byref(c), ctypes.byref(s), 8) == -1
+
+
+def test_the_longest_table(q2d):
+    c, s = cache_of(q2d, page_size=65536, table_pages=2 ** 14, table_stride=2 ** 14)
+    assert q2d._lib.q2d_attention_cached_workspace(ctypes.byref(c), ctypes.byref(s), 8) >= 0
