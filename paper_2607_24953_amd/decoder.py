@@ -82,9 +82,14 @@ class Decoder(torch.nn.Module):
 
     @torch.no_grad()
     def generate(self, prompts, count, page_size=64):
-        """Greedy continuations [len(prompts), count] of a list of prompts (1-D token tensors)."""
+        """Greedy continuations [len(prompts), count] of a list of prompts (1-D token tensors, none
+        of them empty: there is nothing to continue)."""
         device = self.slopes.device
         n = [len(p) for p in prompts]
+        if not n or min(n) == 0 or count < 0:
+            raise ValueError("prompts of one token or more, and a count of 0 or more, are expected")
+        if count == 0:
+            return torch.empty((len(n), 0), dtype=torch.int64, device=device)
         per = -(-(max(n) + count) // page_size)
         caches = self.caches(len(n) * per, page_size)
         table = torch.arange(len(n) * per, dtype=torch.int32, device=device).view(len(n), per)
