@@ -68,10 +68,12 @@ def _on(device, t):
         _same_device(device, t)
 
 
-def _vector(t, n, dtype, device, what):
-    """Pointer of an optional contiguous device vector or matrix of n elements."""
+def _vector(t, n, dtype, device, what, shape=None):
+    """Pointer of an optional contiguous device vector of n elements, or a tensor of ``shape``."""
     if t is None:
         return None
+    if shape is not None and t.dim() != 1 and t.shape != shape:
+        raise Q2DError("%s: a tensor of shape %s is expected" % (what, shape))
     if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
         raise Q2DError("%s: a contiguous %s tensor of %d elements is expected" % (what, dtype, n))
     _on(device, t)
@@ -122,10 +124,10 @@ def _problem(q, k, v, out, lse, scale, causal, window, softcap, slopes, document
     if slopes is not None:
         a.slopes = _vector(slopes, Hq, torch.float32, device, "slopes")
     if documents is not None:
-        a.documents = _vector(documents, B * Lk, torch.int32, device, "documents")
+        a.documents = _vector(documents, B * Lk, torch.int32, device, "documents", (B, Lk))
     if prefix is not None:
         a.prefix = _vector(prefix, B, torch.int32, device, "prefix")
-    a.lse = _vector(lse, B * Hq * Lq, torch.float32, device, "lse")
+    a.lse = _vector(lse, B * Hq * Lq, torch.float32, device, "lse", (B, Hq, Lq))
     return a, sizes
 
 
