@@ -303,7 +303,7 @@ __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const
         if (docs && wave < (BN + 63) / 64) load_words64(&doc_of[stage][64 * wave], docs, t * BN + 64 * wave, a.len_k);
     };
     tile_loop<NS, 2 * kBytes / (NW * 1024)>(end, see, fetch, check, tile);
-    if (left_out)
+    if (__builtin_expect(left_out, false))
         add_rows<BN, WN>(end, see, jw, a.len_k, k, a.k.sl, k, a.k.sl, D, [&](int j) __attribute__((always_inline)) {
             const T *kj = k + (int64_t)j * a.k.sl, *vj = v + (int64_t)j * a.v.sl;
             const float qk = row_dot(q, row, kj, h, D), dp = row_dot(g, row, vj, h, D);
@@ -523,7 +523,7 @@ __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1)
         tile_loop<NS, 2 * kBytes / (NW * 1024)>(end, see, fetch, check, tile);
         block_barrier();           // the next head's first tile takes stage 0
     }
-    for (int gh = first; left_out && gh < last; ++gh) {
+    for (int gh = first; __builtin_expect(left_out, false) && gh < last; ++gh) {
         const int hq = hk * group + gh;
         const T *q = (const T *)a.q.p + b * a.q.sb + hq * a.q.sh;
         const T *g = (const T *)a.dout.p + b * a.dout.sb + hq * a.dout.sh;
@@ -740,7 +740,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
             float back = 1.f;
 #pragma unroll
             for (int x = 0; x < 4; ++x) bits |= half[0][x] | half[1][x];
-            if (__any((bits & 0x7c007c00u) == 0)) {
+            if (__builtin_expect(__any((bits & 0x7c007c00u) == 0), false)) {
                 float top = 0.f;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) top = fmaxf(top, CAP ? pu[r] : z[r]);
@@ -799,7 +799,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
 #pragma unroll
                 for (int r = 0; r < 16; ++r) e[r] = p_of(r) != 0.f ? e[r] : 0.f;
             }
-            if (__any(back != 1.f)) e *= back;
+            if (__builtin_expect(__any(back != 1.f), false)) e *= back;
             Frag<T> ef;
             unroll<2 * DS>([&](auto yc) __attribute__((always_inline)) {
                 constexpr int y = decltype(yc)::value, i = t * kStep + KS + y;
@@ -841,7 +841,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const Attent
         }
         const T *kj = (const T *)a.k.p + b * a.k.sb + (int64_t)j * a.k.sl + hk * a.k.sh;
         const T *vj = (const T *)a.v.p + b * a.v.sb + (int64_t)j * a.v.sl + hk * a.v.sh;
-        for (int gh = first; left_out && gh < last; ++gh) {
+        for (int gh = first; __builtin_expect(left_out, false) && gh < last; ++gh) {
             const int hq = hk * group + gh;
             const T *q = (const T *)a.q.p + b * a.q.sb + hq * a.q.sh;
             const T *g = (const T *)a.dout.p + b * a.dout.sb + hq * a.dout.sh;
