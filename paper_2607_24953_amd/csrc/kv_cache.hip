@@ -216,11 +216,14 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const CacheCopyArgs a, int
     if (8 * dg >= D) return;
     T *x = (T *)(u.values ? a.v : a.k) + u.head * (u.values ? a.v_sh : a.k_sh) + 8 * dg;
     const int64_t st = u.values ? a.v_st : a.k_st, base = u.at * kBlockTokens * D;
-    float e[8][8] = {};
-    const uint32_t byte = u.at < 0 ? 0 : *((u.values ? a.cache.vs : a.cache.ks) + u.at);
     if (u.at < 0) {
-        // (no page: zeros)
-    } else if (!u.values) {
+        const float none[8] = {};
+        for (int s = max(s0, u.lo); s < min(s0 + 8, u.hi); ++s) store8(x + (u.row0 + s) * st, none);
+        return;
+    }
+    float e[8][8];
+    const uint32_t byte = *((u.values ? a.cache.vs : a.cache.ks) + u.at);
+    if (!u.values) {
         const uint8_t *p = a.cache.k + base + 8 * dg;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
