@@ -42,9 +42,9 @@ constexpr int kComputeUnits = 256;
 // Caps up to kNarrowCap (the usual ones are 20 to 50) take tanh with an error of 2^-23 of 1, scores
 // then with one of 2^-23 of the cap: below 2^-17, far below the bf16 operands' rounding.  That
 // error would grow with the cap (weights off by a factor of 2 at 10^7), so those above take
-// tanh with a small relative error, for ten instructions more a score: 2 x 4096 tokens, 16
-// heads, 128 dims, forward 325 us in place of 260, backward 917 in place of 746.  One kernel does so, with a bias whose
-// slopes may be 0.
+// tanh with a small relative error, for ten instructions more a score: 2 x 4096 tokens, 16 heads
+// of 128 dims, forward 325 us in place of 260, backward 917 in place of 746.  One kernel does so,
+// with a bias whose slopes may be 0.
 constexpr float kNarrowCap = 64.f;
 constexpr int kAnyCap = 7;
 
@@ -58,10 +58,12 @@ inline int mods_of(const AttentionMask &m, bool f32)
 // workgroups (of 128 keys) of its own and then joined from float32 in memory.  Where there are
 // fewer than four workgroups a compute unit, as many parts as bring them there: 1 x 4096
 // tokens, 32 on 8 heads, 128 dims, backward 844 -> 684 us with 4.  With documents, whose
-// workgroups differ in work, 16 a compute unit: 16384 tokens, 32 on 8 heads, 64 dims, 1525 ->
-// 1260 us.  But not so many that writing and reading the parts outweighs it, a part a
-// thousand (from one workgroup a compute unit on, four thousand) rows of queries at most: 4 x
-// 1024 tokens of the first case are 269 us with 1 part and 306 with 4.
+// workgroups differ in work, 16 a compute unit in place of 4: 16384 tokens, 32 on 8 heads, 64 dims,
+// 1611 -> 1332 us; 4 x 4096 tokens 1339 -> 1124, with 128 dims 1941 -> 1838; 8192 tokens, 32 on 4
+// heads, 128 dims 1310 -> 1252; 2 x 2048 tokens, 16 on 4 heads, 64 dims 195 and 194.  But not so
+// many that writing and reading the parts outweighs it, a part a thousand (from one workgroup a
+// compute unit on, four thousand) rows of queries at most: 4 x 1024 tokens of the first case are
+// 269 us with 1 part and 306 with 4.
 inline int dkv_splits(int64_t batch, int64_t len_q, int64_t len_k, int heads_q, int heads_kv, bool documents)
 {
     const int64_t n = batch * heads_kv * ((len_k + 127) / 128), group = heads_q / heads_kv;

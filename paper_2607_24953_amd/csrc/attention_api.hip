@@ -277,12 +277,15 @@ struct CachedSplit {
     int64_t tiles, stat_at, bytes;
 };
 
-// Query tiles of 16 rows where the sequences have no more on average (decoding), of 128
-// otherwise: a tile of 128 wastes what it does not fill, one of 16 reads the cache again for
-// each.  Sequences' tokens are cut into parts where the tiles alone would leave compute units
-// short of four workgroups.  Four, though two run at once: 8 sequences of unequal length and
-// work, 12644 rows, take 384 us so and 428 us with two (4 equal ones of 64 new tokens each 82 and
-// 70 us: the parts' way through memory, which equal work does not earn back).
+// Query tiles of 16 rows where the sequences have no more on average (decoding with up to 16
+// query heads a key head), of 128 otherwise: a tile of 128 wastes what it does not fill, one of 16
+// reads the cache again for each.  The rule looks at the call's average alone, and prompts take
+// decoding sequences of the same call along: 60 of 600 to 8160 tokens and two prompts of 512
+// take 222 us, in two calls 135 and 34 (two of 2048: 302, and 132 and 158).
+// Sequences' tokens are cut into parts where the tiles alone would leave compute units short of
+// four workgroups.  Four, though two run at once: 8 sequences of unequal length and work, 12644
+// rows, take 384 us so and 428 us with two (4 equal ones of 64 new tokens each 82 and 70 us: the
+// parts' way through memory, which equal work does not earn back).
 CachedSplit split_cached(const q2d_kv_cache *c, const q2d_sequences *s, int32_t heads_q)
 {
     CachedSplit p;

@@ -9,9 +9,11 @@
 // Roundings besides the results': for bfloat16 operands, P and dS to bfloat16 as operands of
 // the second products (as P in the forward kernel; P to float16 on its way to dK, see
 // attention_dkv_pair_kernel), and delta is formed from the stored O, which has been rounded to
-// bfloat16: it shifts dP by up to 2^-8 of |dO||O| and saves a second copy of O in float32.  All
-// of them together leave gradients off by 0.0025 of their norm, of which the rounding of the
-// gradients themselves is 0.0017.  For float32 there is none.
+// bfloat16: it shifts dP by up to 2^-8 of |dO||O| and saves a second copy of O in float32 (rows
+// that see few keys, where it counts the most, have an exact one: exact_delta).  In units of
+// rounding the exact gradient once, dV is off by 1.3 to 1.4 (its rounding and P's), dQ and dK by 1.4
+// to 1.6, with a steep distance bias or interleaved documents up to 1.7 (their rounding, dS's, and
+// delta): 0.0024 of their norm where one rounding is 0.0017.  For float32 there is none.
 //
 // As in the forward kernel, the first products leave the tile in the registers that the
 // second ones take as operand: S, dP as [query][key] where keys are owned (columns), as
@@ -84,7 +86,7 @@ __device__ __forceinline__ float exact_delta(const AttentionArgs &a, int b, int 
 }
 
 // delta of 4 rows a wave: 16 lanes a row.  Bound by memory: 4 x 4096 tokens, 32 heads of 128
-// dims, bfloat16, 268 MB in 54 us (5 TB/s).
+// dims, bfloat16, 268 MB in 56 us (4.8 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void attention_delta_kernel(const AttentionArgs a)
 {
@@ -143,8 +145,8 @@ __global__ __launch_bounds__(64) void document_ranges_kernel(const int32_t *docs
 // The tiles of a loop that have masked pairs, and their rows of x (and y) that are not finite:
 // f(row), for a wave
 template <int ROWS, int WIDTH, typename T, typename See, typename F>
-__device__ __forceinline__ void add_rows(int end, See &&see, int first, int n, const T *x, int64_t sx, const T *y, int64_t sy, int D,
-                                         F &&f)
+__device__ __forceinline__ void add_rows(int end, See &&see, int first, int n, const T *x, int64_t sx, const T *y, int64_t sy,
+                                         int D, F &&f)
 {
     Schedule sched;
     for (Visit at = sched.take(end, see); at.tile >= 0; at = sched.take(end, see)) {
@@ -211,8 +213,10 @@ __device__ __forceinline__ void add_row(v16f *acc, const T *row, float w, bool s
 // A workgroup's layout and NARROW are the forward kernel's.  Three products a tile, S, dP and
 // dS K, all of 32 x 32 tiles with the row's numbers (lse, delta) in one lane pair.  Bound by the
 // matrix cores with the exponentials between: 4 x 4096 tokens, 32 heads of 128 dims, causal,
-// bfloat16 0.87 ms (940 TFLOP/s of its three products); with a cap, 2 x 4096 tokens, 16 heads
-// 0.33 ms (620); 64 dims in documents (16384 tokens, 32 on 8 heads) 0.50 ms (500).
+// bfloat16 0.83 ms (990 TFLOP/s of its three products; matrix unit busy for 45 % of the time,
+// vector unit 35 %); with a cap, 2 x 4096 tokens, 16 heads 0.32 ms (650; 27 and 48 %); 64 dims in
+// documents (16384 tokens, 32 on 8 heads) 0.50 ms (500; 21 and 34 %, 42 % of the waves' cycles
+// waiting).  128 dims spill five registers (20 bytes a lane), float32 with 128 dims 46 to 92.
 template <typename T, int DC, int MODS, bool NARROW>
 __global__ __launch_bounds__(256, NARROW ? 1 : 2) void attention_dq_kernel(const AttentionArgs a)
 {
@@ -416,9 +420,10 @@ __global__ __launch_bounds__(256) void attention_dkv_sum_kernel(const AttentionA
 // A workgroup of four waves owns 128 keys and its waves share tiles of 64 (float32: 32)
 // queries; or (NARROW) 32 keys, and each wave takes its quarter of tiles of 128 queries.  The
 // key's column lies in one lane pair; the queries' lse and delta come from LDS, four numbers a
-// read.  With 64 dims K, V, dK and dV of 32 keys fit beside two waves a SIMD; vector
-// instructions bound it: 16384 tokens in ten documents, 32 on 8 heads, causal, bfloat16
-// 0.69 ms (495 TFLOP/s of four products, for what is seen).
+// read.  With 64 dims K, V, dK and dV of 32 keys fit beside two waves a SIMD: 16384 tokens in
+// ten documents, 32 on 8 heads, causal, bfloat16 0.65 ms (520 TFLOP/s of four products, for what is
+// seen; vector unit busy for 34 % of the time, matrix unit 22 %, 44 % of the waves' cycles waiting:
+// for the barrier of each tile, and at the end for workgroups of unequal length).
 template <typename T, int DC, int MODS, bool NARROW>
 __global__ __launch_bounds__(256, DC <= 64 && sizeof(T) == 2 && !NARROW ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a)
 {
@@ -625,10 +630,10 @@ __device__ __forceinline__ u4v to_half(const v16f &x, int s)
 // one tile later, dS.  P passes in the registers' own order (operand fragments) as float16, with
 // the cap's derivative multiplied in: as bfloat16 its rounding would add to that of dS (dK off by
 // 0.0030 of its norm in place of 0.0024, 0.0017 of it the rounding of dK itself).
-// Measured, 4 x 4096 tokens, 32 heads of 128 dims, causal: 1.5 ms, 700 to 770 TFLOP/s of its four
-// products; one wave for both, its products interleaved by hand, was slower at every size tried.
-// Waiting (38 % of the waves' cycles) is for the other wave at the barrier of each tile, and for
-// the vector unit between the products.
+// Measured, 4 x 4096 tokens, 32 heads of 128 dims, causal: 1.43 to 1.5 ms, 730 to 770 TFLOP/s of its
+// four products (matrix unit busy for 31 % of the time, vector unit 33 %); one wave for both, its
+// products interleaved by hand, was slower at every size tried.  Waiting (37 % of the waves'
+// cycles) is for the other wave at the barrier of each tile, and between the products.
 template <int DC, int MODS>
 __global__ __launch_bounds__(512, 2) void attention_dkv_pair_kernel(const AttentionArgs a)
 {

@@ -13,8 +13,8 @@
 // With few query rows the time goes into reading the cache: a sequence's tokens are dealt to
 // the waves of several workgroups, the waves of one join through LDS and the workgroups
 // through a second kernel.  64 sequences of 600 to 8160 tokens, 32 on 8 heads of 128 dims: 557 MB
-// in 128 us (4.4 TB/s, where a large copy moves 4.9 and a library's sum reads 4.0), and 11 us
-// for the join; one sequence of 4097 tokens, whose bytes are 2 us: 10 and 6 us, latencies of a
+// in 123 us (4.5 TB/s, where a large copy moves 4.9 and a library's sum reads 4.0), and 11 us
+// for the join; one sequence of 4097 tokens, whose bytes are 2 us: 10 and 5 us, latencies of a
 // few dependent loads and of two launches.
 //
 // P is rounded to bfloat16 (to nearest even) as in the forward kernel on whole sequences; keys
@@ -399,8 +399,8 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
 // 16 (b / 2) + 8 h + 4 (b % 2) + i for output row 8 b + 4 h + i, a lane ends with 8 neighbouring
 // tokens for each k-step, and value fragments are single 16-byte reads.
 // Bound as the forward kernel is, with the conversion beside it: 4 prompts of 4096 tokens, 32
-// heads of 128 dims 0.77 ms (710 TFLOP/s); capped, 12644 rows of 8 unequal sequences in 0.37 ms
-// (460 TFLOP/s), the vector unit's.
+// heads of 128 dims 0.77 to 0.83 ms (660 to 710 TFLOP/s); capped, 12644 rows of 8 unequal
+// sequences in 0.37 ms (460 TFLOP/s; vector unit busy for 58 % of the time, matrix unit 20 %).
 template <int DC, int MODS>
 __global__ __launch_bounds__(256, 2) void attention_cached_rows_kernel(const CachedArgs a)
 {

@@ -13,15 +13,17 @@
 //
 // What bounds it.  bfloat16, 128 dims: a 32 x 32 tile of scores is 16 MFMAs of 32 cycles
 // beside the exponentials, maximum, sum and rounding of 16 scores a lane, which two waves a SIMD
-// lay over one another, but not without gaps: 4 x 4096 tokens, 32 heads, causal 0.66 ms (820
-// TFLOP/s), without causal order 990, where a library's product of 8192 x 8192 x 8192 reaches
-// 1157; the causal loss is workgroups of unequal length at the end.  A cap adds a second exponential
-// and a reciprocal a score: 16384 tokens, 32 on 8 heads, window of 4096: 1.42 ms, 680 TFLOP/s,
-// bound by the vector unit, as is every case with 64 dims (half the products, the same softmax;
-// 16384 tokens in ten documents, 32 on 8 heads: 0.40 ms, 425 TFLOP/s, tiles that documents cut
-// counted for what is seen of them).  float32: the float32 matrix rate (153 TFLOP/s) and, in the
-// NARROW form, one wave a SIMD that waits for its only LDS stage: 3 x 777 queries on 1999 keys, 6 on 2
-// heads, 72 dims in documents 0.18 ms, 26 TFLOP/s.
+// lay over one another, but not without gaps: 4 x 4096 tokens, 32 heads, causal 0.64 to 0.68 ms
+// (810 to 860 TFLOP/s; matrix unit busy for 37 % of the time, vector unit 42 %), without causal order
+// 950 to 990, where a library's product of 8192 x 8192 x 8192 reaches 1157; the causal loss is
+// workgroups of unequal length at the end.  A cap adds a second exponential and a reciprocal a
+// score: 16384 tokens, 32 on 8 heads, window of 4096: 1.42 ms, 680 TFLOP/s, vector unit busy for
+// 68 %, matrix unit 28 %.  64 dims have half the products for the same softmax, and in documents
+// workgroups of unequal length: 16384 tokens in ten documents, 32 on 8 heads: 0.40 ms, 425 TFLOP/s
+// (tiles that documents cut counted for what is seen of them), vector unit 42 %, matrix unit 18 %,
+// and 40 % of the waves' cycles waiting.  float32: the float32 matrix rate (153 TFLOP/s) and, in
+// the NARROW form, one wave a SIMD that waits for its only LDS stage: 3 x 777 queries on 1999 keys,
+// 6 on 2 heads, 72 dims in documents 0.18 ms, 26 TFLOP/s.
 #include "attention_common.hpp"
 
 namespace q2d {

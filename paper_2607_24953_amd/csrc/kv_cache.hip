@@ -1,8 +1,8 @@
 // Writing new tokens into the paged 8-bit cache, and reading tokens back as values.
 //
 // Both are memory-bound: 16384 tokens of 32 heads and 128 dims, bfloat16, keys and values, are
-// written (403 MB read and written) in 106 us, 3.8 TB/s, and read back in 71 us, 5.7 TB/s,
-// where a large copy reaches 4.9.  One token of each of 64 sequences takes 7 and 6 us, a launch and
+// written (403 MB read and written) in 100 to 109 us, 3.7 to 4 TB/s, and read back in 71 to 84 us,
+// 4.8 to 5.7 TB/s, where a large copy reaches 4.9.  One token of each of 64 sequences takes 7 and 6 us, a launch and
 // the chain offsets, page table, block.  The write gains nothing from more bytes under way: a
 // lane's 8 rows are loaded at once, and the scale needs all of them.
 //
