@@ -84,3 +84,37 @@ def test_read_without_offsets(q2d):
         want = torch.zeros((24, 2, 64), dtype=torch.float64)
         want[3:8], want[15:16] = p.dense(0)[which], p.dense(1)[which]
         assert torch.equal(x.cpu().double(), want)
+
+
+def test_padded_batch_in_a_graph(q2d):
+    """One captured call for up to 12 new tokens of three sequences, replayed with other counts: rows
+    behind the last one are zeros each time, whatever the replay before left in them."""
+    p = filled(q2d, [300, 65, 90], 2, 64)
+    table, lens = p.table.cuda(), p.lens().cuda()
+    q = torch.randn((12, 8, 64), generator=torch.Generator().manual_seed(72)).to(torch.bfloat16).cuda()
+    off = torch.tensor([0, 4, 8, 12]).cuda()
+    out, k, v = torch.empty_like(q), *(torch.empty((12, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+
+    def step():
+        q2d.q2d_attention_cached(q, p.cache, table, lens, off, out=out)
+        q2d.q2d_kv_read(p.cache, table, lens, 12, off, k=k, v=v)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()                                  # the workspace's allocation, outside the capture
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    for counts in ([4, 4, 4], [1, 0, 2], [3, 3, 0], [0, 0, 0], [12, 0, 0], [1, 1, 1]):
+        ends = torch.tensor(counts).cumsum(0)
+        off[1:].copy_(ends)
+        graph.replay()
+        torch.cuda.synchronize()
+        n = int(ends[-1])
+        got = [t.clone() for t in (out, k, v)]
+        step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, (out, k, v)):
+            assert torch.equal(a, b) and not a[n:].any() and bool(a[:n].any(-1).all())
