@@ -525,6 +525,90 @@ int64_t q2d_attention_cached_workspace(const q2d_kv_cache *c, const q2d_sequence
 q2d_status q2d_attention_cached(const q2d_kv_cache *c, const q2d_sequences *s, const q2d_cached_attention *a,
                                 void *workspace, int64_t workspace_bytes, hipStream_t stream);
 
+/*
+ * Root-mean-square norm with the residual's addition, in front of a linear layer:
+ *   h_j    = x_j + residual_j, formed in float32 and rounded to x's type (h = x without a
+ *            residual)
+ *   rstd   = 1 / sqrt(mean_j h_j^2 + eps), formed in 64 bits and rounded to float32 once
+ *   y_j    = (h_j * rstd) * weight_j, both products rounded to float32
+ * y goes out in Q2D_F32 or Q2D_BF16, or straight into the operands of the layer's GEMMs: q4
+ * (FP4_2D with block 32 or 64, or FP4_1D) and q8 (MXFP8) hold what q2d_quantize,
+ * q2d_quantize_1d and mxfp8_quantize make of the float32 y with round to nearest, bit for bit.
+ * Any of y, q4 and q8 may be wanted together, one at least.
+ *
+ * Row r of a tensor starts at its pointer + r * ld elements (ld >= cols with more than one
+ * row).  rows may be 0 without operands.  Values that are not finite follow the formulas: a row
+ * with a NaN is NaN, one with an infinity has rstd 0.
+ */
+typedef struct {
+    int32_t x_dtype, residual_dtype, weight_dtype, y_dtype;    /* q2d_dtype */
+    int64_t rows, cols;
+    double eps;                  /* from 2^-126, finite */
+    const void *x;        int64_t ldx;
+    const void *residual; int64_t ld_residual;                 /* or NULL */
+    const void *weight;          /* [cols] */
+    void *h;              int64_t ldh;                         /* x's type; set if and only if residual is */
+    void *y;              int64_t ldy;                         /* or NULL */
+    float *rstd;                 /* [rows], which q2d_rmsnorm_bwd needs */
+} q2d_rmsnorm;
+
+/* Forward.  What is written shares no memory with anything else, but that h may be x or the
+ * residual itself (Q2D_EINVAL otherwise). */
+q2d_status q2d_rmsnorm_fwd(const q2d_rmsnorm *n, q2d_tensor *q4, q2d_tensor *q8, hipStream_t stream);
+
+/*
+ * Its gradient, with g = dy * weight and n = h * rstd:
+ *   dx = rstd * (g - n * mean_j(g_j n_j)) + dh      for x and for the residual
+ *   dw = the sum over rows of dy * n                float32; NULL: not wanted
+ * dh is the gradient that reaches h by other ways (or NULL); dh and dx have h's type.  With
+ * operands in place of y, dy is the gradient of what they stand for.
+ */
+typedef struct {
+    int32_t h_dtype, dy_dtype, weight_dtype;
+    int64_t rows, cols;
+    const void *h;  int64_t ldh;
+    const void *dy; int64_t lddy;
+    const void *dh; int64_t lddh;
+    void *dx;       int64_t lddx;
+    const void *weight;
+    const float *rstd;
+    float *dw;
+} q2d_rmsnorm_grad;
+
+/* Bytes of device workspace that q2d_rmsnorm_bwd needs, possibly 0; -1 for invalid sizes. */
+int64_t q2d_rmsnorm_workspace(int64_t rows, int64_t cols);
+
+/* Backward.  workspace on a 256-byte boundary (may be NULL for 0 bytes).  dx and dw share no
+ * memory with anything else, but that dx may be dh itself, or dy where the types are the same
+ * (Q2D_EINVAL otherwise).  Results do not depend on the order in which workgroups run. */
+q2d_status q2d_rmsnorm_bwd(const q2d_rmsnorm_grad *n, void *workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/*
+ * 2-norm over all elements of n tensors, and their scaling where it is above a bound: the
+ * clipping of a training step's gradients.  Tensor i has counts[i] (0 or more) elements of type
+ * dtypes[i] at data[i], without gaps.  The arrays are host memory, read before the call returns.
+ * Sums are formed in 64 bits, in an order that the sizes alone set.  workspace: at least
+ * q2d_grad_workspace(n) bytes of device memory on an 8-byte boundary.
+ */
+int64_t q2d_grad_workspace(int32_t n);
+
+/* *norm (device) = the 2-norm; 0 without elements. */
+q2d_status q2d_grad_norm(int32_t n, const void *const *data, const int64_t *counts, const int32_t *dtypes, float *norm,
+                         void *workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/*
+ * out[i] = data[i] * min(1, max_norm / norm): the factor is formed in 64 bits and rounded to
+ * float32, the product rounds to float32 and then to the tensor's type.  A norm that is not finite
+ * leaves the values as they are (the caller sees it in *norm).  out NULL: in place.
+ * given   device: the norm to go by (of tensors on several GPUs, say), or NULL: the norm of
+ *         these tensors is computed first and written to *norm.  One of given and norm is NULL.
+ * An output may be its own input (in place) and shares no memory with anything else of the call
+ * (Q2D_EINVAL); the same tensor twice is refused by that.  With given, workspace may be NULL.
+ */
+q2d_status q2d_clip_grads(int32_t n, const void *const *data, void *const *out, const int64_t *counts, const int32_t *dtypes,
+                          double max_norm, const float *given, float *norm, void *workspace, int64_t workspace_bytes,
+                          hipStream_t stream);
+
 /* Static description of a status code (never NULL). */
 const char *q2d_status_string(q2d_status s);
 

@@ -13,6 +13,7 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
+typedef short s2v __attribute__((ext_vector_type(2)));
 typedef unsigned int u4v __attribute__((ext_vector_type(4)));
 
 // 16-byte streaming load: a quantizer's input is read once, so it should not
@@ -143,6 +144,50 @@ __device__ __forceinline__ uint16_t f_to_bf16_rne(float f)
     if ((b & 0x7F800000u) == 0x7F800000u) return (uint16_t)((b >> 16) | ((b & 0xFFFFu) ? 0x40u : 0u));
     b += 0x7FFFu + ((b >> 16) & 1u);
     return (uint16_t)(b >> 16);
+}
+
+// Round-to-nearest E2M1 pair into byte SEL of `old`, from two float32 bit patterns
+template <int SEL>
+__device__ __forceinline__ uint32_t rtn_pair_f32(uint32_t old, uint32_t lo, uint32_t hi, float scale)
+{
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(old, bits_f(lo), bits_f(hi), scale, SEL);
+}
+
+// 8 x 8 transpose of 4-bit elements: nibble j of in[i] becomes nibble i of
+// out[j].  Three exchange stages of doubling width (nibbles within row pairs,
+// bytes across distance 2, half-words across distance 4).
+__device__ __forceinline__ void nibble_transpose8(const uint32_t in[8], uint32_t out[8])
+{
+    uint32_t m[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m[i] = in[i];
+#pragma unroll
+    for (int p = 0; p < 8; p += 2) {
+        const uint32_t t = ((m[p] >> 4) ^ m[p + 1]) & 0x0F0F0F0Fu;
+        m[p + 1] ^= t;
+        m[p] ^= t << 4;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i += (i & 1) ? 3 : 1) {         // 0, 1, 4, 5
+        const uint32_t x = m[i], y = m[i + 2];
+        m[i] = __builtin_amdgcn_perm(y, x, 0x06020400u);     // bytes x0 y0 x2 y2
+        m[i + 2] = __builtin_amdgcn_perm(y, x, 0x07030501u); // bytes x1 y1 x3 y3
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = m[i], y = m[i + 4];
+        out[i] = __builtin_amdgcn_perm(y, x, 0x05040100u);       // x.lo, y.lo
+        out[i + 4] = __builtin_amdgcn_perm(y, x, 0x07060302u);   // x.hi, y.hi
+    }
+}
+
+// E4M3 pair (low element first) into 16-bit word SEL of `old`, from two float32 bit patterns
+template <bool SEL>
+__device__ __forceinline__ uint32_t fp8_pair_f32(uint32_t old, uint32_t lo, uint32_t hi, float scale)
+{
+    const s2v r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(__builtin_bit_cast(s2v, old), bits_f(lo), bits_f(hi),
+                                                           scale, SEL);
+    return __builtin_bit_cast(uint32_t, r);
 }
 
 // A lane's 8 x 8 sub-block of a matrix with contiguous rows of `pitch` bytes, from

@@ -65,13 +65,8 @@ struct Elem<uint16_t> {
     static __device__ __forceinline__ uint32_t bits(const uint16_t *p) { return (uint32_t)*p << 16; }
 };
 
-// Round-to-nearest E2M1 pair into byte SEL of `old`: f32 sources as two
-// float32 bit patterns, bf16 sources as one packed register (low half first).
-template <int SEL>
-__device__ __forceinline__ uint32_t rtn_pair_f32(uint32_t old, uint32_t lo, uint32_t hi, float scale)
-{
-    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(old, bits_f(lo), bits_f(hi), scale, SEL);
-}
+// Round-to-nearest E2M1 pair into byte SEL of `old`: bf16 sources as one packed register
+// (low half first).
 template <int SEL>
 __device__ __forceinline__ uint32_t rtn_pair_bf16(uint32_t old, uint32_t packed, float scale)
 {
@@ -103,34 +98,6 @@ __device__ __forceinline__ uint32_t sr_row_pair(int sel, const uint32_t *row, ui
     if constexpr (sizeof(T) == 2) p = f2v{bits_f(row[sel] << 16), bits_f(row[sel] & 0xFFFF0000u)};
     else p = f2v{bits_f(row[2 * sel]), bits_f(row[2 * sel + 1])};
     return sr_pair(sel, p, seed, scale);
-}
-
-// 8 x 8 transpose of 4-bit elements: nibble j of in[i] becomes nibble i of
-// out[j].  Three exchange stages of doubling width (nibbles within row pairs,
-// bytes across distance 2, half-words across distance 4).
-__device__ __forceinline__ void nibble_transpose8(const uint32_t in[8], uint32_t out[8])
-{
-    uint32_t m[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m[i] = in[i];
-#pragma unroll
-    for (int p = 0; p < 8; p += 2) {
-        const uint32_t t = ((m[p] >> 4) ^ m[p + 1]) & 0x0F0F0F0Fu;
-        m[p + 1] ^= t;
-        m[p] ^= t << 4;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; i += (i & 1) ? 3 : 1) {         // 0, 1, 4, 5
-        const uint32_t x = m[i], y = m[i + 2];
-        m[i] = __builtin_amdgcn_perm(y, x, 0x06020400u);     // bytes x0 y0 x2 y2
-        m[i + 2] = __builtin_amdgcn_perm(y, x, 0x07030501u); // bytes x1 y1 x3 y3
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t x = m[i], y = m[i + 4];
-        out[i] = __builtin_amdgcn_perm(y, x, 0x05040100u);       // x.lo, y.lo
-        out[i + 4] = __builtin_amdgcn_perm(y, x, 0x07060302u);   // x.hi, y.hi
-    }
 }
 
 // Philox4x32-10 block of counter (g lo, g hi, o0, o1), one 32x32->64 multiply per

@@ -23,7 +23,6 @@ namespace {
 
 constexpr int kTile = 128;
 
-typedef short s2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ uint32_t load_bits(const void *x, bool is_f32, int64_t idx)
@@ -38,13 +37,6 @@ __device__ __forceinline__ uint32_t fp8_pair_bf16(uint32_t old, uint32_t packed,
 {
     const s2v r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(__builtin_bit_cast(s2v, old),
                                                             __builtin_bit_cast(bf16x2, packed), scale, SEL);
-    return __builtin_bit_cast(uint32_t, r);
-}
-template <bool SEL>
-__device__ __forceinline__ uint32_t fp8_pair_f32(uint32_t old, uint32_t lo, uint32_t hi, float scale)
-{
-    const s2v r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(__builtin_bit_cast(s2v, old), bits_f(lo), bits_f(hi),
-                                                           scale, SEL);
     return __builtin_bit_cast(uint32_t, r);
 }
 

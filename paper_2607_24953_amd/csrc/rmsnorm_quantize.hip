@@ -1,0 +1,286 @@
+// Quantized operands of a root-mean-square norm, from the rows and their statistics.
+//
+// The work split is the quantizers': a workgroup of eight waves owns a 128 x 256 tile, a wave a
+// 32 x 128 strip of it, a lane an 8 x 8 sub-block (rows 8 * (lane / 16) .. + 7, columns 8 * (lane %
+// 16) .. + 7).  The lane forms y = (h * rstd) * w in float32 and converts it to each format that
+// is wanted, so h is read once for all of them.  A 1 x 32 block spans the 4 lanes that differ in
+// lane bits 0-1, a 32 x 1 block those that differ in bits 4-5, a 32 x 32 block all 16.
+#include "norm_common.hpp"
+#include "norms.hpp"
+
+namespace q2d {
+
+namespace {
+
+constexpr int kRows = 128, kCols = 256, kThreads = 512;
+
+// byte of a block's scale: its exponent, or 0xFF for a block that is not finite
+__device__ __forceinline__ uint8_t scale_byte(uint32_t amax, int e) { return amax < 0x7F800000u ? (uint8_t)(e + 127) : (uint8_t)0xFF; }
+__device__ __forceinline__ float pow2(int e) { return bits_f((uint32_t)(127 + e) << 23); }
+
+__device__ __forceinline__ uint32_t fp4_word(const uint32_t (&v)[8], float scale)
+{
+    uint32_t w = 0;
+    w = rtn_pair_f32<0>(w, v[0], v[1], scale);
+    w = rtn_pair_f32<1>(w, v[2], v[3], scale);
+    w = rtn_pair_f32<2>(w, v[4], v[5], scale);
+    return rtn_pair_f32<3>(w, v[6], v[7], scale);
+}
+__device__ __forceinline__ uint2 fp8_words(const uint32_t (&v)[8], float scale)
+{
+    uint32_t lo = 0, hi = 0;
+    lo = fp8_pair_f32<false>(lo, v[0], v[1], scale);
+    lo = fp8_pair_f32<true>(lo, v[2], v[3], scale);
+    hi = fp8_pair_f32<false>(hi, v[4], v[5], scale);
+    hi = fp8_pair_f32<true>(hi, v[6], v[7], scale);
+    return make_uint2(lo, hi);
+}
+
+// F32: h is float32.  VEC: as in the quantizers (0 -- element by element; 1 -- rows of any
+// alignment; 2 -- rows on 16-byte boundaries).  FP4: 0 none, 1 2D blocks, 2 1D blocks.
+template <bool F32, int VEC, int FP4, bool MX>
+__global__ __launch_bounds__(kThreads) void rmsnorm_quantize_kernel(const NormQuantArgs a)
+{
+    constexpr int E = F32 ? 4 : 2, NV = 2 * E;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wr = wave >> 1, wc = wave & 1, rg = lane >> 4, cc = lane & 15;
+    const int64_t tiles_c = (a.cols_pad + kCols - 1) / kCols;
+    const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
+    const int64_t r0 = tr * kRows + wr * 32 + 8 * rg, c0 = tc * kCols + wc * 128 + 8 * cc;
+
+    // ---- y of the sub-block, 0 outside the matrix
+    uint32_t y[8][8];
+    {
+        uint32_t v[8][NV];
+        const uint8_t *h = reinterpret_cast<const uint8_t *>(a.h) + (r0 * a.ldh + c0) * E;
+        if constexpr (VEC != 0) {
+            load_sub_block<E, VEC == 2, 0>(v, h, a.ldh * E, a.rows - r0, a.cols - c0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    auto at = [&](int j) __attribute__((always_inline)) -> uint32_t {
+                        return r0 + i < a.rows && c0 + j < a.cols ? f_bits(load_value(a.h, !F32, (r0 + i) * a.ldh + c0 + j)) : 0u;
+                    };
+                    v[i][k] = F32 ? at(k) : (at(2 * k) >> 16) | at(2 * k + 1);
+                }
+        }
+        float w[8], rstd[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = c0 + j < a.cols ? load_value(a.w, a.w_bf16, c0 + j) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rstd[i] = r0 + i < a.rows ? a.rstd[r0 + i] : 0.f;
+        const bool edge = __builtin_amdgcn_ballot_w64(a.rows - r0 < 8 || a.cols - c0 < 8) != 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float h = F32 ? bits_f(v[i][F32 ? j : 0]) : bits_f((j & 1) ? v[i][j / (F32 ? 1 : 2)] & 0xFFFF0000u : v[i][j / (F32 ? 1 : 2)] << 16);
+                y[i][j] = f_bits((h * rstd[i]) * w[j]);
+            }
+        if (edge) {
+            // (a weight or a row that is not finite must not reach past the matrix)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[i][j] = r0 + i < a.rows && c0 + j < a.cols ? y[i][j] : 0u;
+        }
+    }
+
+    // ---- block maxima on |bits| (NaN > inf > finite, as unsigned integers)
+    uint32_t rm[8], cm[8];
+    if constexpr (FP4 == 2 || MX) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = max(m, y[i][j] & 0x7FFFFFFFu);
+            m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+            rm[i] = max(m, (uint32_t)__shfl_xor((int)m, 2));
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = max(m, y[i][j] & 0x7FFFFFFFu);
+            m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+            cm[j] = max(m, (uint32_t)__shfl_xor((int)m, 32));
+        }
+    }
+
+    if constexpr (FP4 != 0) {
+        __shared__ uint32_t st_r[kRows][33];
+        __shared__ uint32_t st_c[kCols][17];
+        __shared__ uint8_t st_rs[FP4 == 2 ? kRows : 1][8];
+        __shared__ uint8_t st_cs[FP4 == 2 ? kCols : 1][4];
+        uint32_t am = 0;
+        uint32_t rowp[8], colp[8];
+        if constexpr (FP4 == 1) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) am = max(am, y[i][j] & 0x7FFFFFFFu);
+            am = max(am, (uint32_t)__shfl_xor((int)am, 1));
+            am = max(am, (uint32_t)__shfl_xor((int)am, 2));
+            am = max(am, (uint32_t)__shfl_xor((int)am, 16));
+            am = max(am, (uint32_t)__shfl_xor((int)am, 32));
+            if (a.block == 64) {
+                // the block beside it in this wave, then the paired wave's strip
+                __shared__ uint32_t am64[4][4];
+                am = max(am, (uint32_t)__shfl_xor((int)am, 4));
+                if (rg == 0 && (cc & 7) == 0) am64[wr][wc * 2 + (cc >> 3)] = am;
+                __syncthreads();
+                am = max(am, am64[wr ^ 1][wc * 2 + (cc >> 3)]);
+            }
+            const float scale = pow2(fp4_block_exponent(am));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rowp[i] = am < 0x7F800000u ? fp4_word(y[i], scale) : 0u;
+            nibble_transpose8(rowp, colp);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rowp[i] = rm[i] < 0x7F800000u ? fp4_word(y[i], pow2(fp4_block_exponent(rm[i]))) : 0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t col[8] = {y[0][j], y[1][j], y[2][j], y[3][j], y[4][j], y[5][j], y[6][j], y[7][j]};
+                colp[j] = cm[j] < 0x7F800000u ? fp4_word(col, pow2(fp4_block_exponent(cm[j]))) : 0u;
+            }
+            if ((cc & 3) == 0) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) st_rs[wr * 32 + 8 * rg + i][wc * 4 + (cc >> 2)] = scale_byte(rm[i], fp4_block_exponent(rm[i]));
+            }
+            if (rg == 0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) st_cs[wc * 128 + 8 * cc + j][wr] = scale_byte(cm[j], fp4_block_exponent(cm[j]));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) st_r[wr * 32 + 8 * rg + i][wc * 16 + cc] = rowp[i];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) st_c[wc * 128 + 8 * cc + j][wr * 4 + rg] = colp[j];
+        __syncthreads();
+        const QuantOut &q = a.q4;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int item = threadIdx.x + kThreads * p;
+            if (q.codes) {
+                const int line = item >> 3, part = item & 7;
+                const int64_t r = tr * kRows + line;
+                if (r < a.rows && tc * kCols + part * 32 < a.cols_pad)
+                    *reinterpret_cast<uint4 *>(q.codes + r * q.ld_codes + tc * (kCols / 2) + part * 16) =
+                        make_uint4(st_r[line][4 * part], st_r[line][4 * part + 1], st_r[line][4 * part + 2], st_r[line][4 * part + 3]);
+            }
+            if (q.codes_t) {
+                const int line = item >> 2, part = item & 3;
+                const int64_t c = tc * kCols + line;
+                if (c < a.cols)
+                    *reinterpret_cast<uint4 *>(q.codes_t + c * q.ld_codes_t + tr * (kRows / 2) + part * 16) =
+                        make_uint4(st_c[line][4 * part], st_c[line][4 * part + 1], st_c[line][4 * part + 2], st_c[line][4 * part + 3]);
+            }
+        }
+        if constexpr (FP4 == 2) {
+            // scale words, K-tile major
+            const int t = threadIdx.x;
+            if (t < kRows) {
+                const int64_t r = tr * kRows + t;
+                if (q.codes && r < a.rows) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        if (tc * kCols + k * 128 < a.cols_pad)
+                            *reinterpret_cast<uint32_t *>(q.scales + (tc * 2 + k) * q.ld_scales + 4 * r) =
+                                *reinterpret_cast<const uint32_t *>(&st_rs[t][4 * k]);
+                }
+            } else if (t >= kThreads - kCols) {
+                const int cl = t - (kThreads - kCols);
+                const int64_t c = tc * kCols + cl;
+                if (q.codes_t && c < a.cols)
+                    *reinterpret_cast<uint32_t *>(q.scales_t + tr * q.ld_scales_t + 4 * c) = *reinterpret_cast<const uint32_t *>(&st_cs[cl][0]);
+            }
+        } else if (rg == 0 && (cc & 3) == 0 && tc * kCols + wc * 128 < a.cols_pad) {
+            const uint8_t byte = scale_byte(am, fp4_block_exponent(am));
+            const int64_t rb = r0 >> 5, cb = c0 >> 5;
+            if (q.codes && r0 < a.rows) q.scales[rb * q.ld_scales + cb] = byte;
+            if (q.codes_t && c0 < a.cols) q.scales_t[cb * q.ld_scales_t + rb] = byte;
+        }
+    }
+
+    if constexpr (MX) {
+        __shared__ uint32_t st_c[kCols][33];
+        __shared__ uint8_t st_rs[kRows][8];
+        __shared__ uint8_t st_cs[kCols][4];
+        const QuantOut &q = a.q8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int e = fp8_block_exponent(rm[i]);
+            const uint2 w = rm[i] < 0x7F800000u ? fp8_words(y[i], pow2(e)) : make_uint2(0, 0);
+            if (q.codes && r0 + i < a.rows && c0 < a.cols_pad) *reinterpret_cast<uint2 *>(q.codes + (r0 + i) * q.ld_codes + c0) = w;
+            if ((cc & 3) == 0) st_rs[wr * 32 + 8 * rg + i][wc * 4 + (cc >> 2)] = scale_byte(rm[i], e);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int e = fp8_block_exponent(cm[j]);
+            const uint32_t col[8] = {y[0][j], y[1][j], y[2][j], y[3][j], y[4][j], y[5][j], y[6][j], y[7][j]};
+            const uint2 w = cm[j] < 0x7F800000u ? fp8_words(col, pow2(e)) : make_uint2(0, 0);
+            st_c[wc * 128 + 8 * cc + j][wr * 8 + 2 * rg] = w.x;
+            st_c[wc * 128 + 8 * cc + j][wr * 8 + 2 * rg + 1] = w.y;
+            if (rg == 0) st_cs[wc * 128 + 8 * cc + j][wr] = scale_byte(cm[j], e);
+        }
+        __syncthreads();
+        if (q.codes_t) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const int item = threadIdx.x + kThreads * p;
+                const int line = item >> 3, part = item & 7;
+                const int64_t c = tc * kCols + line;
+                if (c < a.cols)
+                    *reinterpret_cast<uint4 *>(q.codes_t + c * q.ld_codes_t + tr * kRows + part * 16) =
+                        make_uint4(st_c[line][4 * part], st_c[line][4 * part + 1], st_c[line][4 * part + 2], st_c[line][4 * part + 3]);
+            }
+        }
+        const int t = threadIdx.x;
+        if (t < kRows) {
+            const int64_t r = tr * kRows + t;
+            if (q.codes && r < a.rows) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (tc * kCols + k * 128 < a.cols_pad)
+                        *reinterpret_cast<uint32_t *>(q.scales + r * q.ld_scales + (tc * 2 + k) * 4) = *reinterpret_cast<const uint32_t *>(&st_rs[t][4 * k]);
+            }
+        } else if (t >= kThreads - kCols) {
+            const int cl = t - (kThreads - kCols);
+            const int64_t c = tc * kCols + cl;
+            if (q.codes_t && c < a.cols)
+                *reinterpret_cast<uint32_t *>(q.scales_t + c * q.ld_scales_t + tr * 4) = *reinterpret_cast<const uint32_t *>(&st_cs[cl][0]);
+        }
+    }
+}
+
+template <bool F32, int VEC>
+hipError_t launch_v(const NormQuantArgs &a, hipStream_t s)
+{
+    const int64_t blocks = (a.rows_pad / kRows) * ((a.cols_pad + kCols - 1) / kCols);
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks), block(kThreads);
+    switch (a.fp4 * 2 + (a.mx ? 1 : 0)) {
+    case 1: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 0, true>), grid, block, 0, s, a); break;
+    case 2: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 1, false>), grid, block, 0, s, a); break;
+    case 3: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 1, true>), grid, block, 0, s, a); break;
+    case 4: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 2, false>), grid, block, 0, s, a); break;
+    default: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 2, true>), grid, block, 0, s, a); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rmsnorm_quantize(const NormQuantArgs &a, hipStream_t stream)
+{
+    const int bytes = a.h_bf16 ? 2 : 4;
+    const bool aligned = reinterpret_cast<uintptr_t>(a.h) % 16 == 0 && (a.ldh * bytes) % 16 == 0;
+    const int vec = aligned ? 2 : a.cols >= 8 ? 1 : 0;
+    if (a.h_bf16)
+        return vec == 2 ? launch_v<false, 2>(a, stream) : vec == 1 ? launch_v<false, 1>(a, stream) : launch_v<false, 0>(a, stream);
+    return vec == 2 ? launch_v<true, 2>(a, stream) : vec == 1 ? launch_v<true, 1>(a, stream) : launch_v<true, 0>(a, stream);
+}
+
+}  // namespace q2d
