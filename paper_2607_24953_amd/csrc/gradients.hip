@@ -37,19 +37,41 @@ __device__ __forceinline__ int tensor_of(const Tensors &t, int piece) { return s
 
 __device__ __forceinline__ bool is_bf16(const Tensors &t, int i) { return (t.bf16[i >> 5] >> (i & 31)) & 1; }
 
+// Eight-element chunks that a lane has in flight, and of a piece
+constexpr int kFlight = 4, kChunks = (int)(kPiece / (8 * 256));
+
+template <bool BF16>
+__device__ __forceinline__ double square_piece(const void *data, int64_t at, int64_t left)
+{
+    const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * (BF16 ? 2 : 4);
+    double s = 0.0;
+#pragma unroll 1
+    for (int k0 = 0; k0 < kChunks; k0 += kFlight) {
+        Eight<BF16> e[kFlight];
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+            const int c = 8 * ((k0 + k) * 256 + threadIdx.x);
+            e[k].load(p + c * (BF16 ? 2 : 4), left - c);
+        }
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const double v = e[k].at(j);
+                s = __builtin_fma(v, v, s);
+            }
+    }
+    return s;
+}
+
 __global__ __launch_bounds__(256) void grad_square_kernel(const Tensors t, double *parts)
 {
     __shared__ double lds[4];
     double s = 0.0;
     for (int piece = blockIdx.x; piece < t.pieces; piece += gridDim.x) {
         const int i = tensor_of(t, piece);
-        const int64_t at = (piece - t.first[i]) * kPiece;
-        const int64_t end = at + kPiece < t.count[i] ? at + kPiece : t.count[i];
-        const bool bf16 = is_bf16(t, i);
-        for (int64_t k = at + threadIdx.x; k < end; k += 256) {
-            const double v = load_value(t.data[i], bf16, k);
-            s += v * v;
-        }
+        const int64_t at = (piece - t.first[i]) * kPiece, left = t.count[i] - at;
+        s += is_bf16(t, i) ? square_piece<true>(t.data[i], at, left) : square_piece<false>(t.data[i], at, left);
     }
     s = group_sum(s, 4, lds);
     if (threadIdx.x == 0) parts[blockIdx.x] = s;
@@ -70,6 +92,34 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const double *parts, int
     if (threadIdx.x == 0) *norm = (float)s;
 }
 
+template <bool BF16>
+__device__ __forceinline__ void scale_piece(const void *data, void *out, int64_t at, int64_t left, bool clip, float f)
+{
+    const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * (BF16 ? 2 : 4);
+    uint8_t *o = reinterpret_cast<uint8_t *>(out) + at * (BF16 ? 2 : 4);
+#pragma unroll 1
+    for (int k0 = 0; k0 < kChunks; k0 += kFlight) {
+        Eight<BF16> e[kFlight];
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+            const int c = 8 * ((k0 + k) * 256 + threadIdx.x);
+            e[k].load(p + c * (BF16 ? 2 : 4), left - c);
+        }
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+            const int c = 8 * ((k0 + k) * 256 + threadIdx.x);
+            if (clip) {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = e[k].at(j) * f;
+                e[k].set(v);
+            }
+            e[k].store(o + c * (BF16 ? 2 : 4), left - c);
+        }
+    }
+}
+
+// (the last pieces first: the square sums read them last, and some are still in the cache)
 __global__ __launch_bounds__(256) void grad_scale_kernel(const Tensors t, const double *parts, int n, const float *given,
                                                          double max_norm, float *norm)
 {
@@ -79,16 +129,12 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(const Tensors t, const 
     // a norm that is not finite leaves the gradients as they are
     const bool clip = (float)total < __builtin_inff() && total > max_norm;
     const float f = clip ? (float)(max_norm / total) : 1.f;
-    for (int piece = blockIdx.x; piece < t.pieces; piece += gridDim.x) {
+    for (int piece = t.pieces - 1 - (int)blockIdx.x; piece >= 0; piece -= gridDim.x) {
         const int i = tensor_of(t, piece);
         if (!clip && t.out[i] == t.data[i]) continue;
-        const int64_t at = (piece - t.first[i]) * kPiece;
-        const int64_t end = at + kPiece < t.count[i] ? at + kPiece : t.count[i];
-        const bool bf16 = is_bf16(t, i);
-        for (int64_t k = at + threadIdx.x; k < end; k += 256) {
-            const float v = load_value(t.data[i], bf16, k);
-            store_value(t.out[i], bf16, k, clip ? v * f : v);
-        }
+        const int64_t at = (piece - t.first[i]) * kPiece, left = t.count[i] - at;
+        if (is_bf16(t, i)) scale_piece<true>(t.data[i], t.out[i], at, left, clip, f);
+        else scale_piece<false>(t.data[i], t.out[i], at, left, clip, f);
     }
 }
 

@@ -1,4 +1,10 @@
 // Gradient of the root-mean-square norm.
+//
+// With n = h * rstd and g = dy * w: dx = rstd * (g - n * mean(g n)) + dh, dw = sum over rows of dy n.
+// One read of h, dy and dh: a row stays in registers between the sum for its mean and the products
+// with it, as in the forward kernel.  A workgroup takes every gridDim.x-th row and keeps its part
+// of dw in registers, in 64 bits; the parts lie one behind the other in the workspace and a second
+// kernel adds them up.  Every sum has one owner and one order.
 #include "norm_common.hpp"
 #include "norms.hpp"
 #include "kernels.hpp"
@@ -7,71 +13,234 @@ namespace q2d {
 
 namespace {
 
-// c = mean(dy * w * h) * rstd of each row
-__global__ __launch_bounds__(256) void rmsnorm_grad_rows_kernel(const NormGradArgs a, float *means)
+// workgroups of a launch at most
+constexpr int64_t kParts = 1024;
+
+// HB, DB: h and dh, dy are bfloat16.  LANES, CH: as in the forward kernel.
+template <bool HB, bool DB, int LANES, int CH>
+__global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const NormGradArgs a, float *part)
 {
-    __shared__ double lds[4];
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const float rstd = a.rstd[row];
-        double s = 0.0;
-        for (int64_t c = threadIdx.x; c < a.cols; c += 256)
-            s += (load_value(a.dy, a.dy_bf16, row * a.lddy + c) * load_value(a.w, a.w_bf16, c)) *
-                 (load_value(a.h, a.h_bf16, row * a.ldh + c) * rstd);
-        s = group_sum(s, 4, lds);
-        if (threadIdx.x == 0) means[row] = (float)(s / (double)a.cols);
+    constexpr int EH = HB ? 2 : 4, ED = DB ? 2 : 4;
+    constexpr int kPer = LANES ? 256 / (LANES ? LANES : 1) : 1;        // rows at a time
+    __shared__ double lds[2][16];
+    const int t = LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x, step = LANES ? LANES : blockDim.x;
+    const int sub = LANES ? threadIdx.x / (LANES ? LANES : 1) : 0;
+    float w[CH][8];
+    double acc[CH][8];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const int64_t c = 8 * (t + k * (int64_t)step);
+        load_eight(w[k], a.w, a.w_bf16, c, a.cols - c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[k][j] = 0.0;
+    }
+    int turn = 0;
+    for (int64_t first = blockIdx.x * (int64_t)kPer; first < a.rows; first += gridDim.x * (int64_t)kPer, turn ^= 1) {
+        const int64_t row = first + sub;
+        // (lanes of a row beyond the last one hold nothing)
+        const bool some = row < a.rows;
+        const int64_t cols = some ? a.cols : 0;
+        const uint8_t *hp = reinterpret_cast<const uint8_t *>(a.h) + row * a.ldh * EH;
+        const uint8_t *dyp = reinterpret_cast<const uint8_t *>(a.dy) + row * a.lddy * ED;
+        const uint8_t *dhp = reinterpret_cast<const uint8_t *>(a.dh) + row * a.lddh * EH;
+        uint8_t *dxp = reinterpret_cast<uint8_t *>(a.dx) + row * a.lddx * EH;
+        Eight<HB> h[CH], dh[CH];
+        Eight<DB> dy[CH];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int64_t c = 8 * (t + k * (int64_t)step);
+            h[k].load(hp + c * EH, cols - c);
+            dy[k].load(dyp + c * ED, cols - c);
+            if (a.dh) dh[k].load(dhp + c * EH, cols - c);
+            else dh[k].zero();
+        }
+        const float rstd = some ? a.rstd[row] : 0.f;
+        double sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < CH; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float n = h[k].at(j) * rstd, d = dy[k].at(j);
+                sum = __builtin_fma((double)(d * w[k][j]), (double)n, sum);
+                acc[k][j] = __builtin_fma((double)d, (double)n, acc[k][j]);
+            }
+        if constexpr (LANES) sum = lane_sum<LANES ? LANES : 64>(sum);
+        else sum = group_sum(sum, blockDim.x >> 6, lds[turn]);
+        const float mean = (float)(sum / (double)a.cols);
+        // (n and g are formed again: kept over the sum they would take 32 registers a chunk)
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            h[k].opaque();
+            dy[k].opaque();
+        }
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int64_t c = 8 * (t + k * (int64_t)step);
+            if (c >= cols) break;
+            float dx[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float n = h[k].at(j) * rstd;
+                dx[j] = rstd * (dy[k].at(j) * w[k][j] - n * mean) + dh[k].at(j);
+            }
+            Eight<HB> o;
+            o.set(dx);
+            o.store(dxp + c * EH, cols - c);
+        }
+    }
+    if (!part) return;
+    part += blockIdx.x * a.cols;
+    if constexpr (LANES) {
+        // the rows' lanes of a column, in order
+        __shared__ double sums[kPer][8 * (LANES ? LANES : 1) + 2];
+        for (int k = 0; k < CH; ++k) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[sub][8 * t + j] = acc[k][j];
+            __syncthreads();
+            for (int i = threadIdx.x; i < 8 * LANES; i += 256) {
+                const int64_t c = 8 * (int64_t)LANES * k + i;
+                double s = 0.0;
+                for (int p = 0; p < kPer; ++p) s += sums[p][i];
+                if (c < a.cols) part[c] = (float)s;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int64_t c = 8 * (t + k * (int64_t)step);
+            Eight<false> o;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = (float)acc[k][j];
+            o.set(v);
+            o.store(reinterpret_cast<uint8_t *>(part + c), a.cols - c);
+        }
     }
 }
 
-// 256 columns of every gridDim.y-th row: dx, and the sum of dy * xhat over these rows
+// Rows that no workgroup's registers hold: their means first
+__global__ __launch_bounds__(1024) void rmsnorm_grad_means_kernel(const NormGradArgs a, float *means)
+{
+    const int64_t row = group_index();
+    if (row >= a.rows) return;
+    __shared__ double lds[16];
+    const float rstd = a.rstd[row];
+    double s = 0.0;
+    for (int64_t c = 8 * (int64_t)threadIdx.x; c < a.cols; c += 8 * 1024) {
+        float d[8], w[8], h[8];
+        load_eight(d, a.dy, a.dy_bf16, row * a.lddy + c, a.cols - c);
+        load_eight(w, a.w, a.w_bf16, c, a.cols - c);
+        load_eight(h, a.h, a.h_bf16, row * a.ldh + c, a.cols - c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s = __builtin_fma((double)(d[j] * w[j]), (double)(h[j] * rstd), s);
+    }
+    s = group_sum(s, 16, lds);
+    if (threadIdx.x == 0) means[row] = (float)(s / (double)a.cols);
+}
+
+// .. then 2048 columns of every gridDim.y-th row
 __global__ __launch_bounds__(256) void rmsnorm_grad_tile_kernel(const NormGradArgs a, const float *means, float *part)
 {
-    const int64_t c = blockIdx.x * (int64_t)256 + threadIdx.x;
-    if (c >= a.cols) return;
-    const float w = load_value(a.w, a.w_bf16, c);
-    float sum = 0.f;
+    const int64_t c = 8 * (blockIdx.x * (int64_t)256 + threadIdx.x), n = a.cols - c;
+    if (n <= 0) return;
+    float w[8];
+    load_eight(w, a.w, a.w_bf16, c, n);
+    double acc[8] = {};
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-        const float rstd = a.rstd[row];
-        const float xh = load_value(a.h, a.h_bf16, row * a.ldh + c) * rstd;
-        const float dy = load_value(a.dy, a.dy_bf16, row * a.lddy + c);
-        float dx = rstd * (dy * w - xh * means[row]);
-        if (a.dh) dx += load_value(a.dh, a.h_bf16, row * a.lddh + c);
-        store_value(a.dx, a.h_bf16, row * a.lddx + c, dx);
-        sum += dy * xh;
+        const float rstd = a.rstd[row], mean = means[row];
+        float h[8], d[8], dh[8] = {};
+        load_eight(h, a.h, a.h_bf16, row * a.ldh + c, n);
+        load_eight(d, a.dy, a.dy_bf16, row * a.lddy + c, n);
+        if (a.dh) load_eight(dh, a.dh, a.h_bf16, row * a.lddh + c, n);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float x = h[j] * rstd;
+            acc[j] = __builtin_fma((double)d[j], (double)x, acc[j]);
+            dh[j] += rstd * (d[j] * w[j] - x * mean);
+        }
+        store_eight(dh, a.dx, a.h_bf16, row * a.lddx + c, n);
     }
-    if (a.dw) part[blockIdx.y * a.cols + c] = sum;
+    if (!part) return;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)acc[j];
+    store_eight(v, part, 0, blockIdx.y * a.cols + c, n);
 }
 
-__global__ __launch_bounds__(256) void rmsnorm_grad_join_kernel(const float *part, int64_t parts, int64_t cols, float *dw)
+// dw of 32 columns: 16 lanes a column take every 16th part
+__global__ __launch_bounds__(512) void rmsnorm_grad_join_kernel(const float *part, int64_t parts, int64_t cols, float *dw)
 {
-    const int64_t c = blockIdx.x * (int64_t)256 + threadIdx.x;
-    if (c >= cols) return;
+    __shared__ double sums[16][33];
+    const int col = threadIdx.x & 31, sub = threadIdx.x >> 5;
+    const int64_t c = blockIdx.x * (int64_t)32 + col;
     double s = 0.0;
-    for (int64_t i = 0; i < parts; ++i) s += part[i * cols + c];
-    dw[c] = (float)s;
+    if (c < cols) {
+#pragma unroll 8
+        for (int64_t i = sub; i < parts; i += 16) s += part[i * cols + c];
+    }
+    sums[sub][col] = s;
+    __syncthreads();
+    if (sub == 0 && c < cols) {
+        for (int i = 1; i < 16; ++i) s += sums[i][col];
+        dw[c] = (float)s;
+    }
 }
-
-int64_t parts_of(int64_t rows) { return rows < 256 ? rows : 256; }
 
 inline int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
+
+constexpr int64_t kLong = 16384;       // columns that a workgroup's registers hold
+
+// rows that a workgroup has at a time
+int64_t rows_at_once(int64_t cols) { return cols <= 256 ? 16 : cols <= 1024 ? 4 : 1; }
+
+// workgroups, each with one part of dw
+int64_t parts_of(int64_t rows, int64_t cols)
+{
+    if (cols > kLong) return rows < 256 ? rows : 256;
+    const int64_t per = rows_at_once(cols), turns = (rows + per - 1) / per;
+    return turns < kParts ? turns : kParts;
+}
+
+int64_t means_bytes(int64_t rows, int64_t cols) { return cols > kLong ? up256(rows * 4) : 0; }
+
+template <bool HB, bool DB>
+hipError_t launch_grad(const NormGradArgs &a, unsigned parts, float *part, hipStream_t s)
+{
+    const int64_t chunks = (a.cols + 7) / 8;
+    if (chunks <= 32) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 16, 2>), dim3(parts), dim3(256), 0, s, a, part);
+    else if (chunks <= 128) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 64, 2>), dim3(parts), dim3(256), 0, s, a, part);
+    else if (chunks <= 1024) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, 1>), dim3(parts), dim3((unsigned)((chunks + 63) / 64 * 64)), 0, s, a, part);
+    else hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, 2>), dim3(parts), dim3((unsigned)((chunks + 127) / 128 * 64)), 0, s, a, part);
+    return hipGetLastError();
+}
 
 }  // namespace
 
 int64_t rmsnorm_grad_workspace(int64_t rows, int64_t cols)
 {
-    return up256(rows * 4) + up256(parts_of(rows) * cols * 4);
+    return means_bytes(rows, cols) + up256(parts_of(rows, cols) * cols * 4);
 }
 
 hipError_t launch_rmsnorm_grad(const NormGradArgs &a, hipStream_t stream)
 {
-    const unsigned tiles = (unsigned)((a.cols + 255) / 256);
-    float *means = reinterpret_cast<float *>(a.workspace), *part = reinterpret_cast<float *>(a.workspace + up256(a.rows * 4));
-    const int64_t parts = parts_of(a.rows);
+    const int64_t parts = parts_of(a.rows, a.cols);
+    float *means = reinterpret_cast<float *>(a.workspace);
+    float *sums = reinterpret_cast<float *>(a.workspace + means_bytes(a.rows, a.cols)), *part = a.dw ? sums : nullptr;
     if (a.rows > 0) {
-        const int64_t most = 1 << 20;
-        hipLaunchKernelGGL(rmsnorm_grad_rows_kernel, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(256), 0, stream, a, means);
-        hipLaunchKernelGGL(rmsnorm_grad_tile_kernel, dim3(tiles, (unsigned)parts), dim3(256), 0, stream, a, means, part);
+        hipError_t e;
+        if (a.cols > kLong) {
+            hipLaunchKernelGGL(rmsnorm_grad_means_kernel, row_grid(a.rows), dim3(1024), 0, stream, a, means);
+            hipLaunchKernelGGL(rmsnorm_grad_tile_kernel, dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)parts), dim3(256), 0, stream, a, means, part);
+            e = hipGetLastError();
+        } else if (a.h_bf16) {
+            e = a.dy_bf16 ? launch_grad<true, true>(a, (unsigned)parts, part, stream) : launch_grad<true, false>(a, (unsigned)parts, part, stream);
+        } else {
+            e = a.dy_bf16 ? launch_grad<false, true>(a, (unsigned)parts, part, stream) : launch_grad<false, false>(a, (unsigned)parts, part, stream);
+        }
+        if (e != hipSuccess) return e;
     }
-    if (a.dw) hipLaunchKernelGGL(rmsnorm_grad_join_kernel, dim3(tiles), dim3(256), 0, stream, part, parts, a.cols, a.dw);
+    if (a.dw) hipLaunchKernelGGL(rmsnorm_grad_join_kernel, dim3((unsigned)((a.cols + 31) / 32)), dim3(512), 0, stream, sums, parts, a.cols, a.dw);
     return hipGetLastError();
 }
 

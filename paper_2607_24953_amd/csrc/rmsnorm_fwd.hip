@@ -1,4 +1,10 @@
 // Root-mean-square norm of rows, with the residual's addition.
+//
+// One read of x and the residual: a row stays in registers between the sum of its squares and
+// the products with it.  A lane holds CH chunks of eight neighbouring elements (16 bytes of
+// bfloat16), chunk k of a row in lane k % (lanes of the row).  The squares are summed in 64 bits,
+// where those of any float32 neither overflow nor vanish; the vector unit has time for it beside
+// the memory.
 #include "norm_common.hpp"
 #include "norms.hpp"
 
@@ -6,41 +12,141 @@ namespace q2d {
 
 namespace {
 
-__global__ __launch_bounds__(256) void rmsnorm_rows_kernel(const NormArgs a)
+// XB: x is bfloat16.  RT: no residual, a float32 or a bfloat16 one.  LANES: of a row: 16 or 64
+// (a workgroup of 256 takes several rows), or 0 for all of the workgroup.
+template <bool XB, int RT, int LANES, int CH>
+__global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_rows_kernel(const NormArgs a)
 {
-    __shared__ double lds[4];
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const int64_t x0 = row * a.ldx, r0 = row * a.ldr, h0 = row * a.ldh, y0 = row * a.ldy;
-        auto h_at = [&](int64_t c) __attribute__((always_inline)) {
-            float v = load_value(a.x, a.x_bf16, x0 + c);
-            if (a.r) {
-                v += load_value(a.r, a.r_bf16, r0 + c);
-                if (a.x_bf16) v = bf16_to_f(f_to_bf16_rne(v));
-            }
-            return v;
-        };
-        double s = 0.0;
-        for (int64_t c = threadIdx.x; c < a.cols; c += 256) {
-            const double v = h_at(c);
-            s += v * v;
+    constexpr int EX = XB ? 2 : 4, ER = RT == 2 ? 2 : 4;
+    const int t = LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x, step = LANES ? LANES : blockDim.x;
+    const int64_t row = LANES ? group_index() * (256 / (LANES ? LANES : 1)) + threadIdx.x / (LANES ? LANES : 1) : group_index();
+    if (LANES == 0 && row >= a.rows) return;
+    // (lanes of a row beyond the last one hold nothing)
+    const int64_t cols = row < a.rows ? a.cols : 0;
+    const uint8_t *x = reinterpret_cast<const uint8_t *>(a.x) + row * a.ldx * EX;
+    const uint8_t *r = reinterpret_cast<const uint8_t *>(a.r) + row * a.ldr * ER;
+    Eight<XB> h[CH];
+    double sum = 0.0;
+    {
+        Eight<RT == 2> d[CH];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int64_t c = 8 * (t + k * (int64_t)step);
+            h[k].load(x + c * EX, cols - c);
+            if constexpr (RT != 0) d[k].load(r + c * ER, cols - c);
         }
-        const float rstd = rstd_of(group_sum(s, 4, lds), a.cols, a.eps);
-        if (threadIdx.x == 0) a.rstd[row] = rstd;
-        for (int64_t c = threadIdx.x; c < a.cols; c += 256) {
-            const float v = h_at(c);
-            if (a.h) store_value(a.h, a.x_bf16, h0 + c, v);
-            if (a.y) store_value(a.y, a.y_bf16, y0 + c, (v * rstd) * load_value(a.w, a.w_bf16, c));
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            if constexpr (RT != 0) {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = h[k].at(j) + d[k].at(j);
+                h[k].set(v);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const double v = h[k].at(j);
+                sum = __builtin_fma(v, v, sum);
+            }
         }
     }
+    if constexpr (RT != 0) {
+        uint8_t *out = reinterpret_cast<uint8_t *>(a.h) + row * a.ldh * EX;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int64_t c = 8 * (t + k * (int64_t)step);
+            h[k].store(out + c * EX, cols - c);
+        }
+    }
+    if constexpr (LANES) {
+        sum = lane_sum<LANES ? LANES : 64>(sum);
+    } else {
+        __shared__ double lds[16];
+        sum = group_sum(sum, blockDim.x >> 6, lds);
+    }
+    const float rstd = rstd_of(sum, a.cols, a.eps);
+    if (t == 0 && row < a.rows) a.rstd[row] = rstd;
+    if (!a.y) return;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const int64_t c = 8 * (t + k * (int64_t)step);
+        if (c >= cols) break;
+        float w[8], y[8];
+        load_eight(w, a.w, a.w_bf16, c, cols - c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = (h[k].at(j) * rstd) * w[j];
+        store_eight(y, a.y, a.y_bf16, row * a.ldy + c, cols - c);
+    }
+}
+
+// Rows that no workgroup's registers hold: a second read of what this lane read or wrote
+__global__ __launch_bounds__(1024) void rmsnorm_long_rows_kernel(const NormArgs a)
+{
+    const int64_t row = group_index();
+    if (row >= a.rows) return;
+    double sum = 0.0;
+    for (int64_t c = 8 * (int64_t)threadIdx.x; c < a.cols; c += 8 * 1024) {
+        float v[8], d[8];
+        load_eight(v, a.x, a.x_bf16, row * a.ldx + c, a.cols - c);
+        if (a.r) {
+            load_eight(d, a.r, a.r_bf16, row * a.ldr + c, a.cols - c);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] += d[j];
+                if (a.x_bf16) v[j] = round_bf16(v[j]);
+            }
+            store_eight(v, a.h, a.x_bf16, row * a.ldh + c, a.cols - c);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)v[j], (double)v[j], sum);
+    }
+    __shared__ double lds[16];
+    const float rstd = rstd_of(group_sum(sum, 16, lds), a.cols, a.eps);
+    if (threadIdx.x == 0) a.rstd[row] = rstd;
+    if (!a.y) return;
+    const void *h = a.r ? a.h : a.x;
+    const int64_t ldh = a.r ? a.ldh : a.ldx;
+    for (int64_t c = 8 * (int64_t)threadIdx.x; c < a.cols; c += 8 * 1024) {
+        float v[8], w[8];
+        load_eight(v, h, a.x_bf16, row * ldh + c, a.cols - c);
+        load_eight(w, a.w, a.w_bf16, c, a.cols - c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (v[j] * rstd) * w[j];
+        store_eight(v, a.y, a.y_bf16, row * a.ldy + c, a.cols - c);
+    }
+}
+
+// `per` rows a workgroup.  (Work-items along one dimension of a launch stay below 2^32: rows beyond
+// 2^20 workgroups go along the second.)
+template <bool XB, int RT, int LANES, int CH>
+hipError_t launch_c(const NormArgs &a, int64_t per, unsigned threads, hipStream_t s)
+{
+    hipLaunchKernelGGL((rmsnorm_rows_kernel<XB, RT, LANES, CH>), row_grid((a.rows + per - 1) / per), dim3(threads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <bool XB, int RT>
+hipError_t launch_r(const NormArgs &a, hipStream_t s)
+{
+    const int64_t chunks = (a.cols + 7) / 8;
+    if (chunks <= 32) return launch_c<XB, RT, 16, 2>(a, 16, 256, s);
+    if (chunks <= 128) return launch_c<XB, RT, 64, 2>(a, 4, 256, s);
+    const auto threads = [&](int ch) { return (unsigned)((chunks + 64 * ch - 1) / (64 * ch) * 64); };
+    if (chunks <= 2048) return launch_c<XB, RT, 0, 2>(a, 1, threads(2), s);
+    return launch_c<XB, RT, 0, 4>(a, 1, threads(4), s);
 }
 
 }  // namespace
 
 hipError_t launch_rmsnorm_rows(const NormArgs &a, hipStream_t stream)
 {
-    const int64_t most = 1 << 20;
-    hipLaunchKernelGGL(rmsnorm_rows_kernel, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(256), 0, stream, a);
-    return hipGetLastError();
+    if (a.cols > 32768) {
+        hipLaunchKernelGGL(rmsnorm_long_rows_kernel, row_grid(a.rows), dim3(1024), 0, stream, a);
+        return hipGetLastError();
+    }
+    const int rt = !a.r ? 0 : a.r_bf16 ? 2 : 1;
+    if (a.x_bf16) return rt == 0 ? launch_r<true, 0>(a, stream) : rt == 1 ? launch_r<true, 1>(a, stream) : launch_r<true, 2>(a, stream);
+    return rt == 0 ? launch_r<false, 0>(a, stream) : rt == 1 ? launch_r<false, 1>(a, stream) : launch_r<false, 2>(a, stream);
 }
 
 }  // namespace q2d
