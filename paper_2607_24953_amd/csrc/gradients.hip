@@ -1,10 +1,11 @@
 // 2-norm over many tensors, and their scaling.
 //
-// A launch takes up to kTensors tensors as kernel arguments, so that no table has to be copied to
-// the device.  They are cut into pieces of kPiece elements; a workgroup takes every gridDim.x-th
-// piece and writes one partial sum, in 64 bits: squares of float32 neither overflow nor vanish
-// there, and the order of the additions is fixed.  The scaling kernel's workgroups each add all
-// partial sums up again, in the same order, which saves a launch between the two.
+// A launch takes its tensors as kernel arguments, as many as fit 4 KB, so that no table has to be
+// copied to the device.  They are cut into pieces of one size, the last of a tensor shorter; a
+// workgroup takes every gridDim.x-th piece and writes one partial sum, in 64 bits: squares of float32
+// neither overflow nor vanish there, and the order of the additions is fixed.  The scaling
+// kernel's workgroups each add all partial sums up again, in the same order, which saves a
+// launch between the two.
 #include "q2d.h"
 #include "kernels.hpp"
 #include "layout.hpp"
@@ -19,39 +20,51 @@ namespace q2d {
 
 namespace {
 
-constexpr int kTensors = 128;
-constexpr int64_t kPiece = 16384;
+// elements of a turn of a workgroup's 256 lanes, eight each; a piece is 1 to kTurns of them
+constexpr int kTurn = 2048, kTurns = 8;
 constexpr int kMaxParts = 2048;
 
+// N tensors; SCALED: with a place for the results
+template <int N, bool SCALED>
 struct Tensors {
-    const void *data[kTensors];
-    void *out[kTensors];
-    int64_t count[kTensors];
-    int32_t first[kTensors];       // the tensor's first piece
-    int32_t n, pieces;
-    uint32_t bf16[kTensors / 32];  // a bit a tensor
+    const void *data[N];
+    void *out[SCALED ? N : 1];
+    int32_t first[N];              // a tensor's first piece
+    int32_t last[N];               // elements of its last one
+    int32_t n, pieces, turns;
+    uint32_t bf16[(N + 31) / 32];  // a bit a tensor
+    static constexpr int kMost = N;
+    static constexpr bool kScaled = SCALED;
 };
+typedef Tensors<240, false> Squared;
+typedef Tensors<160, true> Scaled;
+static_assert(sizeof(Squared) + 8 <= 4096 && sizeof(Scaled) + 40 <= 4096, "kernel arguments");
 
-// tensor of a piece
-__device__ __forceinline__ int tensor_of(const Tensors &t, int piece) { return seg_search(t.first, t.n, piece); }
+// A piece: its tensor, first element and length
+struct Piece { int tensor; bool bf16; int64_t at; int length; };
+template <typename T>
+__device__ __forceinline__ Piece piece_of(const T &t, int piece)
+{
+    const int i = seg_search(t.first, t.n, piece), size = t.turns * kTurn;
+    const bool last = piece + 1 == (i + 1 < t.n ? t.first[i + 1] : t.pieces);
+    return {i, (bool)((t.bf16[i >> 5] >> (i & 31)) & 1), (int64_t)(piece - t.first[i]) * size, last ? t.last[i] : size};
+}
 
-__device__ __forceinline__ bool is_bf16(const Tensors &t, int i) { return (t.bf16[i >> 5] >> (i & 31)) & 1; }
-
-// Eight-element chunks that a lane has in flight, and of a piece
-constexpr int kFlight = 4, kChunks = (int)(kPiece / (8 * 256));
+// turns whose loads a lane has in flight
+constexpr int kFlight = 4;
 
 template <bool BF16>
-__device__ __forceinline__ double square_piece(const void *data, int64_t at, int64_t left)
+__device__ __forceinline__ double square_piece(const void *data, int64_t at, int length)
 {
     const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * (BF16 ? 2 : 4);
     double s = 0.0;
 #pragma unroll 1
-    for (int k0 = 0; k0 < kChunks; k0 += kFlight) {
+    for (int c0 = 8 * threadIdx.x; c0 < length; c0 += kFlight * kTurn) {
         Eight<BF16> e[kFlight];
 #pragma unroll
         for (int k = 0; k < kFlight; ++k) {
-            const int c = 8 * ((k0 + k) * 256 + threadIdx.x);
-            e[k].load(p + c * (BF16 ? 2 : 4), left - c);
+            const int c = c0 + k * kTurn;
+            e[k].load(p + c * (BF16 ? 2 : 4), length - c);
         }
 #pragma unroll
         for (int k = 0; k < kFlight; ++k)
@@ -64,14 +77,13 @@ __device__ __forceinline__ double square_piece(const void *data, int64_t at, int
     return s;
 }
 
-__global__ __launch_bounds__(256) void grad_square_kernel(const Tensors t, double *parts)
+__global__ __launch_bounds__(256) void grad_square_kernel(const Squared t, double *parts)
 {
     __shared__ double lds[4];
     double s = 0.0;
     for (int piece = blockIdx.x; piece < t.pieces; piece += gridDim.x) {
-        const int i = tensor_of(t, piece);
-        const int64_t at = (piece - t.first[i]) * kPiece, left = t.count[i] - at;
-        s += is_bf16(t, i) ? square_piece<true>(t.data[i], at, left) : square_piece<false>(t.data[i], at, left);
+        const Piece p = piece_of(t, piece);
+        s += p.bf16 ? square_piece<true>(t.data[p.tensor], p.at, p.length) : square_piece<false>(t.data[p.tensor], p.at, p.length);
     }
     s = group_sum(s, 4, lds);
     if (threadIdx.x == 0) parts[blockIdx.x] = s;
@@ -93,34 +105,34 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const double *parts, int
 }
 
 template <bool BF16>
-__device__ __forceinline__ void scale_piece(const void *data, void *out, int64_t at, int64_t left, bool clip, float f)
+__device__ __forceinline__ void scale_piece(const void *data, void *out, int64_t at, int length, bool clip, float f)
 {
     const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * (BF16 ? 2 : 4);
     uint8_t *o = reinterpret_cast<uint8_t *>(out) + at * (BF16 ? 2 : 4);
 #pragma unroll 1
-    for (int k0 = 0; k0 < kChunks; k0 += kFlight) {
+    for (int c0 = 8 * threadIdx.x; c0 < length; c0 += kFlight * kTurn) {
         Eight<BF16> e[kFlight];
 #pragma unroll
         for (int k = 0; k < kFlight; ++k) {
-            const int c = 8 * ((k0 + k) * 256 + threadIdx.x);
-            e[k].load(p + c * (BF16 ? 2 : 4), left - c);
+            const int c = c0 + k * kTurn;
+            e[k].load(p + c * (BF16 ? 2 : 4), length - c);
         }
 #pragma unroll
         for (int k = 0; k < kFlight; ++k) {
-            const int c = 8 * ((k0 + k) * 256 + threadIdx.x);
+            const int c = c0 + k * kTurn;
             if (clip) {
                 float v[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = e[k].at(j) * f;
                 e[k].set(v);
             }
-            e[k].store(o + c * (BF16 ? 2 : 4), left - c);
+            e[k].store(o + c * (BF16 ? 2 : 4), length - c);
         }
     }
 }
 
 // (the last pieces first: the square sums read them last, and some are still in the cache)
-__global__ __launch_bounds__(256) void grad_scale_kernel(const Tensors t, const double *parts, int n, const float *given,
+__global__ __launch_bounds__(256) void grad_scale_kernel(const Scaled t, const double *parts, int n, const float *given,
                                                          double max_norm, float *norm)
 {
     __shared__ double lds[4];
@@ -130,11 +142,10 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(const Tensors t, const 
     const bool clip = (float)total < __builtin_inff() && total > max_norm;
     const float f = clip ? (float)(max_norm / total) : 1.f;
     for (int piece = t.pieces - 1 - (int)blockIdx.x; piece >= 0; piece -= gridDim.x) {
-        const int i = tensor_of(t, piece);
-        if (!clip && t.out[i] == t.data[i]) continue;
-        const int64_t at = (piece - t.first[i]) * kPiece, left = t.count[i] - at;
-        if (is_bf16(t, i)) scale_piece<true>(t.data[i], t.out[i], at, left, clip, f);
-        else scale_piece<false>(t.data[i], t.out[i], at, left, clip, f);
+        const Piece p = piece_of(t, piece);
+        if (!clip && t.out[p.tensor] == t.data[p.tensor]) continue;
+        if (p.bf16) scale_piece<true>(t.data[p.tensor], t.out[p.tensor], p.at, p.length, clip, f);
+        else scale_piece<false>(t.data[p.tensor], t.out[p.tensor], p.at, p.length, clip, f);
     }
 }
 
@@ -157,7 +168,7 @@ q2d_status check_set(const Set &g)
         const uintptr_t size = (uintptr_t)dtype_bytes((q2d_dtype)g.dtypes[i]);
         if (!g.data[i] || !aligned(g.data[i], size)) return Q2D_EINVAL;
         if (g.out && (!g.out[i] || !aligned(g.out[i], size))) return Q2D_EINVAL;
-        pieces += cdiv(g.counts[i], kPiece);
+        pieces += cdiv(g.counts[i], kTurn);
         if (pieces > INT32_MAX) return Q2D_EUNSUPPORTED;
     }
     return Q2D_OK;
@@ -192,52 +203,65 @@ q2d_status check_apart(const Set &g)
     return Q2D_OK;
 }
 
-int64_t launches_of(int32_t n) { return (n + kTensors - 1) / kTensors; }
-
 // Partial sums of a call at most: kMaxParts shared by its launches, one a launch at least
-int64_t parts_of(int32_t n) { return kMaxParts + launches_of(n); }
+int64_t parts_of(int32_t n) { return kMaxParts + n / Squared::kMost + 1; }
 
-// Runs f(tensors, workgroups) for each launch of a set; false for an error of the runtime
-template <typename F>
-bool for_launches(const Set &g, F f)
+// Fills t with the tensors of a set from i on, as many as fit; the first one that did not
+template <typename T>
+int32_t fill(const Set &g, int32_t i, int turns, T &t)
+{
+    const int64_t size = turns * (int64_t)kTurn;
+    int64_t pieces = 0;
+    t = T{};
+    for (; i < g.n && t.n < T::kMost; ++i) {
+        if (g.counts[i] == 0) continue;
+        const int64_t k = cdiv(g.counts[i], size);
+        t.data[t.n] = g.data[i];
+        if (T::kScaled) t.out[t.n] = g.out ? g.out[i] : const_cast<void *>(g.data[i]);
+        t.first[t.n] = (int32_t)pieces;
+        t.last[t.n] = (int32_t)(g.counts[i] - (k - 1) * size);
+        if (g.dtypes[i] == Q2D_BF16) t.bf16[t.n >> 5] |= 1u << (t.n & 31);
+        pieces += k;
+        ++t.n;
+    }
+    t.pieces = (int32_t)pieces;
+    t.turns = turns;
+    return i;
+}
+
+int64_t elements(const Set &g)
 {
     int64_t all = 0;
-    for (int32_t i = 0; i < g.n; ++i) all += cdiv(g.counts[i], kPiece);
-    for (int32_t i = 0; i < g.n;) {
-        Tensors t;
-        t.n = 0;
-        int64_t pieces = 0;
-        for (auto &b : t.bf16) b = 0;
-        for (; i < g.n && t.n < kTensors; ++i) {
-            if (g.counts[i] == 0) continue;
-            t.data[t.n] = g.data[i];
-            t.out[t.n] = g.out ? g.out[i] : const_cast<void *>(g.data[i]);
-            t.count[t.n] = g.counts[i];
-            t.first[t.n] = (int32_t)pieces;
-            if (g.dtypes[i] == Q2D_BF16) t.bf16[t.n >> 5] |= 1u << (t.n & 31);
-            pieces += cdiv(g.counts[i], kPiece);
-            ++t.n;
-        }
-        if (t.n == 0) break;
-        t.pieces = (int32_t)pieces;
-        for (int k = t.n; k < kTensors; ++k) {
-            t.data[k] = nullptr; t.out[k] = nullptr; t.count[k] = 0; t.first[k] = t.pieces;
-        }
-        if (!f(t, (unsigned)std::min<int64_t>(pieces, std::max<int64_t>(1, kMaxParts * pieces / all)))) return false;
-    }
-    return true;
+    for (int32_t i = 0; i < g.n; ++i) all += g.counts[i];
+    return all;
+}
+
+// Turns of a piece: a workgroup for each of 1024 pieces first, then longer ones.  (In one size of
+// 8 turns the 0.8 M float32 of a small model's gradients took 5.1 us for their squares.)
+int turns_of(int64_t all)
+{
+    int t = 1;
+    while (t < kTurns && all / (2 * t * kTurn) >= 1024) t *= 2;
+    return t;
 }
 
 // Partial sums of the set into parts; their number, or -1
-int square_sums(const Set &g, double *parts, hipStream_t stream)
+int square_sums(const Set &g, int64_t all, double *parts, hipStream_t stream)
 {
+    const int turns = turns_of(all);
     int n = 0;
-    const bool ok = for_launches(g, [&](const Tensors &t, unsigned groups) {
+    Squared t;
+    for (int32_t i = 0; i < g.n;) {
+        i = fill(g, i, turns, t);
+        if (t.n == 0) break;
+        // a launch's share of the parts, by its pieces
+        const int64_t share = (int64_t)((double)kMaxParts * t.pieces * turns * kTurn / (double)(all + t.n * (int64_t)turns * kTurn));
+        const int groups = (int)std::min<int64_t>(t.pieces, std::max<int64_t>(1, std::min<int64_t>(share, kMaxParts)));
         hipLaunchKernelGGL(grad_square_kernel, dim3(groups), dim3(256), 0, stream, t, parts + n);
-        n += (int)groups;
-        return hipGetLastError() == hipSuccess;
-    });
-    return ok ? n : -1;
+        if (hipGetLastError() != hipSuccess) return -1;
+        n += groups;
+    }
+    return n;
 }
 
 }  // namespace
@@ -258,7 +282,7 @@ q2d_status q2d_grad_norm(int32_t n, const void *const *data, const int64_t *coun
     if (s != Q2D_OK) return s;
     if (!norm || !aligned(norm, 4) || !workspace || !aligned(workspace, 8) || workspace_bytes < q2d_grad_workspace(n)) return Q2D_EINVAL;
     double *parts = reinterpret_cast<double *>(workspace);
-    const int k = square_sums(g, parts, stream);
+    const int k = square_sums(g, elements(g), parts, stream);
     if (k < 0) return Q2D_ELAUNCH;
     hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, stream, parts, k, norm);
     return hipGetLastError() == hipSuccess ? Q2D_OK : Q2D_ELAUNCH;
@@ -278,22 +302,27 @@ q2d_status q2d_clip_grads(int32_t n, const void *const *data, void *const *out, 
     if (!one || (given && norm) || !aligned(one, 4)) return Q2D_EINVAL;
     double *parts = nullptr;
     int k = 0;
+    const int64_t all = elements(g);
     if (!given) {
         if (!workspace || !aligned(workspace, 8) || workspace_bytes < q2d_grad_workspace(n)) return Q2D_EINVAL;
         parts = reinterpret_cast<double *>(workspace);
-        k = square_sums(g, parts, stream);
+        k = square_sums(g, all, parts, stream);
         if (k < 0) return Q2D_ELAUNCH;
         if (k == 0) {       // no elements: nothing to scale
             hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, stream, parts, 0, norm);
             return hipGetLastError() == hipSuccess ? Q2D_OK : Q2D_ELAUNCH;
         }
     }
-    const bool ok = for_launches(g, [&](const Tensors &t, unsigned groups) {
-        hipLaunchKernelGGL(grad_scale_kernel, dim3(groups), dim3(256), 0, stream, t, parts, k, given, max_norm, norm);
-        norm = nullptr;      // (written by the first launch)
-        return hipGetLastError() == hipSuccess;
-    });
-    return ok ? Q2D_OK : Q2D_ELAUNCH;
+    const int turns = turns_of(all);
+    Scaled t;
+    for (int32_t i = 0; i < n;) {
+        i = fill(g, i, turns, t);
+        if (t.n == 0) break;
+        hipLaunchKernelGGL(grad_scale_kernel, dim3(std::min(t.pieces, kMaxParts)), dim3(256), 0, stream, t, parts, k, given, max_norm, norm);
+        if (hipGetLastError() != hipSuccess) return Q2D_ELAUNCH;
+        norm = nullptr;     // (written by the first launch)
+    }
+    return Q2D_OK;
 }
 
 }  // extern "C"

@@ -5,6 +5,8 @@ from __future__ import annotations
 
 import array
 import ctypes
+import operator
+import struct
 
 import torch
 
@@ -27,12 +29,17 @@ class _NormGrad(ctypes.Structure):
                 ("weight", ctypes.c_void_p), ("rstd", ctypes.c_void_p), ("dw", ctypes.c_void_p)]
 
 
+# the same structures, packed
+_NORM = struct.Struct("4i2qdQqQqQQqQqQ")
+_GRAD = struct.Struct("3i4x2qQqQqQqQqQQQ")
+assert _NORM.size == ctypes.sizeof(_Norm) and _GRAD.size == ctypes.sizeof(_NormGrad)
+
 _P, _I64, _I32, _F64 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_double
 _TP = ctypes.POINTER(_Tensor)
 for _name, _args, _res in (
-        ("q2d_rmsnorm_fwd", [ctypes.POINTER(_Norm), _TP, _TP, _P], _I32),
+        ("q2d_rmsnorm_fwd", [_P, _TP, _TP, _P], _I32),
         ("q2d_rmsnorm_workspace", [_I64, _I64], _I64),
-        ("q2d_rmsnorm_bwd", [ctypes.POINTER(_NormGrad), _P, _I64, _P], _I32),
+        ("q2d_rmsnorm_bwd", [_P, _P, _I64, _P], _I32),
         ("q2d_grad_workspace", [_I32], _I64),
         ("q2d_grad_norm", [_I32, _P, _P, _P, _P, _P, _I64, _P], _I32),
         ("q2d_clip_grads", [_I32, _P, _P, _P, _P, _F64, _P, _P, _P, _I64, _P], _I32)):
@@ -52,44 +59,58 @@ def _call(device, name, *args):
 
 def _rows(t, shape, device, what):
     """(pointer, row pitch) of a [rows, cols] tensor with unit stride along its rows."""
-    if t.shape != shape or (t.stride(1) != 1 and shape[1] > 1):
-        raise Q2DError("%s: a tensor of shape %s with unit stride along the rows is expected" % (what, tuple(shape)))
+    if t.shape != shape:
+        raise Q2DError("%s: a tensor of shape %s is expected" % (what, tuple(shape)))
+    pitch, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise Q2DError("%s: unit stride along the rows is expected" % what)
     if t.device != device:
         _same_device(device, t)
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), pitch
 
 
 def _vector(t, n, device, what, dtype=None):
-    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+    if t.shape != (n,) or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
         raise Q2DError("%s: a contiguous %s vector of %d elements is expected" % (what, dtype or "device", n))
     if t.device != device:
         _same_device(device, t)
     return t.data_ptr()
 
 
-def _problem(x, weight, eps, residual, h, rstd):
-    if x.dim() != 2 or not x.is_cuda:
+def _forward(x, weight, eps, residual, h, rstd, y, q4, q8):
+    """q2d_rmsnorm_fwd, with h and rstd made where they are None; returns them."""
+    device, shape = x.device, x.shape
+    if device.type != "cuda" or len(shape) != 2:
         raise Q2DError("expected x as a 2-D device tensor")
-    shape, device = x.shape, x.device
-    n = _Norm(x_dtype=_dtype_code(x.dtype), weight_dtype=_dtype_code(weight.dtype), rows=shape[0], cols=shape[1], eps=eps)
-    n.x, n.ldx = _rows(x, shape, device, "x")
-    n.weight = _vector(weight, shape[1], device, "weight")
+    rows, cols = shape
+    xp, ldx = _rows(x, shape, device, "x")
+    rp = ldr = hp = ldh = yp = ldy = r_code = y_code = 0
+    x_code = _dtype_code(x.dtype)
     if residual is not None:
         if h is None:
             h = torch.empty(shape, dtype=x.dtype, device=device)
         elif h.dtype != x.dtype:
             raise Q2DError("h: the dtype of x is expected")
-        n.residual_dtype = _dtype_code(residual.dtype)
-        n.residual, n.ld_residual = _rows(residual, shape, device, "residual")
-        n.h, n.ldh = _rows(h, shape, device, "h")
+        r_code = _dtype_code(residual.dtype)
+        rp, ldr = _rows(residual, shape, device, "residual")
+        hp, ldh = _rows(h, shape, device, "h")
     elif h is not None:
         raise Q2DError("h is x itself without a residual")
     else:
         h = x
+    if y is not None:
+        y_code = _dtype_code(y.dtype)
+        yp, ldy = _rows(y, shape, device, "y")
     if rstd is None:
-        rstd = torch.empty(shape[0], dtype=torch.float32, device=device)
-    n.rstd = _vector(rstd, shape[0], device, "rstd", torch.float32)
-    return n, h, rstd
+        rstd = torch.empty(rows, dtype=torch.float32, device=device)
+        sp = rstd.data_ptr()
+    else:
+        sp = _vector(rstd, rows, device, "rstd", torch.float32)
+    # (packed: a ctypes structure filled field by field takes 2 us more)
+    _call(device, "q2d_rmsnorm_fwd",
+          _NORM.pack(x_code, r_code, _dtype_code(weight.dtype), y_code, rows, cols, eps, xp, ldx, rp, ldr,
+                     _vector(weight, cols, device, "weight"), hp, ldh, yp, ldy, sp), q4, q8)
+    return h, rstd
 
 
 def q2d_rmsnorm_fwd(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual: torch.Tensor | None = None,
@@ -98,12 +119,9 @@ def q2d_rmsnorm_fwd(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, re
     """Root-mean-square norm of the rows of h = x + residual (x [rows, cols]; h in x's dtype, x
     itself without a residual) times weight [cols]; returns (y, h, rstd).  rstd (float32 [rows])
     is what q2d_rmsnorm_bwd needs.  h may be x or residual itself: in place."""
-    n, h, rstd = _problem(x, weight, eps, residual, h, rstd)
     if y is None:
         y = torch.empty(x.shape, dtype=y_dtype, device=x.device)
-    n.y_dtype = _dtype_code(y.dtype)
-    n.y, n.ldy = _rows(y, x.shape, x.device, "y")
-    _call(x.device, "q2d_rmsnorm_fwd", ctypes.byref(n), None, None)
+    h, rstd = _forward(x, weight, eps, residual, h, rstd, y, None, None)
     return y, h, rstd
 
 
@@ -115,20 +133,21 @@ def q2d_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-
     h; returns (list of QTensors, h, rstd).  The codes are those of the quantizers for the
     float32 y, rounded to nearest.  block: edge of the 2D blocks (32 or 64); orientations: (True,
     False) for the rowwise copies alone, which a forward GEMM reads; out: QTensors to fill."""
-    n, h, rstd = _problem(x, weight, eps, residual, h, rstd)
     formats = tuple(formats)
     kinds = [f == MXFP8 for f in formats]
     if not formats or any(f not in (FP4_2D, FP4_1D, MXFP8) for f in formats) or len(set(kinds)) != len(kinds):
         raise Q2DError("formats: one of FP4_2D and FP4_1D, MXFP8, or one of each is expected")
+    if x.dim() != 2:
+        raise Q2DError("expected x as a 2-D device tensor")
     if out is None:
-        out = [QTensor(f, n.rows, n.cols, x.device, block if f == FP4_2D else 32, orientations) for f in formats]
+        out = [QTensor(f, *x.shape, x.device, block if f == FP4_2D else 32, orientations) for f in formats]
     elif len(out) != len(formats) or any(q.fmt != f or q.nseg is not None for q, f in zip(out, formats)):
         raise Q2DError("out: a QTensor for each of formats is expected")
     _same_device(x.device, *out)
     q = [None, None]
     for t, mx in zip(out, kinds):
         q[mx] = t.ptr()
-    _call(x.device, "q2d_rmsnorm_fwd", ctypes.byref(n), q[0], q[1])
+    h, rstd = _forward(x, weight, eps, residual, h, rstd, None, *q)
     return out, h, rstd
 
 
@@ -138,32 +157,34 @@ def q2d_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rst
     """Gradients (dx, dw) of the norm from dy, and h and rstd of the forward call: dx (h's dtype)
     for x and for the residual, with dh, the gradient that reaches h by other ways, added; dw
     (float32 [cols]) for the weight, None with need_dw=False.  dx may be dh itself."""
-    if h.dim() != 2 or not h.is_cuda:
+    device, shape = h.device, h.shape
+    if device.type != "cuda" or len(shape) != 2:
         raise Q2DError("expected h as a 2-D device tensor")
-    shape, device = h.shape, h.device
-    n = _NormGrad(h_dtype=_dtype_code(h.dtype), dy_dtype=_dtype_code(dy.dtype), weight_dtype=_dtype_code(weight.dtype),
-                  rows=shape[0], cols=shape[1])
-    n.h, n.ldh = _rows(h, shape, device, "h")
-    n.dy, n.lddy = _rows(dy, shape, device, "dy")
-    n.weight = _vector(weight, shape[1], device, "weight")
-    n.rstd = _vector(rstd, shape[0], device, "rstd", torch.float32)
+    rows, cols = shape
     if dx is None:
         dx = torch.empty(shape, dtype=h.dtype, device=device)
     if dx.dtype != h.dtype or (dh is not None and dh.dtype != h.dtype):
         raise Q2DError("dh and dx: the dtype of h is expected")
-    n.dx, n.lddx = _rows(dx, shape, device, "dx")
+    dhp = lddh = wp = 0
     if dh is not None:
-        n.dh, n.lddh = _rows(dh, shape, device, "dh")
+        dhp, lddh = _rows(dh, shape, device, "dh")
     if need_dw:
         if dw is None:
-            dw = torch.empty(shape[1], dtype=torch.float32, device=device)
-        n.dw = _vector(dw, shape[1], device, "dw", torch.float32)
+            dw = torch.empty(cols, dtype=torch.float32, device=device)
+        wp = _vector(dw, cols, device, "dw", torch.float32)
     elif dw is not None:
         raise Q2DError("dw is not computed with need_dw=False")
-    size = _lib.q2d_rmsnorm_workspace(n.rows, n.cols)
-    ws = torch.empty(max(size, 0), dtype=torch.uint8, device=device)
-    _call(device, "q2d_rmsnorm_bwd", ctypes.byref(n), ws.data_ptr(), max(size, 0))
+    size = max(_lib.q2d_rmsnorm_workspace(rows, cols), 0)
+    ws = torch.empty(size, dtype=torch.uint8, device=device)
+    _call(device, "q2d_rmsnorm_bwd",
+          _GRAD.pack(_dtype_code(h.dtype), _dtype_code(dy.dtype), _dtype_code(weight.dtype), rows, cols,
+                     *_rows(h, shape, device, "h"), *_rows(dy, shape, device, "dy"), dhp, lddh,
+                     *_rows(dx, shape, device, "dx"), _vector(weight, cols, device, "weight"),
+                     _vector(rstd, rows, device, "rstd", torch.float32), wp), ws.data_ptr(), size)
     return dx, dw
+
+
+_DTYPE_OF = operator.attrgetter("dtype")
 
 
 def _dense(t):
@@ -176,9 +197,9 @@ def _dense(t):
     return True
 
 
-def _gradients(tensors, what, like=None):
-    """(number, pointers, counts, dtypes) of a list of tensors, as arrays for the C ABI, and their
-    device; with ``like``, tensors that match those in dtype, shape and strides."""
+def _gradients(tensors, what):
+    """A list of tensors, their pointers, counts and dtypes as arrays for the C ABI, and whether all
+    are contiguous."""
     tensors = list(tensors)
     if not tensors:
         raise Q2DError("%s: a list of device tensors is expected" % what)
@@ -192,12 +213,12 @@ def _gradients(tensors, what, like=None):
     if len(devices) > 1 or min(devices) < 0:
         raise Q2DError("%s: tensors on one device are expected" % what)
     try:
-        dtypes = array.array("i", [_DTYPE_CODES[t.dtype] for t in tensors])
+        dtypes = array.array("i", map(_DTYPE_CODES.__getitem__, map(_DTYPE_OF, tensors)))
     except KeyError:
         raise Q2DError("%s: float32 or bfloat16 tensors are expected" % what) from None
     pointers = array.array("Q", map(torch.Tensor.data_ptr, tensors))
     counts = array.array("q", map(torch.Tensor.numel, tensors))
-    return tensors, pointers, counts, dtypes
+    return tensors, pointers, counts, dtypes, dense
 
 
 def _address(a):
@@ -207,7 +228,7 @@ def _address(a):
 def q2d_grad_norm(tensors, norm: torch.Tensor | None = None) -> torch.Tensor:
     """2-norm over all elements of a list of tensors (float32 or bfloat16, without gaps), as a
     float32 device scalar."""
-    tensors, pointers, counts, dtypes = _gradients(tensors, "tensors")
+    tensors, pointers, counts, dtypes, _ = _gradients(tensors, "tensors")
     device = tensors[0].device
     norm = _scalar(norm, device, "norm")
     size = _lib.q2d_grad_workspace(len(tensors))
@@ -231,14 +252,14 @@ def q2d_clip_grads(tensors, max_norm: float, norm: torch.Tensor | None = None, o
     ``out``; returns the norm (float32 device scalar).  norm: the value to go by, the 2-norm over
     tensors of several GPUs for one; None: that of q2d_grad_norm.  A norm that is not finite
     leaves the values as they are.  Nothing waits for the device."""
-    tensors, pointers, counts, dtypes = _gradients(tensors, "tensors")
+    tensors, pointers, counts, dtypes, dense = _gradients(tensors, "tensors")
     device = tensors[0].device
     outs = None
     if out is not None:
-        out, outs, out_counts, out_dtypes = _gradients(out, "out")
-        if out_dtypes != dtypes or out_counts != counts or out[0].device != device or \
-                [t.shape for t in out] != [t.shape for t in tensors] or \
-                any(a.stride() != b.stride() for a, b in zip(out, tensors)):
+        out, outs, out_counts, out_dtypes, out_dense = _gradients(out, "out")
+        # (contiguous ones need the same number of elements only)
+        if out_dtypes != dtypes or out_counts != counts or out[0].device != device or (
+                not (dense and out_dense) and any(a.shape != b.shape or a.stride() != b.stride() for a, b in zip(out, tensors))):
             raise Q2DError("out: a tensor like each of tensors is expected")
     given = norm
     norm = _scalar(norm, device, "norm")
