@@ -1,4 +1,5 @@
-"""PyTorch autograd forms: the quantized linear layer (Sec. 3; App. C, App. E) and attention.
+"""PyTorch autograd forms: the quantized linear layer (Sec. 3; App. C, App. E), alone or behind a
+root-mean-square norm, that norm by itself, and attention.
 
 ``Q2DLinear`` is a bias-free linear layer y = x W^T whose forward and backward
 GEMMs run on quantized operands through ``q2d_linear_fwd`` / ``q2d_linear_bwd``:
@@ -21,6 +22,12 @@ layers the same random bits at the same storage indices).  The weight
 bfloat16) before quantization; Y and dX have the input's dtype, dW is computed
 in float32 and cast to the weight's dtype.
 
+``Q2DNormLinear`` is the same layer on norm(x + residual): q2d_rmsnorm_quantize writes the
+GEMMs' operand, so X is neither written nor read in 16 bits, and Q(X) is rounded once, from
+float32.  ``rms_norm`` gives the normed values themselves.  Both return the sum x + residual
+beside their output, for the residual stream, and their backward takes its gradient in the
+same pass (q2d_rmsnorm_bwd).
+
 ``attention`` is q2d_attention_fwd with q2d_attention_bwd as its gradient.
 
 Options mirror the paper's ablations: ``mode_*`` "rtn" / "sr" choose the
@@ -36,8 +43,8 @@ import math
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import (FP4_1D, FP4_2D, Q2DError, q2d_attention_bwd, q2d_attention_fwd, q2d_linear_bwd,
-               q2d_linear_fwd)
+from . import (FP4_1D, FP4_2D, Q2DError, q2d_attention_bwd, q2d_attention_fwd, q2d_gemm, q2d_linear_bwd,
+               q2d_linear_fwd, q2d_quantize, q2d_rmsnorm_bwd, q2d_rmsnorm_fwd, q2d_rmsnorm_quantize, QTensor)
 
 _DTYPES = (torch.float32, torch.bfloat16)
 
@@ -105,6 +112,120 @@ class Q2DLinear(torch.nn.Module):
         return "in=%d, out=%d, x=%s, w=%s, dy=%s, activations=%s, block=%d, seed=%#x" % (
             self.in_features, self.out_features, self.mode_x, self.mode_w, self.mode_dy,
             self.activations, self.block, self.seed)
+
+
+def _rows(t, cols):
+    """t as rows of cols elements that do not share memory, a copy where it has none such."""
+    t = t.reshape(-1, cols)
+    pitch, one = t.stride()
+    return t if (one == 1 or cols == 1) and (pitch >= cols or t.shape[0] < 2) else t.contiguous()
+
+
+def _norm_backward(ctx, dy, dh, h, weight, rstd):
+    """Gradients of x, the residual and the norm's weight from that of y (None: none) and of h."""
+    need_x, need_r, need_w = ctx.needs_input_grad[:3]
+    cols = h.shape[1]
+    dh = None if dh is None else _rows(dh.to(h.dtype), cols)
+    if dy is None:
+        dx, dw = dh, None
+    else:
+        dx, dw = q2d_rmsnorm_bwd(dy, h, weight, rstd, dh=dh, need_dw=need_w)
+    return (None if dx is None or not need_x else dx.reshape(ctx.x_shape),
+            None if dx is None or not need_r else dx.reshape(ctx.x_shape).to(ctx.r_dtype),
+            None if dw is None else dw.to(weight.dtype))
+
+
+def _norm_inputs(ctx, x, residual, weight):
+    """x and residual as rows."""
+    cols = weight.shape[0] if weight.dim() == 1 else -1
+    if x.dim() == 0 or x.shape[-1] != cols or (residual is not None and residual.shape != x.shape):
+        raise Q2DError("x and residual of one shape [..., %d] are expected" % cols)
+    ctx.x_shape, ctx.r_dtype = x.shape, None if residual is None else residual.dtype
+    ctx.set_materialize_grads(False)
+    return _rows(x, cols), None if residual is None else _rows(residual, cols)
+
+
+class _NormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps, y_dtype):
+        x2, r2 = _norm_inputs(ctx, x, residual, weight)
+        y, h, rstd = q2d_rmsnorm_fwd(x2, weight.detach(), eps, residual=r2, y_dtype=y_dtype)
+        ctx.save_for_backward(h, weight, rstd)
+        y = y.reshape(x.shape)
+        return (y,) if residual is None else (y, h.reshape(x.shape))
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh=None):
+        h, weight, rstd = ctx.saved_tensors
+        dy = None if dy is None else _rows(dy, h.shape[1])
+        return (*_norm_backward(ctx, dy, dh, h, weight.detach(), rstd), None, None)
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual: torch.Tensor | None = None,
+             y_dtype=torch.bfloat16):
+    """Root-mean-square norm of x [..., cols] times weight [cols], with gradients for all three (once:
+    these have none of their own).  With a residual (x's shape) the norm is of h = x + residual
+    and (y, h) is returned, otherwise y."""
+    out = _NormFunction.apply(x, residual, weight, eps, y_dtype)
+    return out[0] if residual is None else out
+
+
+class _NormLinearFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, norm_weight, weight, layer):
+        x2, r2 = _norm_inputs(ctx, x, residual, norm_weight)
+        n = layer._calls
+        layer._calls += 1
+        # (only the backward pass reads the transposed copies)
+        both = (True, any(ctx.needs_input_grad))
+        (qX,), h, rstd = q2d_rmsnorm_quantize(x2, norm_weight.detach(), layer.eps, residual=r2,
+                                              formats=(FP4_1D if layer.activations == "1d" else FP4_2D,),
+                                              block=layer.block, orientations=both)
+        w = weight.detach()
+        w = (w if w.dtype in _DTYPES else w.float()).contiguous()
+        qW = q2d_quantize(w, layer.mode_w, layer.seed, 3 * n + 1, block=layer.block,
+                          out=QTensor(FP4_2D, *w.shape, w.device, layer.block, both))
+        Y = q2d_gemm(qX, 0, qW, 0, out_dtype=layer.out_dtype)
+        ctx.save_for_backward(h, norm_weight, rstd)
+        ctx.qX, ctx.qW = qX, qW
+        ctx.layer, ctx.offset_dy, ctx.w_dtype = layer, 3 * n + 2, weight.dtype
+        Y = Y.reshape(*x.shape[:-1], w.shape[0])
+        return (Y,) if residual is None else (Y, h.reshape(x.shape))
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dY, dh=None):
+        h, norm_weight, rstd = ctx.saved_tensors
+        layer, dy, dW = ctx.layer, None, None
+        if dY is not None:
+            if ctx.qX is None:
+                raise Q2DError("the operands are gone after a backward pass: a second one needs a second forward pass")
+            dY2 = dY.reshape(-1, dY.shape[-1])
+            dY2 = (dY2 if dY2.dtype in _DTYPES else dY2.float()).contiguous()
+            dy, dW, _ = q2d_linear_bwd(dY2, ctx.qX, ctx.qW, layer.mode_dy, layer.seed, ctx.offset_dy, dx_dtype=dY2.dtype,
+                                       dw_dtype=torch.float32, block=layer.block)
+            dW = dW.to(ctx.w_dtype)
+        ctx.qX = ctx.qW = None
+        return (*_norm_backward(ctx, dy, dh, h, norm_weight.detach(), rstd), dW, None)
+
+
+class Q2DNormLinear(Q2DLinear):
+    """Q2DLinear behind a root-mean-square norm with the residual's addition (see the module
+    docstring): y = Q(norm(h) * norm_weight) Q(W)^T with h = x + residual.  X is rounded to
+    nearest, with the truncation-free scales."""
+
+    def __init__(self, in_features: int, out_features: int, *, eps: float = 1e-5, out_dtype=torch.bfloat16, **options):
+        if options.get("mode_x", "rtn") != "rtn":
+            raise ValueError("the norm's output is rounded to nearest (mode_x 'rtn')")
+        super().__init__(in_features, out_features, **options)
+        self.eps, self.out_dtype = eps, out_dtype
+        self.norm_weight = torch.nn.Parameter(torch.ones(in_features, device=self.weight.device, dtype=self.weight.dtype))
+
+    def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
+        """y, or with a residual (y, x + residual)."""
+        out = _NormLinearFunction.apply(x, residual, self.norm_weight, self.weight, self)
+        return out[0] if residual is None else out
 
 
 class _AttentionFunction(torch.autograd.Function):

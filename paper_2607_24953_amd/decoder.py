@@ -3,7 +3,10 @@ them, trained on packed documents and then answering from a paged 8-bit key/valu
 
 ``Decoder.forward`` is the training path (Q2DLinear, ``autograd.attention`` with a document
 mask); ``Decoder.step`` takes new tokens of several sequences, prompts or single tokens,
-through q2d_kv_write and q2d_attention_cached.
+through q2d_kv_write and q2d_attention_cached.  Norms are torch's LayerNorm, or with
+``norm="rms"`` the library's root-mean-square norm, which adds the residual and writes the
+operands of the linear layer behind it (Q2DNormLinear).  ``train`` clips the gradients by their
+global norm where asked to (q2d_clip_grads).
 
 ``python -m paper_2607_24953_amd.decoder`` trains one on documents that repeat a random phrase and
 prints the loss and how well it continues such documents out of the cache.
@@ -15,21 +18,24 @@ import sys
 
 import torch
 
-from . import KVCache, q2d_attention_cached, q2d_kv_write
-from .autograd import Q2DLinear, attention
+from . import KVCache, q2d_attention_cached, q2d_clip_grads, q2d_kv_write
+from .autograd import Q2DLinear, Q2DNormLinear, attention, rms_norm
 
 
 class Block(torch.nn.Module):
     """Attention and a two-layer feed-forward part, each on the normed residual stream."""
 
+    Normed = Q2DLinear      # the layers behind a norm
+
     def __init__(self, hidden, heads, kv_heads, softcap, device):
         super().__init__()
         self.heads, self.kv_heads, self.dim, self.softcap = heads, kv_heads, hidden // heads, softcap
-        self.qkv = Q2DLinear(hidden, (heads + 2 * kv_heads) * self.dim, device=device)
+        self.qkv = self.Normed(hidden, (heads + 2 * kv_heads) * self.dim, device=device)
         self.o = Q2DLinear(hidden, hidden, device=device)
-        self.up = Q2DLinear(hidden, 4 * hidden, device=device)
+        self.up = self.Normed(hidden, 4 * hidden, device=device)
         self.down = Q2DLinear(4 * hidden, hidden, device=device)
-        self.norms = torch.nn.ModuleList(torch.nn.LayerNorm(hidden, device=device) for _ in range(2))
+        if self.Normed is Q2DLinear:
+            self.norms = torch.nn.ModuleList(torch.nn.LayerNorm(hidden, device=device) for _ in range(2))
 
     def forward(self, x, attend):
         """attend(q, k, v) -> attention's output, all [..., heads, dim]"""
@@ -40,29 +46,65 @@ class Block(torch.nn.Module):
         return x + self.down(torch.relu(self.up(self.norms[1](x).to(dt)))).float()
 
 
+class RMSBlock(Block):
+    """The same on root-mean-square norms: each adds the branch before it to the stream and writes
+    the operands of the linear layer behind it."""
+
+    Normed = Q2DNormLinear
+
+    def forward(self, x, attend, branch=None):
+        """The stream x and what is still to be added to it (None: nothing) -> the same behind this
+        block."""
+        if branch is None:
+            y = self.qkv(x)
+        else:
+            y, x = self.qkv(x, branch)
+        q, k, v = y.unflatten(-1, (-1, self.dim)).split((self.heads, self.kv_heads, self.kv_heads), dim=-2)
+        y, x = self.up(x, self.o(attend(q, k, v).flatten(-2)))
+        return x, self.down(torch.relu(y))
+
+
 class Decoder(torch.nn.Module):
     """Token embedding, blocks, and logits by the embedding.  Positions enter by the heads'
     distance bias (slopes), which training and the cached path share."""
 
-    def __init__(self, vocabulary=64, hidden=256, layers=2, heads=4, kv_heads=2, softcap=30.0, device="cuda"):
+    def __init__(self, vocabulary=64, hidden=256, layers=2, heads=4, kv_heads=2, softcap=30.0, device="cuda",
+                 norm="layer"):
         super().__init__()
+        if norm not in ("layer", "rms"):
+            raise ValueError("norm must be 'layer' or 'rms'")
         self.embedding = torch.nn.Embedding(vocabulary, hidden, device=device)
         torch.nn.init.normal_(self.embedding.weight, std=hidden ** -0.5)
-        self.blocks = torch.nn.ModuleList(Block(hidden, heads, kv_heads, softcap, device) for _ in range(layers))
-        self.norm = torch.nn.LayerNorm(hidden, device=device)
+        self.rms = norm == "rms"
+        block = RMSBlock if self.rms else Block
+        self.blocks = torch.nn.ModuleList(block(hidden, heads, kv_heads, softcap, device) for _ in range(layers))
+        if self.rms:
+            self.norm_weight = torch.nn.Parameter(torch.ones(hidden, device=device))
+        else:
+            self.norm = torch.nn.LayerNorm(hidden, device=device)
         # half the heads look near, half far
         slopes = [2.0 ** -(1 + 7 * i / max(1, heads - 1)) for i in range(heads)]
         self.register_buffer("slopes", torch.tensor(slopes, dtype=torch.float32, device=device))
 
-    def _logits(self, x):
-        return self.norm(x) @ self.embedding.weight.t()
+    def _block(self, b, x, branch, attend):
+        return b(x, attend, branch) if self.rms else (b(x, attend), None)
+
+    def _logits(self, x, branch):
+        if self.rms:
+            y = rms_norm(x, self.norm_weight, residual=branch, y_dtype=torch.float32)
+            y = y if branch is None else y[0]
+        else:
+            y = self.norm(x)
+        return y @ self.embedding.weight.t()
 
     def forward(self, tokens, documents=None):
         """Logits of tokens [batch, length]; documents [batch, length] (int32): packed rows."""
-        x = self.embedding(tokens)
+        x, branch = self.embedding(tokens), None
         for b in self.blocks:
-            x = b(x, lambda q, k, v: attention(q, k, v, softcap=b.softcap, slopes=self.slopes, documents=documents))
-        return self._logits(x)
+            def attend(q, k, v):
+                return attention(q, k, v, softcap=b.softcap, slopes=self.slopes, documents=documents)
+            x, branch = self._block(b, x, branch, attend)
+        return self._logits(x, branch)
 
     def caches(self, pages, page_size=64):
         b = self.blocks[0]
@@ -72,13 +114,13 @@ class Decoder(torch.nn.Module):
     def step(self, tokens, caches, table, lens, offsets=None):
         """Logits of the new tokens [tokens] of several sequences (rows offsets[b] ..
         offsets[b + 1]; None: equally many each), which join the caches; lens counts them."""
-        x = self.embedding(tokens)
+        x, branch = self.embedding(tokens), None
         for b, cache in zip(self.blocks, caches):
             def attend(q, k, v):
                 q2d_kv_write(cache, k, v, table, lens, offsets)
                 return q2d_attention_cached(q, cache, table, lens, offsets, softcap=b.softcap, slopes=self.slopes)
-            x = b(x, attend)
-        return self._logits(x)
+            x, branch = self._block(b, x, branch, attend)
+        return self._logits(x, branch)
 
     @torch.no_grad()
     def generate(self, prompts, count, page_size=64):
@@ -123,8 +165,9 @@ def repeated_phrases(rows, length, vocabulary, generator, device):
     return tokens.to(device), documents.to(device), known.to(device)
 
 
-def train(model, steps, rows=16, length=256, vocabulary=64, lr=1e-3, seed=0):
-    """Trains on repeated_phrases; returns the loss of every step."""
+def train(model, steps, rows=16, length=256, vocabulary=64, lr=1e-3, seed=0, clip=None):
+    """Trains on repeated_phrases; returns the loss of every step.  clip: the largest global norm
+    of the gradients."""
     g = torch.Generator().manual_seed(seed)
     opt = torch.optim.AdamW(model.parameters(), lr=lr, weight_decay=0.0)
     losses = []
@@ -136,6 +179,8 @@ def train(model, steps, rows=16, length=256, vocabulary=64, lr=1e-3, seed=0):
         loss = torch.nn.functional.cross_entropy(logits[known], tokens[:, 1:][known])
         opt.zero_grad(set_to_none=True)
         loss.backward()
+        if clip is not None:
+            q2d_clip_grads([p.grad for p in model.parameters() if p.grad is not None], clip)
         opt.step()
         losses.append(float(loss.detach()))
     return losses
@@ -144,10 +189,12 @@ def train(model, steps, rows=16, length=256, vocabulary=64, lr=1e-3, seed=0):
 def main(argv=None) -> int:
     p = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     p.add_argument("--steps", type=int, default=300)
+    p.add_argument("--norm", choices=["layer", "rms"], default="layer")
+    p.add_argument("--clip", type=float, default=None, help="largest global norm of the gradients")
     a = p.parse_args(argv)
     torch.manual_seed(0)
-    model = Decoder()
-    losses = train(model, a.steps)
+    model = Decoder(norm=a.norm)
+    losses = train(model, a.steps, clip=a.clip)
     for i in range(0, a.steps, max(1, a.steps // 10)):
         print("step %4d  loss %.3f" % (i, losses[i]), flush=True)
     g = torch.Generator().manual_seed(1)
