@@ -8,187 +8,194 @@
 // and effective-deviation maps of the forward/backward comparison (Fig. 1): zero
 // for 2D blocks, non-zero for 1D blocks.
 //
-// One workgroup per 128 x 128 output tile.  The tile's codes (128 stored rows of
-// 64 bytes for FP4, 128 for MXFP8) are staged in LDS with 16-byte loads; then
-// each wave writes 32 output rows, two per instruction, a lane covering four
-// consecutive columns (16-byte float32 / 8-byte bfloat16 stores: full 512- or
-// 256-byte rows per half wave).  A transposed copy (stored K = rows) is read
-// from LDS column-wise.  Values are exact in float32 (an E2M1 or E4M3 code times
-// a power of two, rounded once only when it leaves float32 range); bfloat16
-// output is the round-to-nearest-even of that value.
+// The quantizers' work split: a workgroup of eight waves owns a 128 x 256 tile, a wave a 32 x 128
+// strip of it, a lane an 8 x 8 sub-block (rows 8 * (lane / 16) .. + 7, columns 8 * (lane % 16) ..
+// + 7); few tiles are cut into one-wave workgroups.  A row-packed copy is read straight into
+// the lanes.  A transposed copy (stored K = rows) goes through LDS, from where a lane takes its
+// eight columns' words and transposes them in registers.  A lane stores eight neighbouring
+// elements of a row at a time (16 bytes of bfloat16, at any address).  Values are exact in float32
+// (an E2M1 or E4M3 code times a power of two, rounded once only when it leaves float32 range);
+// bfloat16 output is the round-to-nearest-even of that value.
+//
+// Element by element from LDS, with the scales read beside it, the transposed MXFP8 copy of
+// 16384 x 4096 took 145 us and a tile of its own 9 us; now 60 and 3.5 us.
 #include "device_common.hpp"
 #include "kernels.hpp"
+#include "norm_common.hpp"
 
 namespace q2d {
 
 namespace {
 
-constexpr int kTile = 128;
+constexpr uint32_t kNaN = 0x7FC00000u;
 
-__device__ __forceinline__ uint16_t bf16_rne(float f)
+// a scale byte as the power of two that it stands for
+__device__ __forceinline__ float scale_value(uint32_t byte)
 {
-    const uint32_t u = f_bits(f);
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0x7FC0;
-    return (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
+    return bits_f(byte == 0xFFu ? kNaN : byte ? byte << 23 : 0x00400000u);
 }
 
-// value of an E2M1 nibble times 2^e
-__device__ __forceinline__ float fp4_value(uint32_t n, int e)
+// values of eight E2M1 nibbles, times 1
+__device__ __forceinline__ void fp4_values(uint32_t w, float (&v)[8])
 {
-    const uint32_t m = n & 7u;
-    // twice the magnitude: 0, 1, 2, 3, 4, 6, 8, 12
-    const uint32_t twice = m < 2u ? m : (2u + (m & 1u)) << ((m >> 1) - 1u);
-    const float v = ldexpf((float)twice, e - 1);
-    return (n & 8u) ? -v : v;
+    const f32v2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1);
+    const f32v2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3);
+    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
 }
 
-// value of an E4M3FN byte times 2^e (S.1111.111 is NaN)
-__device__ __forceinline__ float e4m3_value(uint32_t b, int e)
+// values of four E4M3FN bytes (S.1111.111 is NaN)
+__device__ __forceinline__ void fp8_values(uint32_t w, float *v)
 {
-    if ((b & 0x7Fu) == 0x7Fu) return __uint_as_float(0x7FC00000u);
-    const uint32_t E = (b >> 3) & 15u, m = b & 7u;
-    const float v = E ? ldexpf((float)(8u + m), (int)E - 10 + e) : ldexpf((float)m, e - 9);
-    return (b & 0x80u) ? -v : v;
+    const f32v2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
 }
 
-// FMT: 0 = FP4 2D blocks, 1 = MXFP8, 2 = FP4 1D blocks.  TRANS: the copy is
-// stored with K = rows (element (r, c) in stored row c).
-template <int FMT, bool TRANS, bool BF16>
-__global__ __launch_bounds__(256) void dequantize_kernel(const DequantArgs a)
+// 4 x 4 transpose of bytes: byte j of in[i] becomes byte i of out[j]
+__device__ __forceinline__ void byte_transpose4(const uint32_t (&in)[4], uint32_t (&out)[4])
 {
-    constexpr int kRowBytes = FMT == 1 ? 128 : 64;      // bytes of 128 codes
-    constexpr int kPitch = kRowBytes + 4;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kTile * kPitch];
-    const int64_t tiles_c = (a.cols + kTile - 1) / kTile;
+    const uint32_t a = __builtin_amdgcn_perm(in[1], in[0], 0x05010400u), b = __builtin_amdgcn_perm(in[3], in[2], 0x05010400u);
+    const uint32_t c = __builtin_amdgcn_perm(in[1], in[0], 0x07030602u), d = __builtin_amdgcn_perm(in[3], in[2], 0x07030602u);
+    out[0] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+    out[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    out[2] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+    out[3] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+}
+
+// FMT: 0 = FP4 2D blocks, 1 = MXFP8, 2 = FP4 1D blocks.  TRANS: the copy is stored with K = rows
+// (element (r, c) in stored row c).  WR x WC strips, one a wave.
+template <int FMT, bool TRANS, bool BF16, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC) void dequantize_kernel(const DequantArgs a)
+{
+    constexpr int kRows = 32 * WR, kCols = 128 * WC, kThreads = 64 * WR * WC;
+    constexpr int kWords = FMT == 1 ? 2 : 1;             // words of eight codes
+    const int64_t tiles_c = (a.cols + kCols - 1) / kCols;
     const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
-    const int64_t r0 = tr * kTile, c0 = tc * kTile;
-    const int t = threadIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wr = wave / WC, wc = wave % WC, rg = lane >> 4, cc = lane & 15;
+    const int64_t r0 = tr * kRows + wr * 32 + 8 * rg, c0 = tc * kCols + wc * 128 + 8 * cc;
+    const bool some = r0 < a.rows && c0 < a.cols;
 
-    // ---- stage: stored rows s0 .. s0+127 (rows for a row-packed copy, columns
-    // for a transposed one), K bytes of this tile
-    {
-        const int64_t s0 = TRANS ? c0 : r0, k0 = TRANS ? r0 : c0;
-        const int64_t ns = TRANS ? a.cols : a.rows;
-        const int sl = t >> 1, half = t & 1;
-        constexpr int kVec = kRowBytes / 32;               // 16-byte vectors per thread
-        const int64_t s = s0 + sl;
-        uint8_t *dst = lds + sl * kPitch + half * (kRowBytes / 2);
+    // ---- the scale bytes of the sub-block's rows (row-packed copy) or columns, one for a 2D block
+    constexpr int kScales = FMT == 0 ? 1 : 8;
+    uint32_t sb[kScales];
 #pragma unroll
-        for (int v = 0; v < kVec; ++v) {
-            uint4 q = make_uint4(0u, 0u, 0u, 0u);
-            if (s < ns)
-                q = *reinterpret_cast<const uint4 *>(a.codes + s * a.ld_codes + k0 * kRowBytes / kTile +
-                                                     half * (kRowBytes / 2) + 16 * v);
-            uint32_t *d = reinterpret_cast<uint32_t *>(dst + 16 * v);
-            d[0] = q.x; d[1] = q.y; d[2] = q.z; d[3] = q.w;
+    for (int i = 0; i < kScales; ++i) {
+        const int64_t s = (TRANS ? c0 : r0) + i, k = TRANS ? r0 : c0;
+        sb[i] = 0;
+        if (!some || (kScales > 1 && s >= (TRANS ? a.cols : a.rows))) continue;
+        sb[i] = FMT == 0 ? a.scales[(s >> 5) * a.ld_scales + (k >> 5)]
+              : FMT == 2 ? a.scales[(k >> 7) * a.ld_scales + 4 * s + ((k >> 5) & 3)]
+                         : a.scales[s * a.ld_scales + (k >> 5)];
+    }
+
+    // ---- the codes: w[i] has the eight of row i
+    uint32_t w[8][kWords];
+    if constexpr (!TRANS) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) w[i][k] = 0;
+            if (!some || r0 + i >= a.rows) continue;
+            const uint8_t *p = a.codes + (r0 + i) * a.ld_codes + (FMT == 1 ? c0 : c0 / 2);
+            if constexpr (FMT == 1) {
+                const uint2 q = *reinterpret_cast<const uint2 *>(p);
+                w[i][0] = q.x; w[i][kWords - 1] = q.y;
+            } else {
+                w[i][0] = *reinterpret_cast<const uint32_t *>(p);
+            }
+        }
+    } else {
+        // stored rows of kRows codes, 16 bytes a lane
+        constexpr int kLine = WR * 4 * kWords, kParts = kLine / 4;         // words, 16-byte parts
+        __shared__ uint32_t st[kCols][kLine + 1];
+#pragma unroll
+        for (int q = 0; q < kCols * kParts / kThreads; ++q) {
+            const int item = threadIdx.x + kThreads * q, line = item / kParts, part = item % kParts;
+            const int64_t c = tc * kCols + line;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (c < a.cols) v = *reinterpret_cast<const uint4 *>(a.codes + c * a.ld_codes + tr * (4 * kLine) + 16 * part);
+            st[line][4 * part] = v.x; st[line][4 * part + 1] = v.y; st[line][4 * part + 2] = v.z; st[line][4 * part + 3] = v.w;
+        }
+        __syncthreads();
+        uint32_t col[8][kWords];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) col[j][k] = st[wc * 128 + 8 * cc + j][(wr * 4 + rg) * kWords + k];
+        if constexpr (FMT == 1) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t in[4] = {col[4 * h][k], col[4 * h + 1][k], col[4 * h + 2][k], col[4 * h + 3][k]};
+                    uint32_t out[4];
+                    byte_transpose4(in, out);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[4 * k + i][h] = out[i];
+                }
+        } else {
+            uint32_t in[8], out[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) in[j] = col[j][0];
+            nibble_transpose8(in, out);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i][0] = out[i];
         }
     }
-    __syncthreads();
+    if (!some) return;
 
-    // scale byte of stored row s, K index k
-    auto scale_byte = [&](int64_t s, int64_t k) -> uint32_t {
-        if (FMT == 0) return a.scales[(s >> 5) * a.ld_scales + (k >> 5)];
-        if (FMT == 2) return a.scales[(k >> 7) * a.ld_scales + 4 * s + ((k >> 5) & 3)];
-        return a.scales[s * a.ld_scales + (k >> 5)];
-    };
-
-    const int wave = t >> 6, lane = t & 63;
-    const int cg = lane & 31;
-    const int64_t c = c0 + 4 * cg;
-#pragma unroll 2
-    for (int it = 0; it < 16; ++it) {
-        const int rl = wave * 32 + 2 * it + (lane >> 5);
-        const int64_t r = r0 + rl;
-        if (r >= a.rows || c >= a.cols) continue;
-        // codes of the four elements (r, c .. c+3)
-        uint32_t code[4];
-        if (!TRANS) {
-            if (FMT == 1) {
-                const uint32_t w = *reinterpret_cast<const uint32_t *>(lds + rl * kPitch + 4 * cg);
+    float scale[kScales];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) code[j] = (w >> (8 * j)) & 0xFFu;
-            } else {
-                const uint32_t w = *reinterpret_cast<const uint16_t *>(lds + rl * kPitch + 2 * cg);
+    for (int i = 0; i < kScales; ++i) scale[i] = scale_value(sb[i]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) code[j] = (w >> (4 * j)) & 15u;
-            }
+    for (int i = 0; i < 8; ++i) {
+        const int64_t r = r0 + i;
+        if (r >= a.rows) break;
+        float v[8];
+        if constexpr (FMT == 1) {
+            fp8_values(w[i][0], v);
+            fp8_values(w[i][kWords - 1], v + 4);
         } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint8_t *row = lds + (4 * cg + j) * kPitch;
-                code[j] = FMT == 1 ? row[rl] : (row[rl >> 1] >> (4 * (rl & 1))) & 15u;
-            }
+            fp4_values(w[i][0], v);
         }
-        // scale bytes: one for a 2D block or a row block (the four columns share
-        // it), one per column for column blocks
-        uint32_t sb[4];
-        if (!TRANS) {
-            const uint32_t s = scale_byte(r, c);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sb[j] = s;
-        } else if (FMT == 0) {
-            const uint32_t s = scale_byte(c, r);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sb[j] = s;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sb[j] = c + j < a.cols ? scale_byte(c + j, r) : 0u;
-        }
-        float v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int e = (int)sb[j] - 127;
-            v[j] = sb[j] == 0xFFu ? __uint_as_float(0x7FC00000u)
-                                  : (FMT == 1 ? e4m3_value(code[j], e) : fp4_value(code[j], e));
-        }
-        const bool full = c + 4 <= a.cols;
-        if (BF16) {
-            uint16_t *o = reinterpret_cast<uint16_t *>(a.out) + r * a.ldo + c;
-            if (full && a.out_vec) {
-                *reinterpret_cast<uint2 *>(o) =
-                    make_uint2((uint32_t)bf16_rne(v[0]) | (uint32_t)bf16_rne(v[1]) << 16,
-                               (uint32_t)bf16_rne(v[2]) | (uint32_t)bf16_rne(v[3]) << 16);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (c + j < a.cols) o[j] = bf16_rne(v[j]);
-            }
-        } else {
-            float *o = reinterpret_cast<float *>(a.out) + r * a.ldo + c;
-            if (full && a.out_vec) {
-                *reinterpret_cast<float4 *>(o) = make_float4(v[0], v[1], v[2], v[3]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (c + j < a.cols) o[j] = v[j];
-            }
-        }
+        for (int j = 0; j < 8; ++j) v[j] *= scale[kScales == 1 ? 0 : TRANS ? j : i];
+        store_eight(v, a.out, BF16, r * a.ldo + c0, a.cols - c0);
         if (a.exps) {
-            int8_t *x = a.exps + r * a.lde + c;
+            int8_t *x = a.exps + r * a.lde + c0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c + j < a.cols) x[j] = sb[j] == 0xFFu ? (int8_t)-128 : (int8_t)((int)sb[j] - 127);
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t b = sb[kScales == 1 ? 0 : TRANS ? j : i];
+                if (c0 + j < a.cols) x[j] = b == 0xFFu ? (int8_t)-128 : (int8_t)((int)b - 127);
+            }
         }
     }
+}
+
+template <int FMT, bool TRANS, bool BF16>
+hipError_t launch_tiles(const DequantArgs &a, hipStream_t s)
+{
+    auto tiles = [&](int64_t rows, int64_t cols) { return ((a.rows + rows - 1) / rows) * ((a.cols + cols - 1) / cols); };
+    // (as the quantizers: up to 128 tiles, a strip a workgroup)
+    if (tiles(128, 256) <= 128) {
+        hipLaunchKernelGGL((dequantize_kernel<FMT, TRANS, BF16, 1, 1>), dim3((unsigned)tiles(32, 128)), dim3(64), 0, s, a);
+    } else {
+        if (tiles(128, 256) >= (int64_t(1) << 23)) return hipErrorInvalidValue;      // (work-items of a launch: below 2^32)
+        hipLaunchKernelGGL((dequantize_kernel<FMT, TRANS, BF16, 4, 2>), dim3((unsigned)tiles(128, 256)), dim3(512), 0, s, a);
+    }
+    return hipGetLastError();
 }
 
 template <int FMT, bool TRANS>
 hipError_t launch_fmt(const DequantArgs &a, hipStream_t s)
 {
-    const int64_t tiles = ((a.rows + kTile - 1) / kTile) * ((a.cols + kTile - 1) / kTile);
-    if (a.out_bf16)
-        hipLaunchKernelGGL((dequantize_kernel<FMT, TRANS, true>), dim3((unsigned)tiles), dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL((dequantize_kernel<FMT, TRANS, false>), dim3((unsigned)tiles), dim3(256), 0, s, a);
-    return hipGetLastError();
+    return a.out_bf16 ? launch_tiles<FMT, TRANS, true>(a, s) : launch_tiles<FMT, TRANS, false>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_dequantize(const DequantArgs &a, hipStream_t stream)
 {
-    const int64_t tiles = ((a.rows + kTile - 1) / kTile) * ((a.cols + kTile - 1) / kTile);
-    if (tiles <= 0 || tiles > 0x7FFFFFFF) return hipErrorInvalidValue;
     switch (a.fmt * 2 + (a.transposed ? 1 : 0)) {
     case 0: return launch_fmt<0, false>(a, stream);
     case 1: return launch_fmt<0, true>(a, stream);
