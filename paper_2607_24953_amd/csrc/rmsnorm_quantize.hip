@@ -12,8 +12,6 @@ namespace q2d {
 
 namespace {
 
-constexpr int kRows = 128, kCols = 256, kThreads = 512;
-
 // byte of a block's scale: its exponent, or 0xFF for a block that is not finite
 __device__ __forceinline__ uint8_t scale_byte(uint32_t amax, int e) { return amax < 0x7F800000u ? (uint8_t)(e + 127) : (uint8_t)0xFF; }
 __device__ __forceinline__ float pow2(int e) { return bits_f((uint32_t)(127 + e) << 23); }
@@ -37,13 +35,16 @@ __device__ __forceinline__ uint2 fp8_words(const uint32_t (&v)[8], float scale)
 }
 
 // F32: h is float32.  VEC: as in the quantizers (0 -- element by element; 1 -- rows of any
-// alignment; 2 -- rows on 16-byte boundaries).  FP4: 0 none, 1 2D blocks, 2 1D blocks.
-template <bool F32, int VEC, int FP4, bool MX>
-__global__ __launch_bounds__(kThreads) void rmsnorm_quantize_kernel(const NormQuantArgs a)
+// alignment; 2 -- rows on 16-byte boundaries).  FP4: 0 none, 1 2D blocks, 2 1D blocks.  WR x WC
+// strips a workgroup, one a wave.
+template <bool F32, int VEC, int FP4, bool MX, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC) void rmsnorm_quantize_kernel(const NormQuantArgs a)
 {
+    static_assert((WR == 4 && WC == 2) || (WR == 1 && WC == 1), "a tile, or a strip of its own");
+    constexpr int kRows = 32 * WR, kCols = 128 * WC, kThreads = 64 * WR * WC;
     constexpr int E = F32 ? 4 : 2, NV = 2 * E;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wr = wave >> 1, wc = wave & 1, rg = lane >> 4, cc = lane & 15;
+    const int wr = wave / WC, wc = wave % WC, rg = lane >> 4, cc = lane & 15;
     const int64_t tiles_c = (a.cols_pad + kCols - 1) / kCols;
     const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
     const int64_t r0 = tr * kRows + wr * 32 + 8 * rg, c0 = tc * kCols + wc * 128 + 8 * cc;
@@ -110,10 +111,10 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quantize_kernel(const NormQu
     }
 
     if constexpr (FP4 != 0) {
-        __shared__ uint32_t st_r[kRows][33];
-        __shared__ uint32_t st_c[kCols][17];
-        __shared__ uint8_t st_rs[FP4 == 2 ? kRows : 1][8];
-        __shared__ uint8_t st_cs[FP4 == 2 ? kCols : 1][4];
+        __shared__ uint32_t st_r[kRows][16 * WC + 1];
+        __shared__ uint32_t st_c[kCols][4 * WR + 1];
+        __shared__ uint8_t st_rs[FP4 == 2 ? kRows : 1][4 * WC];
+        __shared__ uint8_t st_cs[FP4 == 2 ? kCols : 1][WR];
         uint32_t am = 0;
         uint32_t rowp[8], colp[8];
         if constexpr (FP4 == 1) {
@@ -125,7 +126,7 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quantize_kernel(const NormQu
             am = max(am, (uint32_t)__shfl_xor((int)am, 2));
             am = max(am, (uint32_t)__shfl_xor((int)am, 16));
             am = max(am, (uint32_t)__shfl_xor((int)am, 32));
-            if (a.block == 64) {
+            if (WR == 4 && a.block == 64) {
                 // the block beside it in this wave, then the paired wave's strip
                 __shared__ uint32_t am64[4][4];
                 am = max(am, (uint32_t)__shfl_xor((int)am, 4));
@@ -164,14 +165,14 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quantize_kernel(const NormQu
         for (int p = 0; p < 2; ++p) {
             const int item = threadIdx.x + kThreads * p;
             if (q.codes) {
-                const int line = item >> 3, part = item & 7;
+                const int line = item / (4 * WC), part = item % (4 * WC);
                 const int64_t r = tr * kRows + line;
                 if (r < a.rows && tc * kCols + part * 32 < a.cols_pad)
                     *reinterpret_cast<uint4 *>(q.codes + r * q.ld_codes + tc * (kCols / 2) + part * 16) =
                         make_uint4(st_r[line][4 * part], st_r[line][4 * part + 1], st_r[line][4 * part + 2], st_r[line][4 * part + 3]);
             }
             if (q.codes_t) {
-                const int line = item >> 2, part = item & 3;
+                const int line = item / WR, part = item % WR;
                 const int64_t c = tc * kCols + line;
                 if (c < a.cols)
                     *reinterpret_cast<uint4 *>(q.codes_t + c * q.ld_codes_t + tr * (kRows / 2) + part * 16) =
@@ -179,22 +180,22 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quantize_kernel(const NormQu
             }
         }
         if constexpr (FP4 == 2) {
-            // scale words, K-tile major
-            const int t = threadIdx.x;
-            if (t < kRows) {
+            // scale words, K-tile major; of a strip of its own one byte a column
+            for (int t = threadIdx.x; t < kRows; t += kThreads) {
                 const int64_t r = tr * kRows + t;
                 if (q.codes && r < a.rows) {
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
+                    for (int k = 0; k < WC; ++k)
                         if (tc * kCols + k * 128 < a.cols_pad)
-                            *reinterpret_cast<uint32_t *>(q.scales + (tc * 2 + k) * q.ld_scales + 4 * r) =
+                            *reinterpret_cast<uint32_t *>(q.scales + (tc * WC + k) * q.ld_scales + 4 * r) =
                                 *reinterpret_cast<const uint32_t *>(&st_rs[t][4 * k]);
                 }
-            } else if (t >= kThreads - kCols) {
-                const int cl = t - (kThreads - kCols);
-                const int64_t c = tc * kCols + cl;
-                if (q.codes_t && c < a.cols)
-                    *reinterpret_cast<uint32_t *>(q.scales_t + tr * q.ld_scales_t + 4 * c) = *reinterpret_cast<const uint32_t *>(&st_cs[cl][0]);
+            }
+            for (int t = kThreads - 1 - threadIdx.x; t < kCols; t += kThreads) {
+                const int64_t c = tc * kCols + t;
+                if (!q.codes_t || c >= a.cols) continue;
+                if constexpr (WR == 4) *reinterpret_cast<uint32_t *>(q.scales_t + tr * q.ld_scales_t + 4 * c) = *reinterpret_cast<const uint32_t *>(&st_cs[t][0]);
+                else q.scales_t[(tr >> 2) * q.ld_scales_t + 4 * c + (tr & 3)] = st_cs[t][0];
             }
         } else if (rg == 0 && (cc & 3) == 0 && tc * kCols + wc * 128 < a.cols_pad) {
             const uint8_t byte = scale_byte(am, fp4_block_exponent(am));
@@ -205,9 +206,9 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quantize_kernel(const NormQu
     }
 
     if constexpr (MX) {
-        __shared__ uint32_t st_c[kCols][33];
-        __shared__ uint8_t st_rs[kRows][8];
-        __shared__ uint8_t st_cs[kCols][4];
+        __shared__ uint32_t st_c[kCols][8 * WR + 1];
+        __shared__ uint8_t st_rs[kRows][4 * WC];
+        __shared__ uint8_t st_cs[kCols][WR];
         const QuantOut &q = a.q8;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -230,45 +231,53 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quantize_kernel(const NormQu
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
                 const int item = threadIdx.x + kThreads * p;
-                const int line = item >> 3, part = item & 7;
+                const int line = item / (2 * WR), part = item % (2 * WR);
                 const int64_t c = tc * kCols + line;
                 if (c < a.cols)
                     *reinterpret_cast<uint4 *>(q.codes_t + c * q.ld_codes_t + tr * kRows + part * 16) =
                         make_uint4(st_c[line][4 * part], st_c[line][4 * part + 1], st_c[line][4 * part + 2], st_c[line][4 * part + 3]);
             }
         }
-        const int t = threadIdx.x;
-        if (t < kRows) {
+        for (int t = threadIdx.x; t < kRows; t += kThreads) {
             const int64_t r = tr * kRows + t;
             if (q.codes && r < a.rows) {
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < WC; ++k)
                     if (tc * kCols + k * 128 < a.cols_pad)
-                        *reinterpret_cast<uint32_t *>(q.scales + r * q.ld_scales + (tc * 2 + k) * 4) = *reinterpret_cast<const uint32_t *>(&st_rs[t][4 * k]);
+                        *reinterpret_cast<uint32_t *>(q.scales + r * q.ld_scales + (tc * WC + k) * 4) = *reinterpret_cast<const uint32_t *>(&st_rs[t][4 * k]);
             }
-        } else if (t >= kThreads - kCols) {
-            const int cl = t - (kThreads - kCols);
-            const int64_t c = tc * kCols + cl;
-            if (q.codes_t && c < a.cols)
-                *reinterpret_cast<uint32_t *>(q.scales_t + c * q.ld_scales_t + tr * 4) = *reinterpret_cast<const uint32_t *>(&st_cs[cl][0]);
+        }
+        for (int t = kThreads - 1 - threadIdx.x; t < kCols; t += kThreads) {
+            const int64_t c = tc * kCols + t;
+            if (!q.codes_t || c >= a.cols) continue;
+            if constexpr (WR == 4) *reinterpret_cast<uint32_t *>(q.scales_t + c * q.ld_scales_t + tr * 4) = *reinterpret_cast<const uint32_t *>(&st_cs[t][0]);
+            else q.scales_t[c * q.ld_scales_t + tr] = st_cs[t][0];
         }
     }
 }
 
+template <bool F32, int VEC, int WR, int WC>
+hipError_t launch_w(const NormQuantArgs &a, hipStream_t s)
+{
+    constexpr int kRows = 32 * WR, kCols = 128 * WC, kThreads = 64 * WR * WC;
+    const int64_t blocks = (a.rows_pad / kRows) * ((a.cols_pad + kCols - 1) / kCols);
+    const dim3 grid((unsigned)blocks), block(kThreads);
+    switch (a.fp4 * 2 + (a.mx ? 1 : 0)) {
+    case 1: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 0, true, WR, WC>), grid, block, 0, s, a); break;
+    case 2: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 1, false, WR, WC>), grid, block, 0, s, a); break;
+    case 3: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 1, true, WR, WC>), grid, block, 0, s, a); break;
+    case 4: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 2, false, WR, WC>), grid, block, 0, s, a); break;
+    default: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 2, true, WR, WC>), grid, block, 0, s, a); break;
+    }
+    return hipGetLastError();
+}
+
+// Up to 128 tiles, a strip a workgroup (64 x 64 blocks reach over two strips and stay in tiles)
 template <bool F32, int VEC>
 hipError_t launch_v(const NormQuantArgs &a, hipStream_t s)
 {
-    const int64_t blocks = (a.rows_pad / kRows) * ((a.cols_pad + kCols - 1) / kCols);
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks), block(kThreads);
-    switch (a.fp4 * 2 + (a.mx ? 1 : 0)) {
-    case 1: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 0, true>), grid, block, 0, s, a); break;
-    case 2: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 1, false>), grid, block, 0, s, a); break;
-    case 3: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 1, true>), grid, block, 0, s, a); break;
-    case 4: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 2, false>), grid, block, 0, s, a); break;
-    default: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 2, true>), grid, block, 0, s, a); break;
-    }
-    return hipGetLastError();
+    const bool strips = a.block == 32 && (a.rows_pad / 128) * ((a.cols_pad + 255) / 256) <= 128;
+    return strips ? launch_w<F32, VEC, 1, 1>(a, s) : launch_w<F32, VEC, 4, 2>(a, s);
 }
 
 }  // namespace
