@@ -16,6 +16,24 @@ namespace {
 __device__ __forceinline__ uint8_t scale_byte(uint32_t amax, int e) { return amax < 0x7F800000u ? (uint8_t)(e + 127) : (uint8_t)0xFF; }
 __device__ __forceinline__ float pow2(int e) { return bits_f((uint32_t)(127 + e) << 23); }
 
+// maximum over the 4 lanes of a 1 x 32 block (bits 0-1 of the lane), and of a 32 x 1 block (bits 4-5)
+__device__ __forceinline__ uint32_t row_max(uint32_t m)
+{
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp((int)m, (int)m, 0xB1, 0xF, 0xF, false));     // quad_perm 1 0 3 2
+    return max(m, (uint32_t)__builtin_amdgcn_update_dpp((int)m, (int)m, 0x4E, 0xF, 0xF, false));  // quad_perm 2 3 0 1
+}
+__device__ __forceinline__ uint32_t column_max(uint32_t m)
+{
+    // (the swaps leave the pair's two values in the same lane)
+    const auto a = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+    m = max((uint32_t)a[0], (uint32_t)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    return max((uint32_t)b[0], (uint32_t)b[1]);
+}
+
+// four words of a staged line (their pitch is odd: no 16-byte read)
+__device__ __forceinline__ uint4 words16(const uint32_t *p) { return make_uint4(p[0], p[1], p[2], p[3]); }
+
 __device__ __forceinline__ uint32_t fp4_word(const uint32_t (&v)[8], float scale)
 {
     uint32_t w = 0;
@@ -38,7 +56,7 @@ __device__ __forceinline__ uint2 fp8_words(const uint32_t (&v)[8], float scale)
 // alignment; 2 -- rows on 16-byte boundaries).  FP4: 0 none, 1 2D blocks, 2 1D blocks.  WR x WC
 // strips a workgroup, one a wave.
 template <bool F32, int VEC, int FP4, bool MX, int WR, int WC>
-__global__ __launch_bounds__(64 * WR * WC) void rmsnorm_quantize_kernel(const NormQuantArgs a)
+__global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(WR == 4 ? 4 : 1))) void rmsnorm_quantize_kernel(const NormQuantArgs a)
 {
     static_assert((WR == 4 && WC == 2) || (WR == 1 && WC == 1), "a tile, or a strip of its own");
     constexpr int kRows = 32 * WR, kCols = 128 * WC, kThreads = 64 * WR * WC;
@@ -68,10 +86,8 @@ __global__ __launch_bounds__(64 * WR * WC) void rmsnorm_quantize_kernel(const No
                 }
         }
         float w[8], rstd[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = c0 + j < a.cols ? load_value(a.w, a.w_bf16, c0 + j) : 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) rstd[i] = r0 + i < a.rows ? a.rstd[r0 + i] : 0.f;
+        load_eight(w, a.w, a.w_bf16, c0, a.cols - c0);
+        load_eight(rstd, a.rstd, 0, r0, a.rows - r0);
         const bool edge = __builtin_amdgcn_ballot_w64(a.rows - r0 < 8 || a.cols - c0 < 8) != 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -89,77 +105,86 @@ __global__ __launch_bounds__(64 * WR * WC) void rmsnorm_quantize_kernel(const No
         }
     }
 
-    // ---- block maxima on |bits| (NaN > inf > finite, as unsigned integers)
-    uint32_t rm[8], cm[8];
-    if constexpr (FP4 == 2 || MX) {
+    // ---- convert (block maxima on |bits|: NaN > inf > finite, as unsigned integers), one format
+    // and direction after the other, so that little lives beside y
+    constexpr bool BLOCKS = FP4 == 1, LINES = FP4 == 2;
+    __shared__ uint32_t st4_r[FP4 ? kRows : 1][16 * WC + 1];
+    __shared__ uint32_t st4_c[FP4 ? kCols : 1][4 * WR + 1];
+    __shared__ uint8_t st4_rs[LINES ? kRows : 1][4 * WC], st4_cs[LINES ? kCols : 1][WR];
+    __shared__ uint32_t st8_c[MX ? kCols : 1][8 * WR + 1];
+    __shared__ uint8_t st8_rs[MX ? kRows : 1][4 * WC], st8_cs[MX ? kCols : 1][WR];
+    const int rl = wr * 32 + 8 * rg, cl = wc * 128 + 8 * cc;
+    uint32_t am = 0;
+    if constexpr (BLOCKS) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) am = max(am, y[i][j] & 0x7FFFFFFFu);
+        am = column_max(row_max(am));
+        if (WR == 4 && a.block == 64) {
+            // the block beside it in this wave, then the paired wave's strip
+            __shared__ uint32_t am64[4][4];
+            am = max(am, (uint32_t)__shfl_xor((int)am, 4));
+            if (rg == 0 && (cc & 7) == 0) am64[wr][wc * 2 + (cc >> 3)] = am;
+            __syncthreads();
+            am = max(am, am64[wr ^ 1][wc * 2 + (cc >> 3)]);
+        }
+        const float scale = pow2(fp4_block_exponent(am));
+        uint32_t rowp[8], colp[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rowp[i] = am < 0x7F800000u ? fp4_word(y[i], scale) : 0u;
+        nibble_transpose8(rowp, colp);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) st4_r[rl + i][wc * 16 + cc] = rowp[i];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) st4_c[cl + j][wr * 4 + rg] = colp[j];
+    }
+    if constexpr (LINES || MX) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             uint32_t m = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) m = max(m, y[i][j] & 0x7FFFFFFFu);
-            m = max(m, (uint32_t)__shfl_xor((int)m, 1));
-            rm[i] = max(m, (uint32_t)__shfl_xor((int)m, 2));
+            m = row_max(m);
+            const bool finite = m < 0x7F800000u;
+            if constexpr (LINES) {
+                const int e = fp4_block_exponent(m);
+                st4_r[rl + i][wc * 16 + cc] = finite ? fp4_word(y[i], pow2(e)) : 0u;
+                if ((cc & 3) == 0) st4_rs[rl + i][wc * 4 + (cc >> 2)] = scale_byte(m, e);
+            }
+            if constexpr (MX) {
+                const int e = fp8_block_exponent(m);
+                const uint2 w = finite ? fp8_words(y[i], pow2(e)) : make_uint2(0, 0);
+                if (a.q8.codes && r0 + i < a.rows && c0 < a.cols_pad) *reinterpret_cast<uint2 *>(a.q8.codes + (r0 + i) * a.q8.ld_codes + c0) = w;
+                if ((cc & 3) == 0) st8_rs[rl + i][wc * 4 + (cc >> 2)] = scale_byte(m, e);
+            }
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
+            const uint32_t col[8] = {y[0][j], y[1][j], y[2][j], y[3][j], y[4][j], y[5][j], y[6][j], y[7][j]};
             uint32_t m = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = max(m, y[i][j] & 0x7FFFFFFFu);
-            m = max(m, (uint32_t)__shfl_xor((int)m, 16));
-            cm[j] = max(m, (uint32_t)__shfl_xor((int)m, 32));
+            for (int i = 0; i < 8; ++i) m = max(m, col[i] & 0x7FFFFFFFu);
+            m = column_max(m);
+            const bool finite = m < 0x7F800000u;
+            if constexpr (LINES) {
+                const int e = fp4_block_exponent(m);
+                st4_c[cl + j][wr * 4 + rg] = finite ? fp4_word(col, pow2(e)) : 0u;
+                if (rg == 0) st4_cs[cl + j][wr] = scale_byte(m, e);
+            }
+            if constexpr (MX) {
+                const int e = fp8_block_exponent(m);
+                const uint2 w = finite ? fp8_words(col, pow2(e)) : make_uint2(0, 0);
+                st8_c[cl + j][wr * 8 + 2 * rg] = w.x;
+                st8_c[cl + j][wr * 8 + 2 * rg + 1] = w.y;
+                if (rg == 0) st8_cs[cl + j][wr] = scale_byte(m, e);
+            }
         }
     }
+    __syncthreads();
 
+    // ---- stores, 16 bytes a lane
     if constexpr (FP4 != 0) {
-        __shared__ uint32_t st_r[kRows][16 * WC + 1];
-        __shared__ uint32_t st_c[kCols][4 * WR + 1];
-        __shared__ uint8_t st_rs[FP4 == 2 ? kRows : 1][4 * WC];
-        __shared__ uint8_t st_cs[FP4 == 2 ? kCols : 1][WR];
-        uint32_t am = 0;
-        uint32_t rowp[8], colp[8];
-        if constexpr (FP4 == 1) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) am = max(am, y[i][j] & 0x7FFFFFFFu);
-            am = max(am, (uint32_t)__shfl_xor((int)am, 1));
-            am = max(am, (uint32_t)__shfl_xor((int)am, 2));
-            am = max(am, (uint32_t)__shfl_xor((int)am, 16));
-            am = max(am, (uint32_t)__shfl_xor((int)am, 32));
-            if (WR == 4 && a.block == 64) {
-                // the block beside it in this wave, then the paired wave's strip
-                __shared__ uint32_t am64[4][4];
-                am = max(am, (uint32_t)__shfl_xor((int)am, 4));
-                if (rg == 0 && (cc & 7) == 0) am64[wr][wc * 2 + (cc >> 3)] = am;
-                __syncthreads();
-                am = max(am, am64[wr ^ 1][wc * 2 + (cc >> 3)]);
-            }
-            const float scale = pow2(fp4_block_exponent(am));
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rowp[i] = am < 0x7F800000u ? fp4_word(y[i], scale) : 0u;
-            nibble_transpose8(rowp, colp);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rowp[i] = rm[i] < 0x7F800000u ? fp4_word(y[i], pow2(fp4_block_exponent(rm[i]))) : 0u;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t col[8] = {y[0][j], y[1][j], y[2][j], y[3][j], y[4][j], y[5][j], y[6][j], y[7][j]};
-                colp[j] = cm[j] < 0x7F800000u ? fp4_word(col, pow2(fp4_block_exponent(cm[j]))) : 0u;
-            }
-            if ((cc & 3) == 0) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) st_rs[wr * 32 + 8 * rg + i][wc * 4 + (cc >> 2)] = scale_byte(rm[i], fp4_block_exponent(rm[i]));
-            }
-            if (rg == 0) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) st_cs[wc * 128 + 8 * cc + j][wr] = scale_byte(cm[j], fp4_block_exponent(cm[j]));
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) st_r[wr * 32 + 8 * rg + i][wc * 16 + cc] = rowp[i];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) st_c[wc * 128 + 8 * cc + j][wr * 4 + rg] = colp[j];
-        __syncthreads();
         const QuantOut &q = a.q4;
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
@@ -168,90 +193,70 @@ __global__ __launch_bounds__(64 * WR * WC) void rmsnorm_quantize_kernel(const No
                 const int line = item / (4 * WC), part = item % (4 * WC);
                 const int64_t r = tr * kRows + line;
                 if (r < a.rows && tc * kCols + part * 32 < a.cols_pad)
-                    *reinterpret_cast<uint4 *>(q.codes + r * q.ld_codes + tc * (kCols / 2) + part * 16) =
-                        make_uint4(st_r[line][4 * part], st_r[line][4 * part + 1], st_r[line][4 * part + 2], st_r[line][4 * part + 3]);
+                    *reinterpret_cast<uint4 *>(q.codes + r * q.ld_codes + tc * (kCols / 2) + part * 16) = words16(&st4_r[line][4 * part]);
             }
             if (q.codes_t) {
                 const int line = item / WR, part = item % WR;
                 const int64_t c = tc * kCols + line;
-                if (c < a.cols)
-                    *reinterpret_cast<uint4 *>(q.codes_t + c * q.ld_codes_t + tr * (kRows / 2) + part * 16) =
-                        make_uint4(st_c[line][4 * part], st_c[line][4 * part + 1], st_c[line][4 * part + 2], st_c[line][4 * part + 3]);
+                if (c < a.cols) *reinterpret_cast<uint4 *>(q.codes_t + c * q.ld_codes_t + tr * (kRows / 2) + part * 16) = words16(&st4_c[line][4 * part]);
             }
         }
-        if constexpr (FP4 == 2) {
-            // scale words, K-tile major; of a strip of its own one byte a column
-            for (int t = threadIdx.x; t < kRows; t += kThreads) {
-                const int64_t r = tr * kRows + t;
-                if (q.codes && r < a.rows) {
-#pragma unroll
-                    for (int k = 0; k < WC; ++k)
-                        if (tc * kCols + k * 128 < a.cols_pad)
-                            *reinterpret_cast<uint32_t *>(q.scales + (tc * WC + k) * q.ld_scales + 4 * r) =
-                                *reinterpret_cast<const uint32_t *>(&st_rs[t][4 * k]);
-                }
-            }
-            for (int t = kThreads - 1 - threadIdx.x; t < kCols; t += kThreads) {
-                const int64_t c = tc * kCols + t;
-                if (!q.codes_t || c >= a.cols) continue;
-                if constexpr (WR == 4) *reinterpret_cast<uint32_t *>(q.scales_t + tr * q.ld_scales_t + 4 * c) = *reinterpret_cast<const uint32_t *>(&st_cs[t][0]);
-                else q.scales_t[(tr >> 2) * q.ld_scales_t + 4 * c + (tr & 3)] = st_cs[t][0];
-            }
-        } else if (rg == 0 && (cc & 3) == 0 && tc * kCols + wc * 128 < a.cols_pad) {
+    }
+    if constexpr (BLOCKS) {
+        if (rg == 0 && (cc & 3) == 0 && tc * kCols + wc * 128 < a.cols_pad) {
+            const QuantOut &q = a.q4;
             const uint8_t byte = scale_byte(am, fp4_block_exponent(am));
             const int64_t rb = r0 >> 5, cb = c0 >> 5;
             if (q.codes && r0 < a.rows) q.scales[rb * q.ld_scales + cb] = byte;
             if (q.codes_t && c0 < a.cols) q.scales_t[cb * q.ld_scales_t + rb] = byte;
         }
     }
-
     if constexpr (MX) {
-        __shared__ uint32_t st_c[kCols][8 * WR + 1];
-        __shared__ uint8_t st_rs[kRows][4 * WC];
-        __shared__ uint8_t st_cs[kCols][WR];
         const QuantOut &q = a.q8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = fp8_block_exponent(rm[i]);
-            const uint2 w = rm[i] < 0x7F800000u ? fp8_words(y[i], pow2(e)) : make_uint2(0, 0);
-            if (q.codes && r0 + i < a.rows && c0 < a.cols_pad) *reinterpret_cast<uint2 *>(q.codes + (r0 + i) * q.ld_codes + c0) = w;
-            if ((cc & 3) == 0) st_rs[wr * 32 + 8 * rg + i][wc * 4 + (cc >> 2)] = scale_byte(rm[i], e);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int e = fp8_block_exponent(cm[j]);
-            const uint32_t col[8] = {y[0][j], y[1][j], y[2][j], y[3][j], y[4][j], y[5][j], y[6][j], y[7][j]};
-            const uint2 w = cm[j] < 0x7F800000u ? fp8_words(col, pow2(e)) : make_uint2(0, 0);
-            st_c[wc * 128 + 8 * cc + j][wr * 8 + 2 * rg] = w.x;
-            st_c[wc * 128 + 8 * cc + j][wr * 8 + 2 * rg + 1] = w.y;
-            if (rg == 0) st_cs[wc * 128 + 8 * cc + j][wr] = scale_byte(cm[j], e);
-        }
-        __syncthreads();
         if (q.codes_t) {
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
                 const int item = threadIdx.x + kThreads * p;
                 const int line = item / (2 * WR), part = item % (2 * WR);
                 const int64_t c = tc * kCols + line;
-                if (c < a.cols)
-                    *reinterpret_cast<uint4 *>(q.codes_t + c * q.ld_codes_t + tr * kRows + part * 16) =
-                        make_uint4(st_c[line][4 * part], st_c[line][4 * part + 1], st_c[line][4 * part + 2], st_c[line][4 * part + 3]);
+                if (c < a.cols) *reinterpret_cast<uint4 *>(q.codes_t + c * q.ld_codes_t + tr * kRows + part * 16) = words16(&st8_c[line][4 * part]);
             }
         }
+    }
+    // scale words of rows and columns (1D FP4: K-tile major); of a strip of its own one byte a column
+    if constexpr (LINES || MX) {
         for (int t = threadIdx.x; t < kRows; t += kThreads) {
             const int64_t r = tr * kRows + t;
-            if (q.codes && r < a.rows) {
+            if (r >= a.rows) continue;
 #pragma unroll
-                for (int k = 0; k < WC; ++k)
-                    if (tc * kCols + k * 128 < a.cols_pad)
-                        *reinterpret_cast<uint32_t *>(q.scales + r * q.ld_scales + (tc * WC + k) * 4) = *reinterpret_cast<const uint32_t *>(&st_rs[t][4 * k]);
+            for (int k = 0; k < WC; ++k) {
+                const int64_t word = tc * WC + k;
+                if (word * 128 >= a.cols_pad) continue;
+                if constexpr (LINES) {
+                    if (a.q4.codes) *reinterpret_cast<uint32_t *>(a.q4.scales + word * a.q4.ld_scales + 4 * r) = *reinterpret_cast<const uint32_t *>(&st4_rs[t][4 * k]);
+                }
+                if constexpr (MX) {
+                    if (a.q8.codes) *reinterpret_cast<uint32_t *>(a.q8.scales + r * a.q8.ld_scales + 4 * word) = *reinterpret_cast<const uint32_t *>(&st8_rs[t][4 * k]);
+                }
             }
         }
         for (int t = kThreads - 1 - threadIdx.x; t < kCols; t += kThreads) {
             const int64_t c = tc * kCols + t;
-            if (!q.codes_t || c >= a.cols) continue;
-            if constexpr (WR == 4) *reinterpret_cast<uint32_t *>(q.scales_t + c * q.ld_scales_t + tr * 4) = *reinterpret_cast<const uint32_t *>(&st_cs[t][0]);
-            else q.scales_t[c * q.ld_scales_t + tr] = st_cs[t][0];
+            if (c >= a.cols) continue;
+            if constexpr (LINES) {
+                const QuantOut &q = a.q4;
+                if (q.codes_t) {
+                    if constexpr (WR == 4) *reinterpret_cast<uint32_t *>(q.scales_t + tr * q.ld_scales_t + 4 * c) = *reinterpret_cast<const uint32_t *>(&st4_cs[t][0]);
+                    else q.scales_t[(tr >> 2) * q.ld_scales_t + 4 * c + (tr & 3)] = st4_cs[t][0];
+                }
+            }
+            if constexpr (MX) {
+                const QuantOut &q = a.q8;
+                if (q.codes_t) {
+                    if constexpr (WR == 4) *reinterpret_cast<uint32_t *>(q.scales_t + c * q.ld_scales_t + tr * 4) = *reinterpret_cast<const uint32_t *>(&st8_cs[t][0]);
+                    else q.scales_t[c * q.ld_scales_t + tr] = st8_cs[t][0];
+                }
+            }
         }
     }
 }
