@@ -57,21 +57,23 @@ struct Eight {
     // the first n of eight elements from p (n >= 8: all, n <= 0: none), the others 0
     __device__ __forceinline__ void load(const uint8_t *p, int64_t n)
     {
+        // (zeros first: written beside the load, they would have to wait for it)
+        zero();
         if (n >= 8) {
 #pragma unroll
             for (int k = 0; k < NW / 4; ++k) {
                 const u4v v = load16(p + 16 * k);
                 w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
             }
-            return;
-        }
-        zero();
+        } else if (n > 0) {
+            // (lanes behind the last element do not take a wave through these)
 #pragma unroll
-        for (int j = 0; j < 7; ++j)
-            if (j < n) {
-                if constexpr (BF16) w[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[j] << (16 * (j & 1));
-                else w[j] = reinterpret_cast<const uint32_t *>(p)[j];
-            }
+            for (int j = 0; j < 7; ++j)
+                if (j < n) {
+                    if constexpr (BF16) w[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[j] << (16 * (j & 1));
+                    else w[j] = reinterpret_cast<const uint32_t *>(p)[j];
+                }
+        }
     }
     __device__ __forceinline__ void store(uint8_t *p, int64_t n) const
     {
@@ -80,6 +82,7 @@ struct Eight {
             for (int k = 0; k < NW / 4; ++k) store16(p + 16 * k, u4v{w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]});
             return;
         }
+        if (n <= 0) return;
 #pragma unroll
         for (int j = 0; j < 7; ++j)
             if (j < n) {

@@ -52,58 +52,33 @@ __device__ __forceinline__ uint2 fp8_words(const uint32_t (&v)[8], float scale)
     return make_uint2(lo, hi);
 }
 
-// F32: h is float32.  VEC: as in the quantizers (0 -- element by element; 1 -- rows of any
-// alignment; 2 -- rows on 16-byte boundaries).  FP4: 0 none, 1 2D blocks, 2 1D blocks.  WR x WC
-// strips a workgroup, one a wave.
-template <bool F32, int VEC, int FP4, bool MX, int WR, int WC>
-__global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(WR == 4 ? 4 : 1))) void rmsnorm_quantize_kernel(const NormQuantArgs a)
+// y = (h * rstd) * w of a sub-block, 0 outside the matrix (rows, cols: what it has from here on):
+// a weight or a row that is not finite must not reach past it
+template <bool HB>
+__device__ __forceinline__ void norm_sub_block(uint32_t (&y)[8][8], const Eight<HB> (&h)[8], const float (&w)[8], const float (&rstd)[8],
+                                               int64_t rows, int64_t cols)
 {
-    static_assert((WR == 4 && WC == 2) || (WR == 1 && WC == 1), "a tile, or a strip of its own");
-    constexpr int kRows = 32 * WR, kCols = 128 * WC, kThreads = 64 * WR * WC;
-    constexpr int E = F32 ? 4 : 2, NV = 2 * E;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wr = wave / WC, wc = wave % WC, rg = lane >> 4, cc = lane & 15;
-    const int64_t tiles_c = (a.cols_pad + kCols - 1) / kCols;
-    const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
-    const int64_t r0 = tr * kRows + wr * 32 + 8 * rg, c0 = tc * kCols + wc * 128 + 8 * cc;
-
-    // ---- y of the sub-block, 0 outside the matrix
-    uint32_t y[8][8];
-    {
-        uint32_t v[8][NV];
-        const uint8_t *h = reinterpret_cast<const uint8_t *>(a.h) + (r0 * a.ldh + c0) * E;
-        if constexpr (VEC != 0) {
-            load_sub_block<E, VEC == 2, 0>(v, h, a.ldh * E, a.rows - r0, a.cols - c0);
-        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    auto at = [&](int j) __attribute__((always_inline)) -> uint32_t {
-                        return r0 + i < a.rows && c0 + j < a.cols ? f_bits(load_value(a.h, !F32, (r0 + i) * a.ldh + c0 + j)) : 0u;
-                    };
-                    v[i][k] = F32 ? at(k) : (at(2 * k) >> 16) | at(2 * k + 1);
-                }
-        }
-        float w[8], rstd[8];
-        load_eight(w, a.w, a.w_bf16, c0, a.cols - c0);
-        load_eight(rstd, a.rstd, 0, r0, a.rows - r0);
-        const bool edge = __builtin_amdgcn_ballot_w64(a.rows - r0 < 8 || a.cols - c0 < 8) != 0;
+        for (int j = 0; j < 8; ++j) y[i][j] = f_bits((h[i].at(j) * rstd[i]) * w[j]);
+    if (__builtin_amdgcn_ballot_w64(rows < 8 || cols < 8) != 0) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float h = F32 ? bits_f(v[i][F32 ? j : 0]) : bits_f((j & 1) ? v[i][j / (F32 ? 1 : 2)] & 0xFFFF0000u : v[i][j / (F32 ? 1 : 2)] << 16);
-                y[i][j] = f_bits((h * rstd[i]) * w[j]);
-            }
-        if (edge) {
-            // (a weight or a row that is not finite must not reach past the matrix)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[i][j] = r0 + i < a.rows && c0 + j < a.cols ? y[i][j] : 0u;
-        }
+            for (int j = 0; j < 8; ++j) y[i][j] = i < rows && j < cols ? y[i][j] : 0u;
     }
+}
+
+// A workgroup's part of an operand: WR x WC strips, one a wave, from y of each lane's sub-block (0
+// outside the matrix) at (r0, c0); tr and tc count tiles of this size.
+template <int FP4, bool MX, int WR, int WC>
+__device__ __forceinline__ void store_operands(const NormQuantArgs &a, const uint32_t (&y)[8][8], const int64_t tr, const int64_t tc)
+{
+    constexpr int kRows = 32 * WR, kCols = 128 * WC, kThreads = 64 * WR * WC;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wr = wave / WC, wc = wave % WC, rg = lane >> 4, cc = lane & 15;
+    const int64_t r0 = tr * kRows + wr * 32 + 8 * rg, c0 = tc * kCols + wc * 128 + 8 * cc;
 
     // ---- convert (block maxima on |bits|: NaN > inf > finite, as unsigned integers), one format
     // and direction after the other, so that little lives beside y
@@ -261,40 +236,103 @@ __global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(WR
     }
 }
 
-template <bool F32, int VEC, int WR, int WC>
-hipError_t launch_w(const NormQuantArgs &a, hipStream_t s)
+// Both formats by one workgroup, or, in strips, by one each (gridDim.y 2): a lone wave takes 4
+// cycles an instruction, and the conversions are most of its time (64 x 4096 in FP4 and
+// MXFP8 SPLIT_FIGURES)
+template <int FP4, bool MX, int WR, int WC>
+__device__ __forceinline__ void store_formats(const NormQuantArgs &a, const uint32_t (&y)[8][8], const int64_t tr, const int64_t tc)
 {
-    constexpr int kRows = 32 * WR, kCols = 128 * WC, kThreads = 64 * WR * WC;
-    const int64_t blocks = (a.rows_pad / kRows) * ((a.cols_pad + kCols - 1) / kCols);
-    const dim3 grid((unsigned)blocks), block(kThreads);
-    switch (a.fp4 * 2 + (a.mx ? 1 : 0)) {
-    case 1: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 0, true, WR, WC>), grid, block, 0, s, a); break;
-    case 2: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 1, false, WR, WC>), grid, block, 0, s, a); break;
-    case 3: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 1, true, WR, WC>), grid, block, 0, s, a); break;
-    case 4: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 2, false, WR, WC>), grid, block, 0, s, a); break;
-    default: hipLaunchKernelGGL((rmsnorm_quantize_kernel<F32, VEC, 2, true, WR, WC>), grid, block, 0, s, a); break;
+    if constexpr (FP4 != 0 && MX && WR == 1) {
+        if (blockIdx.y == 0) store_operands<FP4, false, WR, WC>(a, y, tr, tc);
+        else store_operands<0, true, WR, WC>(a, y, tr, tc);
+    } else {
+        store_operands<FP4, MX, WR, WC>(a, y, tr, tc);
     }
-    return hipGetLastError();
+}
+
+// From h and its rows' statistics.  HB: h is bfloat16.  ALIGNED: its rows are on 16-byte boundaries.
+// FP4: 0 none, 1 2D blocks, 2 1D blocks.
+template <bool HB, bool ALIGNED, int FP4, bool MX, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(WR == 4 ? 4 : 1))) void rmsnorm_quantize_kernel(const NormQuantArgs a)
+{
+    static_assert((WR == 4 && WC == 2) || (WR == 1 && WC == 1), "a tile, or a strip of its own");
+    constexpr int E = HB ? 2 : 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t tiles_c = (a.cols_pad + 128 * WC - 1) / (128 * WC);
+    // (the last rows first: the rows kernel has written them last, and the cache still holds some
+    // of them.  16384 x 4096 float32 in FP4 with the rows kernel 189 us, so 178)
+    const int64_t tile = gridDim.x - 1 - blockIdx.x, tr = tile / tiles_c, tc = tile - tr * tiles_c;
+    const int64_t r0 = tr * (32 * WR) + (wave / WC) * 32 + 8 * (lane >> 4), c0 = tc * (128 * WC) + (wave % WC) * 128 + 8 * (lane & 15);
+    const int64_t cols = a.cols - c0;
+
+    uint32_t y[8][8];
+    {
+        Eight<HB> h[8];
+        const uint8_t *p = reinterpret_cast<const uint8_t *>(a.h) + (r0 * a.ldh + c0) * E;
+        if constexpr (ALIGNED) {
+            uint32_t v[8][2 * E];
+            load_sub_block<E, true, 0>(v, p, a.ldh * E, a.rows - r0, cols);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int k = 0; k < 2 * E; ++k) h[i].w[k] = v[i][k];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i].load(p + i * a.ldh * E, r0 + i < a.rows ? cols : 0);
+        }
+        float w[8], rstd[8];
+        load_eight(w, a.w, a.w_bf16, c0, cols);
+        load_eight(rstd, a.rstd, 0, r0, a.rows - r0);
+        norm_sub_block(y, h, w, rstd, a.rows - r0, cols);
+    }
+    store_formats<FP4, MX, WR, WC>(a, y, tr, tc);
+}
+
+// f(FP4, MX) for the formats of a call
+template <typename F>
+void for_formats(const NormQuantArgs &a, F f)
+{
+    switch (a.fp4 * 2 + (a.mx ? 1 : 0)) {
+    case 1: f(std::integral_constant<int, 0>{}, std::true_type{}); break;
+    case 2: f(std::integral_constant<int, 1>{}, std::false_type{}); break;
+    case 3: f(std::integral_constant<int, 1>{}, std::true_type{}); break;
+    case 4: f(std::integral_constant<int, 2>{}, std::false_type{}); break;
+    default: f(std::integral_constant<int, 2>{}, std::true_type{}); break;
+    }
+}
+
+template <bool HB, bool ALIGNED, int WR, int WC>
+void launch_w(const NormQuantArgs &a, hipStream_t s)
+{
+    const int64_t blocks = (a.rows_pad / (32 * WR)) * ((a.cols_pad + 128 * WC - 1) / (128 * WC));
+    for_formats(a, [&](auto fp4, auto mx) {
+        hipLaunchKernelGGL((rmsnorm_quantize_kernel<HB, ALIGNED, decltype(fp4)::value, decltype(mx)::value, WR, WC>),
+                           dim3((unsigned)blocks, WR == 1 && a.fp4 && a.mx ? 2 : 1), dim3(64 * WR * WC), 0, s, a);
+    });
 }
 
 // Up to 128 tiles, a strip a workgroup (64 x 64 blocks reach over two strips and stay in tiles)
-template <bool F32, int VEC>
-hipError_t launch_v(const NormQuantArgs &a, hipStream_t s)
+template <bool HB, bool ALIGNED>
+void launch_v(const NormQuantArgs &a, hipStream_t s)
 {
     const bool strips = a.block == 32 && (a.rows_pad / 128) * ((a.cols_pad + 255) / 256) <= 128;
-    return strips ? launch_w<F32, VEC, 1, 1>(a, s) : launch_w<F32, VEC, 4, 2>(a, s);
+    if (strips) launch_w<HB, ALIGNED, 1, 1>(a, s);
+    else launch_w<HB, ALIGNED, 4, 2>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_rmsnorm_quantize(const NormQuantArgs &a, hipStream_t stream)
 {
-    const int bytes = a.h_bf16 ? 2 : 4;
-    const bool aligned = reinterpret_cast<uintptr_t>(a.h) % 16 == 0 && (a.ldh * bytes) % 16 == 0;
-    const int vec = aligned ? 2 : a.cols >= 8 ? 1 : 0;
-    if (a.h_bf16)
-        return vec == 2 ? launch_v<false, 2>(a, stream) : vec == 1 ? launch_v<false, 1>(a, stream) : launch_v<false, 0>(a, stream);
-    return vec == 2 ? launch_v<true, 2>(a, stream) : vec == 1 ? launch_v<true, 1>(a, stream) : launch_v<true, 0>(a, stream);
+    const bool aligned = reinterpret_cast<uintptr_t>(a.h) % 16 == 0 && a.ldh % (a.h_bf16 ? 8 : 4) == 0;
+    if (a.h_bf16) {
+        if (aligned) launch_v<true, true>(a, stream);
+        else launch_v<true, false>(a, stream);
+    } else {
+        if (aligned) launch_v<false, true>(a, stream);
+        else launch_v<false, false>(a, stream);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace q2d

@@ -88,7 +88,7 @@ def _forward(x, weight, eps, residual, h, rstd, y, q4, q8):
     x_code = _dtype_code(x.dtype)
     if residual is not None:
         if h is None:
-            h = torch.empty(shape, dtype=x.dtype, device=device)
+            h = torch.empty_like(x, memory_format=torch.contiguous_format)
         elif h.dtype != x.dtype:
             raise Q2DError("h: the dtype of x is expected")
         r_code = _dtype_code(residual.dtype)
@@ -120,7 +120,7 @@ def q2d_rmsnorm_fwd(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, re
     itself without a residual) times weight [cols]; returns (y, h, rstd).  rstd (float32 [rows])
     is what q2d_rmsnorm_bwd needs.  h may be x or residual itself: in place."""
     if y is None:
-        y = torch.empty(x.shape, dtype=y_dtype, device=x.device)
+        y = torch.empty_like(x, dtype=y_dtype, memory_format=torch.contiguous_format)
     h, rstd = _forward(x, weight, eps, residual, h, rstd, y, None, None)
     return y, h, rstd
 
@@ -141,9 +141,10 @@ def q2d_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-
         raise Q2DError("expected x as a 2-D device tensor")
     if out is None:
         out = [QTensor(f, *x.shape, x.device, block if f == FP4_2D else 32, orientations) for f in formats]
-    elif len(out) != len(formats) or any(q.fmt != f or q.nseg is not None for q, f in zip(out, formats)):
-        raise Q2DError("out: a QTensor for each of formats is expected")
-    _same_device(x.device, *out)
+    else:
+        if len(out) != len(formats) or any(q.fmt != f or q.nseg is not None for q, f in zip(out, formats)):
+            raise Q2DError("out: a QTensor for each of formats is expected")
+        _same_device(x.device, *out)
     q = [None, None]
     for t, mx in zip(out, kinds):
         q[mx] = t.ptr()
@@ -162,7 +163,7 @@ def q2d_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rst
         raise Q2DError("expected h as a 2-D device tensor")
     rows, cols = shape
     if dx is None:
-        dx = torch.empty(shape, dtype=h.dtype, device=device)
+        dx = torch.empty_like(h, memory_format=torch.contiguous_format)
     if dx.dtype != h.dtype or (dh is not None and dh.dtype != h.dtype):
         raise Q2DError("dh and dx: the dtype of h is expected")
     dhp = lddh = wp = 0
