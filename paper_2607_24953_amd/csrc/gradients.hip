@@ -53,7 +53,7 @@ __device__ __forceinline__ Piece piece_of(const T &t, int piece)
 // turns whose loads a lane has in flight
 constexpr int kFlight = 4;
 
-template <bool BF16>
+template <bool BF16, bool ONCE>
 __device__ __forceinline__ double square_piece(const void *data, int64_t at, int length)
 {
     const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * (BF16 ? 2 : 4);
@@ -64,7 +64,7 @@ __device__ __forceinline__ double square_piece(const void *data, int64_t at, int
 #pragma unroll
         for (int k = 0; k < kFlight; ++k) {
             const int c = c0 + k * kTurn;
-            e[k].load(p + c * (BF16 ? 2 : 4), length - c);
+            e[k].template load<ONCE>(p + c * (BF16 ? 2 : 4), length - c);
         }
 #pragma unroll
         for (int k = 0; k < kFlight; ++k)
@@ -77,13 +77,14 @@ __device__ __forceinline__ double square_piece(const void *data, int64_t at, int
     return s;
 }
 
+template <bool ONCE>
 __global__ __launch_bounds__(256) void grad_square_kernel(const Squared t, double *parts)
 {
     __shared__ double lds[4];
     double s = 0.0;
     for (int piece = blockIdx.x; piece < t.pieces; piece += gridDim.x) {
         const Piece p = piece_of(t, piece);
-        s += p.bf16 ? square_piece<true>(t.data[p.tensor], p.at, p.length) : square_piece<false>(t.data[p.tensor], p.at, p.length);
+        s += p.bf16 ? square_piece<true, ONCE>(t.data[p.tensor], p.at, p.length) : square_piece<false, ONCE>(t.data[p.tensor], p.at, p.length);
     }
     s = group_sum(s, 4, lds);
     if (threadIdx.x == 0) parts[blockIdx.x] = s;
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const double *parts, int
     if (threadIdx.x == 0) *norm = (float)s;
 }
 
-template <bool BF16>
+template <bool BF16, bool ONCE>
 __device__ __forceinline__ void scale_piece(const void *data, void *out, int64_t at, int length, bool clip, float f)
 {
     const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * (BF16 ? 2 : 4);
@@ -115,7 +116,7 @@ __device__ __forceinline__ void scale_piece(const void *data, void *out, int64_t
 #pragma unroll
         for (int k = 0; k < kFlight; ++k) {
             const int c = c0 + k * kTurn;
-            e[k].load(p + c * (BF16 ? 2 : 4), length - c);
+            e[k].template load<ONCE>(p + c * (BF16 ? 2 : 4), length - c);
         }
 #pragma unroll
         for (int k = 0; k < kFlight; ++k) {
@@ -126,12 +127,13 @@ __device__ __forceinline__ void scale_piece(const void *data, void *out, int64_t
                 for (int j = 0; j < 8; ++j) v[j] = e[k].at(j) * f;
                 e[k].set(v);
             }
-            e[k].store(o + c * (BF16 ? 2 : 4), length - c);
+            e[k].template store<ONCE>(o + c * (BF16 ? 2 : 4), length - c);
         }
     }
 }
 
 // (the last pieces first: the square sums read them last, and some are still in the cache)
+template <bool ONCE>
 __global__ __launch_bounds__(256) void grad_scale_kernel(const Scaled t, const double *parts, int n, const float *given,
                                                          double max_norm, float *norm)
 {
@@ -144,8 +146,8 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(const Scaled t, const d
     for (int piece = t.pieces - 1 - (int)blockIdx.x; piece >= 0; piece -= gridDim.x) {
         const Piece p = piece_of(t, piece);
         if (!clip && t.out[p.tensor] == t.data[p.tensor]) continue;
-        if (p.bf16) scale_piece<true>(t.data[p.tensor], t.out[p.tensor], p.at, p.length, clip, f);
-        else scale_piece<false>(t.data[p.tensor], t.out[p.tensor], p.at, p.length, clip, f);
+        if (p.bf16) scale_piece<true, ONCE>(t.data[p.tensor], t.out[p.tensor], p.at, p.length, clip, f);
+        else scale_piece<false, ONCE>(t.data[p.tensor], t.out[p.tensor], p.at, p.length, clip, f);
     }
 }
 
@@ -236,6 +238,15 @@ int64_t elements(const Set &g)
     return all;
 }
 
+// Whether the cache keeps the tensors between the two passes
+constexpr int64_t kKept = int64_t(768) << 20;
+bool kept_between(const Set &g)
+{
+    int64_t bytes = 0;
+    for (int32_t i = 0; i < g.n; ++i) bytes += g.counts[i] * dtype_bytes((q2d_dtype)g.dtypes[i]);
+    return bytes <= kKept;
+}
+
 // Turns of a piece: a workgroup for each of 1024 pieces first, then longer ones.  (In one size of
 // 8 turns the 0.8 M float32 of a small model's gradients took 5.1 us for their squares.)
 int turns_of(int64_t all)
@@ -246,7 +257,7 @@ int turns_of(int64_t all)
 }
 
 // Partial sums of the set into parts; their number, or -1
-int square_sums(const Set &g, int64_t all, double *parts, hipStream_t stream)
+int square_sums(const Set &g, int64_t all, bool once, double *parts, hipStream_t stream)
 {
     const int turns = turns_of(all);
     int n = 0;
@@ -257,7 +268,8 @@ int square_sums(const Set &g, int64_t all, double *parts, hipStream_t stream)
         // a launch's share of the parts, by its pieces
         const int64_t share = (int64_t)((double)kMaxParts * t.pieces * turns * kTurn / (double)(all + t.n * (int64_t)turns * kTurn));
         const int groups = (int)std::min<int64_t>(t.pieces, std::max<int64_t>(1, std::min<int64_t>(share, kMaxParts)));
-        hipLaunchKernelGGL(grad_square_kernel, dim3(groups), dim3(256), 0, stream, t, parts + n);
+        if (once) hipLaunchKernelGGL(grad_square_kernel<true>, dim3(groups), dim3(256), 0, stream, t, parts + n);
+        else hipLaunchKernelGGL(grad_square_kernel<false>, dim3(groups), dim3(256), 0, stream, t, parts + n);
         if (hipGetLastError() != hipSuccess) return -1;
         n += groups;
     }
@@ -282,7 +294,7 @@ q2d_status q2d_grad_norm(int32_t n, const void *const *data, const int64_t *coun
     if (s != Q2D_OK) return s;
     if (!norm || !aligned(norm, 4) || !workspace || !aligned(workspace, 8) || workspace_bytes < q2d_grad_workspace(n)) return Q2D_EINVAL;
     double *parts = reinterpret_cast<double *>(workspace);
-    const int k = square_sums(g, elements(g), parts, stream);
+    const int k = square_sums(g, elements(g), true, parts, stream);
     if (k < 0) return Q2D_ELAUNCH;
     hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, stream, parts, k, norm);
     return hipGetLastError() == hipSuccess ? Q2D_OK : Q2D_ELAUNCH;
@@ -303,10 +315,11 @@ q2d_status q2d_clip_grads(int32_t n, const void *const *data, void *const *out, 
     double *parts = nullptr;
     int k = 0;
     const int64_t all = elements(g);
+    const bool kept = kept_between(g);
     if (!given) {
         if (!workspace || !aligned(workspace, 8) || workspace_bytes < q2d_grad_workspace(n)) return Q2D_EINVAL;
         parts = reinterpret_cast<double *>(workspace);
-        k = square_sums(g, all, parts, stream);
+        k = square_sums(g, all, !kept, parts, stream);
         if (k < 0) return Q2D_ELAUNCH;
         if (k == 0) {       // no elements: nothing to scale
             hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, stream, parts, 0, norm);
@@ -318,7 +331,9 @@ q2d_status q2d_clip_grads(int32_t n, const void *const *data, void *const *out, 
     for (int32_t i = 0; i < n;) {
         i = fill(g, i, turns, t);
         if (t.n == 0) break;
-        hipLaunchKernelGGL(grad_scale_kernel, dim3(std::min(t.pieces, kMaxParts)), dim3(256), 0, stream, t, parts, k, given, max_norm, norm);
+        const dim3 groups(std::min(t.pieces, kMaxParts));
+        if (kept) hipLaunchKernelGGL(grad_scale_kernel<true>, groups, dim3(256), 0, stream, t, parts, k, given, max_norm, norm);
+        else hipLaunchKernelGGL(grad_scale_kernel<false>, groups, dim3(256), 0, stream, t, parts, k, given, max_norm, norm);
         if (hipGetLastError() != hipSuccess) return Q2D_ELAUNCH;
         norm = nullptr;     // (written by the first launch)
     }

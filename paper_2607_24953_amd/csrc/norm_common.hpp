@@ -29,8 +29,19 @@ __device__ __forceinline__ float round_bf16(float v) { return bits_f(pack_bf16(v
 // 16 bytes at any address of an element: the hardware takes a 16-byte access there too, in the same
 // instruction, so rows need no alignment
 typedef u4v u4v_any __attribute__((aligned(2)));
-__device__ __forceinline__ u4v load16(const uint8_t *p) { return *reinterpret_cast<const u4v_any *>(p); }
-__device__ __forceinline__ void store16(uint8_t *p, u4v v) { *reinterpret_cast<u4v_any *>(p) = v; }
+// (ONCE: of data that is not read or written again soon)
+template <bool ONCE = false>
+__device__ __forceinline__ u4v load16(const uint8_t *p)
+{
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u4v_any *>(p));
+    else return *reinterpret_cast<const u4v_any *>(p);
+}
+template <bool ONCE = false>
+__device__ __forceinline__ void store16(uint8_t *p, u4v v)
+{
+    if constexpr (ONCE) __builtin_nontemporal_store(v, reinterpret_cast<u4v_any *>(p));
+    else *reinterpret_cast<u4v_any *>(p) = v;
+}
 
 // Eight neighbouring elements, the unit of every vector access here, as they lie in memory: NW words of bf16 pairs (4) or float32 (8)
 template <bool BF16>
@@ -55,6 +66,7 @@ struct Eight {
         for (int k = 0; k < NW; ++k) asm volatile("" : "+v"(w[k]));
     }
     // the first n of eight elements from p (n >= 8: all, n <= 0: none), the others 0
+    template <bool ONCE = false>
     __device__ __forceinline__ void load(const uint8_t *p, int64_t n)
     {
         // (zeros first: written beside the load, they would have to wait for it)
@@ -62,7 +74,7 @@ struct Eight {
         if (n >= 8) {
 #pragma unroll
             for (int k = 0; k < NW / 4; ++k) {
-                const u4v v = load16(p + 16 * k);
+                const u4v v = load16<ONCE>(p + 16 * k);
                 w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
             }
         } else if (n > 0) {
@@ -75,11 +87,12 @@ struct Eight {
                 }
         }
     }
+    template <bool ONCE = false>
     __device__ __forceinline__ void store(uint8_t *p, int64_t n) const
     {
         if (n >= 8) {
 #pragma unroll
-            for (int k = 0; k < NW / 4; ++k) store16(p + 16 * k, u4v{w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]});
+            for (int k = 0; k < NW / 4; ++k) store16<ONCE>(p + 16 * k, u4v{w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]});
             return;
         }
         if (n <= 0) return;

@@ -13,11 +13,10 @@ namespace q2d {
 
 namespace {
 
-// workgroups of a launch at most
-constexpr int64_t kParts = 1024;
 
-// HB, DB: h and dh, dy are bfloat16.  LANES, CH: as in the forward kernel.
-template <bool HB, bool DB, int LANES, int CH>
+// HB, DB: h and dh, dy are bfloat16.  LANES, CH: as in the forward kernel.  ONCE: the rows come from
+// memory rather than from the cache.
+template <bool HB, bool DB, int LANES, int CH, bool ONCE>
 __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const NormGradArgs a, float *part)
 {
     constexpr int EH = HB ? 2 : 4, ED = DB ? 2 : 4;
@@ -25,12 +24,14 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
     __shared__ double lds[2][16];
     const int t = LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x, step = LANES ? LANES : blockDim.x;
     const int sub = LANES ? threadIdx.x / (LANES ? LANES : 1) : 0;
+    // (two chunks of weights beside two of everything else do not fit 128 registers)
+    constexpr bool KEPT = LANES != 0 || CH == 1;
     float w[CH][8];
     double acc[CH][8];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         const int64_t c = 8 * (t + k * (int64_t)step);
-        load_eight(w[k], a.w, a.w_bf16, c, a.cols - c);
+        if constexpr (KEPT) load_eight(w[k], a.w, a.w_bf16, c, a.cols - c);
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[k][j] = 0.0;
     }
@@ -49,21 +50,23 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             const int64_t c = 8 * (t + k * (int64_t)step);
-            h[k].load(hp + c * EH, cols - c);
-            dy[k].load(dyp + c * ED, cols - c);
-            if (a.dh) dh[k].load(dhp + c * EH, cols - c);
+            h[k].template load<ONCE && HB>(hp + c * EH, cols - c);
+            dy[k].template load<ONCE && DB>(dyp + c * ED, cols - c);
+            if (a.dh) dh[k].template load<ONCE && HB>(dhp + c * EH, cols - c);
             else dh[k].zero();
         }
         const float rstd = some ? a.rstd[row] : 0.f;
         double sum = 0.0;
 #pragma unroll
-        for (int k = 0; k < CH; ++k)
+        for (int k = 0; k < CH; ++k) {
+            if constexpr (!KEPT) load_eight(w[k], a.w, a.w_bf16, 8 * (t + k * (int64_t)step), a.cols - 8 * (t + k * (int64_t)step));
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float n = h[k].at(j) * rstd, d = dy[k].at(j);
                 sum = __builtin_fma((double)(d * w[k][j]), (double)n, sum);
                 acc[k][j] = __builtin_fma((double)d, (double)n, acc[k][j]);
             }
+        }
         if constexpr (LANES) sum = lane_sum<LANES ? LANES : 64>(sum);
         else sum = group_sum(sum, blockDim.x >> 6, lds[turn]);
         const float mean = (float)(sum / (double)a.cols);
@@ -77,6 +80,7 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
         for (int k = 0; k < CH; ++k) {
             const int64_t c = 8 * (t + k * (int64_t)step);
             if (c >= cols) break;
+            if constexpr (!KEPT) load_eight(w[k], a.w, a.w_bf16, c, a.cols - c);
             float dx[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -189,30 +193,46 @@ __global__ __launch_bounds__(512) void rmsnorm_grad_join_kernel(const float *par
 
 inline int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 
+// bytes that the cache may still hold from the kernels before
+constexpr int64_t kCached = int64_t(192) << 20;
+
 constexpr int64_t kLong = 16384;       // columns that a workgroup's registers hold
 
 // rows that a workgroup has at a time
 int64_t rows_at_once(int64_t cols) { return cols <= 256 ? 16 : cols <= 1024 ? 4 : 1; }
 
+// waves of a workgroup
+int64_t waves_of(int64_t cols) { return cols <= 1024 ? 4 : cols <= 8192 ? (cols + 511) / 512 : (cols + 1023) / 1024; }
+
 // workgroups, each with one part of dw
 int64_t parts_of(int64_t rows, int64_t cols)
 {
     if (cols > kLong) return rows < 256 ? rows : 256;
-    const int64_t per = rows_at_once(cols), turns = (rows + per - 1) / per;
-    return turns < kParts ? turns : kParts;
+    // as many as are there at once (registers: 16 waves a CU, 8 of those with several rows), each
+    // with equally many turns
+    const int64_t most = 256 * (cols <= 1024 ? 2 : waves_of(cols) < 16 ? 16 / waves_of(cols) : 1);
+    const int64_t per = rows_at_once(cols), groups = (rows + per - 1) / per, turns = (groups + most - 1) / most;
+    return turns == 0 ? 0 : (groups + turns - 1) / turns;
 }
 
 int64_t means_bytes(int64_t rows, int64_t cols) { return cols > kLong ? up256(rows * 4) : 0; }
 
-template <bool HB, bool DB>
+template <bool HB, bool DB, bool ONCE>
 hipError_t launch_grad(const NormGradArgs &a, unsigned parts, float *part, hipStream_t s)
 {
-    const int64_t chunks = (a.cols + 7) / 8;
-    if (chunks <= 32) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 16, 2>), dim3(parts), dim3(256), 0, s, a, part);
-    else if (chunks <= 128) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 64, 2>), dim3(parts), dim3(256), 0, s, a, part);
-    else if (chunks <= 1024) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, 1>), dim3(parts), dim3((unsigned)((chunks + 63) / 64 * 64)), 0, s, a, part);
-    else hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, 2>), dim3(parts), dim3((unsigned)((chunks + 127) / 128 * 64)), 0, s, a, part);
+    const dim3 grid(parts), block((unsigned)(64 * waves_of(a.cols)));
+    if (a.cols <= 256) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 16, 2, ONCE>), grid, block, 0, s, a, part);
+    else if (a.cols <= 1024) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 64, 2, ONCE>), grid, block, 0, s, a, part);
+    else if (a.cols <= 8192) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, 1, ONCE>), grid, block, 0, s, a, part);
+    else hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, 2, ONCE>), grid, block, 0, s, a, part);
     return hipGetLastError();
+}
+
+template <bool HB, bool DB>
+hipError_t launch_types(const NormGradArgs &a, unsigned parts, float *part, hipStream_t s)
+{
+    const int64_t bytes = a.rows * a.cols * ((a.dh ? 2 : 1) * (HB ? 2 : 4) + (DB ? 2 : 4));
+    return bytes > kCached ? launch_grad<HB, DB, true>(a, parts, part, s) : launch_grad<HB, DB, false>(a, parts, part, s);
 }
 
 }  // namespace
@@ -234,9 +254,9 @@ hipError_t launch_rmsnorm_grad(const NormGradArgs &a, hipStream_t stream)
             hipLaunchKernelGGL(rmsnorm_grad_tile_kernel, dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)parts), dim3(256), 0, stream, a, means, part);
             e = hipGetLastError();
         } else if (a.h_bf16) {
-            e = a.dy_bf16 ? launch_grad<true, true>(a, (unsigned)parts, part, stream) : launch_grad<true, false>(a, (unsigned)parts, part, stream);
+            e = a.dy_bf16 ? launch_types<true, true>(a, (unsigned)parts, part, stream) : launch_types<true, false>(a, (unsigned)parts, part, stream);
         } else {
-            e = a.dy_bf16 ? launch_grad<false, true>(a, (unsigned)parts, part, stream) : launch_grad<false, false>(a, (unsigned)parts, part, stream);
+            e = a.dy_bf16 ? launch_types<false, true>(a, (unsigned)parts, part, stream) : launch_types<false, false>(a, (unsigned)parts, part, stream);
         }
         if (e != hipSuccess) return e;
     }
