@@ -213,12 +213,16 @@ def _gradients(tensors, what):
     devices = set(map(torch.Tensor.get_device, tensors))
     if len(devices) > 1 or min(devices) < 0:
         raise Q2DError("%s: tensors on one device are expected" % what)
-    try:
-        dtypes = array.array("i", map(_DTYPE_CODES.__getitem__, map(_DTYPE_OF, tensors)))
-    except KeyError:
-        raise Q2DError("%s: float32 or bfloat16 tensors are expected" % what) from None
-    pointers = array.array("Q", map(torch.Tensor.data_ptr, tensors))
-    counts = array.array("q", map(torch.Tensor.numel, tensors))
+    kinds = set(map(_DTYPE_OF, tensors))
+    if not kinds <= _DTYPE_CODES.keys():
+        raise Q2DError("%s: float32 or bfloat16 tensors are expected" % what)
+    if len(kinds) == 1:
+        dtypes = array.array("i", [_DTYPE_CODES[kinds.pop()]]) * len(tensors)
+    else:
+        dtypes = array.array("i", [_DTYPE_CODES[t.dtype] for t in tensors])
+    # (from lists: an array grown element by element takes a quarter longer)
+    pointers = array.array("Q", list(map(torch.Tensor.data_ptr, tensors)))
+    counts = array.array("q", list(map(torch.Tensor.numel, tensors)))
     return tensors, pointers, counts, dtypes, dense
 
 
