@@ -537,7 +537,8 @@ q2d_status q2d_attention_cached(const q2d_kv_cache *c, const q2d_sequences *s, c
  * Any of y, q4 and q8 may be wanted together, one at least.
  *
  * Row r of a tensor starts at its pointer + r * ld elements (ld >= cols with more than one
- * row).  rows may be 0 without operands.  Values that are not finite follow the formulas: a row
+ * row); rows up to 2^31 - 1, cols up to 2^27 (Q2D_EUNSUPPORTED above).  rows may be 0 without
+ * operands.  Values that are not finite follow the formulas: a row
  * with a NaN is NaN, one with an infinity has rstd 0.
  */
 typedef struct {
@@ -602,8 +603,8 @@ q2d_status q2d_grad_norm(int32_t n, const void *const *data, const int64_t *coun
  * leaves the values as they are (the caller sees it in *norm).  out NULL: in place.
  * given   device: the norm to go by (of tensors on several GPUs, say), or NULL: the norm of
  *         these tensors is computed first and written to *norm.  One of given and norm is NULL.
- * An output may be its own input (in place) and shares no memory with anything else of the call
- * (Q2D_EINVAL); the same tensor twice is refused by that.  With given, workspace may be NULL.
+ * An output may be its own input (in place) and shares no memory with anything else of the call,
+ * the norm and the workspace among it (Q2D_EINVAL); the same tensor twice is refused by that.  With given, workspace may be NULL.
  */
 q2d_status q2d_clip_grads(int32_t n, const void *const *data, void *const *out, const int64_t *counts, const int32_t *dtypes,
                           double max_norm, const float *given, float *norm, void *workspace, int64_t workspace_bytes,

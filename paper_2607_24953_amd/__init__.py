@@ -285,7 +285,7 @@ def q2d_dequantize(q: QTensor, copy: int = 0, out_dtype=torch.float32, exps: boo
     R, C = q.rows, q.cols
     if out is None:
         out = torch.empty((R, C), dtype=out_dtype, device=q.device)
-    if out.dim() != 2 or out.stride(1) != 1 or tuple(out.shape) != (R, C):
+    elif out.dim() != 2 or out.stride(1) != 1 or tuple(out.shape) != (R, C):
         raise Q2DError("output must be a row-major R x C tensor")
     e = torch.empty((R, C), dtype=torch.int8, device=q.device) if exps else None
     _same_device(q.device, out, e)

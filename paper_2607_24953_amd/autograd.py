@@ -173,12 +173,11 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual:
 
 class _NormLinearFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, residual, norm_weight, weight, layer):
+    def forward(ctx, x, residual, norm_weight, weight, layer, both):
         x2, r2 = _norm_inputs(ctx, x, residual, norm_weight)
         n = layer._calls
         layer._calls += 1
-        # (only the backward pass reads the transposed copies)
-        both = (True, any(ctx.needs_input_grad))
+        both = (True, both and any(ctx.needs_input_grad))
         (qX,), h, rstd = q2d_rmsnorm_quantize(x2, norm_weight.detach(), layer.eps, residual=r2,
                                               formats=(FP4_1D if layer.activations == "1d" else FP4_2D,),
                                               block=layer.block, orientations=both)
@@ -207,7 +206,7 @@ class _NormLinearFunction(torch.autograd.Function):
                                        dw_dtype=torch.float32, block=layer.block)
             dW = dW.to(ctx.w_dtype)
         ctx.qX = ctx.qW = None
-        return (*_norm_backward(ctx, dy, dh, h, norm_weight.detach(), rstd), dW, None)
+        return (*_norm_backward(ctx, dy, dh, h, norm_weight.detach(), rstd), dW, None, None)
 
 
 class Q2DNormLinear(Q2DLinear):
@@ -224,7 +223,8 @@ class Q2DNormLinear(Q2DLinear):
 
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
         """y, or with a residual (y, x + residual)."""
-        out = _NormLinearFunction.apply(x, residual, self.norm_weight, self.weight, self)
+        # (only a backward pass reads the transposed copies)
+        out = _NormLinearFunction.apply(x, residual, self.norm_weight, self.weight, self, torch.is_grad_enabled())
         return out[0] if residual is None else out
 
 

@@ -12,8 +12,8 @@
 #include "norm_common.hpp"
 
 #include <algorithm>
+#include <exception>
 #include <math.h>
-#include <new>
 #include <vector>
 
 namespace q2d {
@@ -176,25 +176,31 @@ q2d_status check_set(const Set &g)
     return Q2D_OK;
 }
 
-// Whether what the call writes meets anything else that it reads or writes: an output may be its
-// own input, in place, and nothing else.
-q2d_status check_apart(const Set &g)
+// Whether what the call writes meets anything else that it reads or writes: a tensor's output may be
+// its own input, in place, and nothing else.  given, norm and the workspace: where not null.
+q2d_status check_apart(const Set &g, const void *given, const void *norm, const void *workspace, int64_t workspace_bytes)
 {
-    struct Range { uintptr_t at, end; int32_t i; bool out; };
+    struct Range { uintptr_t at, end; bool out; };
     std::vector<Range> r;
+    auto add = [&](const void *p, uintptr_t bytes, bool out) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        if (p && bytes) r.push_back({at, at + bytes, out});
+    };
     try {
-        r.reserve(2 * (size_t)g.n);
+        r.reserve(2 * (size_t)g.n + 3);
         for (int32_t i = 0; i < g.n; ++i) {
             const uintptr_t bytes = (uintptr_t)g.counts[i] * dtype_bytes((q2d_dtype)g.dtypes[i]);
-            if (!bytes) continue;
-            const uintptr_t d = reinterpret_cast<uintptr_t>(g.data[i]), o = g.out ? reinterpret_cast<uintptr_t>(g.out[i]) : d;
-            r.push_back({o, o + bytes, i, true});
-            if (o != d) r.push_back({d, d + bytes, i, false});
+            const void *out = g.out ? g.out[i] : g.data[i];
+            add(out, bytes, true);
+            if (out != g.data[i]) add(g.data[i], bytes, false);
         }
-    } catch (const std::bad_alloc &) {
+        add(given, 4, false);
+        add(norm, 4, true);
+        add(workspace, (uintptr_t)workspace_bytes, true);
+        std::sort(r.begin(), r.end(), [](const Range &a, const Range &b) { return a.at < b.at; });
+    } catch (const std::exception &) {
         return Q2D_EUNSUPPORTED;
     }
-    std::sort(r.begin(), r.end(), [](const Range &a, const Range &b) { return a.at < b.at; });
     // the furthest ends so far, of outputs and of all: inputs may share memory with one another
     uintptr_t end_out = 0, end_all = 0;
     for (const Range &x : r) {
@@ -306,18 +312,19 @@ q2d_status q2d_clip_grads(int32_t n, const void *const *data, void *const *out, 
 {
     const Set g = {n, data, out, counts, dtypes};
     q2d_status s = check_set(g);
-    if (s == Q2D_OK) s = check_apart(g);
     if (s != Q2D_OK) return s;
     if (!(max_norm >= 0.0) || !std::isfinite(max_norm)) return Q2D_EINVAL;
     // either a norm to go by, or a place for the norm
     const float *one = given ? given : norm;
     if (!one || (given && norm) || !aligned(one, 4)) return Q2D_EINVAL;
+    if (!given && (!workspace || !aligned(workspace, 8) || workspace_bytes < q2d_grad_workspace(n))) return Q2D_EINVAL;
+    s = check_apart(g, given, norm, given ? nullptr : workspace, q2d_grad_workspace(n));
+    if (s != Q2D_OK) return s;
     double *parts = nullptr;
     int k = 0;
     const int64_t all = elements(g);
     const bool kept = kept_between(g);
     if (!given) {
-        if (!workspace || !aligned(workspace, 8) || workspace_bytes < q2d_grad_workspace(n)) return Q2D_EINVAL;
         parts = reinterpret_cast<double *>(workspace);
         k = square_sums(g, all, !kept, parts, stream);
         if (k < 0) return Q2D_ELAUNCH;

@@ -10,6 +10,7 @@ namespace {
 using namespace q2d;
 
 constexpr int64_t kMaxIndex = int64_t(1) << 47;
+constexpr int64_t kMaxRows = INT32_MAX, kMaxCols = int64_t(1) << 27;
 
 // A tensor's rows in memory, in bytes
 struct Rows {
@@ -76,7 +77,7 @@ extern "C" {
 q2d_status q2d_rmsnorm_fwd(const q2d_rmsnorm *n, q2d_tensor *q4, q2d_tensor *q8, hipStream_t stream)
 {
     if (!n || n->rows < 0 || n->cols <= 0) return Q2D_EINVAL;
-    if (n->rows > kMaxDim || n->cols > kMaxDim) return Q2D_EUNSUPPORTED;
+    if (n->rows > kMaxRows || n->cols > kMaxCols) return Q2D_EUNSUPPORTED;
     // (eps within float32's normal numbers: 1 / sqrt(eps) stays below 2^63)
     if (!(n->eps >= 0x1p-126) || !std::isfinite(n->eps)) return Q2D_EINVAL;
     if (!valid_dtype((q2d_dtype)n->weight_dtype) || !n->weight || !aligned(n->weight, dtype_bytes((q2d_dtype)n->weight_dtype))) return Q2D_EINVAL;
@@ -143,14 +144,14 @@ q2d_status q2d_rmsnorm_fwd(const q2d_rmsnorm *n, q2d_tensor *q4, q2d_tensor *q8,
 
 int64_t q2d_rmsnorm_workspace(int64_t rows, int64_t cols)
 {
-    if (rows < 0 || cols <= 0 || rows > kMaxDim || cols > kMaxDim) return -1;
+    if (rows < 0 || cols <= 0 || rows > kMaxRows || cols > kMaxCols) return -1;
     return rmsnorm_grad_workspace(rows, cols);
 }
 
 q2d_status q2d_rmsnorm_bwd(const q2d_rmsnorm_grad *n, void *workspace, int64_t workspace_bytes, hipStream_t stream)
 {
     if (!n || n->rows < 0 || n->cols <= 0) return Q2D_EINVAL;
-    if (n->rows > kMaxDim || n->cols > kMaxDim) return Q2D_EUNSUPPORTED;
+    if (n->rows > kMaxRows || n->cols > kMaxCols) return Q2D_EUNSUPPORTED;
     if (!valid_dtype((q2d_dtype)n->weight_dtype) || !n->weight || !aligned(n->weight, dtype_bytes((q2d_dtype)n->weight_dtype))) return Q2D_EINVAL;
     if ((n->rows && !n->rstd) || !aligned(n->rstd, 4) || !aligned(n->dw, 4)) return Q2D_EINVAL;
     Rows h, dy, dh, dx;

@@ -207,7 +207,11 @@ int64_t waves_of(int64_t cols) { return cols <= 1024 ? 4 : cols <= 8192 ? (cols 
 // workgroups, each with one part of dw
 int64_t parts_of(int64_t rows, int64_t cols)
 {
-    if (cols > kLong) return rows < 256 ? rows : 256;
+    if (cols > kLong) {
+        // (the parts' memory stays at 128 MB where rows are very long)
+        const int64_t fit = (int64_t(1) << 25) / cols, most = fit < 8 ? 8 : fit > 256 ? 256 : fit;
+        return rows < most ? rows : most;
+    }
     // as many as are there at once (registers: 16 waves a CU, 8 of those with several rows), each
     // with equally many turns
     const int64_t most = 256 * (cols <= 1024 ? 2 : waves_of(cols) < 16 ? 16 / waves_of(cols) : 1);

@@ -89,7 +89,7 @@ def test_rms_norm_refusals(q2d):
 
 @pytest.mark.parametrize("options", [dict(), dict(activations="1d"), dict(block=64), dict(out_dtype=F32), dict(dtype=BF16)], ids=str)
 @pytest.mark.parametrize("residual", [True, False])
-def test_norm_linear(q2d, options, residual):
+def test_norm_linear(q2d, options, residual, monkeypatch):
     """The layer is its operators, one after the other."""
     from paper_2607_24953_amd.autograd import Q2DNormLinear
     layer = Q2DNormLinear(160, 96, device=DEV, seed=11, **options)
@@ -112,9 +112,14 @@ def test_norm_linear(q2d, options, residual):
     assert torch.equal(flat(X.grad), dx) and torch.equal(layer.weight.grad, dW.to(layer.weight.dtype))
     assert torch.equal(layer.norm_weight.grad, dw.to(nw.dtype)) and (not residual or torch.equal(flat(R.grad), dx.to(BF16)))
     # evaluation writes the rowwise copies alone, with the same result
+    from paper_2607_24953_amd import autograd
+    seen = []
+    monkeypatch.setattr(autograd, "q2d_rmsnorm_quantize",
+                        lambda *a, **kw: seen.append(kw["orientations"]) or q2d.q2d_rmsnorm_quantize(*a, **kw))
+    layer(X, R)
     with torch.no_grad():
         again = layer(X, R)
-    assert torch.equal(again[0] if residual else again, Y)
+    assert torch.equal(again[0] if residual else again, Y) and seen == [(True, True), (True, False)]
 
 
 def test_norm_linear_second_backward(q2d):

@@ -218,6 +218,33 @@ def test_operands_not_finite(q2d, formats, rows):
             assert_same_bytes(gpu_buffers(q), want)
 
 
+def test_values_beside_operands(q2d):
+    """The C entry point writes values and operands in one call."""
+    import ctypes
+    from paper_2607_24953_amd import norms as N
+    X, R, W = make((70, 300), BF16, 27), make((70, 300), BF16, 28), weight(300, F32)
+    want, h, rstd = q2d.q2d_rmsnorm_quantize(X, W, EPS, residual=R, formats=(0, 1))
+    y = q2d.q2d_rmsnorm_fwd(X, W, EPS, residual=R, y_dtype=F32)[0]
+    qs, y2, h2, rstd2 = [q2d.QTensor(f, 70, 300, DEV) for f in (0, 1)], torch.zeros_like(y), torch.zeros_like(h), torch.zeros_like(rstd)
+    n = N._Norm(x_dtype=1, residual_dtype=1, weight_dtype=0, y_dtype=0, rows=70, cols=300, eps=EPS, x=X.data_ptr(), ldx=300,
+                residual=R.data_ptr(), ld_residual=300, weight=W.data_ptr(), h=h2.data_ptr(), ldh=300, y=y2.data_ptr(), ldy=300,
+                rstd=rstd2.data_ptr())
+    assert q2d._lib.q2d_rmsnorm_fwd(ctypes.byref(n), qs[0].ptr(), qs[1].ptr(), torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(y, y2) and torch.equal(h, h2) and torch.equal(rstd, rstd2)
+    for a, b in zip(want, qs):
+        assert_same_bytes(gpu_buffers(b), gpu_buffers(a))
+
+
+def test_subnormal_bfloat16(q2d):
+    """bfloat16 sums, outputs and gradients below the normal numbers keep their digits."""
+    X = torch.full((3, 64), 2.0 ** -130, dtype=BF16, device=DEV)
+    R = torch.full((3, 64), 2.0 ** -131, dtype=BF16, device=DEV)
+    y, h, rstd = q2d.q2d_rmsnorm_fwd(X, torch.ones(64, device=DEV), 1.0, residual=R)
+    assert bool((h.cpu().double() == 1.5 * 2.0 ** -130).all()) and bool((y.cpu().double() == 1.5 * 2.0 ** -130).all())
+    dx, _ = q2d.q2d_rmsnorm_bwd(y, h, torch.ones(64, device=DEV), rstd, dh=h)
+    assert bool((dx.cpu().double() == 3 * 2.0 ** -130).all())
+
+
 def test_operands_in_place(q2d):
     for rows in (2, 40, 300):
         X, R, W = make((rows, 640), BF16, 27), make((rows, 640), BF16, 28), weight(640, F32)

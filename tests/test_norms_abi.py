@@ -41,7 +41,7 @@ def fwd(q2d, n, q4=None, q8=None):
 
 @pytest.mark.parametrize("bad,status", [
     (dict(x_dtype=2), 1), (dict(residual_dtype=-1), 1), (dict(weight_dtype=7), 1), (dict(y_dtype=2), 1), (dict(rows=-1), 1),
-    (dict(cols=0), 1), (dict(cols=-5), 1), (dict(rows=2 ** 31 + 1), 2), (dict(cols=2 ** 31 + 1), 2), (dict(eps=0.0), 1),
+    (dict(cols=0), 1), (dict(cols=-5), 1), (dict(rows=2 ** 31 + 1), 2), (dict(rows=2 ** 31), 2), (dict(cols=2 ** 27 + 1, ldx=2 ** 28), 2), (dict(eps=0.0), 1),
     (dict(eps=-1e-5), 1), (dict(eps=float("nan")), 1), (dict(eps=float("inf")), 1), (dict(eps=1e-39), 1), (dict(x=None), 1),
     (dict(weight=None), 1), (dict(rstd=None), 1), (dict(rstd=FAKE + 5 * MB + 2), 1), (dict(h=None), 1), (dict(residual=None), 1),
     (dict(y=None), 1), (dict(ldx=63), 1), (dict(ldh=0), 1), (dict(ldy=-64), 1), (dict(ld_residual=32), 1), (dict(x=FAKE + 1), 1),
@@ -87,7 +87,7 @@ def grad(q2d, **kw):
 
 @pytest.mark.parametrize("bad,status", [
     (dict(h_dtype=2), 1), (dict(dy_dtype=2), 1), (dict(weight_dtype=2), 1), (dict(rows=-1), 1), (dict(cols=0), 1),
-    (dict(rows=2 ** 31 + 1), 2), (dict(h=None), 1), (dict(dy=None), 1), (dict(dx=None), 1), (dict(weight=None), 1),
+    (dict(rows=2 ** 31), 2), (dict(cols=2 ** 27 + 1), 2), (dict(h=None), 1), (dict(dy=None), 1), (dict(dx=None), 1), (dict(weight=None), 1),
     (dict(rstd=None), 1), (dict(ldh=1), 1), (dict(lddx=63), 1), (dict(dw=FAKE + 6 * MB + 2), 1), (dict(lddy=2 ** 60), 2),
     (dict(dx=FAKE), 1), (dict(dx=FAKE + MB, dy_dtype=0), 1), (dict(dx=FAKE + MB + 2), 1), (dict(dx=FAKE + 2 * MB, lddx=65), 1),
     (dict(dx=FAKE + 4 * MB), 1), (dict(dw=FAKE), 1), (dict(dw=FAKE + 3 * MB), 1), (dict(dw=FAKE + 5 * MB), 1),
@@ -123,7 +123,9 @@ def test_clip_refusals(q2d):
     for kw in (dict(dtypes=[0, 2]), dict(counts=[64, -1]), dict(max_norm=-1.0), dict(max_norm=float("nan")),
                dict(max_norm=float("inf")), dict(norm=None), dict(given=d, norm=c), dict(given=d + 1, norm=None), dict(ws=None),
                dict(ws=FAKE + 33 * MB + 4), dict(size=8), dict(out=[c, None]), dict(out=[c, c]), dict(out=[c, c + 128]),
-               dict(out=[b, a]), dict(out=[a + 4, b]), dict(out=[c, d + 2]), dict(norm=FAKE + 32 * MB + 2)):
+               dict(out=[b, a]), dict(out=[a + 4, b]), dict(out=[c, d + 2]), dict(norm=FAKE + 32 * MB + 2),
+               dict(norm=a), dict(norm=b + 252), dict(ws=a), dict(ws=b - 64), dict(out=[c, d], norm=a + 8), dict(given=b + 4, norm=None),
+               dict(norm=FAKE + 33 * MB + 8)):
         assert clip(q2d, [a, b], **kw) == 1, kw
     assert clip(q2d, [a, None]) == 1 and clip(q2d, [a, a]) == 1 and clip(q2d, [a, a + 64]) == 1 and clip(q2d, [a, b + 1]) == 1
     assert clip(q2d, [a], counts=[2 ** 40 + 1]) == 2
