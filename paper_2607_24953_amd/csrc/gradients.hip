@@ -266,14 +266,15 @@ int turns_of(int64_t all)
 int square_sums(const Set &g, int64_t all, bool once, double *parts, hipStream_t stream)
 {
     const int turns = turns_of(all);
+    int64_t pieces = 0;
+    for (int32_t i = 0; i < g.n; ++i) pieces += cdiv(g.counts[i], turns * (int64_t)kTurn);
     int n = 0;
     Squared t;
     for (int32_t i = 0; i < g.n;) {
         i = fill(g, i, turns, t);
         if (t.n == 0) break;
-        // a launch's share of the parts, by its pieces
-        const int64_t share = (int64_t)((double)kMaxParts * t.pieces * turns * kTurn / (double)(all + t.n * (int64_t)turns * kTurn));
-        const int groups = (int)std::min<int64_t>(t.pieces, std::max<int64_t>(1, std::min<int64_t>(share, kMaxParts)));
+        // a launch's share of kMaxParts, by its pieces: all shares, each rounded down, stay within it
+        const int groups = (int)std::min<int64_t>(t.pieces, std::max<int64_t>(1, kMaxParts * (int64_t)t.pieces / pieces));
         if (once) hipLaunchKernelGGL(grad_square_kernel<true>, dim3(groups), dim3(256), 0, stream, t, parts + n);
         else hipLaunchKernelGGL(grad_square_kernel<false>, dim3(groups), dim3(256), 0, stream, t, parts + n);
         if (hipGetLastError() != hipSuccess) return -1;

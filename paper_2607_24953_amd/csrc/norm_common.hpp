@@ -8,17 +8,6 @@ namespace q2d {
 typedef __bf16 bf16v2 __attribute__((ext_vector_type(2)));
 typedef float f32v2 __attribute__((ext_vector_type(2)));
 
-// element i of a float32 or bfloat16 array
-__device__ __forceinline__ float load_value(const void *p, int bf16, int64_t i)
-{
-    return bf16 ? bf16_to_f(reinterpret_cast<const uint16_t *>(p)[i]) : reinterpret_cast<const float *>(p)[i];
-}
-__device__ __forceinline__ void store_value(void *p, int bf16, int64_t i, float v)
-{
-    if (bf16) reinterpret_cast<uint16_t *>(p)[i] = f_to_bf16_rne(v);
-    else reinterpret_cast<float *>(p)[i] = v;
-}
-
 // two float32 values as one word of bfloat16, rounded to nearest even
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
