@@ -604,7 +604,8 @@ q2d_status q2d_grad_norm(int32_t n, const void *const *data, const int64_t *coun
  * given   device: the norm to go by (of tensors on several GPUs, say), or NULL: the norm of
  *         these tensors is computed first and written to *norm.  One of given and norm is NULL.
  * An output may be its own input (in place) and shares no memory with anything else of the call,
- * the norm and the workspace among it (Q2D_EINVAL); the same tensor twice is refused by that.  With given, workspace may be NULL.
+ * the norm and the workspace among it (Q2D_EINVAL); the same tensor twice is refused by that.
+ * (That check holds 48 bytes of host memory a tensor while it runs; Q2D_EUNSUPPORTED without.)  With given, workspace may be NULL.
  */
 q2d_status q2d_clip_grads(int32_t n, const void *const *data, void *const *out, const int64_t *counts, const int32_t *dtypes,
                           double max_norm, const float *given, float *norm, void *workspace, int64_t workspace_bytes,

@@ -127,11 +127,15 @@ def _norm_backward(ctx, dy, dh, h, weight, rstd):
     cols = h.shape[1]
     dh = None if dh is None else _rows(dh.to(h.dtype), cols)
     if dy is None:
-        dx, dw = dh, None
+        # (a copy: dh may be another tensor's gradient too)
+        dx, dw = None if dh is None else dh.clone(memory_format=torch.contiguous_format), None
     else:
         dx, dw = q2d_rmsnorm_bwd(dy, h, weight, rstd, dh=dh, need_dw=need_w)
-    return (None if dx is None or not need_x else dx.reshape(ctx.x_shape),
-            None if dx is None or not need_r else dx.reshape(ctx.x_shape).to(ctx.r_dtype),
+    if dx is not None:
+        # (one object for both where the types agree: as two views of it, either could become its
+        # tensor's .grad and share memory with the other's)
+        dx = dx.reshape(ctx.x_shape)
+    return (dx if need_x else None, dx.to(ctx.r_dtype) if need_r and dx is not None else None,
             None if dw is None else dw.to(weight.dtype))
 
 

@@ -74,6 +74,23 @@ def test_rms_norm_gradients_that_are_missing(q2d):
         y.sum().backward()
 
 
+def test_gradients_share_no_memory(q2d):
+    """Gradients of x, the residual and other tensors can be changed in place, one by one."""
+    from paper_2607_24953_amd.autograd import rms_norm
+    W = torch.ones(64, device=DEV)
+    for use in ("y", "h", "both"):
+        X, R, Z = (rand(6, 64, seed=i).requires_grad_() for i in (1, 3, 5))
+        y, h = rms_norm(X, W, residual=R, y_dtype=F32)
+        k = rand(6, 64, seed=9)
+        (((h + Z) * k).sum() if use == "h" else (y * k).sum() if use == "y" else ((h + Z) * k).sum() + y.sum()).backward()
+        grads = [t.grad for t in (X, R, Z) if t.grad is not None]
+        keep = [g.clone() for g in grads]
+        assert len({g.untyped_storage().data_ptr() for g in grads}) == len(grads)
+        for i, g in enumerate(grads):
+            g.mul_(2)
+            assert all(torch.equal(a, b * (2 if j <= i else 1)) for j, (a, b) in enumerate(zip(grads, keep)))
+
+
 def test_rms_norm_refusals(q2d):
     from paper_2607_24953_amd.autograd import rms_norm
     W = torch.ones(64, device=DEV)
