@@ -115,13 +115,14 @@ __device__ __forceinline__ void load_eight(float (&v)[8], const void *base, int 
         for (int j = 0; j < 8; ++j) v[j] = e.at(j);
     }
 }
+template <bool ONCE = false>
 __device__ __forceinline__ void store_eight(const float (&v)[8], void *base, int bf16, int64_t i, int64_t n)
 {
     uint8_t *p = reinterpret_cast<uint8_t *>(base);
     if (bf16) {
         Eight<true> e;
         e.set(v);
-        e.store(p + 2 * i, n);
+        e.template store<ONCE>(p + 2 * i, n);
     } else {
         Eight<false> e;
         e.set(v);

@@ -31,8 +31,14 @@ __device__ __forceinline__ uint32_t column_max(uint32_t m)
     return max((uint32_t)b[0], (uint32_t)b[1]);
 }
 
-// four words of a staged line (their pitch is odd: no 16-byte read)
-__device__ __forceinline__ uint4 words16(const uint32_t *p) { return make_uint4(p[0], p[1], p[2], p[3]); }
+// 16 bytes of codes from four words of a staged line (their pitch is odd: no 16-byte read)
+template <bool ONCE>
+__device__ __forceinline__ void store_codes(uint8_t *p, const uint32_t *words)
+{
+    const u4v v = {words[0], words[1], words[2], words[3]};
+    if constexpr (ONCE) __builtin_nontemporal_store(v, reinterpret_cast<u4v *>(p));
+    else *reinterpret_cast<u4v *>(p) = v;
+}
 
 __device__ __forceinline__ uint32_t fp4_word(const uint32_t (&v)[8], float scale)
 {
@@ -72,7 +78,7 @@ __device__ __forceinline__ void norm_sub_block(uint32_t (&y)[8][8], const Eight<
 
 // A workgroup's part of an operand: WR x WC strips, one a wave, from y of each lane's sub-block (0
 // outside the matrix) at (r0, c0); tr and tc count tiles of this size.
-template <int FP4, bool MX, int WR, int WC>
+template <int FP4, bool MX, int WR, int WC, bool ONCE>
 __device__ __forceinline__ void store_operands(const NormQuantArgs &a, const uint32_t (&y)[8][8], const int64_t tr, const int64_t tc)
 {
     constexpr int kRows = 32 * WR, kCols = 128 * WC, kThreads = 64 * WR * WC;
@@ -168,12 +174,12 @@ __device__ __forceinline__ void store_operands(const NormQuantArgs &a, const uin
                 const int line = item / (4 * WC), part = item % (4 * WC);
                 const int64_t r = tr * kRows + line;
                 if (r < a.rows && tc * kCols + part * 32 < a.cols_pad)
-                    *reinterpret_cast<uint4 *>(q.codes + r * q.ld_codes + tc * (kCols / 2) + part * 16) = words16(&st4_r[line][4 * part]);
+                    store_codes<false>(q.codes + r * q.ld_codes + tc * (kCols / 2) + part * 16, &st4_r[line][4 * part]);
             }
             if (q.codes_t) {
                 const int line = item / WR, part = item % WR;
                 const int64_t c = tc * kCols + line;
-                if (c < a.cols) *reinterpret_cast<uint4 *>(q.codes_t + c * q.ld_codes_t + tr * (kRows / 2) + part * 16) = words16(&st4_c[line][4 * part]);
+                if (c < a.cols) store_codes<ONCE>(q.codes_t + c * q.ld_codes_t + tr * (kRows / 2) + part * 16, &st4_c[line][4 * part]);
             }
         }
     }
@@ -194,7 +200,7 @@ __device__ __forceinline__ void store_operands(const NormQuantArgs &a, const uin
                 const int item = threadIdx.x + kThreads * p;
                 const int line = item / (2 * WR), part = item % (2 * WR);
                 const int64_t c = tc * kCols + line;
-                if (c < a.cols) *reinterpret_cast<uint4 *>(q.codes_t + c * q.ld_codes_t + tr * kRows + part * 16) = words16(&st8_c[line][4 * part]);
+                if (c < a.cols) store_codes<ONCE>(q.codes_t + c * q.ld_codes_t + tr * kRows + part * 16, &st8_c[line][4 * part]);
             }
         }
     }
@@ -239,20 +245,20 @@ __device__ __forceinline__ void store_operands(const NormQuantArgs &a, const uin
 // Both formats by one workgroup, or, in strips, by one each (gridDim.y 2): a lone wave takes 4
 // cycles an instruction, and the conversions are most of its time (64 x 4096 in FP4 and
 // MXFP8 with the rows kernel 9.9 us, so 9.4)
-template <int FP4, bool MX, int WR, int WC>
+template <int FP4, bool MX, int WR, int WC, bool ONCE>
 __device__ __forceinline__ void store_formats(const NormQuantArgs &a, const uint32_t (&y)[8][8], const int64_t tr, const int64_t tc)
 {
     if constexpr (FP4 != 0 && MX && WR == 1) {
-        if (blockIdx.y == 0) store_operands<FP4, false, WR, WC>(a, y, tr, tc);
-        else store_operands<0, true, WR, WC>(a, y, tr, tc);
+        if (blockIdx.y == 0) store_operands<FP4, false, WR, WC, ONCE>(a, y, tr, tc);
+        else store_operands<0, true, WR, WC, ONCE>(a, y, tr, tc);
     } else {
-        store_operands<FP4, MX, WR, WC>(a, y, tr, tc);
+        store_operands<FP4, MX, WR, WC, ONCE>(a, y, tr, tc);
     }
 }
 
 // From h and its rows' statistics.  HB: h is bfloat16.  ALIGNED: its rows are on 16-byte boundaries.
-// FP4: 0 none, 1 2D blocks, 2 1D blocks.
-template <bool HB, bool ALIGNED, int FP4, bool MX, int WR, int WC>
+// FP4: 0 none, 1 2D blocks, 2 1D blocks.  ONCE: the transposed codes go past the cache.
+template <bool HB, bool ALIGNED, int FP4, bool MX, int WR, int WC, bool ONCE>
 __global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(WR == 4 ? 4 : 1))) void rmsnorm_quantize_kernel(const NormQuantArgs a)
 {
     static_assert((WR == 4 && WC == 2) || (WR == 1 && WC == 1), "a tile, or a strip of its own");
@@ -285,7 +291,7 @@ __global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(WR
         load_eight(rstd, a.rstd, 0, r0, a.rows - r0);
         norm_sub_block(y, h, w, rstd, a.rows - r0, cols);
     }
-    store_formats<FP4, MX, WR, WC>(a, y, tr, tc);
+    store_formats<FP4, MX, WR, WC, ONCE>(a, y, tr, tc);
 }
 
 // f(FP4, MX) for the formats of a call
@@ -301,12 +307,12 @@ void for_formats(const NormQuantArgs &a, F f)
     }
 }
 
-template <bool HB, bool ALIGNED, int WR, int WC>
+template <bool HB, bool ALIGNED, int WR, int WC, bool ONCE>
 void launch_w(const NormQuantArgs &a, hipStream_t s)
 {
     const int64_t blocks = (a.rows_pad / (32 * WR)) * ((a.cols_pad + 128 * WC - 1) / (128 * WC));
     for_formats(a, [&](auto fp4, auto mx) {
-        hipLaunchKernelGGL((rmsnorm_quantize_kernel<HB, ALIGNED, decltype(fp4)::value, decltype(mx)::value, WR, WC>),
+        hipLaunchKernelGGL((rmsnorm_quantize_kernel<HB, ALIGNED, decltype(fp4)::value, decltype(mx)::value, WR, WC, ONCE>),
                            dim3((unsigned)blocks, WR == 1 && a.fp4 && a.mx ? 2 : 1), dim3(64 * WR * WC), 0, s, a);
     });
 }
@@ -316,8 +322,15 @@ template <bool HB, bool ALIGNED>
 void launch_v(const NormQuantArgs &a, hipStream_t s)
 {
     const bool strips = a.block == 32 && (a.rows_pad / 128) * ((a.cols_pad + 255) / 256) <= 128;
-    if (strips) launch_w<HB, ALIGNED, 1, 1>(a, s);
-    else launch_w<HB, ALIGNED, 4, 2>(a, s);
+    // Transposed codes of 48 MB or more go past the cache: the backward pass reads them, long after,
+    // and the rowwise ones stay for the GEMM that comes next.  16384 x 4096 bfloat16 in FP4 and MXFP8
+    // with the rows kernel 131 -> 123 us, with two GEMMs behind it 230 -> 219; 32768 x 4096 in FP4 and
+    // a GEMM 263 -> 257; half of that, 33 MB, 132.8 -> 133.2.  (A call that reads the transposed copies
+    // at once pays for it: with q2d_dequantize of all four 250 -> 270.)
+    const int64_t bytes = a.rows * a.cols * ((a.fp4 && a.q4.codes_t ? 1 : 0) + (a.mx && a.q8.codes_t ? 2 : 0)) / 2;
+    if (strips) launch_w<HB, ALIGNED, 1, 1, false>(a, s);
+    else if (bytes >= int64_t(48) << 20) launch_w<HB, ALIGNED, 4, 2, true>(a, s);
+    else launch_w<HB, ALIGNED, 4, 2, false>(a, s);
 }
 
 }  // namespace
