@@ -174,7 +174,7 @@ __global__ __launch_bounds__(64 * WR * WC) void dequantize_kernel(const DequantA
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] *= scale[kScales == 1 ? 0 : TRANS ? j : i];
-        store_eight<ONCE && BF16>(v, a.out, BF16, r * a.ldo + c0, a.cols - c0);
+        store_run<ONCE && BF16>(v, a.out, BF16, r * a.ldo + c0, a.cols - c0);
         if (a.exps) {
             int8_t *x = a.exps + r * a.lde + c0;
 #pragma unroll

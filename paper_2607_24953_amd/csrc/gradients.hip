@@ -50,26 +50,43 @@ __device__ __forceinline__ Piece piece_of(const T &t, int piece)
     return {i, (bool)((t.bf16[i >> 5] >> (i & 31)) & 1), (int64_t)(piece - t.first[i]) * size, last ? t.last[i] : size};
 }
 
-// turns whose loads a lane has in flight
-constexpr int kFlight = 4;
+// 16 bytes of a tensor.  (With eight float32 a lane each of its two loads took every other 16 bytes
+// of its lines: 150M float32 clipped 337 us, so 306)
+template <bool BF16>
+struct Unit : Run<BF16, BF16 ? 8 : 4> {
+    static constexpr int kN = BF16 ? 8 : 4, kBytes = 16 / kN;
+    __device__ __forceinline__ void scale(float f)
+    {
+        float v[kN];
+#pragma unroll
+        for (int j = 0; j < kN; ++j) v[j] = this->at(j) * f;
+        this->set(v);
+    }
+};
 
+// bytes that a lane has in flight
+constexpr int kFlight = 64;
+
+// (ONCE: no second pass follows)
 template <bool BF16, bool ONCE>
 __device__ __forceinline__ double square_piece(const void *data, int64_t at, int length)
 {
-    const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * (BF16 ? 2 : 4);
+    typedef Unit<BF16> U;
+    constexpr int kUnits = kFlight / 8 / U::kBytes, kStep = 256 * U::kN;
+    const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * U::kBytes;
     double s = 0.0;
 #pragma unroll 1
-    for (int c0 = 8 * threadIdx.x; c0 < length; c0 += kFlight * kTurn) {
-        Eight<BF16> e[kFlight];
+    for (int c0 = U::kN * threadIdx.x; c0 < length; c0 += kUnits * kStep) {
+        U e[kUnits];
 #pragma unroll
-        for (int k = 0; k < kFlight; ++k) {
-            const int c = c0 + k * kTurn;
-            e[k].template load<ONCE>(p + c * (BF16 ? 2 : 4), length - c);
+        for (int k = 0; k < kUnits; ++k) {
+            const int c = c0 + k * kStep;
+            e[k].template load<ONCE>(p + c * U::kBytes, length - c);
         }
 #pragma unroll
-        for (int k = 0; k < kFlight; ++k)
+        for (int k = 0; k < kUnits; ++k)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < U::kN; ++j) {
                 const double v = e[k].at(j);
                 s = __builtin_fma(v, v, s);
             }
@@ -105,35 +122,33 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const double *parts, int
     if (threadIdx.x == 0) *norm = (float)s;
 }
 
-template <bool BF16, bool ONCE>
+template <bool BF16>
 __device__ __forceinline__ void scale_piece(const void *data, void *out, int64_t at, int length, bool clip, float f)
 {
-    const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * (BF16 ? 2 : 4);
-    uint8_t *o = reinterpret_cast<uint8_t *>(out) + at * (BF16 ? 2 : 4);
+    typedef Unit<BF16> U;
+    constexpr int kUnits = kFlight / 8 / U::kBytes, kStep = 256 * U::kN;
+    const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * U::kBytes;
+    uint8_t *o = reinterpret_cast<uint8_t *>(out) + at * U::kBytes;
 #pragma unroll 1
-    for (int c0 = 8 * threadIdx.x; c0 < length; c0 += kFlight * kTurn) {
-        Eight<BF16> e[kFlight];
+    for (int c0 = U::kN * threadIdx.x; c0 < length; c0 += kUnits * kStep) {
+        U e[kUnits];
 #pragma unroll
-        for (int k = 0; k < kFlight; ++k) {
-            const int c = c0 + k * kTurn;
-            e[k].template load<ONCE>(p + c * (BF16 ? 2 : 4), length - c);
+        for (int k = 0; k < kUnits; ++k) {
+            const int c = c0 + k * kStep;
+            e[k].template load<true>(p + c * U::kBytes, length - c);
         }
 #pragma unroll
-        for (int k = 0; k < kFlight; ++k) {
-            const int c = c0 + k * kTurn;
-            if (clip) {
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = e[k].at(j) * f;
-                e[k].set(v);
-            }
-            e[k].template store<ONCE>(o + c * (BF16 ? 2 : 4), length - c);
+        for (int k = 0; k < kUnits; ++k) {
+            const int c = c0 + k * kStep;
+            if (clip) e[k].scale(f);
+            e[k].template store<true>(o + c * U::kBytes, length - c);
         }
     }
 }
 
-// (the last pieces first: the square sums read them last, and some are still in the cache)
-template <bool ONCE>
+// The last pieces first, past the cache: the square sums read them last, and what the cache still
+// holds of them is not pushed out by what is written here (98M bfloat16 124 us, so 99; 400M
+// 845 -> 821)
 __global__ __launch_bounds__(256) void grad_scale_kernel(const Scaled t, const double *parts, int n, const float *given,
                                                          double max_norm, float *norm)
 {
@@ -146,8 +161,8 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(const Scaled t, const d
     for (int piece = t.pieces - 1 - (int)blockIdx.x; piece >= 0; piece -= gridDim.x) {
         const Piece p = piece_of(t, piece);
         if (!clip && t.out[p.tensor] == t.data[p.tensor]) continue;
-        if (p.bf16) scale_piece<true, ONCE>(t.data[p.tensor], t.out[p.tensor], p.at, p.length, clip, f);
-        else scale_piece<false, ONCE>(t.data[p.tensor], t.out[p.tensor], p.at, p.length, clip, f);
+        if (p.bf16) scale_piece<true>(t.data[p.tensor], t.out[p.tensor], p.at, p.length, clip, f);
+        else scale_piece<false>(t.data[p.tensor], t.out[p.tensor], p.at, p.length, clip, f);
     }
 }
 
@@ -244,15 +259,6 @@ int64_t elements(const Set &g)
     return all;
 }
 
-// Whether the cache keeps the tensors between the two passes
-constexpr int64_t kKept = int64_t(768) << 20;
-bool kept_between(const Set &g)
-{
-    int64_t bytes = 0;
-    for (int32_t i = 0; i < g.n; ++i) bytes += g.counts[i] * dtype_bytes((q2d_dtype)g.dtypes[i]);
-    return bytes <= kKept;
-}
-
 // Turns of a piece: a workgroup for each of 1024 pieces first, then longer ones.  (In one size of
 // 8 turns the 0.8 M float32 of a small model's gradients took 5.1 us for their squares.)
 int turns_of(int64_t all)
@@ -324,10 +330,9 @@ q2d_status q2d_clip_grads(int32_t n, const void *const *data, void *const *out, 
     double *parts = nullptr;
     int k = 0;
     const int64_t all = elements(g);
-    const bool kept = kept_between(g);
     if (!given) {
         parts = reinterpret_cast<double *>(workspace);
-        k = square_sums(g, all, !kept, parts, stream);
+        k = square_sums(g, all, false, parts, stream);
         if (k < 0) return Q2D_ELAUNCH;
         if (k == 0) {       // no elements: nothing to scale
             hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, stream, parts, 0, norm);
@@ -340,8 +345,7 @@ q2d_status q2d_clip_grads(int32_t n, const void *const *data, void *const *out, 
         i = fill(g, i, turns, t);
         if (t.n == 0) break;
         const dim3 groups(std::min(t.pieces, kMaxParts));
-        if (kept) hipLaunchKernelGGL(grad_scale_kernel<true>, groups, dim3(256), 0, stream, t, parts, k, given, max_norm, norm);
-        else hipLaunchKernelGGL(grad_scale_kernel<false>, groups, dim3(256), 0, stream, t, parts, k, given, max_norm, norm);
+        hipLaunchKernelGGL(grad_scale_kernel, groups, dim3(256), 0, stream, t, parts, k, given, max_norm, norm);
         if (hipGetLastError() != hipSuccess) return Q2D_ELAUNCH;
         norm = nullptr;     // (written by the first launch)
     }

@@ -15,27 +15,41 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 }
 __device__ __forceinline__ float round_bf16(float v) { return bits_f(pack_bf16(v, v) << 16); }
 
-// 16 bytes at any address of an element: the hardware takes a 16-byte access there too, in the same
-// instruction, so rows need no alignment
-typedef u4v u4v_any __attribute__((aligned(2)));
-// (ONCE: of data that is not read or written again soon)
-template <bool ONCE = false>
-__device__ __forceinline__ u4v load16(const uint8_t *p)
+// 8 or 16 bytes (2 or 4 words) at any address of an element: the hardware takes wide accesses there
+// too, in the same instructions, so rows need no alignment.  ONCE: of data that is not read or written
+// again soon.
+typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+template <int WORDS> struct Wide;
+template <> struct Wide<2> { typedef u2v type; };
+template <> struct Wide<4> { typedef u4v type; };
+template <int WORDS, bool ONCE>
+__device__ __forceinline__ void load_wide(uint32_t *w, const uint8_t *p)
 {
-    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u4v_any *>(p));
-    else return *reinterpret_cast<const u4v_any *>(p);
+    typedef typename Wide<WORDS>::type V;
+    typedef V any __attribute__((aligned(2)));
+    V v;
+    if constexpr (ONCE) v = __builtin_nontemporal_load(reinterpret_cast<const any *>(p));
+    else v = *reinterpret_cast<const any *>(p);
+#pragma unroll
+    for (int k = 0; k < WORDS; ++k) w[k] = v[k];
 }
-template <bool ONCE = false>
-__device__ __forceinline__ void store16(uint8_t *p, u4v v)
+template <int WORDS, bool ONCE>
+__device__ __forceinline__ void store_wide(uint8_t *p, const uint32_t *w)
 {
-    if constexpr (ONCE) __builtin_nontemporal_store(v, reinterpret_cast<u4v_any *>(p));
-    else *reinterpret_cast<u4v_any *>(p) = v;
+    typedef typename Wide<WORDS>::type V;
+    typedef V any __attribute__((aligned(2)));
+    V v;
+#pragma unroll
+    for (int k = 0; k < WORDS; ++k) v[k] = w[k];
+    if constexpr (ONCE) __builtin_nontemporal_store(v, reinterpret_cast<any *>(p));
+    else *reinterpret_cast<any *>(p) = v;
 }
 
-// Eight neighbouring elements, the unit of every vector access here, as they lie in memory: NW words of bf16 pairs (4) or float32 (8)
-template <bool BF16>
-struct Eight {
-    static constexpr int NW = BF16 ? 4 : 8;
+// N (4 or 8) neighbouring elements, the unit of every vector access here, as they lie in memory: NW
+// words of bf16 pairs or float32
+template <bool BF16, int N>
+struct Run {
+    static constexpr int NW = BF16 ? N / 2 : N, kWide = NW < 4 ? 2 : 4;
     uint32_t w[NW];
 
     __device__ __forceinline__ float at(int j) const
@@ -54,22 +68,19 @@ struct Eight {
 #pragma unroll
         for (int k = 0; k < NW; ++k) asm volatile("" : "+v"(w[k]));
     }
-    // the first n of eight elements from p (n >= 8: all, n <= 0: none), the others 0
+    // the first n of N elements from p (n >= N: all, n <= 0: none), the others 0
     template <bool ONCE = false>
     __device__ __forceinline__ void load(const uint8_t *p, int64_t n)
     {
         // (zeros first: written beside the load, they would have to wait for it)
         zero();
-        if (n >= 8) {
+        if (n >= N) {
 #pragma unroll
-            for (int k = 0; k < NW / 4; ++k) {
-                const u4v v = load16<ONCE>(p + 16 * k);
-                w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
-            }
+            for (int k = 0; k < NW; k += kWide) load_wide<kWide, ONCE>(w + k, p + 4 * k);
         } else if (n > 0) {
             // (lanes behind the last element do not take a wave through these)
 #pragma unroll
-            for (int j = 0; j < 7; ++j)
+            for (int j = 0; j < N - 1; ++j)
                 if (j < n) {
                     if constexpr (BF16) w[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[j] << (16 * (j & 1));
                     else w[j] = reinterpret_cast<const uint32_t *>(p)[j];
@@ -79,52 +90,53 @@ struct Eight {
     template <bool ONCE = false>
     __device__ __forceinline__ void store(uint8_t *p, int64_t n) const
     {
-        if (n >= 8) {
+        if (n >= N) {
 #pragma unroll
-            for (int k = 0; k < NW / 4; ++k) store16<ONCE>(p + 16 * k, u4v{w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]});
-            return;
+            for (int k = 0; k < NW; k += kWide) store_wide<kWide, ONCE>(p + 4 * k, w + k);
+        } else if (n > 0) {
+#pragma unroll
+            for (int j = 0; j < N - 1; ++j)
+                if (j < n) {
+                    if constexpr (BF16) reinterpret_cast<uint16_t *>(p)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+                    else reinterpret_cast<uint32_t *>(p)[j] = w[j];
+                }
         }
-        if (n <= 0) return;
-#pragma unroll
-        for (int j = 0; j < 7; ++j)
-            if (j < n) {
-                if constexpr (BF16) reinterpret_cast<uint16_t *>(p)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
-                else reinterpret_cast<uint32_t *>(p)[j] = w[j];
-            }
     }
-    __device__ __forceinline__ void set(const float (&v)[8])
+    __device__ __forceinline__ void set(const float (&v)[N])
     {
 #pragma unroll
-        for (int k = 0; k < NW; ++k) w[k] = BF16 ? pack_bf16(v[2 * k & 7], v[(2 * k + 1) & 7]) : f_bits(v[k & 7]);
+        for (int k = 0; k < NW; ++k) w[k] = BF16 ? pack_bf16(v[2 * k % N], v[(2 * k + 1) % N]) : f_bits(v[k % N]);
     }
 };
+template <bool BF16> using Eight = Run<BF16, 8>;
 
-// Eight elements of a type that is the same for all lanes, from element i of an array
-__device__ __forceinline__ void load_eight(float (&v)[8], const void *base, int bf16, int64_t i, int64_t n)
+// N elements of a type that is the same for all lanes, from element i of an array
+template <int N>
+__device__ __forceinline__ void load_run(float (&v)[N], const void *base, int bf16, int64_t i, int64_t n)
 {
     const uint8_t *p = reinterpret_cast<const uint8_t *>(base);
     if (bf16) {
-        Eight<true> e;
+        Run<true, N> e;
         e.load(p + 2 * i, n);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = e.at(j);
+        for (int j = 0; j < N; ++j) v[j] = e.at(j);
     } else {
-        Eight<false> e;
+        Run<false, N> e;
         e.load(p + 4 * i, n);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = e.at(j);
+        for (int j = 0; j < N; ++j) v[j] = e.at(j);
     }
 }
-template <bool ONCE = false>
-__device__ __forceinline__ void store_eight(const float (&v)[8], void *base, int bf16, int64_t i, int64_t n)
+template <bool ONCE = false, int N>
+__device__ __forceinline__ void store_run(const float (&v)[N], void *base, int bf16, int64_t i, int64_t n)
 {
     uint8_t *p = reinterpret_cast<uint8_t *>(base);
     if (bf16) {
-        Eight<true> e;
+        Run<true, N> e;
         e.set(v);
         e.template store<ONCE>(p + 2 * i, n);
     } else {
-        Eight<false> e;
+        Run<false, N> e;
         e.set(v);
         e.store(p + 4 * i, n);
     }

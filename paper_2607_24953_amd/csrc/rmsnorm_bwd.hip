@@ -19,21 +19,21 @@ namespace {
 template <bool HB, bool DB, int LANES, int CH, bool ONCE>
 __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const NormGradArgs a, float *part)
 {
-    constexpr int EH = HB ? 2 : 4, ED = DB ? 2 : 4;
+    constexpr int EH = HB ? 2 : 4, ED = DB ? 2 : 4, N = 16 / EH;
     constexpr int kPer = LANES ? 256 / (LANES ? LANES : 1) : 1;        // rows at a time
     __shared__ double lds[2][16];
     const int t = LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x, step = LANES ? LANES : blockDim.x;
     const int sub = LANES ? threadIdx.x / (LANES ? LANES : 1) : 0;
     // (two chunks of weights beside two of everything else do not fit 128 registers)
-    constexpr bool KEPT = LANES != 0 || CH == 1;
-    float w[CH][8];
-    double acc[CH][8];
+    constexpr bool KEPT = LANES != 0 || CH * N <= 8;
+    float w[CH][N];
+    double acc[CH][N];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-        const int64_t c = 8 * (t + k * (int64_t)step);
-        if constexpr (KEPT) load_eight(w[k], a.w, a.w_bf16, c, a.cols - c);
+        const int64_t c = N * (t + k * (int64_t)step);
+        if constexpr (KEPT) load_run(w[k], a.w, a.w_bf16, c, a.cols - c);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[k][j] = 0.0;
+        for (int j = 0; j < N; ++j) acc[k][j] = 0.0;
     }
     int turn = 0;
     for (int64_t first = blockIdx.x * (int64_t)kPer; first < a.rows; first += gridDim.x * (int64_t)kPer, turn ^= 1) {
@@ -45,23 +45,23 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
         const uint8_t *dyp = reinterpret_cast<const uint8_t *>(a.dy) + row * a.lddy * ED;
         const uint8_t *dhp = reinterpret_cast<const uint8_t *>(a.dh) + row * a.lddh * EH;
         uint8_t *dxp = reinterpret_cast<uint8_t *>(a.dx) + row * a.lddx * EH;
-        Eight<HB> h[CH], dh[CH];
-        Eight<DB> dy[CH];
+        Run<HB, N> h[CH], dh[CH];
+        Run<DB, N> dy[CH];
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int64_t c = 8 * (t + k * (int64_t)step);
-            h[k].template load<ONCE && HB>(hp + c * EH, cols - c);
-            dy[k].template load<ONCE && DB>(dyp + c * ED, cols - c);
-            if (a.dh) dh[k].template load<ONCE && HB>(dhp + c * EH, cols - c);
+            const int64_t c = N * (t + k * (int64_t)step);
+            h[k].template load<ONCE>(hp + c * EH, cols - c);
+            dy[k].template load<ONCE>(dyp + c * ED, cols - c);
+            if (a.dh) dh[k].template load<ONCE>(dhp + c * EH, cols - c);
             else dh[k].zero();
         }
         const float rstd = some ? a.rstd[row] : 0.f;
         double sum = 0.0;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            if constexpr (!KEPT) load_eight(w[k], a.w, a.w_bf16, 8 * (t + k * (int64_t)step), a.cols - 8 * (t + k * (int64_t)step));
+            if constexpr (!KEPT) load_run(w[k], a.w, a.w_bf16, N * (t + k * (int64_t)step), a.cols - N * (t + k * (int64_t)step));
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < N; ++j) {
                 const float n = h[k].at(j) * rstd, d = dy[k].at(j);
                 sum = __builtin_fma((double)(d * w[k][j]), (double)n, sum);
                 acc[k][j] = __builtin_fma((double)d, (double)n, acc[k][j]);
@@ -78,16 +78,16 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
         }
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int64_t c = 8 * (t + k * (int64_t)step);
+            const int64_t c = N * (t + k * (int64_t)step);
             if (c >= cols) break;
-            if constexpr (!KEPT) load_eight(w[k], a.w, a.w_bf16, c, a.cols - c);
-            float dx[8];
+            if constexpr (!KEPT) load_run(w[k], a.w, a.w_bf16, c, a.cols - c);
+            float dx[N];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < N; ++j) {
                 const float n = h[k].at(j) * rstd;
                 dx[j] = rstd * (dy[k].at(j) * w[k][j] - n * mean) + dh[k].at(j);
             }
-            Eight<HB> o;
+            Run<HB, N> o;
             o.set(dx);
             o.store(dxp + c * EH, cols - c);
         }
@@ -96,14 +96,14 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
     part += blockIdx.x * a.cols;
     if constexpr (LANES) {
         // the rows' lanes of a column, in order
-        __shared__ double sums[kPer][8 * (LANES ? LANES : 1) + 2];
+        __shared__ double sums[kPer][N * (LANES ? LANES : 1) + 2];
         for (int k = 0; k < CH; ++k) {
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sums[sub][8 * t + j] = acc[k][j];
+            for (int j = 0; j < N; ++j) sums[sub][N * t + j] = acc[k][j];
             __syncthreads();
-            for (int i = threadIdx.x; i < 8 * LANES; i += 256) {
-                const int64_t c = 8 * (int64_t)LANES * k + i;
+            for (int i = threadIdx.x; i < N * LANES; i += 256) {
+                const int64_t c = N * (int64_t)LANES * k + i;
                 double s = 0.0;
                 for (int p = 0; p < kPer; ++p) s += sums[p][i];
                 if (c < a.cols) part[c] = (float)s;
@@ -112,11 +112,11 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
     } else {
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int64_t c = 8 * (t + k * (int64_t)step);
-            Eight<false> o;
-            float v[8];
+            const int64_t c = N * (t + k * (int64_t)step);
+            Run<false, N> o;
+            float v[N];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (float)acc[k][j];
+            for (int j = 0; j < N; ++j) v[j] = (float)acc[k][j];
             o.set(v);
             o.store(reinterpret_cast<uint8_t *>(part + c), a.cols - c);
         }
@@ -133,9 +133,9 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_means_kernel(const NormGrad
     double s = 0.0;
     for (int64_t c = 8 * (int64_t)threadIdx.x; c < a.cols; c += 8 * 1024) {
         float d[8], w[8], h[8];
-        load_eight(d, a.dy, a.dy_bf16, row * a.lddy + c, a.cols - c);
-        load_eight(w, a.w, a.w_bf16, c, a.cols - c);
-        load_eight(h, a.h, a.h_bf16, row * a.ldh + c, a.cols - c);
+        load_run(d, a.dy, a.dy_bf16, row * a.lddy + c, a.cols - c);
+        load_run(w, a.w, a.w_bf16, c, a.cols - c);
+        load_run(h, a.h, a.h_bf16, row * a.ldh + c, a.cols - c);
 #pragma unroll
         for (int j = 0; j < 8; ++j) s = __builtin_fma((double)(d[j] * w[j]), (double)(h[j] * rstd), s);
     }
@@ -149,27 +149,27 @@ __global__ __launch_bounds__(256) void rmsnorm_grad_tile_kernel(const NormGradAr
     const int64_t c = 8 * (blockIdx.x * (int64_t)256 + threadIdx.x), n = a.cols - c;
     if (n <= 0) return;
     float w[8];
-    load_eight(w, a.w, a.w_bf16, c, n);
+    load_run(w, a.w, a.w_bf16, c, n);
     double acc[8] = {};
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const float rstd = a.rstd[row], mean = means[row];
         float h[8], d[8], dh[8] = {};
-        load_eight(h, a.h, a.h_bf16, row * a.ldh + c, n);
-        load_eight(d, a.dy, a.dy_bf16, row * a.lddy + c, n);
-        if (a.dh) load_eight(dh, a.dh, a.h_bf16, row * a.lddh + c, n);
+        load_run(h, a.h, a.h_bf16, row * a.ldh + c, n);
+        load_run(d, a.dy, a.dy_bf16, row * a.lddy + c, n);
+        if (a.dh) load_run(dh, a.dh, a.h_bf16, row * a.lddh + c, n);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float x = h[j] * rstd;
             acc[j] = __builtin_fma((double)d[j], (double)x, acc[j]);
             dh[j] += rstd * (d[j] * w[j] - x * mean);
         }
-        store_eight(dh, a.dx, a.h_bf16, row * a.lddx + c, n);
+        store_run(dh, a.dx, a.h_bf16, row * a.lddx + c, n);
     }
     if (!part) return;
     float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = (float)acc[j];
-    store_eight(v, part, 0, blockIdx.y * a.cols + c, n);
+    store_run(v, part, 0, blockIdx.y * a.cols + c, n);
 }
 
 // dw of 32 columns: 16 lanes a column take every 16th part
@@ -224,11 +224,12 @@ int64_t means_bytes(int64_t rows, int64_t cols) { return cols > kLong ? up256(ro
 template <bool HB, bool DB, bool ONCE>
 hipError_t launch_grad(const NormGradArgs &a, unsigned parts, float *part, hipStream_t s)
 {
+    constexpr int M = HB ? 1 : 2;           // chunks of 8 elements
     const dim3 grid(parts), block((unsigned)(64 * waves_of(a.cols)));
-    if (a.cols <= 256) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 16, 2, ONCE>), grid, block, 0, s, a, part);
-    else if (a.cols <= 1024) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 64, 2, ONCE>), grid, block, 0, s, a, part);
-    else if (a.cols <= 8192) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, 1, ONCE>), grid, block, 0, s, a, part);
-    else hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, 2, ONCE>), grid, block, 0, s, a, part);
+    if (a.cols <= 256) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 16, 2 * M, ONCE>), grid, block, 0, s, a, part);
+    else if (a.cols <= 1024) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 64, 2 * M, ONCE>), grid, block, 0, s, a, part);
+    else if (a.cols <= 8192) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, M, ONCE>), grid, block, 0, s, a, part);
+    else hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, 2 * M, ONCE>), grid, block, 0, s, a, part);
     return hipGetLastError();
 }
 

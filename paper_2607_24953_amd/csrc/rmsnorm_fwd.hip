@@ -1,8 +1,8 @@
 // Root-mean-square norm of rows, with the residual's addition.
 //
 // One read of x and the residual: a row stays in registers between the sum of its squares and
-// the products with it.  A lane holds CH chunks of eight neighbouring elements (16 bytes of
-// bfloat16), chunk k of a row in lane k % (lanes of the row).  The squares are summed in 64 bits,
+// the products with it.  A lane holds CH chunks of 16 bytes of x, chunk k of a row in lane k % (lanes
+// of the row).  The squares are summed in 64 bits,
 // where those of any float32 neither overflow nor vanish; the vector unit has time for it beside
 // the memory.
 #include "norm_common.hpp"
@@ -18,7 +18,7 @@ namespace {
 template <bool XB, int RT, int LANES, int CH, bool ONCE>
 __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_rows_kernel(const NormArgs a)
 {
-    constexpr int EX = XB ? 2 : 4, ER = RT == 2 ? 2 : 4;
+    constexpr int EX = XB ? 2 : 4, ER = RT == 2 ? 2 : 4, N = 16 / EX;
     const int t = LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x, step = LANES ? LANES : blockDim.x;
     const int64_t row = LANES ? group_index() * (256 / (LANES ? LANES : 1)) + threadIdx.x / (LANES ? LANES : 1) : group_index();
     if (LANES == 0 && row >= a.rows) return;
@@ -26,26 +26,26 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_rows_kernel(const 
     const int64_t cols = row < a.rows ? a.cols : 0;
     const uint8_t *x = reinterpret_cast<const uint8_t *>(a.x) + row * a.ldx * EX;
     const uint8_t *r = reinterpret_cast<const uint8_t *>(a.r) + row * a.ldr * ER;
-    Eight<XB> h[CH];
+    Run<XB, N> h[CH];
     double sum = 0.0;
     {
-        Eight<RT == 2> d[CH];
+        Run<RT == 2, N> d[CH];
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int64_t c = 8 * (t + k * (int64_t)step);
-            h[k].template load<ONCE && XB>(x + c * EX, cols - c);
-            if constexpr (RT != 0) d[k].template load<ONCE && RT == 2>(r + c * ER, cols - c);
+            const int64_t c = N * (t + k * (int64_t)step);
+            h[k].template load<ONCE>(x + c * EX, cols - c);
+            if constexpr (RT != 0) d[k].template load<ONCE>(r + c * ER, cols - c);
         }
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             if constexpr (RT != 0) {
-                float v[8];
+                float v[N];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = h[k].at(j) + d[k].at(j);
+                for (int j = 0; j < N; ++j) v[j] = h[k].at(j) + d[k].at(j);
                 h[k].set(v);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < N; ++j) {
                 const double v = h[k].at(j);
                 sum = __builtin_fma(v, v, sum);
             }
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_rows_kernel(const 
         uint8_t *out = reinterpret_cast<uint8_t *>(a.h) + row * a.ldh * EX;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int64_t c = 8 * (t + k * (int64_t)step);
+            const int64_t c = N * (t + k * (int64_t)step);
             h[k].store(out + c * EX, cols - c);
         }
     }
@@ -70,13 +70,13 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_rows_kernel(const 
     if (!a.y) return;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-        const int64_t c = 8 * (t + k * (int64_t)step);
+        const int64_t c = N * (t + k * (int64_t)step);
         if (c >= cols) break;
-        float w[8], y[8];
-        load_eight(w, a.w, a.w_bf16, c, cols - c);
+        float w[N], y[N];
+        load_run(w, a.w, a.w_bf16, c, cols - c);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = (h[k].at(j) * rstd) * w[j];
-        store_eight(y, a.y, a.y_bf16, row * a.ldy + c, cols - c);
+        for (int j = 0; j < N; ++j) y[j] = (h[k].at(j) * rstd) * w[j];
+        store_run(y, a.y, a.y_bf16, row * a.ldy + c, cols - c);
     }
 }
 
@@ -88,15 +88,15 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_rows_kernel(const NormArgs 
     double sum = 0.0;
     for (int64_t c = 8 * (int64_t)threadIdx.x; c < a.cols; c += 8 * 1024) {
         float v[8], d[8];
-        load_eight(v, a.x, a.x_bf16, row * a.ldx + c, a.cols - c);
+        load_run(v, a.x, a.x_bf16, row * a.ldx + c, a.cols - c);
         if (a.r) {
-            load_eight(d, a.r, a.r_bf16, row * a.ldr + c, a.cols - c);
+            load_run(d, a.r, a.r_bf16, row * a.ldr + c, a.cols - c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 v[j] += d[j];
                 if (a.x_bf16) v[j] = round_bf16(v[j]);
             }
-            store_eight(v, a.h, a.x_bf16, row * a.ldh + c, a.cols - c);
+            store_run(v, a.h, a.x_bf16, row * a.ldh + c, a.cols - c);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)v[j], (double)v[j], sum);
@@ -109,11 +109,11 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_rows_kernel(const NormArgs 
     const int64_t ldh = a.r ? a.ldh : a.ldx;
     for (int64_t c = 8 * (int64_t)threadIdx.x; c < a.cols; c += 8 * 1024) {
         float v[8], w[8];
-        load_eight(v, h, a.x_bf16, row * ldh + c, a.cols - c);
-        load_eight(w, a.w, a.w_bf16, c, a.cols - c);
+        load_run(v, h, a.x_bf16, row * ldh + c, a.cols - c);
+        load_run(w, a.w, a.w_bf16, c, a.cols - c);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = (v[j] * rstd) * w[j];
-        store_eight(v, a.y, a.y_bf16, row * a.ldy + c, a.cols - c);
+        store_run(v, a.y, a.y_bf16, row * a.ldy + c, a.cols - c);
     }
 }
 
@@ -127,24 +127,25 @@ hipError_t launch_c(const NormArgs &a, int64_t per, unsigned threads, hipStream_
 }
 
 // Inputs larger than the cache are read past it, so that it keeps more of h for the next kernel:
-// 16384 x 4096 bfloat16 95 -> 83 us, with operands in FP4 and MXFP8 148 -> 132.  Not float32 tensors,
-// whose eight elements a lane are two accesses to one line (156 us instead of 149), and not narrow
-// rows, which share lines (100000 x 200 35 us instead of 31).
+// 16384 x 4096 bfloat16 95 -> 83 us, with operands in FP4 and MXFP8 148 -> 132.  Not narrow rows,
+// which share lines (100000 x 200 35 us instead of 31).
 constexpr int64_t kCached = int64_t(192) << 20;
 
 template <bool XB, int RT>
 hipError_t launch_r(const NormArgs &a, hipStream_t s)
 {
-    const int64_t chunks = (a.cols + 7) / 8, bytes = a.rows * a.cols * ((XB ? 2 : 4) + (RT == 0 ? 0 : RT == 1 ? 4 : 2));
+    constexpr int N = XB ? 8 : 4, M = 8 / N;            // elements of a chunk, chunks of 8 elements
+    const int64_t bytes = a.rows * a.cols * ((XB ? 2 : 4) + (RT == 0 ? 0 : RT == 1 ? 4 : 2));
     const bool once = bytes > kCached;
-    if (chunks <= 32) return launch_c<XB, RT, 16, 2, false>(a, 16, 256, s);
-    if (chunks <= 128) return once ? launch_c<XB, RT, 64, 2, true>(a, 4, 256, s) : launch_c<XB, RT, 64, 2, false>(a, 4, 256, s);
-    const auto threads = [&](int ch) { return (unsigned)((chunks + 64 * ch - 1) / (64 * ch) * 64); };
-    if (!XB && chunks <= 1024)     // (the same of float32 rows in two chunks a lane: 149 us, in one 143)
-        return once ? launch_c<XB, RT, 0, 1, true>(a, 1, threads(1), s) : launch_c<XB, RT, 0, 1, false>(a, 1, threads(1), s);
-    if (chunks <= 2048)
+    if (a.cols <= 256) return launch_c<XB, RT, 16, 2 * M, false>(a, 16, 256, s);
+    if (a.cols <= 1024) return once ? launch_c<XB, RT, 64, 2 * M, true>(a, 4, 256, s) : launch_c<XB, RT, 64, 2 * M, false>(a, 4, 256, s);
+    // 16 elements a lane, 8 of float32 (16384 x 4096 149 us with 16), 32 of long rows
+    const auto threads = [&](int ch) { return (unsigned)((a.cols + 64 * N * ch - 1) / (64 * N * ch) * 64); };
+    if (a.cols <= 8192)
         return once ? launch_c<XB, RT, 0, 2, true>(a, 1, threads(2), s) : launch_c<XB, RT, 0, 2, false>(a, 1, threads(2), s);
-    return once ? launch_c<XB, RT, 0, 4, true>(a, 1, threads(4), s) : launch_c<XB, RT, 0, 4, false>(a, 1, threads(4), s);
+    if (a.cols <= 16384)
+        return once ? launch_c<XB, RT, 0, 2 * M, true>(a, 1, threads(2 * M), s) : launch_c<XB, RT, 0, 2 * M, false>(a, 1, threads(2 * M), s);
+    return once ? launch_c<XB, RT, 0, 4 * M, true>(a, 1, threads(4 * M), s) : launch_c<XB, RT, 0, 4 * M, false>(a, 1, threads(4 * M), s);
 }
 
 }  // namespace

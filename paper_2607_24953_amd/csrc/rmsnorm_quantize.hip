@@ -140,8 +140,12 @@ __device__ __forceinline__ void store_operands(const NormQuantArgs &a, const uin
                 if ((cc & 3) == 0) st8_rs[rl + i][wc * 4 + (cc >> 2)] = scale_byte(m, e);
             }
         }
+        // (serving wants the rowwise copies alone: 64 x 4096 in FP4 and MXFP8
+        // with the rows kernel 8.2 us, so 7.4)
+        const bool columns = (LINES && a.q4.codes_t) || (MX && a.q8.codes_t);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
+            if (!columns) break;
             const uint32_t col[8] = {y[0][j], y[1][j], y[2][j], y[3][j], y[4][j], y[5][j], y[6][j], y[7][j]};
             uint32_t m = 0;
 #pragma unroll
@@ -287,8 +291,8 @@ __global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(WR
             for (int i = 0; i < 8; ++i) h[i].load(p + i * a.ldh * E, r0 + i < a.rows ? cols : 0);
         }
         float w[8], rstd[8];
-        load_eight(w, a.w, a.w_bf16, c0, cols);
-        load_eight(rstd, a.rstd, 0, r0, a.rows - r0);
+        load_run(w, a.w, a.w_bf16, c0, cols);
+        load_run(rstd, a.rstd, 0, r0, a.rows - r0);
         norm_sub_block(y, h, w, rstd, a.rows - r0, cols);
     }
     store_formats<FP4, MX, WR, WC, ONCE>(a, y, tr, tc);

@@ -27,7 +27,7 @@ def make(sizes, dtypes, scale=1e-3, seed=0, shift=0):
 
 
 SETS = [[1], [7], [4096], [1, 2, 3, 5, 8, 13], [16384], [16385, 16383, 1], [0, 5, 0], [100003, 9, 70000], [257] * 128,
-        [33] * 129, [1000 + i for i in range(300)], [4_000_001, 3], [12] * 1000]
+        [33] * 129, [1000 + i for i in range(300)], [4_000_001, 3], [12] * 3000]
 
 
 @pytest.mark.parametrize("sizes", SETS, ids=lambda s: "%dx%d" % (len(s), s[0]))
