@@ -5,6 +5,11 @@
 // with it, as in the forward kernel.  A workgroup takes every gridDim.x-th row and keeps its part
 // of dw in registers, in 64 bits; the parts lie one behind the other in the workspace and a second
 // kernel adds them up.  Every sum has one owner and one order.
+//
+// The memory bounds it: 16384 x 4096 bfloat16 with dh 86 us (545 MB, 6.3 TB/s) and 5 for the join,
+// float32 151 in all; 777 x 2049 8.5 + 3.5.  The statistics of a row and the products with it as two
+// kernels, element by element, took 700.  Rows of 8193 to 16384 columns leave one workgroup of up
+// to 16 waves to a CU, with nothing to run while it waits at its barrier (2048 x 12288 68 us, 2.9 TB/s).
 #include "norm_common.hpp"
 #include "norms.hpp"
 #include "kernels.hpp"
@@ -193,7 +198,8 @@ __global__ __launch_bounds__(512) void rmsnorm_grad_join_kernel(const float *par
 
 inline int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 
-// bytes that the cache may still hold from the kernels before
+// bytes that the cache may still hold from the kernels before: above, rows are read past it (16384 x
+// 4096 bfloat16 101 -> 89 us; 8192 x 1024, which it holds, 18.8 -> 20.9)
 constexpr int64_t kCached = int64_t(192) << 20;
 
 constexpr int64_t kLong = 16384;       // columns that a workgroup's registers hold
@@ -213,7 +219,8 @@ int64_t parts_of(int64_t rows, int64_t cols)
         return rows < most ? rows : most;
     }
     // as many as are there at once (registers: 16 waves a CU, 8 of those with several rows), each
-    // with equally many turns
+    // with equally many turns: with twice as many 16384 x 4096 took 104 us instead of 102, 777 x 2049 15.1
+    // instead of 12.6, with three quarters of them the first 113
     const int64_t most = 256 * (cols <= 1024 ? 2 : waves_of(cols) < 16 ? 16 / waves_of(cols) : 1);
     const int64_t per = rows_at_once(cols), groups = (rows + per - 1) / per, turns = (groups + most - 1) / most;
     return turns == 0 ? 0 : (groups + turns - 1) / turns;

@@ -4,7 +4,9 @@
 // the products with it.  A lane holds CH chunks of 16 bytes of x, chunk k of a row in lane k % (lanes
 // of the row).  The squares are summed in 64 bits,
 // where those of any float32 neither overflow nor vanish; the vector unit has time for it beside
-// the memory.
+// the memory, which bounds the kernel: 16384 x 4096, float32 with a bfloat16 residual, 134 us (805
+// MB, 6.0 TB/s); bfloat16 86 us (6.2 TB/s); 777 x 2049 7 us, a single row 3.5, which is latency.
+// Before, a workgroup a row and element by element from memory twice, the first took 378 us.
 #include "norm_common.hpp"
 #include "norms.hpp"
 

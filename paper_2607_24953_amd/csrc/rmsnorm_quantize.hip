@@ -5,6 +5,10 @@
 // 16) .. + 7).  The lane forms y = (h * rstd) * w in float32 and converts it to each format that
 // is wanted, so h is read once for all of them.  A 1 x 32 block spans the 4 lanes that differ in
 // lane bits 0-1, a 32 x 1 block those that differ in bits 4-5, a 32 x 32 block all 16.
+//
+// 16384 x 4096 bfloat16 in FP4 and MXFP8, both orientations: 62 us (134 MB read, 205 written, 5.5
+// TB/s; 128 registers hold four waves a SIMD, of 156 it took 88 us).  Strips of a few rows take 4-5 us,
+// which is a lone wave's 1300 to 2500 instructions.
 #include "norm_common.hpp"
 #include "norms.hpp"
 
