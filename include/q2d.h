@@ -593,7 +593,8 @@ q2d_status q2d_rmsnorm_bwd(const q2d_rmsnorm_grad *n, void *workspace, int64_t w
  */
 int64_t q2d_grad_workspace(int32_t n);
 
-/* *norm (device) = the 2-norm; 0 without elements. */
+/* *norm (device) = the 2-norm; 0 without elements.  norm and the workspace share no memory with
+ * one another or with a tensor (Q2D_EINVAL); tensors may share theirs. */
 q2d_status q2d_grad_norm(int32_t n, const void *const *data, const int64_t *counts, const int32_t *dtypes, float *norm,
                          void *workspace, int64_t workspace_bytes, hipStream_t stream);
 

@@ -229,6 +229,19 @@ q2d_status check_apart(const Set &g, const void *given, const void *norm, const 
     return Q2D_OK;
 }
 
+// The same for q2d_grad_norm, where the tensors are read only
+bool norm_apart(const Set &g, const void *norm, const void *workspace, int64_t workspace_bytes)
+{
+    const uintptr_t n = reinterpret_cast<uintptr_t>(norm), w = reinterpret_cast<uintptr_t>(workspace), w_end = w + (uintptr_t)workspace_bytes;
+    bool apart = n >= w_end || n + 4 <= w;
+    for (int32_t i = 0; i < g.n; ++i) {
+        if (g.counts[i] == 0) continue;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(g.data[i]), end = at + (uintptr_t)g.counts[i] * dtype_bytes((q2d_dtype)g.dtypes[i]);
+        apart &= (n >= end || n + 4 <= at) && (w >= end || w_end <= at);
+    }
+    return apart;
+}
+
 // Partial sums of a call at most: kMaxParts shared by its launches, one a launch at least
 int64_t parts_of(int32_t n) { return kMaxParts + n / Squared::kMost + 1; }
 
@@ -309,6 +322,7 @@ q2d_status q2d_grad_norm(int32_t n, const void *const *data, const int64_t *coun
     const q2d_status s = check_set(g);
     if (s != Q2D_OK) return s;
     if (!norm || !aligned(norm, 4) || !workspace || !aligned(workspace, 8) || workspace_bytes < q2d_grad_workspace(n)) return Q2D_EINVAL;
+    if (!norm_apart(g, norm, workspace, q2d_grad_workspace(n))) return Q2D_EINVAL;
     double *parts = reinterpret_cast<double *>(workspace);
     const int k = square_sums(g, elements(g), true, parts, stream);
     if (k < 0) return Q2D_ELAUNCH;

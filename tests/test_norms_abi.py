@@ -139,6 +139,24 @@ def test_clip_refusals(q2d):
     assert N(1, *one, c + 1, b, size, None) == 1 and N(1, one[0], one[1], (ctypes.c_int32 * 1)(9), c, b, size, None) == 1
 
 
+def test_gradients_norm_memory(q2d):
+    """The norm's place and the workspace, which are written while the tensors are read."""
+    size = q2d._lib.q2d_grad_workspace(2)
+    arr = lambda t, v: (t * 2)(*v)
+
+    def call(norm, ws, data=(FAKE, FAKE + MB), counts=(1024, 1000)):
+        return q2d._lib.q2d_grad_norm(2, arr(ctypes.c_void_p, data), arr(ctypes.c_int64, counts), arr(ctypes.c_int32, (0, 1)), norm, ws,
+                                      size, None)
+    free = FAKE + 4 * MB
+    for norm, ws in ((FAKE, free), (FAKE + 4092, free), (FAKE + MB + 1996, free), (free, free), (free + size - 4, free),
+                     (free, FAKE + 4088), (free, FAKE - size + 8), (free, FAKE + MB + 1992), (free, FAKE + MB - 8)):
+        assert call(norm, ws) == 1, (norm, ws)
+    # tensors without elements have no memory; the next byte is another's
+    assert call(free, free, counts=(0, 0)) == 1
+    for norm, ws in ((free, FAKE + 4096), (FAKE + 4096, free), (free + size, free), (free, FAKE - size)):
+        assert call(norm, ws) != 1, (norm, ws)
+
+
 def test_python_refusals(q2d):
     """Host tensors and mismatched arguments never reach the library."""
     x, w = torch.zeros((4, 8)), torch.ones(8)
