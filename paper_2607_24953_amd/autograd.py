@@ -28,6 +28,10 @@ float32.  ``rms_norm`` gives the normed values themselves.  Both return the sum 
 beside their output, for the residual stream, and their backward takes its gradient in the
 same pass (q2d_rmsnorm_bwd).
 
+A backward pass can be captured into a HIP graph.  Let go of every eager output of the same
+parameters first: torch keeps their gradients' accumulation on the eager stream for as long as one
+lives, and a capture that meets another stream there ends the process.
+
 ``attention`` is q2d_attention_fwd with q2d_attention_bwd as its gradient.
 
 Options mirror the paper's ablations: ``mode_*`` "rtn" / "sr" choose the

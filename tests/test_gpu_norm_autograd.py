@@ -220,6 +220,42 @@ def test_step_in_a_graph(q2d):
     assert all(torch.equal(a, b) for a, b in zip(graphs[0][1], want))
 
 
+def test_backward_in_a_graph(q2d):
+    """rms_norm and Q2DNormLinear with their backward pass captured: each replay gives the bytes of
+    the eager pass.  (No eager output of the leaves is alive while the capture runs.)"""
+    from paper_2607_24953_amd.autograd import Q2DNormLinear, rms_norm
+    T, C, N = 130, 256, 192
+    layer = Q2DNormLinear(C, N, mode_dy="rtn", device=DEV, dtype=F32)
+    with torch.no_grad():
+        layer.weight.copy_(rand(N, C, seed=1, scale=0.05))
+        layer.norm_weight.copy_(1 + rand(C, seed=2, scale=0.1))
+    X, R, W = rand(T, C, seed=3).requires_grad_(), rand(T, C, seed=4).requires_grad_(), (1 + rand(N, seed=5, scale=0.1)).requires_grad_()
+    gy, gh = rand(T, N, seed=6), rand(T, C, seed=7)
+    leaves = [X, R, W, layer.weight, layer.norm_weight]
+
+    def step():
+        Y, h = layer(X, R)
+        y = rms_norm(Y, W, y_dtype=F32)
+        return [y.detach(), h.detach()] + list(torch.autograd.grad((y, h), leaves, (gy, gh)))
+    want = [t.clone() for t in step()]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    for _ in range(4):
+        for t in out:
+            t.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(out, want)):
+            assert torch.equal(a, b), i
+        _ = torch.randn(1000, device=DEV).sum().item()      # eager work between replays
+
+
 def test_other_streams(q2d):
     """Calls on a stream of their own, two at once."""
     X, R, W = rand(3000, 1024, dtype=BF16, seed=1), rand(3000, 1024, dtype=BF16, seed=2), 1 + rand(1024, seed=3, scale=0.1)
