@@ -8,8 +8,9 @@
 //
 // The memory bounds it: 16384 x 4096 bfloat16 with dh 86 us (545 MB, 6.3 TB/s) and 5 for the join,
 // float32 151 in all; 777 x 2049 8.5 + 3.5.  The statistics of a row and the products with it as two
-// kernels, element by element, took 700.  Rows of 8193 to 16384 columns leave one workgroup of up
-// to 16 waves to a CU, with nothing to run while it waits at its barrier (2048 x 12288 68 us, 2.9 TB/s).
+// kernels, element by element, took 700.  Rows of more than 8192 columns are read twice: two chunks a
+// lane and their sums leave one workgroup to a CU, with nothing to run while it waits at its barrier,
+// and spilled registers on top (2048 x 12288 bfloat16 77 us, 2.6 TB/s; twice 60; float32 165, 104).
 #include "norm_common.hpp"
 #include "norms.hpp"
 #include "kernels.hpp"
@@ -17,7 +18,6 @@
 namespace q2d {
 
 namespace {
-
 
 // HB, DB: h and dh, dy are bfloat16.  LANES, CH: as in the forward kernel.  ONCE: the rows come from
 // memory rather than from the cache.
@@ -29,14 +29,12 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
     __shared__ double lds[2][16];
     const int t = LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x, step = LANES ? LANES : blockDim.x;
     const int sub = LANES ? threadIdx.x / (LANES ? LANES : 1) : 0;
-    // (two chunks of weights beside two of everything else do not fit 128 registers)
-    constexpr bool KEPT = LANES != 0 || CH * N <= 8;
     float w[CH][N];
     double acc[CH][N];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         const int64_t c = N * (t + k * (int64_t)step);
-        if constexpr (KEPT) load_run(w[k], a.w, a.w_bf16, c, a.cols - c);
+        load_run(w[k], a.w, a.w_bf16, c, a.cols - c);
 #pragma unroll
         for (int j = 0; j < N; ++j) acc[k][j] = 0.0;
     }
@@ -64,7 +62,6 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
         double sum = 0.0;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            if constexpr (!KEPT) load_run(w[k], a.w, a.w_bf16, N * (t + k * (int64_t)step), a.cols - N * (t + k * (int64_t)step));
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const float n = h[k].at(j) * rstd, d = dy[k].at(j);
@@ -85,7 +82,6 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
         for (int k = 0; k < CH; ++k) {
             const int64_t c = N * (t + k * (int64_t)step);
             if (c >= cols) break;
-            if constexpr (!KEPT) load_run(w[k], a.w, a.w_bf16, c, a.cols - c);
             float dx[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) {
@@ -129,52 +125,69 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
 }
 
 // Rows that no workgroup's registers hold: their means first
+template <bool HB, bool DB>
 __global__ __launch_bounds__(1024) void rmsnorm_grad_means_kernel(const NormGradArgs a, float *means)
 {
+    constexpr int EH = HB ? 2 : 4, ED = DB ? 2 : 4, N = 16 / EH;
     const int64_t row = group_index();
     if (row >= a.rows) return;
     __shared__ double lds[16];
+    const uint8_t *hp = reinterpret_cast<const uint8_t *>(a.h) + row * a.ldh * EH;
+    const uint8_t *dyp = reinterpret_cast<const uint8_t *>(a.dy) + row * a.lddy * ED;
     const float rstd = a.rstd[row];
     double s = 0.0;
-    for (int64_t c = 8 * (int64_t)threadIdx.x; c < a.cols; c += 8 * 1024) {
-        float d[8], w[8], h[8];
-        load_run(d, a.dy, a.dy_bf16, row * a.lddy + c, a.cols - c);
+#pragma unroll 2
+    for (int64_t c = N * (int64_t)threadIdx.x; c < a.cols; c += N * 1024) {
+        Run<HB, N> h;
+        Run<DB, N> dy;
+        float w[N];
+        h.load(hp + c * EH, a.cols - c);
+        dy.load(dyp + c * ED, a.cols - c);
         load_run(w, a.w, a.w_bf16, c, a.cols - c);
-        load_run(h, a.h, a.h_bf16, row * a.ldh + c, a.cols - c);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s = __builtin_fma((double)(d[j] * w[j]), (double)(h[j] * rstd), s);
+        for (int j = 0; j < N; ++j) s = __builtin_fma((double)(dy.at(j) * w[j]), (double)(h.at(j) * rstd), s);
     }
     s = group_sum(s, 16, lds);
     if (threadIdx.x == 0) means[row] = (float)(s / (double)a.cols);
 }
 
-// .. then 2048 columns of every gridDim.y-th row
+// .. then 256 lanes' columns of every gridDim.y-th row, the last rows first: the cache may hold them
+// still
+template <bool HB, bool DB, bool ONCE>
 __global__ __launch_bounds__(256) void rmsnorm_grad_tile_kernel(const NormGradArgs a, const float *means, float *part)
 {
-    const int64_t c = 8 * (blockIdx.x * (int64_t)256 + threadIdx.x), n = a.cols - c;
-    if (n <= 0) return;
-    float w[8];
-    load_run(w, a.w, a.w_bf16, c, n);
-    double acc[8] = {};
-    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+    constexpr int EH = HB ? 2 : 4, ED = DB ? 2 : 4, N = 16 / EH;
+    const int64_t c = N * (blockIdx.x * (int64_t)256 + threadIdx.x), cols = a.cols - c;
+    if (cols <= 0) return;
+    float w[N];
+    load_run(w, a.w, a.w_bf16, c, cols);
+    double acc[N] = {};
+    for (int64_t row = a.rows - 1 - blockIdx.y; row >= 0; row -= gridDim.y) {
+        Run<HB, N> h, dh;
+        Run<DB, N> dy;
+        h.template load<ONCE>(reinterpret_cast<const uint8_t *>(a.h) + (row * a.ldh + c) * EH, cols);
+        dy.template load<ONCE>(reinterpret_cast<const uint8_t *>(a.dy) + (row * a.lddy + c) * ED, cols);
+        if (a.dh) dh.template load<ONCE>(reinterpret_cast<const uint8_t *>(a.dh) + (row * a.lddh + c) * EH, cols);
+        else dh.zero();
         const float rstd = a.rstd[row], mean = means[row];
-        float h[8], d[8], dh[8] = {};
-        load_run(h, a.h, a.h_bf16, row * a.ldh + c, n);
-        load_run(d, a.dy, a.dy_bf16, row * a.lddy + c, n);
-        if (a.dh) load_run(dh, a.dh, a.h_bf16, row * a.lddh + c, n);
+        float dx[N];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float x = h[j] * rstd;
-            acc[j] = __builtin_fma((double)d[j], (double)x, acc[j]);
-            dh[j] += rstd * (d[j] * w[j] - x * mean);
+        for (int j = 0; j < N; ++j) {
+            const float n = h.at(j) * rstd, d = dy.at(j);
+            acc[j] = __builtin_fma((double)d, (double)n, acc[j]);
+            dx[j] = rstd * (d * w[j] - n * mean) + dh.at(j);
         }
-        store_run(dh, a.dx, a.h_bf16, row * a.lddx + c, n);
+        Run<HB, N> o;
+        o.set(dx);
+        o.store(reinterpret_cast<uint8_t *>(a.dx) + (row * a.lddx + c) * EH, cols);
     }
     if (!part) return;
-    float v[8];
+    float v[N];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (float)acc[j];
-    store_run(v, part, 0, blockIdx.y * a.cols + c, n);
+    for (int j = 0; j < N; ++j) v[j] = (float)acc[j];
+    Run<false, N> o;
+    o.set(v);
+    o.store(reinterpret_cast<uint8_t *>(part + blockIdx.y * a.cols + c), cols);
 }
 
 // dw of 32 columns: 16 lanes a column take every 16th part
@@ -202,21 +215,25 @@ inline int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 // 4096 bfloat16 101 -> 89 us; 8192 x 1024, which it holds, 18.8 -> 20.9)
 constexpr int64_t kCached = int64_t(192) << 20;
 
-constexpr int64_t kLong = 16384;       // columns that a workgroup's registers hold
+constexpr int64_t kLong = 8192;        // columns that a workgroup's registers hold
 
 // rows that a workgroup has at a time
 int64_t rows_at_once(int64_t cols) { return cols <= 256 ? 16 : cols <= 1024 ? 4 : 1; }
 
 // waves of a workgroup
-int64_t waves_of(int64_t cols) { return cols <= 1024 ? 4 : cols <= 8192 ? (cols + 511) / 512 : (cols + 1023) / 1024; }
+int64_t waves_of(int64_t cols) { return cols <= 1024 ? 4 : (cols + 511) / 512; }
 
-// workgroups, each with one part of dw
-int64_t parts_of(int64_t rows, int64_t cols)
+// tiles of 256 lanes' columns
+int64_t tiles_of(int64_t cols, bool h_bf16) { return (cols + (h_bf16 ? 2047 : 1023)) / (h_bf16 ? 2048 : 1024); }
+
+// workgroups (of long rows: for each of their tiles), each with one part of dw
+int64_t parts_of(int64_t rows, int64_t cols, bool h_bf16)
 {
     if (cols > kLong) {
-        // (the parts' memory stays at 128 MB where rows are very long)
-        const int64_t fit = (int64_t(1) << 25) / cols, most = fit < 8 ? 8 : fit > 256 ? 256 : fit;
-        return rows < most ? rows : most;
+        // (1024 workgroups: with twice as many 8192 x 12288 float32 took 456 us instead of 434, with half
+        // as many 2048 x 8448 bfloat16 49 instead of 45)
+        const int64_t tiles = tiles_of(cols, h_bf16), most = tiles < 1024 ? 1024 / tiles : 1, turns = (rows + most - 1) / most;
+        return turns == 0 ? 0 : (rows + turns - 1) / turns;
     }
     // as many as are there at once (registers: 16 waves a CU, 8 of those with several rows), each
     // with equally many turns: with twice as many 16384 x 4096 took 104 us instead of 102, 777 x 2049 15.1
@@ -235,15 +252,21 @@ hipError_t launch_grad(const NormGradArgs &a, unsigned parts, float *part, hipSt
     const dim3 grid(parts), block((unsigned)(64 * waves_of(a.cols)));
     if (a.cols <= 256) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 16, 2 * M, ONCE>), grid, block, 0, s, a, part);
     else if (a.cols <= 1024) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 64, 2 * M, ONCE>), grid, block, 0, s, a, part);
-    else if (a.cols <= 8192) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, M, ONCE>), grid, block, 0, s, a, part);
-    else hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, 2 * M, ONCE>), grid, block, 0, s, a, part);
+    else hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, M, ONCE>), grid, block, 0, s, a, part);
     return hipGetLastError();
 }
 
 template <bool HB, bool DB>
-hipError_t launch_types(const NormGradArgs &a, unsigned parts, float *part, hipStream_t s)
+hipError_t launch_types(const NormGradArgs &a, unsigned parts, float *means, float *part, hipStream_t s)
 {
     const int64_t bytes = a.rows * a.cols * ((a.dh ? 2 : 1) * (HB ? 2 : 4) + (DB ? 2 : 4));
+    if (a.cols > kLong) {
+        hipLaunchKernelGGL((rmsnorm_grad_means_kernel<HB, DB>), row_grid(a.rows), dim3(1024), 0, s, a, means);
+        const dim3 grid((unsigned)tiles_of(a.cols, HB), parts);
+        if (bytes > kCached) hipLaunchKernelGGL((rmsnorm_grad_tile_kernel<HB, DB, true>), grid, dim3(256), 0, s, a, means, part);
+        else hipLaunchKernelGGL((rmsnorm_grad_tile_kernel<HB, DB, false>), grid, dim3(256), 0, s, a, means, part);
+        return hipGetLastError();
+    }
     return bytes > kCached ? launch_grad<HB, DB, true>(a, parts, part, s) : launch_grad<HB, DB, false>(a, parts, part, s);
 }
 
@@ -251,24 +274,21 @@ hipError_t launch_types(const NormGradArgs &a, unsigned parts, float *part, hipS
 
 int64_t rmsnorm_grad_workspace(int64_t rows, int64_t cols)
 {
-    return means_bytes(rows, cols) + up256(parts_of(rows, cols) * cols * 4);
+    // (bfloat16's are at least as many as float32's)
+    return means_bytes(rows, cols) + up256(parts_of(rows, cols, true) * cols * 4);
 }
 
 hipError_t launch_rmsnorm_grad(const NormGradArgs &a, hipStream_t stream)
 {
-    const int64_t parts = parts_of(a.rows, a.cols);
+    const int64_t parts = parts_of(a.rows, a.cols, a.h_bf16);
     float *means = reinterpret_cast<float *>(a.workspace);
     float *sums = reinterpret_cast<float *>(a.workspace + means_bytes(a.rows, a.cols)), *part = a.dw ? sums : nullptr;
     if (a.rows > 0) {
         hipError_t e;
-        if (a.cols > kLong) {
-            hipLaunchKernelGGL(rmsnorm_grad_means_kernel, row_grid(a.rows), dim3(1024), 0, stream, a, means);
-            hipLaunchKernelGGL(rmsnorm_grad_tile_kernel, dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)parts), dim3(256), 0, stream, a, means, part);
-            e = hipGetLastError();
-        } else if (a.h_bf16) {
-            e = a.dy_bf16 ? launch_types<true, true>(a, (unsigned)parts, part, stream) : launch_types<true, false>(a, (unsigned)parts, part, stream);
+        if (a.h_bf16) {
+            e = a.dy_bf16 ? launch_types<true, true>(a, (unsigned)parts, means, part, stream) : launch_types<true, false>(a, (unsigned)parts, means, part, stream);
         } else {
-            e = a.dy_bf16 ? launch_types<false, true>(a, (unsigned)parts, part, stream) : launch_types<false, false>(a, (unsigned)parts, part, stream);
+            e = a.dy_bf16 ? launch_types<false, true>(a, (unsigned)parts, means, part, stream) : launch_types<false, false>(a, (unsigned)parts, means, part, stream);
         }
         if (e != hipSuccess) return e;
     }

@@ -8,9 +8,6 @@ import pytest
 
 from test_kernel_resources import READELF, code_objects
 
-# kernel in its mangled name -> bytes a lane; the others take none
-ALLOWED = [(r"rmsnorm_grad_kernelILb[01]ELb[01]ELi0ELi[24]", 304)]      # rows of 8193 to 16384 columns
-
 
 def test_scratch(tmp_path):
     import paper_2607_24953_amd as q2d
@@ -28,8 +25,7 @@ def test_scratch(tmp_path):
             seen += 1
             scratch = int(re.search(r"\.private_segment_fixed_size:\s*(\d+)", part).group(1))
             lds = int(re.search(r"\.group_segment_fixed_size:\s*(\d+)", part).group(1))
-            most = max([n for pattern, n in ALLOWED if re.search(pattern, name.group(1))], default=0)
-            assert scratch <= most, (name.group(1), scratch)
+            assert scratch == 0, (name.group(1), scratch)
             # two workgroups of a tile's kernel fit a CU's 160 KB
             assert lds <= 80 * 1024, (name.group(1), lds)
     assert seen > 60, seen
