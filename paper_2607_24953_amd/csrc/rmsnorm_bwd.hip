@@ -8,9 +8,11 @@
 //
 // The memory bounds it: 16384 x 4096 bfloat16 with dh 86 us (545 MB, 6.3 TB/s) and 5 for the join,
 // float32 151 in all; 777 x 2049 8.5 + 3.5.  The statistics of a row and the products with it as two
-// kernels, element by element, took 700.  Rows of more than 8192 columns are read twice: two chunks a
-// lane and their sums leave one workgroup to a CU, with nothing to run while it waits at its barrier,
-// and spilled registers on top (2048 x 12288 bfloat16 77 us, 2.6 TB/s; twice 60; float32 165, 104).
+// kernels, element by element, took 700.  Rows of more than 16384 columns are
+// read twice; of 8193 to 16384 so 2048 x 12288 bfloat16 took 60 us, float32 101 (in registers, spilled, 77
+// and 165), with dw's parts in LDS 50 and 79 (4.0 and 5.1 TB/s): one workgroup has a CU for itself and
+// nothing runs while it waits at its barrier.  With dw's parts in LDS for all rows, and six or eight
+// waves to a SIMD, 16384 x 4096 took 103 and 102 us instead of 92.
 #include "norm_common.hpp"
 #include "norms.hpp"
 #include "kernels.hpp"
@@ -20,23 +22,29 @@ namespace q2d {
 namespace {
 
 // HB, DB: h and dh, dy are bfloat16.  LANES, CH: as in the forward kernel.  ONCE: the rows come from
-// memory rather than from the cache.
-template <bool HB, bool DB, int LANES, int CH, bool ONCE>
-__global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const NormGradArgs a, float *part)
+// memory rather than from the cache.  FAR: 0, or the most lanes of a workgroup whose parts of dw are in
+// LDS, each lane's own: two chunks' do not fit the registers of 16 waves, and without them two
+// workgroups of 12 fit a CU.
+template <bool HB, bool DB, int LANES, int CH, bool ONCE, int FAR = 0>
+__global__ __launch_bounds__(LANES ? 256 : FAR ? FAR : 1024, LANES ? 1 : FAR == 768 ? 6 : 4) void rmsnorm_grad_kernel(const NormGradArgs a, float *part)
 {
     constexpr int EH = HB ? 2 : 4, ED = DB ? 2 : 4, N = 16 / EH;
     constexpr int kPer = LANES ? 256 / (LANES ? LANES : 1) : 1;        // rows at a time
     __shared__ double lds[2][16];
     const int t = LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x, step = LANES ? LANES : blockDim.x;
     const int sub = LANES ? threadIdx.x / (LANES ? LANES : 1) : 0;
+    __shared__ double far[FAR ? CH * N : 1][FAR ? FAR : 1];
     float w[CH][N];
-    double acc[CH][N];
+    double acc[FAR ? 1 : CH][FAR ? 1 : N];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         const int64_t c = N * (t + k * (int64_t)step);
         load_run(w[k], a.w, a.w_bf16, c, a.cols - c);
 #pragma unroll
-        for (int j = 0; j < N; ++j) acc[k][j] = 0.0;
+        for (int j = 0; j < N; ++j) {
+            if constexpr (FAR) far[k * N + j][threadIdx.x] = 0.0;
+            else acc[k][j] = 0.0;
+        }
     }
     int turn = 0;
     for (int64_t first = blockIdx.x * (int64_t)kPer; first < a.rows; first += gridDim.x * (int64_t)kPer, turn ^= 1) {
@@ -66,7 +74,8 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
             for (int j = 0; j < N; ++j) {
                 const float n = h[k].at(j) * rstd, d = dy[k].at(j);
                 sum = __builtin_fma((double)(d * w[k][j]), (double)n, sum);
-                acc[k][j] = __builtin_fma((double)d, (double)n, acc[k][j]);
+                if constexpr (FAR) far[k * N + j][threadIdx.x] = __builtin_fma((double)d, (double)n, far[k * N + j][threadIdx.x]);
+                else acc[k][j] = __builtin_fma((double)d, (double)n, acc[k][j]);
             }
         }
         if constexpr (LANES) sum = lane_sum<LANES ? LANES : 64>(sum);
@@ -117,7 +126,7 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void rmsnorm_grad_kernel(const 
             Run<false, N> o;
             float v[N];
 #pragma unroll
-            for (int j = 0; j < N; ++j) v[j] = (float)acc[k][j];
+            for (int j = 0; j < N; ++j) v[j] = (float)(FAR ? far[FAR ? k * N + j : 0][FAR ? threadIdx.x : 0] : acc[FAR ? 0 : k][FAR ? 0 : j]);
             o.set(v);
             o.store(reinterpret_cast<uint8_t *>(part + c), a.cols - c);
         }
@@ -215,16 +224,20 @@ inline int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 // 4096 bfloat16 101 -> 89 us; 8192 x 1024, which it holds, 18.8 -> 20.9)
 constexpr int64_t kCached = int64_t(192) << 20;
 
-constexpr int64_t kLong = 8192;        // columns that a workgroup's registers hold
+constexpr int64_t kLong = 16384;       // columns that a workgroup's registers hold
 
 // rows that a workgroup has at a time
 int64_t rows_at_once(int64_t cols) { return cols <= 256 ? 16 : cols <= 1024 ? 4 : 1; }
 
 // waves of a workgroup
-int64_t waves_of(int64_t cols) { return cols <= 1024 ? 4 : (cols + 511) / 512; }
+int64_t waves_of(int64_t cols) { return cols <= 1024 ? 4 : cols <= 8192 ? (cols + 511) / 512 : (cols + 1023) / 1024; }
 
 // tiles of 256 lanes' columns
 int64_t tiles_of(int64_t cols, bool h_bf16) { return (cols + (h_bf16 ? 2047 : 1023)) / (h_bf16 ? 2048 : 1024); }
+
+// rows of nine to twelve waves: two workgroups to a CU with dw's parts in LDS (8192 x 5120 bfloat16
+// 80 us, so 65, float32 105, 101; 2048 rows 26.5, 23.9, and 34.7, 32.4)
+bool two_of_twelve(int64_t cols) { return cols > 4096 && cols <= 6144; }
 
 // workgroups (of long rows: for each of their tiles), each with one part of dw
 int64_t parts_of(int64_t rows, int64_t cols, bool h_bf16)
@@ -238,7 +251,7 @@ int64_t parts_of(int64_t rows, int64_t cols, bool h_bf16)
     // as many as are there at once (registers: 16 waves a CU, 8 of those with several rows), each
     // with equally many turns: with twice as many 16384 x 4096 took 104 us instead of 102, 777 x 2049 15.1
     // instead of 12.6, with three quarters of them the first 113
-    const int64_t most = 256 * (cols <= 1024 ? 2 : waves_of(cols) < 16 ? 16 / waves_of(cols) : 1);
+    const int64_t most = 256 * (cols <= 1024 || two_of_twelve(cols) ? 2 : waves_of(cols) < 16 ? 16 / waves_of(cols) : 1);
     const int64_t per = rows_at_once(cols), groups = (rows + per - 1) / per, turns = (groups + most - 1) / most;
     return turns == 0 ? 0 : (groups + turns - 1) / turns;
 }
@@ -252,7 +265,9 @@ hipError_t launch_grad(const NormGradArgs &a, unsigned parts, float *part, hipSt
     const dim3 grid(parts), block((unsigned)(64 * waves_of(a.cols)));
     if (a.cols <= 256) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 16, 2 * M, ONCE>), grid, block, 0, s, a, part);
     else if (a.cols <= 1024) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 64, 2 * M, ONCE>), grid, block, 0, s, a, part);
-    else hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, M, ONCE>), grid, block, 0, s, a, part);
+    else if (two_of_twelve(a.cols)) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, M, ONCE, 768>), grid, block, 0, s, a, part);
+    else if (a.cols <= 8192) hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, M, ONCE>), grid, block, 0, s, a, part);
+    else hipLaunchKernelGGL((rmsnorm_grad_kernel<HB, DB, 0, 2 * M, ONCE, 1024>), grid, block, 0, s, a, part);
     return hipGetLastError();
 }
 

@@ -295,10 +295,10 @@ def test_backward_rows_anywhere(q2d, cols, pad, shift):
             assert bool((torch.as_strided(dx, (36, pad), (cols + pad, 1), dx.storage_offset() + cols) == 7).all())
 
 
-@pytest.mark.parametrize("shape", [(700, 8200), (205, 8193), (1030, 16385)], ids=str)
+@pytest.mark.parametrize("shape", [(700, 8200), (205, 8193), (1030, 16385), (1100, 5001), (515, 6144), (300, 12289)], ids=str)
 @pytest.mark.parametrize("x,y", [(BF16, F32), (F32, BF16)], ids=str)
 def test_backward_many_long_rows(q2d, shape, x, y):
-    """More long rows than a tile's workgroups take in one turn, and a last turn that is short."""
+    """More long rows than workgroups take in one turn, and a last turn that is short."""
     W = weight(shape[1], F32)
     X, dy, dh = gradient_case(shape, x, y, 45)
     rstd = q2d.q2d_rmsnorm_fwd(X, W)[2]

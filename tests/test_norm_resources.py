@@ -26,6 +26,7 @@ def test_scratch(tmp_path):
             scratch = int(re.search(r"\.private_segment_fixed_size:\s*(\d+)", part).group(1))
             lds = int(re.search(r"\.group_segment_fixed_size:\s*(\d+)", part).group(1))
             assert scratch == 0, (name.group(1), scratch)
-            # two workgroups of a tile's kernel fit a CU's 160 KB
-            assert lds <= 80 * 1024, (name.group(1), lds)
+            # two workgroups fit a CU's 160 KB, but of the norm's gradient with 16 waves
+            most = 144 if re.search(r"rmsnorm_grad_kernel.*Li1024E", name.group(1)) else 80
+            assert lds <= most * 1024, (name.group(1), lds)
     assert seen > 60, seen
