@@ -306,7 +306,8 @@ q2d_status q2d_linear_bwd(const void *dY, q2d_dtype dt, const q2d_tensor *qX,
  *          scale exponent e of each element's block, -128 for scale byte 0xFF.
  *          exps of copy 0 minus exps of copy 1 is the scale-difference map.
  * Q2D_EINVAL for a missing buffer, copy not 0 or 1, or leading dimensions
- * below cols.  Stream-ordered; no host synchronisation.
+ * below cols; Q2D_EUNSUPPORTED for more than 2^35 tiles of 128 x 256 elements.
+ * Stream-ordered; no host synchronisation.
  */
 q2d_status q2d_dequantize(const q2d_tensor *t, int copy, void *out, q2d_dtype out_dt, int64_t ldo,
                           int8_t *exps, int64_t lde, hipStream_t stream);

@@ -477,6 +477,7 @@ q2d_status q2d_dequantize(const q2d_tensor *t, int copy, void *out, q2d_dtype ou
     if (t->block != 32 && !(t->block == 64 && t->fmt == Q2D_FMT_FP4_2D)) return Q2D_EUNSUPPORTED;
     const q2d_status s = check_dims(t->rows, t->cols);
     if (s != Q2D_OK) return s;
+    if (!few_tiles(t->rows, t->cols)) return Q2D_EUNSUPPORTED;
     if (ldo < t->cols || (exps && lde < t->cols)) return Q2D_EINVAL;
     const Layout l = layout_of((q2d_fmt)t->fmt, t->rows, t->cols);
     const uint8_t *codes = copy ? t->codes_t : t->codes;

@@ -70,7 +70,8 @@ __global__ __launch_bounds__(64 * WR * WC) void dequantize_kernel(const DequantA
     constexpr int kRows = 32 * WR, kCols = 128 * WC, kThreads = 64 * WR * WC;
     constexpr int kWords = FMT == 1 ? 2 : 1;             // words of eight codes
     const int64_t tiles_c = (a.cols + kCols - 1) / kCols;
-    const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
+    const int64_t tile = group_index(), tr = tile / tiles_c, tc = tile - tr * tiles_c;
+    if (tr * kRows >= a.rows) return;                    // (a grid of two dimensions may hold more)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wr = wave / WC, wc = wave % WC, rg = lane >> 4, cc = lane & 15;
     const int64_t r0 = tr * kRows + wr * 32 + 8 * rg, c0 = tc * kCols + wc * 128 + 8 * cc;
@@ -197,11 +198,10 @@ hipError_t launch_tiles(const DequantArgs &a, hipStream_t s)
     if (tiles(128, 256) <= 128) {
         hipLaunchKernelGGL((dequantize_kernel<FMT, TRANS, BF16, 1, 1>), dim3((unsigned)tiles(32, 128)), dim3(64), 0, s, a);
     } else {
-        if (tiles(128, 256) >= (int64_t(1) << 23)) return hipErrorInvalidValue;      // (work-items of a launch: below 2^32)
         // bfloat16 output of 96 MB or more past the cache: 16384 x 4096 FP4 37 -> 26 us, MXFP8 transposed
         // 58 -> 35; with a kernel that reads the output behind it 65 -> 61, half the size 30 -> 34.
         // (float32 stores of eight elements are two to a line and stay)
-        const dim3 grid((unsigned)tiles(128, 256)), block(512);
+        const dim3 grid = row_grid(tiles(128, 256)), block(512);
         if (BF16 && a.rows * a.cols * 2 >= int64_t(96) << 20) hipLaunchKernelGGL((dequantize_kernel<FMT, TRANS, BF16, 4, 2, true>), grid, block, 0, s, a);
         else hipLaunchKernelGGL((dequantize_kernel<FMT, TRANS, BF16, 4, 2>), grid, block, 0, s, a);
     }

@@ -78,4 +78,9 @@ inline q2d_status check_dims(int64_t R, int64_t C)
     return Q2D_OK;
 }
 
+// 128 x 256 tiles of one launch, in a grid of two dimensions: 2^20 along the first, 2^15 along the second
+constexpr int64_t kMaxTiles = int64_t(1) << 35;
+
+inline bool few_tiles(int64_t R, int64_t C) { return cdiv(R, 128) * cdiv(C, 256) <= kMaxTiles; }
+
 }  // namespace q2d
