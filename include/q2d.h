@@ -538,9 +538,9 @@ q2d_status q2d_attention_cached(const q2d_kv_cache *c, const q2d_sequences *s, c
  * Any of y, q4 and q8 may be wanted together, one at least.
  *
  * Row r of a tensor starts at its pointer + r * ld elements (ld >= cols with more than one
- * row); rows up to 2^31 - 1, cols up to 2^27 (Q2D_EUNSUPPORTED above).  rows may be 0 without
- * operands.  Values that are not finite follow the formulas: a row
- * with a NaN is NaN, one with an infinity has rstd 0.
+ * row); rows up to 2^31 - 1, cols up to 2^27, operands up to 2^35 tiles of 128 x 256
+ * (Q2D_EUNSUPPORTED above).  rows may be 0 without operands.  Values that are not finite
+ * follow the formulas: a row with a NaN is NaN, one with an infinity has rstd 0.
  */
 typedef struct {
     int32_t x_dtype, residual_dtype, weight_dtype, y_dtype;    /* q2d_dtype */

@@ -94,8 +94,7 @@ q2d_status q2d_rmsnorm_fwd(const q2d_rmsnorm *n, q2d_tensor *q4, q2d_tensor *q8,
         s = check_tensor(q4, (q2d_fmt)q4->fmt, n->rows, n->cols);
     }
     if (s == Q2D_OK && q8) s = check_tensor(q8, Q2D_FMT_MXFP8, n->rows, n->cols);
-    // (work-items of a launch along one dimension: below 2^32)
-    if (s == Q2D_OK && (q4 || q8) && cdiv(n->rows, 128) * cdiv(n->cols, 256) >= int64_t(1) << 23) return Q2D_EUNSUPPORTED;
+    if (s == Q2D_OK && (q4 || q8) && !few_tiles(n->rows, n->cols)) return Q2D_EUNSUPPORTED;
     if (s != Q2D_OK) return s;
 
     // what is written meets nothing else, but that h may take the place of x or of the residual

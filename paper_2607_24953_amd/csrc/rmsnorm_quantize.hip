@@ -275,7 +275,10 @@ __global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(WR
     const int64_t tiles_c = (a.cols_pad + 128 * WC - 1) / (128 * WC);
     // (the last rows first: the rows kernel has written them last, and the cache still holds some
     // of them.  16384 x 4096 float32 in FP4 with the rows kernel 189 us, so 178)
-    const int64_t tile = gridDim.x - 1 - blockIdx.x, tr = tile / tiles_c, tc = tile - tr * tiles_c;
+    // (strips are in a grid of one dimension: its second is the format)
+    const int64_t tile = (a.rows_pad / (32 * WR)) * tiles_c - 1 - (WR == 1 ? (int64_t)blockIdx.x : group_index());
+    if (tile < 0) return;
+    const int64_t tr = tile / tiles_c, tc = tile - tr * tiles_c;
     const int64_t r0 = tr * (32 * WR) + (wave / WC) * 32 + 8 * (lane >> 4), c0 = tc * (128 * WC) + (wave % WC) * 128 + 8 * (lane & 15);
     const int64_t cols = a.cols - c0;
 
@@ -319,9 +322,10 @@ template <bool HB, bool ALIGNED, int WR, int WC, bool ONCE>
 void launch_w(const NormQuantArgs &a, hipStream_t s)
 {
     const int64_t blocks = (a.rows_pad / (32 * WR)) * ((a.cols_pad + 128 * WC - 1) / (128 * WC));
+    const dim3 grid = WR == 1 ? dim3((unsigned)blocks, a.fp4 && a.mx ? 2 : 1) : row_grid(blocks);
     for_formats(a, [&](auto fp4, auto mx) {
         hipLaunchKernelGGL((rmsnorm_quantize_kernel<HB, ALIGNED, decltype(fp4)::value, decltype(mx)::value, WR, WC, ONCE>),
-                           dim3((unsigned)blocks, WR == 1 && a.fp4 && a.mx ? 2 : 1), dim3(64 * WR * WC), 0, s, a);
+                           grid, dim3(64 * WR * WC), 0, s, a);
     });
 }
 

@@ -47,3 +47,26 @@ def test_dequantize_column(q2d, fmt):
         got = out[first:first + STEP]
         assert torch.equal(got.isnan(), want.isnan()), first
         assert torch.equal(got.nan_to_num(0.0), want.nan_to_num(0.0)), first
+
+
+@pytest.mark.parametrize("fmt", ["FP4_1D", "MXFP8"])
+def test_norm_operand_column(q2d, fmt):
+    x = torch.empty((ROWS, 1), dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    for p in x.view(-1).split(1 << 26):
+        p.copy_(1e-2 * torch.randn(p.numel(), generator=g, device=DEV))
+    w, f = torch.tensor([1.3], device=DEV), getattr(q2d, fmt)
+    print("norm operand", fmt, ROWS, flush=True)
+    (q,), _, rstd = q2d.q2d_rmsnorm_quantize(x, w, 1e-4, formats=(f,), orientations=(False, True))
+    for first in range(0, ROWS, STEP):
+        rows = x[first:first + STEP]
+        (want,), _, rs = q2d.q2d_rmsnorm_quantize(rows, w, 1e-4, formats=(f,), orientations=(False, True))
+        got = piece(q2d, q, first)
+        assert torch.equal(rstd[first:first + STEP], rs) and torch.equal(got.codes_t, want.codes_t), first
+        assert torch.equal(got.scales_t, want.scales_t), first
+        # (and the first and last of them by the separate quantizer)
+        for a in (0, rows.shape[0] - 128 - rows.shape[0] % 128):
+            y = q2d.q2d_rmsnorm_fwd(rows[a:a + 128], w, 1e-4, y_dtype=torch.float32)[0]
+            own = q2d.mxfp8_quantize(y) if fmt == "MXFP8" else q2d.q2d_quantize_1d(y)
+            at = a if fmt == "MXFP8" else a // 2
+            assert torch.equal(got.codes_t[:, at:at + own.codes_t.shape[1]], own.codes_t), (first, a)

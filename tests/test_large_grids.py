@@ -30,6 +30,15 @@ const uint64_t *last_grid(void) { return last; }
 """
 
 
+class _Norm(ctypes.Structure):
+    """q2d_rmsnorm."""
+    _fields_ = [("x_dtype", ctypes.c_int32), ("residual_dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+                ("y_dtype", ctypes.c_int32), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("eps", ctypes.c_double),
+                ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("residual", ctypes.c_void_p), ("ld_residual", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("h", ctypes.c_void_p), ("ldh", ctypes.c_int64), ("y", ctypes.c_void_p),
+                ("ldy", ctypes.c_int64), ("rstd", ctypes.c_void_p)]
+
+
 def run(tmp_path, calls):
     if shutil.which("gcc") is None:
         pytest.skip("gcc not found")
@@ -58,6 +67,18 @@ def test_dequantize(tmp_path):
         assert [x[0] for x in run(tmp_path, [dict(fn="dequantize", fmt="fp4", rows=r, cols=c, copy=0, dt=0)])] == [2]
 
 
+def test_norm_operands(tmp_path):
+    sizes = [x for x in SIZES if x[1] <= 2 ** 27]
+    calls = [dict(fn="norm", fmt=f, rows=r, cols=c, dt=d) for f in (["fp4"], ["mxfp8"], ["fp4_1d"], ["fp4", "mxfp8"]) for r, c in sizes
+             for d in (0, 1)]
+    for c, (status, launch, grid) in zip(calls, run(tmp_path, calls)):
+        assert status == 0 and "rmsnorm_quantize_kernel" in launch[0] and launch[1] == 512, (c, status)
+        n = grid[0] * grid[1] * grid[2]
+        assert tiles(c["rows"], c["cols"]) <= n < tiles(c["rows"], c["cols"]) + 2 ** 20, (c, grid)
+    # more than any launch takes
+    assert [x[0] for x in run(tmp_path, [dict(fn="norm", fmt=["fp4"], rows=2 ** 31 - 1, cols=2 ** 21, dt=1)])] == [2]
+
+
 def _main(so):
     class Launch(ctypes.Structure):
         _fields_ = [("name", ctypes.c_char_p), ("grid", ctypes.c_uint32), ("block", ctypes.c_uint32), ("lds", ctypes.c_uint64)]
@@ -82,6 +103,10 @@ def _main(so):
         if c["fn"] == "dequantize":
             t = tensor(c["fmt"], c["rows"], c["cols"], 2)
             s = lib.q2d_dequantize(ctypes.byref(t), c["copy"], P(place), c["dt"], I64(c["cols"]), None, I64(0), None)
+        else:
+            n = _Norm(x_dtype=c["dt"], rows=c["rows"], cols=c["cols"], eps=1e-5, x=place, ldx=c["cols"], weight=2 * place, rstd=3 * place)
+            q = {f == "mxfp8": tensor(f, c["rows"], c["cols"], 4 + 4 * i) for i, f in enumerate(c["fmt"])}
+            s = lib.q2d_rmsnorm_fwd(ctypes.byref(n), *(ctypes.byref(q[k]) if k in q else None for k in (False, True)), None)
         n = rec.recorded()
         l = rec.recorded_launch(n - 1).contents if n else None
         out.append((s, (l.name.decode(), l.block) if n else None, rec.last_grid()[:3]))
