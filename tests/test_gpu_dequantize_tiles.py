@@ -1,0 +1,49 @@
+"""q2d_dequantize at sizes whose matrices are cut into whole tiles (more than 128 of 128 x 256), against the
+oracle: all formats, both copies, ragged edges, exponents, outputs of any pitch and alignment, and the
+bfloat16 outputs of 96 MB and more that are written past the cache."""
+import pytest
+import torch
+
+import synth
+from test_gpu_dequantize import DEV, FMTS, check_copy, q2d, quantize_both      # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+# the last tile's rows and columns: 52 and 132, 1 and 77, 33 and 128; odd row pitches of the exponents
+SHAPES = [(2100, 2180), (4225, 1101), (16417, 128)]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("fmt", FMTS)
+def test_tiles(q2d, shape, fmt):
+    x = synth.normal(shape, 1.0, 910 + shape[0], torch.bfloat16, device=DEV)
+    synth.add_outlier_channels(x, 9, frac=0.03)
+    x[3, 40], x[shape[0] - 1, shape[1] - 1], x[700, 100] = float("nan"), float("inf"), 3e38
+    q, o = quantize_both(q2d, x, fmt)
+    for copy in (0, 1):
+        for dt in (torch.float32, torch.bfloat16):
+            print(shape, fmt, copy, dt, flush=True)
+            check_copy(q2d, q, o, fmt, copy, dt, "%s %s copy %d %s" % (shape, fmt, copy, dt))
+            big = torch.full((shape[0], shape[1] + 11), 7.0, dtype=dt, device=DEV)
+            check_copy(q2d, q, o, fmt, copy, dt, "strided", out=big[:, 1:1 + shape[1]])
+            assert bool((big[:, 0] == 7).all()) and bool((big[:, 1 + shape[1]:] == 7).all())
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("shape", [(8200, 6150), (16384, 4096)], ids=str)
+def test_output_past_the_cache(q2d, fmt, shape):
+    """bfloat16 output of 96 MB and more is the rounded float32 output."""
+    x = synth.normal(shape, 1.0, 912, torch.bfloat16, device=DEV)
+    synth.add_outlier_channels(x, 10, frac=0.03)
+    x[5, 5], x[100, shape[1] - 1], x[shape[0] - 1, 64] = float("nan"), float("inf"), 3.3e38
+    q = (q2d.mxfp8_quantize(x) if fmt == "mxfp8" else q2d.q2d_quantize_1d(x) if fmt == "fp4_1d" else
+         q2d.q2d_quantize(x, block=64 if fmt == "fp4_b64" else 32))
+    for copy in (0, 1):
+        want, e = q2d.q2d_dequantize(q, copy, exps=True)
+        big = torch.full((shape[0], shape[1] + 3), 7.0, dtype=torch.bfloat16, device=DEV)
+        for out in (None, big[:, 1:1 + shape[1]]):
+            print(shape, fmt, copy, out is None, flush=True)
+            got, e2 = q2d.q2d_dequantize(q, copy, torch.bfloat16, exps=True, out=out)
+            assert torch.equal(e, e2) and torch.equal(got.isnan(), want.isnan())
+            assert torch.equal(got.nan_to_num(0.0), want.to(torch.bfloat16).nan_to_num(0.0))
+        assert bool((big[:, 0] == 7).all()) and bool((big[:, 1 + shape[1]:] == 7).all())
