@@ -4,6 +4,7 @@ bfloat16 outputs of 96 MB and more that are written past the cache."""
 import pytest
 import torch
 
+import oracle
 import synth
 from test_gpu_dequantize import DEV, FMTS, check_copy, q2d, quantize_both      # noqa: F401
 
@@ -27,6 +28,28 @@ def test_tiles(q2d, shape, fmt):
             big = torch.full((shape[0], shape[1] + 11), 7.0, dtype=dt, device=DEV)
             check_copy(q2d, q, o, fmt, copy, dt, "strided", out=big[:, 1:1 + shape[1]])
             assert bool((big[:, 0] == 7).all()) and bool((big[:, 1 + shape[1]:] == 7).all())
+
+
+@pytest.mark.parametrize("shape", [(2100, 2180), (130, 200), (33, 129), (5, 3)], ids=str)
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("pad,shift", [(0, 1), (1, 0), (3, 5), (8, 8)])
+def test_exponents_anywhere(q2d, shape, fmt, pad, shift):
+    """Exponents of any pitch and alignment; what lies between their rows is left alone."""
+    rows, cols = shape
+    x = synth.normal(shape, 1.0, 911, torch.bfloat16, device=DEV)
+    x[rows - 1, 0] = float("nan")
+    q, o = quantize_both(q2d, x, fmt)
+    out = torch.empty(shape, device=DEV)
+    for copy in (0, 1):
+        buf = torch.full((rows * (cols + pad) + shift,), 77, dtype=torch.int8, device=DEV)
+        e = torch.as_strided(buf, shape, (cols + pad, 1), shift)
+        assert q2d._lib.q2d_dequantize(q.ptr(), copy, out.data_ptr(), 0, cols, e.data_ptr(), cols + pad,
+                                       torch.cuda.current_stream().cuda_stream) == 0
+        want = torch.from_numpy(oracle.scale_exponents(o, copy, "fp4" if fmt == "fp4_b64" else fmt)).to(torch.int8)
+        assert torch.equal(e.cpu(), want) and int(e[rows - 1, 0]) == -128
+        assert bool((buf[:shift] == 77).all())
+        if pad:
+            assert bool((torch.as_strided(buf, (rows, pad), (cols + pad, 1), shift + cols) == 77).all())
 
 
 @pytest.mark.parametrize("fmt", FMTS)
