@@ -57,6 +57,14 @@ def _call(device, name, *args):
     _check(getattr(_lib, name)(*args, _stream(device)), name)
 
 
+def _modified(tensors):
+    """Tells autograd of the caller's tensors (None: none) that a call has written: a backward pass
+    that needs their old values is refused."""
+    written = [t for t in tensors if t is not None]
+    if written:
+        torch.autograd.graph.increment_version(written)
+
+
 def _rows(t, shape, device, what):
     """(pointer, row pitch) of a [rows, cols] tensor with unit stride along its rows."""
     if t.shape != shape:
@@ -118,10 +126,13 @@ def q2d_rmsnorm_fwd(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, re
                     rstd: torch.Tensor | None = None):
     """Root-mean-square norm of the rows of h = x + residual (x [rows, cols]; h in x's dtype, x
     itself without a residual) times weight [cols]; returns (y, h, rstd).  rstd (float32 [rows])
-    is what q2d_rmsnorm_bwd needs.  h may be x or residual itself: in place."""
+    is what q2d_rmsnorm_bwd needs.  h may be x or residual itself: in place.  Tensors handed in as
+    y, h and rstd count as modified for autograd."""
+    given = y, h, rstd
     if y is None:
         y = torch.empty_like(x, dtype=y_dtype, memory_format=torch.contiguous_format)
     h, rstd = _forward(x, weight, eps, residual, h, rstd, y, None, None)
+    _modified(given)
     return y, h, rstd
 
 
@@ -132,7 +143,8 @@ def q2d_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-
     QTensor for each of ``formats`` (one of FP4_2D and FP4_1D, MXFP8, or both), from one read of
     h; returns (list of QTensors, h, rstd).  The codes are those of the quantizers for the
     float32 y, rounded to nearest.  block: edge of the 2D blocks (32 or 64); orientations: (True,
-    False) for the rowwise copies alone, which a forward GEMM reads; out: QTensors to fill."""
+    False) for the rowwise copies alone, which a forward GEMM reads; out: QTensors to fill.  h and
+    rstd handed in count as modified for autograd."""
     formats = tuple(formats)
     kinds = [f == MXFP8 for f in formats]
     if not formats or any(f not in (FP4_2D, FP4_1D, MXFP8) for f in formats) or len(set(kinds)) != len(kinds):
@@ -148,7 +160,9 @@ def q2d_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-
     q = [None, None]
     for t, mx in zip(out, kinds):
         q[mx] = t.ptr()
+    given = h, rstd
     h, rstd = _forward(x, weight, eps, residual, h, rstd, None, *q)
+    _modified(given)
     return out, h, rstd
 
 
@@ -157,7 +171,9 @@ def q2d_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rst
                     need_dw: bool = True):
     """Gradients (dx, dw) of the norm from dy, and h and rstd of the forward call: dx (h's dtype)
     for x and for the residual, with dh, the gradient that reaches h by other ways, added; dw
-    (float32 [cols]) for the weight, None with need_dw=False.  dx may be dh itself."""
+    (float32 [cols]) for the weight, None with need_dw=False.  dx may be dh itself.  dx and dw handed
+    in count as modified for autograd."""
+    given = dx, dw
     device, shape = h.device, h.shape
     if device.type != "cuda" or len(shape) != 2:
         raise Q2DError("expected h as a 2-D device tensor")
@@ -182,6 +198,7 @@ def q2d_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rst
                      *_rows(h, shape, device, "h"), *_rows(dy, shape, device, "dy"), dhp, lddh,
                      *_rows(dx, shape, device, "dx"), _vector(weight, cols, device, "weight"),
                      _vector(rstd, rows, device, "rstd", torch.float32), wp), ws.data_ptr(), size)
+    _modified(given)
     return dx, dw
 
 
@@ -232,14 +249,15 @@ def _address(a):
 
 def q2d_grad_norm(tensors, norm: torch.Tensor | None = None) -> torch.Tensor:
     """2-norm over all elements of a list of tensors (float32 or bfloat16, without gaps), as a
-    float32 device scalar."""
+    float32 device scalar.  A norm handed in counts as modified for autograd."""
     tensors, pointers, counts, dtypes, _ = _gradients(tensors, "tensors")
-    device = tensors[0].device
+    device, given = tensors[0].device, norm
     norm = _scalar(norm, device, "norm")
     size = _lib.q2d_grad_workspace(len(tensors))
     ws = torch.empty(size, dtype=torch.uint8, device=device)
     _call(device, "q2d_grad_norm", len(tensors), _address(pointers), _address(counts), _address(dtypes), norm.data_ptr(),
           ws.data_ptr(), size)
+    _modified((given,))
     return norm
 
 
@@ -256,7 +274,8 @@ def q2d_clip_grads(tensors, max_norm: float, norm: torch.Tensor | None = None, o
     """Scales a list of tensors by min(1, max_norm / norm), in place or into the tensors of
     ``out``; returns the norm (float32 device scalar).  norm: the value to go by, the 2-norm over
     tensors of several GPUs for one; None: that of q2d_grad_norm.  A norm that is not finite
-    leaves the values as they are.  Nothing waits for the device."""
+    leaves the values as they are.  Nothing waits for the device.  The tensors that are written count
+    as modified for autograd, whatever the norm is."""
     tensors, pointers, counts, dtypes, dense = _gradients(tensors, "tensors")
     device = tensors[0].device
     outs = None
@@ -273,4 +292,6 @@ def q2d_clip_grads(tensors, max_norm: float, norm: torch.Tensor | None = None, o
     _call(device, "q2d_clip_grads", len(tensors), _address(pointers), None if outs is None else _address(outs),
           _address(counts), _address(dtypes), float(max_norm), None if given is None else norm.data_ptr(),
           norm.data_ptr() if given is None else None, ws.data_ptr(), size)
+    # (behind the launches: of 240 tensors it takes 12 us, while the device is at work)
+    torch.autograd.graph.increment_version(tensors if out is None else out)
     return norm
