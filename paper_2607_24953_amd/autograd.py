@@ -125,6 +125,11 @@ def _rows(t, cols):
     return t if (one == 1 or cols == 1) and (pitch >= cols or t.shape[0] < 2) else t.contiguous()
 
 
+def _kernel_type(t):
+    """t in a type that the kernels read (None: none): other ones as float32, as by Q2DLinear."""
+    return t if t is None or t.dtype in _DTYPES else t.float()
+
+
 def _norm_backward(ctx, dy, dh, h, weight, rstd):
     """Gradients of x, the residual and the norm's weight from that of y (None: none) and of h."""
     need_x, need_r, need_w = ctx.needs_input_grad[:3]
@@ -134,12 +139,13 @@ def _norm_backward(ctx, dy, dh, h, weight, rstd):
         # (a copy: dh may be another tensor's gradient too)
         dx, dw = None if dh is None else dh.clone(memory_format=torch.contiguous_format), None
     else:
-        dx, dw = q2d_rmsnorm_bwd(dy, h, weight, rstd, dh=dh, need_dw=need_w)
+        dx, dw = q2d_rmsnorm_bwd(dy, h, _kernel_type(weight), rstd, dh=dh, need_dw=need_w)
     if dx is not None:
         # (one object for both where the types agree: as two views of it, either could become its
         # tensor's .grad and share memory with the other's)
         dx = dx.reshape(ctx.x_shape)
-    return (dx if need_x else None, dx.to(ctx.r_dtype) if need_r and dx is not None else None,
+    return (dx.to(ctx.x_dtype) if need_x and dx is not None else None,
+            dx.to(ctx.r_dtype) if need_r and dx is not None else None,
             None if dw is None else dw.to(weight.dtype))
 
 
@@ -148,7 +154,7 @@ def _norm_inputs(ctx, x, residual, weight):
     cols = weight.shape[0] if weight.dim() == 1 else -1
     if x.dim() == 0 or x.shape[-1] != cols or (residual is not None and residual.shape != x.shape):
         raise Q2DError("x and residual of one shape [..., %d] are expected" % cols)
-    ctx.x_shape, ctx.r_dtype = x.shape, None if residual is None else residual.dtype
+    ctx.x_shape, ctx.x_dtype, ctx.r_dtype = x.shape, x.dtype, None if residual is None else residual.dtype
     ctx.set_materialize_grads(False)
     return _rows(x, cols), None if residual is None else _rows(residual, cols)
 
@@ -182,15 +188,14 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual:
 class _NormLinearFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, norm_weight, weight, layer, both):
-        x2, r2 = _norm_inputs(ctx, x, residual, norm_weight)
+        x2, r2 = (_kernel_type(t) for t in _norm_inputs(ctx, x, residual, norm_weight))
         n = layer._calls
         layer._calls += 1
         both = (True, both and any(ctx.needs_input_grad))
-        (qX,), h, rstd = q2d_rmsnorm_quantize(x2, norm_weight.detach(), layer.eps, residual=r2,
+        (qX,), h, rstd = q2d_rmsnorm_quantize(x2, _kernel_type(norm_weight.detach()), layer.eps, residual=r2,
                                               formats=(FP4_1D if layer.activations == "1d" else FP4_2D,),
                                               block=layer.block, orientations=both)
-        w = weight.detach()
-        w = (w if w.dtype in _DTYPES else w.float()).contiguous()
+        w = _kernel_type(weight.detach()).contiguous()
         qW = q2d_quantize(w, layer.mode_w, layer.seed, 3 * n + 1, block=layer.block,
                           out=QTensor(FP4_2D, *w.shape, w.device, layer.block, both))
         Y = q2d_gemm(qX, 0, qW, 0, out_dtype=layer.out_dtype)
@@ -198,7 +203,7 @@ class _NormLinearFunction(torch.autograd.Function):
         ctx.qX, ctx.qW = qX, qW
         ctx.layer, ctx.offset_dy, ctx.w_dtype = layer, 3 * n + 2, weight.dtype
         Y = Y.reshape(*x.shape[:-1], w.shape[0])
-        return (Y,) if residual is None else (Y, h.reshape(x.shape))
+        return (Y,) if residual is None else (Y, h.reshape(x.shape).to(x.dtype))
 
     @staticmethod
     @once_differentiable
@@ -208,8 +213,7 @@ class _NormLinearFunction(torch.autograd.Function):
         if dY is not None:
             if ctx.qX is None:
                 raise Q2DError("the operands are gone after a backward pass: a second one needs a second forward pass")
-            dY2 = dY.reshape(-1, dY.shape[-1])
-            dY2 = (dY2 if dY2.dtype in _DTYPES else dY2.float()).contiguous()
+            dY2 = _kernel_type(dY.reshape(-1, dY.shape[-1])).contiguous()
             dy, dW, _ = q2d_linear_bwd(dY2, ctx.qX, ctx.qW, layer.mode_dy, layer.seed, ctx.offset_dy, dx_dtype=dY2.dtype,
                                        dw_dtype=torch.float32, block=layer.block)
             dW = dW.to(ctx.w_dtype)
@@ -220,7 +224,9 @@ class _NormLinearFunction(torch.autograd.Function):
 class Q2DNormLinear(Q2DLinear):
     """Q2DLinear behind a root-mean-square norm with the residual's addition (see the module
     docstring): y = Q(norm(h) * norm_weight) Q(W)^T with h = x + residual.  X is rounded to
-    nearest, with the truncation-free scales."""
+    nearest, with the truncation-free scales.  Inputs and weights of other types than float32 and
+    bfloat16 are taken as float32; x + residual and the gradients come back in their own type, Y in
+    ``out_dtype``."""
 
     def __init__(self, in_features: int, out_features: int, *, eps: float = 1e-5, out_dtype=torch.bfloat16, **options):
         if options.get("mode_x", "rtn") != "rtn":
