@@ -235,6 +235,12 @@ class Q2DNormLinear(Q2DLinear):
         self.eps, self.out_dtype = eps, out_dtype
         self.norm_weight = torch.nn.Parameter(torch.ones(in_features, device=self.weight.device, dtype=self.weight.dtype))
 
+    def reset_parameters(self):
+        super().reset_parameters()
+        # (Q2DLinear's constructor calls this before there is one)
+        if "norm_weight" in self._parameters:
+            torch.nn.init.ones_(self.norm_weight)
+
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
         """y, or with a residual (y, x + residual)."""
         # (only a backward pass reads the transposed copies)
