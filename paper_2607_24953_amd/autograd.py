@@ -217,7 +217,7 @@ class _NormLinearFunction(torch.autograd.Function):
             dy, dW, _ = q2d_linear_bwd(dY2, ctx.qX, ctx.qW, layer.mode_dy, layer.seed, ctx.offset_dy, dx_dtype=dY2.dtype,
                                        dw_dtype=torch.float32, block=layer.block)
             dW = dW.to(ctx.w_dtype)
-        ctx.qX = ctx.qW = None
+            ctx.qX = ctx.qW = None
         return (*_norm_backward(ctx, dy, dh, h, norm_weight.detach(), rstd), dW, None, None)
 
 

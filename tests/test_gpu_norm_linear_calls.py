@@ -1,4 +1,5 @@
-"""Q2DNormLinear on types that the kernels do not read: taken as float32, as by Q2DLinear."""
+"""Q2DNormLinear on types that the kernels do not read, taken as float32 as by Q2DLinear, and its backward
+pass in parts."""
 import pytest
 import torch
 
@@ -44,3 +45,25 @@ def test_other_types(x, w, residual):
         assert (a is None) == (b is None), i
         if a is not None:
             assert a.dtype == k and torch.equal(a, b.to(k)), i
+
+
+def test_backward_by_the_sum_alone_first():
+    """A pass through x + residual reads no operands: the pass through Y may still come."""
+    from paper_2607_24953_amd.autograd import Q2DNormLinear
+    dY, dH = rand(50, 96, dtype=BF16, seed=3), rand(50, 160, seed=4)
+    grads = []
+    for apart in (True, False):
+        layer = Q2DNormLinear(160, 96, seed=7, device=DEV)
+        with torch.no_grad():
+            layer.weight.copy_(rand(96, 160, seed=5, scale=0.1))
+        X, R = rand(50, 160, seed=1).requires_grad_(), rand(50, 160, seed=2).requires_grad_()
+        Y, H = layer(X, R)
+        if apart:
+            H.backward(dH, retain_graph=True)
+            assert torch.equal(X.grad, dH) and layer.weight.grad is None
+            Y.backward(dY)
+        else:
+            torch.autograd.backward((Y, H), (dY, dH))
+        grads.append([t.grad for t in (X, R, layer.weight, layer.norm_weight)])
+    # (dh's addition is the last step of dx, in float32 both times)
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
