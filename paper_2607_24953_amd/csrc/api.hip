@@ -486,7 +486,6 @@ q2d_status q2d_dequantize(const q2d_tensor *t, int copy, void *out, q2d_dtype ou
     if (!codes || !check_pair(codes, ldc, copy ? l.ld_codes_t : l.ld_codes, scales, lds,
                               copy ? l.ld_scales_t : l.ld_scales))
         return Q2D_EINVAL;
-    const int eb = dtype_bytes(out_dt);
     DequantArgs a;
     a.codes = codes; a.ld_codes = ldc;
     a.scales = scales; a.ld_scales = lds;
@@ -495,7 +494,6 @@ q2d_status q2d_dequantize(const q2d_tensor *t, int copy, void *out, q2d_dtype ou
     a.transposed = copy;
     a.out = out; a.ldo = ldo;
     a.out_bf16 = out_dt == Q2D_BF16;
-    a.out_vec = aligned(out, 4 * eb) && (ldo % 4) == 0;
     a.exps = exps; a.lde = lde;
     if (launch_dequantize(a, stream) != hipSuccess) return Q2D_ELAUNCH;
     return Q2D_OK;

@@ -112,7 +112,6 @@ struct DequantArgs {
     int transposed;                             // the copy stores element (r, c) in row c
     void *out; int64_t ldo;                     // elements
     int out_bf16;
-    int out_vec;                                // out and ldo allow 4-element vector stores
     int8_t *exps; int64_t lde;                  // optional per-element scale exponents
 };
 
