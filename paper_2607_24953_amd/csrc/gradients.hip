@@ -67,15 +67,15 @@ struct Unit : Run<BF16, BF16 ? 8 : 4> {
     }
 };
 
-// bytes that a lane has in flight
-constexpr int kFlight = 64;
+// 16-byte accesses that a lane has in flight
+template <bool BF16> constexpr int kFlight = BF16 ? 4 : 2;
 
 // (ONCE: no second pass follows)
 template <bool BF16, bool ONCE>
 __device__ __forceinline__ double square_piece(const void *data, int64_t at, int length)
 {
     typedef Unit<BF16> U;
-    constexpr int kUnits = kFlight / 8 / U::kBytes, kStep = 256 * U::kN;
+    constexpr int kUnits = kFlight<BF16>, kStep = 256 * U::kN;
     const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * U::kBytes;
     double s = 0.0;
 #pragma unroll 1
@@ -129,7 +129,7 @@ template <bool BF16>
 __device__ __forceinline__ void scale_piece(const void *data, void *out, int64_t at, int length, bool clip, float f)
 {
     typedef Unit<BF16> U;
-    constexpr int kUnits = kFlight / 8 / U::kBytes, kStep = 256 * U::kN;
+    constexpr int kUnits = kFlight<BF16>, kStep = 256 * U::kN;
     const uint8_t *p = reinterpret_cast<const uint8_t *>(data) + at * U::kBytes;
     uint8_t *o = reinterpret_cast<uint8_t *>(out) + at * U::kBytes;
 #pragma unroll 1

@@ -138,7 +138,7 @@ __device__ __forceinline__ void store_run(const float (&v)[N], void *base, int b
     } else {
         Run<false, N> e;
         e.set(v);
-        e.store(p + 4 * i, n);
+        e.template store<ONCE>(p + 4 * i, n);
     }
 }
 
