@@ -18,7 +18,7 @@
 // bfloat16 output is the round-to-nearest-even of that value.
 //
 // Element by element from LDS, with the scales read beside it, the transposed MXFP8 copy of
-// 16384 x 4096 took 139 us as bfloat16 and 164 as float32; now 35 and 90 (6.1 and 3.7 TB/s).
+// 16384 x 4096 took 139 us as bfloat16 and 164 as float32; now 35 and 85 (5.9 and 4.0 TB/s).
 #include "device_common.hpp"
 #include "kernels.hpp"
 #include "norm_common.hpp"
@@ -39,7 +39,7 @@ __device__ __forceinline__ float scale_value(uint32_t byte)
 __device__ __forceinline__ uint8_t exponent(uint32_t byte) { return (uint8_t)(byte - 127u); }
 
 // The first n of eight exponents at any address, together where all are wanted.  (One byte at a time,
-// 16384 x 4096 float32 with exponents took 113 us, MXFP8 132)
+// 16384 x 4096 float32 with exponents took 113 us, MXFP8 132; so 85 and 100)
 __device__ __forceinline__ void store_exponents(int8_t *p, const uint8_t (&b)[8], int64_t n)
 {
     typedef u2v any __attribute__((aligned(1)));
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(64 * WR * WC) void dequantize_kernel(const DequantA
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] *= scale[kScales == 1 ? 0 : TRANS ? j : i];
-        store_run<ONCE && BF16>(v, a.out, BF16, r * a.ldo + c0, a.cols - c0);
+        store_run<ONCE>(v, a.out, BF16, r * a.ldo + c0, a.cols - c0);
         if (a.exps) {
             uint8_t b[8];
 #pragma unroll
@@ -220,8 +220,13 @@ hipError_t launch_tiles(const DequantArgs &a, hipStream_t s)
         // 58 -> 35; with a kernel that reads the output behind it 65 -> 61, half the size 30 -> 34.
         // (float32 stores of eight elements are two to a line and stay)
         const dim3 grid = row_grid(tiles(128, 256)), block(512);
-        if (BF16 && a.rows * a.cols * 2 >= int64_t(96) << 20) hipLaunchKernelGGL((dequantize_kernel<FMT, TRANS, BF16, 4, 2, true>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((dequantize_kernel<FMT, TRANS, BF16, 4, 2>), grid, block, 0, s, a);
+        if constexpr (BF16) {
+            if (a.rows * a.cols * 2 >= int64_t(96) << 20) {
+                hipLaunchKernelGGL((dequantize_kernel<FMT, TRANS, BF16, 4, 2, true>), grid, block, 0, s, a);
+                return hipGetLastError();
+            }
+        }
+        hipLaunchKernelGGL((dequantize_kernel<FMT, TRANS, BF16, 4, 2>), grid, block, 0, s, a);
     }
     return hipGetLastError();
 }
