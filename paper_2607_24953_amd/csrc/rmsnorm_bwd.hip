@@ -3,16 +3,22 @@
 // With n = h * rstd and g = dy * w: dx = rstd * (g - n * mean(g n)) + dh, dw = sum over rows of dy n.
 // One read of h, dy and dh: a row stays in registers between the sum for its mean and the products
 // with it, as in the forward kernel.  A workgroup takes every gridDim.x-th row and keeps its part
-// of dw in registers, in 64 bits; the parts lie one behind the other in the workspace and a second
-// kernel adds them up.  Every sum has one owner and one order.
+// of dw over all of them, in 64 bits: in registers, for rows of 4097 to 6144 and of 8193 to 16384 columns in
+// LDS.  The parts lie one behind the other in the workspace and a second kernel adds them up.  Every
+// sum has one owner and one order.
 //
 // The memory bounds it: 16384 x 4096 bfloat16 with dh 86 us (545 MB, 6.3 TB/s) and 5 for the join,
 // float32 151 in all; 777 x 2049 8.5 + 3.5.  The statistics of a row and the products with it as two
 // kernels, element by element, took 700.  Rows of more than 16384 columns are
-// read twice; of 8193 to 16384 so 2048 x 12288 bfloat16 took 60 us, float32 101 (in registers, spilled, 77
-// and 165), with dw's parts in LDS 50 and 79 (4.0 and 5.1 TB/s): one workgroup has a CU for itself and
-// nothing runs while it waits at its barrier.  With dw's parts in LDS for all rows, and six or eight
-// waves to a SIMD, 16384 x 4096 took 103 and 102 us instead of 92.
+// read twice (2048 x 17000 bfloat16 27 + 51 us); of 8193 to 16384 so 2048 x 12288 bfloat16 took 60 us,
+// float32 101 (in registers, spilled, 77 and 165), with dw's parts in LDS 50 and 79 (4.0 and 5.1 TB/s): one
+// workgroup has a CU for itself and nothing runs while it waits at its barrier.  With dw's parts in LDS for
+// all rows, and six or eight waves to a SIMD, 16384 x 4096 took 103 and 102 us instead of 92.
+//
+// Rows of up to 1024 columns are further from that: the registers hold two waves a SIMD, each with one
+// row at a time, and chunks that narrow rows leave empty stand for bytes that are not in flight.  bfloat16
+// with dh: 65536 x 512 63 us (4.3 TB/s), 8192 x 1024 16 (from the cache), 100000 x 200 34 (4.7), 500000 x 128
+// 110 (4.6), 500000 x 64 107 (2.4).
 #include "norm_common.hpp"
 #include "norms.hpp"
 #include "kernels.hpp"
