@@ -63,11 +63,23 @@ __device__ __forceinline__ void fp4_values(uint32_t w, float (&v)[8])
     v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
 }
 
-// values of four E4M3FN bytes (S.1111.111 is NaN)
+// values of four E4M3FN bytes (S.1111.111 is a NaN of either sign)
 __device__ __forceinline__ void fp8_values(uint32_t w, float *v)
 {
     const f32v2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
     v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+}
+
+// whether a wave has a NaN code: seven ones and one more carry into a byte's highest bit
+template <int WORDS>
+__device__ __forceinline__ bool fp8_nan(const uint32_t (&w)[8][WORDS])
+{
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) any |= (w[i][k] & 0x7F7F7F7Fu) + 0x01010101u;
+    return __builtin_amdgcn_ballot_w64((any & 0x80808080u) != 0) != 0;
 }
 
 // 4 x 4 transpose of bytes: byte j of in[i] becomes byte i of out[j]
@@ -185,6 +197,8 @@ __global__ __launch_bounds__(64 * WR * WC) void dequantize_kernel(const DequantA
     float scale[kScales];
 #pragma unroll
     for (int i = 0; i < kScales; ++i) scale[i] = scale_value(sb[i]);
+    bool nan = false;
+    if constexpr (FMT == 1) nan = fp8_nan(w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int64_t r = r0 + i;
@@ -198,6 +212,11 @@ __global__ __launch_bounds__(64 * WR * WC) void dequantize_kernel(const DequantA
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] *= scale[kScales == 1 ? 0 : TRANS ? j : i];
+        if (FMT == 1 && nan) {
+            // (the conversion's NaN are negative ones)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = v[j] == v[j] ? v[j] : bits_f(kNaN);
+        }
         store_run<ONCE>(v, a.out, BF16, r * a.ldo + c0, a.cols - c0);
         if (a.exps) {
             uint8_t b[8];

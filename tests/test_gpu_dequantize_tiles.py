@@ -70,3 +70,37 @@ def test_output_past_the_cache(q2d, fmt, shape):
             assert torch.equal(e, e2) and torch.equal(got.isnan(), want.isnan())
             assert torch.equal(got.nan_to_num(0.0), want.to(torch.bfloat16).nan_to_num(0.0))
         assert bool((big[:, 0] == 7).all()) and bool((big[:, 1 + shape[1]:] == 7).all())
+
+
+# strips, tiles, and bfloat16 past the cache
+@pytest.mark.parametrize("repeat", [(1, 1), (9, 20), (33, 25)], ids=str)
+@pytest.mark.parametrize("fmt", ["fp4_1d", "mxfp8"])
+@pytest.mark.parametrize("copy", [0, 1])
+def test_every_code_and_scale(q2d, fmt, copy, repeat):
+    """All codes under all scale bytes, one scale byte a line; every NaN is 0x7FC00000 (0x7FC0)."""
+    lines, width = 256 * repeat[0], 256 * repeat[1]
+    shape = (lines, width) if copy == 0 else (width, lines)
+    q = q2d.QTensor(q2d.MXFP8 if fmt == "mxfp8" else q2d.FP4_1D, *shape, DEV, 32, (copy == 0, copy == 1))
+    codes, scales = (q.codes, q.scales) if copy == 0 else (q.codes_t, q.scales_t)
+    byte = torch.arange(256).repeat(repeat[0]).to(torch.uint8)
+    if fmt == "mxfp8":
+        one = torch.arange(256).repeat(repeat[1]).to(torch.uint8)
+        values = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).to(torch.float64).repeat(repeat[1])
+        scales.copy_(byte[:, None].expand(scales.shape))
+    else:
+        nibbles = torch.arange(256).repeat(repeat[1]) % 16
+        one = (nibbles[::2] | nibbles[1::2] << 4).to(torch.uint8)
+        table = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64)
+        values = torch.cat((table, -table))[nibbles]
+        scales.copy_(byte.repeat_interleave(4)[None].expand(scales.shape))
+    codes.copy_(one[None].expand(codes.shape))
+    want = torch.ldexp(values[None], byte[:, None].to(torch.int64) - 127)
+    want[byte == 255] = float("nan")
+    want = want.float() if copy == 0 else want.float().t()
+    bad = want.isnan()
+    for dt, bits in ((torch.float32, torch.int32), (torch.bfloat16, torch.int16)):
+        print(fmt, copy, repeat, dt, flush=True)
+        got = q2d.q2d_dequantize(q, copy, dt).cpu()
+        w = want.to(dt).contiguous().view(bits)
+        w[bad] = 0x7FC00000 if dt == torch.float32 else 0x7FC0
+        assert torch.equal(got.view(bits), w)
