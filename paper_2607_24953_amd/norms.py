@@ -292,6 +292,6 @@ def q2d_clip_grads(tensors, max_norm: float, norm: torch.Tensor | None = None, o
     _call(device, "q2d_clip_grads", len(tensors), _address(pointers), None if outs is None else _address(outs),
           _address(counts), _address(dtypes), float(max_norm), None if given is None else norm.data_ptr(),
           norm.data_ptr() if given is None else None, ws.data_ptr(), size)
-    # (behind the launches: of 240 tensors it takes 12 us, while the device is at work)
+    # (behind the launches, while the device is at work: 6 us of 240 tensors)
     torch.autograd.graph.increment_version(tensors if out is None else out)
     return norm
